@@ -417,6 +417,72 @@ int rwkvq_linear_dispatch_post(const rwkvq_matrix* mats, const void* const* xs, 
                                const rwkvq_post_op* posts, void* const* ys, int n_mats, int x_dtype, int y_dtype,
                                void* stream);
 
+/* ---- operators of a multi-head block beside its projections: layer norm, linear attention ----------
+ *
+ * rwkvq_layer_norm: y = (x - mean) rstd (.) weight + bias over the last n of every row's groups x n values,
+ *   rstd = 1 / sqrt(var + eps), var = the mean of (x - mean)^2.  groups = 1 is the norm in front of a
+ *   projection; groups = n_heads, n = head_dim is the norm of each head behind the attention.
+ *   x, y: [M] rows of groups * n values of x_dtype (fp16, bf16 or binary32), x_stride and y_stride elements
+ *   apart (0 = groups * n); weight, bias: DEVICE [groups * n] floats, NULL = 1 and 0; mean, rstd: DEVICE
+ *   [M * groups] floats for the backward pass, NULL = not stored.  y may be x.  Binary32 arithmetic, the mean
+ *   before the deviations, y rounded once.  eps > 0.
+ * rwkvq_layer_norm_backward: the gradients for dy: with xhat = (x - mean) rstd and g = dy (.) weight, per group
+ *   dx = rstd (g - mean_n(g) - xhat mean_n(g xhat)),  dweight = sum over rows of dy xhat,  dbias = sum of dy.
+ *   mean and rstd as the forward pass stored them.  dx (may be dy) or both of dweight and dbias may be NULL:
+ *   not computed.  dweight, dbias: DEVICE [groups * n] floats, overwritten.  workspace: DEVICE,
+ *   rwkvq_layer_norm_backward_workspace_size(M, groups, n) bytes, contents irrelevant on entry and undefined on
+ *   exit.  Sums in a fixed order: the same bits every time.
+ * x, y, dx, dy, workspace 16-byte aligned, floats 4.  Rows whose n and strides are multiples of 16 bytes load and
+ *   store 16 bytes at a time.  Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, eps), RWKVQ_ERR_SHAPE (M,
+ *   groups or n < 1, groups * n > 2^24, a stride below groups * n, M * stride > 2^40), RWKVQ_ERR_ALIGN, RWKVQ_ERR_DEVICE. */
+int rwkvq_layer_norm(const void* x, int x_dtype, int M, int groups, int n, long long x_stride, const float* weight,
+                     const float* bias, double eps, void* y, long long y_stride, float* mean, float* rstd, void* stream);
+size_t rwkvq_layer_norm_backward_workspace_size(int M, int groups, int n);
+int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x, long long x_stride, int x_dtype, int M,
+                              int groups, int n, const float* weight, const float* mean, const float* rstd, void* dx,
+                              long long dx_stride, float* dweight, float* dbias, void* workspace, void* stream);
+
+/* rwkvq_linear_attention: the recurrence of a multi-head block, with a decay for each head.  Per sequence and head, with
+ *   r, k, v rows of head_dim values and a state S of head_dim x head_dim floats (row: channel of k, column: channel of v),
+ *     out_t = r_t (S_{t-1} + diag(u) k_t^T v_t),      S_t = exp(-w) S_{t-1} + k_t^T v_t:
+ *   token i < t has the weight exp(-(t-1-i) w) in out_t as in rwkvq_wkv, the current one the bonus u.
+ *   `heads` (HOST) says which rows belong together: r, k, v, out: n_tokens rows (x_dtype, fp16 or bf16) of n_heads
+ *   heads of head_dim values, r_stride .. out_stride elements apart (0 = n_heads * head_dim); sequence b is rows
+ *   offsets[b] .. offsets[b+1] - 1 (DEVICE, n_seqs + 1 entries, not descending; NULL: n_tokens / n_seqs rows each), of any
+ *   length, also none.  Rows of no sequence are not touched.  Offsets are read on the device when the work runs, and
+ *   limited to 0 .. n_tokens there.
+ *   state: the states in front of the sequences ([n_heads][head_dim][head_dim] floats per slot; NULL: zeros), state_out:
+ *   those behind them (may be `state`; NULL: not stored).  slots (DEVICE, n_seqs different entries; NULL: b itself) gives the slot
+ *   of each sequence in both; a sequence whose slot is not in 0 .. n_slots - 1 is left out: nothing of it is written.
+ *   w: DEVICE [n_heads] (positive forgets), u: DEVICE [n_heads][head_dim].  head_dim: a multiple of 8 up to 128.
+ *   Products of 16-bit values are exact and every sum is binary32; where a state or a weight that was computed meets the matrix cores it goes in
+ *   as a sum of two or three bf16 parts (17 bits for an output, 24 for a state).  The same bits every time.
+ *   workspace: DEVICE, rwkvq_linear_attention_workspace_size(heads) bytes (0 is possible: NULL then allowed).
+ * rwkvq_linear_attention_backward: the gradients.  dout like out (out_stride); dstate: gradient for the states behind the
+ *   sequences (NULL: zeros); dr, dk, dv like r, k, v with their strides; dw [n_heads] and du [n_heads][head_dim] floats,
+ *   summed over all sequences and overwritten; dstate_in: gradient for the states in front (NULL: not stored).  state as it
+ *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Gradients may not overlap inputs, except dstate_in = dstate.
+ * r, k, v, out, dout, dr, dk, dv, states, workspace 16-byte aligned; w, u, dw, du, offsets, slots 4; no call synchronises.
+ * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, head_dim), RWKVQ_ERR_SHAPE (a count below 1, n_tokens not a multiple
+ *   of n_seqs without offsets, a stride below n_heads * head_dim, more than 2^31 workgroups), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8),
+ *   RWKVQ_ERR_DEVICE. */
+typedef struct rwkvq_heads {
+    int32_t n_seqs, n_tokens;
+    int32_t n_heads, head_dim;
+    int32_t n_slots, reserved;
+    const int32_t* offsets;
+    const int32_t* slots;
+    int64_t r_stride, k_stride, v_stride, out_stride;
+} rwkvq_heads;
+size_t rwkvq_linear_attention_workspace_size(const rwkvq_heads* heads);
+int rwkvq_linear_attention(const rwkvq_heads* heads, const void* r, const void* k, const void* v, int x_dtype, const float* w,
+                           const float* u, const float* state, float* state_out, void* out, void* workspace, void* stream);
+size_t rwkvq_linear_attention_backward_workspace_size(const rwkvq_heads* heads);
+int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, const void* k, const void* v, const void* dout,
+                                    int x_dtype, const float* w, const float* u, const float* state, const float* dstate,
+                                    void* dr, void* dk, void* dv, float* dw, float* du, float* dstate_in, void* workspace,
+                                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_double, c_int, c_int32, c_longlong, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_double, c_int, c_int32, c_int64, c_longlong, c_size_t, c_void_p
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -23,7 +23,9 @@ EXPORTS = ["rwkvq_version", "rwkvq_status_string", "rwkvq_sq_prepack", "rwkvq_vq
            "rwkvq_linear_dispatch", "rwkvq_proxy_workspace_bytes", "rwkvq_proxy", "rwkvq_sq_encode",
            "rwkvq_vq_assign", "rwkvq_clip_mean", "rwkvq_mu_codebook", "rwkvq_token_shift_mix", "rwkvq_linear_dispatch_mixed",
            "rwkvq_wkv", "rwkvq_relu2", "rwkvq_sigmoid_gate", "rwkvq_linear_dispatch_post", "rwkvq_linear_dispatch_plan", "rwkvq_rkv_wkv", "rwkvq_proxy_static",
-           "rwkvq_set_option", "rwkvq_get_option", "rwkvq_proxy_workspace_size"]
+           "rwkvq_set_option", "rwkvq_get_option", "rwkvq_proxy_workspace_size", "rwkvq_layer_norm",
+           "rwkvq_layer_norm_backward_workspace_size", "rwkvq_layer_norm_backward", "rwkvq_linear_attention_workspace_size",
+           "rwkvq_linear_attention", "rwkvq_linear_attention_backward_workspace_size", "rwkvq_linear_attention_backward"]
 
 
 class rwkvq_mix_input(Structure):
@@ -47,6 +49,12 @@ class rwkvq_matrix(Structure):
                 ("bits", c_int32), ("group", c_int32),
                 ("vdim", c_int32), ("kbits", c_int32), ("block_rows", c_int32), ("block_cols", c_int32),
                 ("codes", c_void_p), ("scales", c_void_p), ("zeros", c_void_p), ("codebooks", c_void_p)]
+
+
+class rwkvq_heads(Structure):
+    _fields_ = [("n_seqs", c_int32), ("n_tokens", c_int32), ("n_heads", c_int32), ("head_dim", c_int32),
+                ("n_slots", c_int32), ("reserved", c_int32), ("offsets", c_void_p), ("slots", c_void_p),
+                ("r_stride", c_int64), ("k_stride", c_int64), ("v_stride", c_int64), ("out_stride", c_int64)]
 
 
 class RwkvqError(RuntimeError):
@@ -138,6 +146,22 @@ def lib() -> ctypes.CDLL:
         L.rwkvq_relu2.argtypes = [c_void_p, c_int, c_longlong, c_void_p, c_void_p]
         L.rwkvq_sigmoid_gate.restype = c_int
         L.rwkvq_sigmoid_gate.argtypes = [c_void_p, c_void_p, c_int, c_longlong, c_void_p, c_void_p]
+        L.rwkvq_layer_norm.restype = c_int
+        L.rwkvq_layer_norm.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_longlong, c_void_p, c_void_p, c_double, c_void_p,
+                                       c_longlong, c_void_p, c_void_p, c_void_p]
+        L.rwkvq_layer_norm_backward_workspace_size.restype = c_size_t
+        L.rwkvq_layer_norm_backward_workspace_size.argtypes = [c_int, c_int, c_int]
+        L.rwkvq_layer_norm_backward.restype = c_int
+        L.rwkvq_layer_norm_backward.argtypes = [c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p,
+                                                c_void_p, c_void_p, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.rwkvq_linear_attention_workspace_size.restype = c_size_t
+        L.rwkvq_linear_attention_workspace_size.argtypes = [c_void_p]
+        L.rwkvq_linear_attention.restype = c_int
+        L.rwkvq_linear_attention.argtypes = [c_void_p] * 4 + [c_int] + [c_void_p] * 7
+        L.rwkvq_linear_attention_backward_workspace_size.restype = c_size_t
+        L.rwkvq_linear_attention_backward_workspace_size.argtypes = [c_void_p]
+        L.rwkvq_linear_attention_backward.restype = c_int
+        L.rwkvq_linear_attention_backward.argtypes = [c_void_p] * 5 + [c_int] + [c_void_p] * 12
         _lib = L
     return _lib
 
@@ -547,4 +571,57 @@ class RkvWkvTable:
 def rwkvq_rkv_wkv(table: RkvWkvTable, w, u, state, out, x_dtype, y_dtype, stream=None, check=True):
     st = lib().rwkvq_rkv_wkv(table.mats, table.xs, table.ys, _ptr(w), _ptr(u), _ptr(state), _ptr(out), x_dtype, y_dtype,
                              _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_layer_norm(x, x_dtype, M, groups, n, weight, bias, eps, y, mean=None, rstd=None, x_stride=0, y_stride=0, stream=None,
+                     check=True):
+    st = lib().rwkvq_layer_norm(_ptr(x), x_dtype, M, groups, n, x_stride, _ptr(weight), _ptr(bias), eps, _ptr(y), y_stride,
+                                _ptr(mean), _ptr(rstd), _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_layer_norm_backward_workspace_size(M: int, groups: int, n: int) -> int:
+    return int(lib().rwkvq_layer_norm_backward_workspace_size(M, groups, n))
+
+
+def rwkvq_layer_norm_backward(dy, x, x_dtype, M, groups, n, weight, mean, rstd, dx, dweight, dbias, workspace, dy_stride=0,
+                              x_stride=0, dx_stride=0, stream=None, check=True):
+    st = lib().rwkvq_layer_norm_backward(_ptr(dy), dy_stride, _ptr(x), x_stride, x_dtype, M, groups, n, _ptr(weight), _ptr(mean),
+                                         _ptr(rstd), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                         _stream(stream))
+    return _check(st) if check else st
+
+
+class Heads:
+    """The host struct of the linear attention calls: which rows are a sequence, their heads, strides in elements (0 = densely
+    packed), and the slots of the states; reusable across calls.  offsets, slots: int32 tensors on the GPU, or None."""
+
+    def __init__(self, n_seqs: int, n_tokens: int, n_heads: int, head_dim: int, offsets=None, slots=None, n_slots: int = 0,
+                 r_stride: int = 0, k_stride: int = 0, v_stride: int = 0, out_stride: int = 0):
+        self.desc = rwkvq_heads(n_seqs, n_tokens, n_heads, head_dim, n_slots, 0, _ptr(offsets), _ptr(slots), r_stride, k_stride,
+                                v_stride, out_stride)
+        self.ref = ctypes.addressof(self.desc)
+        self.keep = (offsets, slots)
+
+
+def rwkvq_linear_attention_workspace_size(heads: Heads) -> int:
+    return int(lib().rwkvq_linear_attention_workspace_size(heads.ref))
+
+
+def rwkvq_linear_attention(heads: Heads, r, k, v, x_dtype, w, u, state, state_out, out, workspace, stream=None, check=True):
+    st = lib().rwkvq_linear_attention(heads.ref, _ptr(r), _ptr(k), _ptr(v), x_dtype, _ptr(w), _ptr(u), _ptr(state), _ptr(state_out),
+                                      _ptr(out), _ptr(workspace), _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_linear_attention_backward_workspace_size(heads: Heads) -> int:
+    return int(lib().rwkvq_linear_attention_backward_workspace_size(heads.ref))
+
+
+def rwkvq_linear_attention_backward(heads: Heads, r, k, v, dout, x_dtype, w, u, state, dstate, dr, dk, dv, dw, du, dstate_in,
+                                    workspace, stream=None, check=True):
+    st = lib().rwkvq_linear_attention_backward(heads.ref, _ptr(r), _ptr(k), _ptr(v), _ptr(dout), x_dtype, _ptr(w), _ptr(u),
+                                               _ptr(state), _ptr(dstate), _ptr(dr), _ptr(dk), _ptr(dv), _ptr(dw), _ptr(du),
+                                               _ptr(dstate_in), _ptr(workspace), _stream(stream))
     return _check(st) if check else st

@@ -562,4 +562,128 @@ int rwkvq_sigmoid_gate(const void* r, const void* y, int x_dtype, long long n, v
     return pointwise(1, r, y, x_dtype, n, out, stream);
 }
 
+static bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+// Sizes and strides of a layer norm call; a stride of 0 becomes groups * n.
+static int check_norm(int x_dtype, int M, int groups, int n, long long* strides, int n_strides) {
+    if (dense_dtype(x_dtype) < 0) return RWKVQ_ERR_UNSUPPORTED;
+    if (M < 1 || groups < 1 || n < 1 || (long long)groups * n > (1ll << 24)) return RWKVQ_ERR_SHAPE;
+    const long long wide = (long long)groups * n;
+    if ((long long)M * groups > 0x7FFFFFFFll) return RWKVQ_ERR_SHAPE;
+    for (int i = 0; i < n_strides; ++i) {
+        if (strides[i] == 0) strides[i] = wide;
+        if (strides[i] < wide || strides[i] > (1ll << 40) / M) return RWKVQ_ERR_SHAPE;
+    }
+    return RWKVQ_OK;
+}
+
+int rwkvq_layer_norm(const void* x, int x_dtype, int M, int groups, int n, long long x_stride, const float* weight,
+                     const float* bias, double eps, void* y, long long y_stride, float* mean, float* rstd, void* stream) {
+    if (!x || !y) return RWKVQ_ERR_NULL;
+    long long strides[2] = {x_stride, y_stride};
+    const int st = check_norm(x_dtype, M, groups, n, strides, 2);
+    if (st != RWKVQ_OK) return st;
+    if (!((float)eps > 0.0f && eps < 1e30)) return RWKVQ_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(y) || !aligned4(weight) || !aligned4(bias) || !aligned4(mean) || !aligned4(rstd))
+        return RWKVQ_ERR_ALIGN;
+    NormDev p{};
+    p.x = x; p.y = y; p.weight = weight; p.bias = bias; p.mean = mean; p.rstd = rstd;
+    p.x_stride = strides[0]; p.y_stride = strides[1];
+    p.M = M; p.groups = groups; p.n = n; p.eps = (float)eps;
+    return launch_norm(p, dense_dtype(x_dtype), (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+size_t rwkvq_layer_norm_backward_workspace_size(int M, int groups, int n) {
+    return check_norm(RWKVQ_F32, M, groups, n, nullptr, 0) == RWKVQ_OK ? norm_backward_workspace_bytes(M, groups, n) : 0;
+}
+
+int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x, long long x_stride, int x_dtype, int M, int groups,
+                              int n, const float* weight, const float* mean, const float* rstd, void* dx, long long dx_stride,
+                              float* dweight, float* dbias, void* workspace, void* stream) {
+    if (!dy || !x || !mean || !rstd || !workspace || !dweight != !dbias || (!dx && !dweight)) return RWKVQ_ERR_NULL;
+    long long strides[3] = {dy_stride, x_stride, dx_stride};
+    const int st = check_norm(x_dtype, M, groups, n, strides, 3);
+    if (st != RWKVQ_OK) return st;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(dx) || !aligned16(workspace) || !aligned4(weight) || !aligned4(mean) ||
+        !aligned4(rstd) || !aligned4(dweight) || !aligned4(dbias))
+        return RWKVQ_ERR_ALIGN;
+    NormDev p{};
+    p.dy = dy; p.x = x; p.weight = weight; p.mean = (float*)mean; p.rstd = (float*)rstd;
+    p.dx = dx; p.dweight = dweight; p.dbias = dbias; p.partial = (float*)workspace;
+    p.dy_stride = strides[0]; p.x_stride = strides[1]; p.dx_stride = strides[2];
+    p.M = M; p.groups = groups; p.n = n;
+    return launch_norm_backward(p, dense_dtype(x_dtype), (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+// The host struct of the attention calls, checked and translated.
+static int check_heads(const rwkvq_heads* in, HeadsDev* h) {
+    if (!in) return RWKVQ_ERR_NULL;
+    if (in->n_seqs < 1 || in->n_tokens < 1 || in->n_heads < 1 || in->head_dim < 1) return RWKVQ_ERR_SHAPE;
+    if (in->head_dim % 8 != 0 || in->head_dim > 128) return RWKVQ_ERR_UNSUPPORTED;
+    if (in->slots && in->n_slots < 1) return RWKVQ_ERR_SHAPE;
+    if (!in->offsets && in->n_tokens % in->n_seqs != 0) return RWKVQ_ERR_SHAPE;
+    const long long wide = (long long)in->n_heads * in->head_dim;
+    // the work of a call goes out as at most eight workgroups per head and 16 tokens begun
+    if (wide > (1 << 24) || (double)in->n_heads * 8.0 * (in->n_tokens / 16.0 + in->n_seqs) > 2147483647.0) return RWKVQ_ERR_SHAPE;
+    const int64_t given[4] = {in->r_stride, in->k_stride, in->v_stride, in->out_stride};
+    long long stride[4];
+    for (int i = 0; i < 4; ++i) {
+        stride[i] = given[i] ? given[i] : wide;
+        if (stride[i] < wide || stride[i] > (1ll << 40) / in->n_tokens) return RWKVQ_ERR_SHAPE;
+        if (stride[i] % 8 != 0) return RWKVQ_ERR_ALIGN;
+    }
+    if (!aligned4(in->offsets) || !aligned4(in->slots)) return RWKVQ_ERR_ALIGN;
+    *h = HeadsDev{};
+    h->n_seqs = in->n_seqs; h->n_tokens = in->n_tokens; h->H = in->n_heads; h->D = in->head_dim; h->n_slots = in->n_slots;
+    h->offsets = in->offsets; h->slots = in->slots;
+    h->r_stride = stride[0]; h->k_stride = stride[1]; h->v_stride = stride[2]; h->out_stride = stride[3];
+    return RWKVQ_OK;
+}
+
+size_t rwkvq_linear_attention_workspace_size(const rwkvq_heads* heads) {
+    HeadsDev h;
+    return check_heads(heads, &h) == RWKVQ_OK ? attention_workspace_bytes(h) : 0;
+}
+
+int rwkvq_linear_attention(const rwkvq_heads* heads, const void* r, const void* k, const void* v, int x_dtype, const float* w,
+                           const float* u, const float* state, float* state_out, void* out, void* workspace, void* stream) {
+    if (!heads || !r || !k || !v || !w || !u || !out) return RWKVQ_ERR_NULL;
+    int st;
+    if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK) return st;
+    HeadsDev h;
+    if ((st = check_heads(heads, &h)) != RWKVQ_OK) return st;
+    if (!workspace && attention_workspace_bytes(h) > 0) return RWKVQ_ERR_NULL;
+    if (!aligned16(r) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state) || !aligned16(state_out) ||
+        !aligned16(workspace) || !aligned4(w) || !aligned4(u))
+        return RWKVQ_ERR_ALIGN;
+    h.r = (const uint16_t*)r; h.k = (const uint16_t*)k; h.v = (const uint16_t*)v; h.out = (uint16_t*)out;
+    h.w = w; h.u = u; h.state = state; h.state_out = state_out; h.partial = (float*)workspace;
+    return launch_attention(h, x_dtype == RWKVQ_F16 ? DT_F16 : DT_BF16, (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+size_t rwkvq_linear_attention_backward_workspace_size(const rwkvq_heads* heads) {
+    HeadsDev h;
+    return check_heads(heads, &h) == RWKVQ_OK ? attention_backward_workspace_bytes(h) : 0;
+}
+
+int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, const void* k, const void* v, const void* dout,
+                                    int x_dtype, const float* w, const float* u, const float* state, const float* dstate, void* dr,
+                                    void* dk, void* dv, float* dw, float* du, float* dstate_in, void* workspace, void* stream) {
+    if (!heads || !r || !k || !v || !dout || !w || !u || !dr || !dk || !dv || !dw || !du || !workspace) return RWKVQ_ERR_NULL;
+    int st;
+    if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK) return st;
+    HeadsDev h;
+    if ((st = check_heads(heads, &h)) != RWKVQ_OK) return st;
+    if (!aligned16(r) || !aligned16(k) || !aligned16(v) || !aligned16(dout) || !aligned16(state) || !aligned16(dstate) ||
+        !aligned16(dr) || !aligned16(dk) || !aligned16(dv) || !aligned16(dstate_in) || !aligned16(workspace) || !aligned4(w) ||
+        !aligned4(u) || !aligned4(dw) || !aligned4(du))
+        return RWKVQ_ERR_ALIGN;
+    h.r = (const uint16_t*)r; h.k = (const uint16_t*)k; h.v = (const uint16_t*)v; h.dout = (const uint16_t*)dout;
+    h.w = w; h.u = u; h.state = state; h.dstate = dstate;
+    h.dr = (uint16_t*)dr; h.dk = (uint16_t*)dk; h.dv = (uint16_t*)dv; h.dw = dw; h.du = du; h.dstate_in = dstate_in;
+    h.partial = (float*)workspace;
+    return launch_attention_backward(h, x_dtype == RWKVQ_F16 ? DT_F16 : DT_BF16, (hipStream_t)stream) == hipSuccess ? RWKVQ_OK
+                                                                                                                : RWKVQ_ERR_DEVICE;
+}
+
 }  // extern "C"

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 
 namespace rwkvq {
@@ -214,6 +215,37 @@ hipError_t launch_token_shift_mix(const void* x, const void* x_prev, int dt, int
 hipError_t launch_wkv(const void* r, const void* k, const void* v, int dt, int M, int d, const float* w, const float* u,
                       float* state, void* out, hipStream_t s);
 hipError_t launch_pointwise(int op, const void* x, const void* y, int dt, long long n, void* out, hipStream_t s);
+
+// Layer norm, forward and backward (norm.hip).
+struct NormDev {
+    const void *x, *dy;
+    const float *weight, *bias;
+    void *y, *dx;
+    float *mean, *rstd, *dweight, *dbias, *partial;
+    long long x_stride, y_stride, dy_stride, dx_stride;
+    int M, groups, n;
+    float eps;
+};
+hipError_t launch_norm(const NormDev& p, int dt, hipStream_t s);
+size_t norm_backward_workspace_bytes(int M, int groups, int n);
+hipError_t launch_norm_backward(const NormDev& p, int dt, hipStream_t s);
+// out0 / out1 = the sums over i < count of the columns below / from `half` of partial [count][width]
+hipError_t launch_sum_partials(const float* partial, int count, int width, int half, float* out0, float* out1, hipStream_t s);
+
+// Linear attention, forward and backward (attention.hip).
+struct HeadsDev {
+    int n_seqs, n_tokens, H, D, n_slots;
+    const int32_t *offsets, *slots;
+    long long r_stride, k_stride, v_stride, out_stride;
+    const uint16_t *r, *k, *v, *dout;
+    const float *w, *u, *state, *dstate;
+    uint16_t *out, *dr, *dk, *dv;
+    float *state_out, *dw, *du, *dstate_in, *partial;
+};
+size_t attention_workspace_bytes(const HeadsDev& h);
+hipError_t launch_attention(const HeadsDev& h, int dt, hipStream_t s);
+size_t attention_backward_workspace_bytes(const HeadsDev& h);
+hipError_t launch_attention_backward(const HeadsDev& h, int dt, hipStream_t s);
 
 // Lets a kernel take `bytes` of dynamic LDS (beyond 64 KB the runtime wants to be told), once per device; bit d of `raised`,
 // a static of the caller's, says that it was done on device d.
