@@ -461,7 +461,7 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  * rwkvq_linear_attention_backward: the gradients.  dout like out (out_stride); dstate: gradient for the states behind the
  *   sequences (NULL: zeros); dr, dk, dv like r, k, v with their strides; dw [n_heads] and du [n_heads][head_dim] floats,
  *   summed over all sequences and overwritten; dstate_in: gradient for the states in front (NULL: not stored).  state as it
- *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Gradients may not overlap inputs, except dstate_in = dstate.
+ *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Results may not overlap inputs.
  * r, k, v, out, dout, dr, dk, dv, states, workspace 16-byte aligned; w, u, dw, du, offsets, slots 4; no call synchronises.
  * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, head_dim), RWKVQ_ERR_SHAPE (a count below 1, n_tokens not a multiple
  *   of n_seqs without offsets, a stride below n_heads * head_dim, more than 2^31 workgroups), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8),

@@ -1,9 +1,8 @@
 // Linear attention with a decay for each head (include/rwkvq.h): out_t = r_t (S_{t-1} + diag(u) k_t^T v_t),
 // S_t = exp(-w) S_{t-1} + k_t^T v_t, and its gradients.  With G_t the gradient of S_t,
 //   G_{t-1} = exp(-w) G_t + r_t^T dout_t,  dr_t = dout_t S_{t-1}^T + u k_t (dout_t . v_t),  dk_t = v_t G_t^T + u r_t (dout_t . v_t),
-//   dv_t = k_t G_t + (r_t . u k_t) dout_t,  du = sum_t r_t k_t (dout_t . v_t),  dw = -sum_t exp(-w) <G_t, S_{t-1}>,
-// the last one as -sum_t r_t Z_{t-1} dout_t - <G_T, Z_T> with Z the derivative of S by -w, Z_t = exp(-w) (Z_{t-1} + S_{t-1}).
-#include "common.h"
+//   dv_t = k_t G_t + (r_t . u k_t) dout_t,  du = sum_t r_t k_t (dout_t . v_t),  dw = -sum_t exp(-w) <G_t, S_{t-1}>.
+#include "matrix_core.h"
 
 namespace rwkvq {
 
@@ -70,134 +69,709 @@ __global__ void __launch_bounds__(DP) attend_tokens_kernel(HeadsDev h) {
             if (c < D) h.state_out[at + (size_t)c * D + j] = S[c];
 }
 
-// dr, dw and du: forwards, thread c with row c of the state and of its derivative by -w.
-template <int DP, bool BF16>
-__global__ void __launch_bounds__(DP) attend_dr_kernel(HeadsDev h) {
-    __shared__ float vs[DP], ds[DP], sum[DP];
-    const int b = blockIdx.x / h.H, head = blockIdx.x % h.H, c = threadIdx.x, D = h.D, slot = slot_of(h, b);
-    float* const part = h.partial + (size_t)blockIdx.x * (D + 1);
-    if (slot < 0) {
-        if (c < D) part[c] = 0.0f;
-        if (c == 0) part[D] = 0.0f;
+// ---- chunks of 64 tokens on the matrix cores ---------------------------------------------------------------------------
+//
+// Inside a chunk, with S the state in front of it and l = exp(-w), token a (0-based) of a sweep has
+//   out_a = l^a q_a S + sum_{i<a} l^(a-1-i) (q_a . key_i) val_i + bonus,      S' = l^n S + sum_i l^(n-1-i) key_i^T val_i,
+// five products on matrix cores.  The same sweep, with other operands and for two of them from the last token to the first, is
+//   out:  q = r,    key = k,    val = v,    bonus (sum_c r u k) v
+//   dr:   q = dout, key = v,    val = k,    bonus (dout . v) u k,    the state transposed
+//   dk:   q = v,    key = dout, val = r,    bonus (v . dout) u r,    backwards, state G transposed
+//   dv:   q = k,    key = r,    val = dout, bonus (sum_c k u r) dout, backwards, state G.
+// The gradient of w comes out of the sweep for dr, which also carries Z, the derivative of its state by -w, within a segment:
+//   Z' = l^n (Z + n S) + sum_i (n-1-i) l^(n-1-i) key_i^T val_i,
+//   dw = -sum_a r_a . (l^a (Z^T + a S^T) dout_a + sum_{i<a} (a-1-i) l^(a-1-i) (dout_a . v_i) k_i) - <G, Z> at the segment's end:
+// every lag enters with its weight, nothing cancels.
+//
+// A workgroup of four wavefronts takes a segment of a sequence, one head and 64 channels of val.  Wavefront `wave` owns tokens
+// 16 wave .. + 15 of a chunk for scores and outputs (computed transposed: a lane holds one token and four consecutive channels or
+// earlier tokens, so that the scores of a token are the next product's operand without leaving their registers) and a quarter of
+// the state's rows for the update, which it publishes in LDS as the next chunk's operand.
+// Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
+// states as two bf16 parts (17 bits), the weighted keys of a state's update as three (24 bits), since states are binary32 results.
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+constexpr int kChunk = 64;                    // tokens
+constexpr int kVals = 64;                     // channels of val of a workgroup
+
+struct Segment { int b, idx, count, first_slot, t0, t1, a0, a1; };     // sequence, its place in it of how many; rows of both
+
+// Segment number `slot` of a call: `cut` tokens each, sequence b from slot offsets[b] / cut + b on (one too many at times: count <= idx).
+__device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int slot, int* found) {
+    Segment s;
+    if (h.offsets) {
+        for (int b = threadIdx.x; b < h.n_seqs; b += blockDim.x) {
+            const int t0 = min(max(h.offsets[b], 0), h.n_tokens), t1 = min(max(h.offsets[b + 1], t0), h.n_tokens);
+            const int from = t0 / cut + b;
+            if (slot >= from && slot <= t1 / cut + b) *found = b;
+        }
+        __syncthreads();
+        s.b = __builtin_amdgcn_readfirstlane(*found);
+        if (s.b < 0) { s.idx = 0; s.count = 0; return s; }
+        rows_of(h, s.b, s.t0, s.t1);
+        s.first_slot = s.t0 / cut + s.b;
+    } else {
+        const int len = h.n_tokens / h.n_seqs, per = (len + cut - 1) / cut;
+        s.b = slot / per;
+        s.t0 = s.b * len; s.t1 = s.t0 + len;
+        s.first_slot = s.b * per;
+    }
+    s.idx = slot - s.first_slot;
+    s.count = max(1, (s.t1 - s.t0 + cut - 1) / cut);
+    s.a0 = min(s.t0 + s.idx * cut, s.t1);
+    s.a1 = min(s.a0 + cut, s.t1);
+    return s;
+}
+
+template <int DP, bool BF16, bool GRADW> struct Lds {
+    static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
+    static constexpr int key = 0, val = key + kChunk * key_row, val_lo = val + kChunk * val_row;
+    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), state_lo = state + kVals * key_row;
+    static constexpr int z = state_lo + kVals * key_row, z_lo = z + kVals * key_row;
+    static constexpr int u_dot = GRADW ? z_lo + kVals * key_row : z, u_val = u_dot + 4 * DP, sums = u_val + 4 * kVals;
+    static constexpr int bytes = sums + 4 * (4 * kVals + 8);
+};
+
+// Two values as packed bf16 and what is left of them.
+__device__ __forceinline__ uint32_t split2(float& a, float& b) {
+    const uint32_t h = Elem<true>::pack(a, b);
+    a -= __uint_as_float(h << 16);
+    b -= __uint_as_float(h & 0xFFFF0000u);
+    return h;
+}
+// Four values as two bf16 parts, 17 bits.
+__device__ __forceinline__ void split4(const float4_t& x, uint2_t& hi, uint2_t& lo) {
+    float v[4] = {x[0], x[1], x[2], x[3]};
+    hi = uint2_t{split2(v[0], v[1]), split2(v[2], v[3])};
+    lo = uint2_t{Elem<true>::pack(v[0], v[1]), Elem<true>::pack(v[2], v[3])};
+}
+// Eight fp16 values as two bf16 parts, exact.
+__device__ __forceinline__ void split_f16(const uint4_t& x, uint4_t& hi, uint4_t& lo) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint2_t p = vq_split(x[i]);
+        hi[i] = p.x; lo[i] = p.y;
+    }
+}
+__device__ __forceinline__ uint2_t lds_transposed(const char* at) {
+    typedef __attribute__((address_space(3))) short4_t* Ptr;
+    return __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)at));
+}
+// The operand whose lane (n, g) holds column 16 c + n of rows 4 g .. + 3 and 16 + 4 g .. + 3 of a tile's rows 32 ks ..: the order of
+// tokens in which scores lie in their registers.
+template <int ROW>
+__device__ __forceinline__ uint4_t column_frag(const char* tile, int ks, int c, int n, int g) {
+    const char* const at = tile + (32 * ks + 4 * g + (n >> 2)) * ROW + 32 * c + 8 * (n & 3);
+    const uint2_t a = lds_transposed(at), b = lds_transposed(at + 16 * ROW);
+    return uint4_t{a.x, a.y, b.x, b.y};
+}
+
+// acc += weight * a state in memory; element (x, vt)[j] is key 16 (KT wave + x) + 4 g + j, val v0 + 16 vt + n.
+template <int KT>
+__device__ __forceinline__ void add_state(float4_t (&acc)[KT][4], const float* from, float weight, bool transposed, int D, int v0, int wave, int n, int g) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) {
+            const int key = 16 * (KT * wave + x) + 4 * g, val = v0 + 16 * vt + n;
+            if (val < D && key < D) {
+                if (transposed) acc[x][vt] += weight * *(const float4_t*)(from + (size_t)val * D + key);
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[x][vt][j] = fmaf(weight, from[(size_t)(key + j) * D + val], acc[x][vt][j]);
+            }
+        }
+}
+template <int KT>
+__device__ __forceinline__ void store_state(const float4_t (&acc)[KT][4], float* to, int D, int v0, int wave, int n, int g) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) {
+            const int key = 16 * (KT * wave + x) + 4 * g, val = v0 + 16 * vt + n;
+            if (val < D && key < D)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) to[(size_t)(key + j) * D + val] = acc[x][vt][j];
+        }
+}
+template <int KT>
+__device__ __forceinline__ void clear(float4_t (&acc)[KT][4]) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) acc[x][vt] = float4_t{0, 0, 0, 0};
+}
+
+// The state at a segment's front, in the order of the sweep.  `parts`: for each segment what it adds to a state; the one whose own
+// part nobody needs (the last one of the sweep) holds the state that the sequence begins with.
+template <int KT>
+__device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsDev& h, const Segment& s, int cut, const float* initial, const float* parts,
+                                            bool reverse, bool transposed, int head, int slot, float w, int v0, int wave, int n, int g) {
+    clear(acc);
+    const size_t size = (size_t)h.D * h.D;
+    if (s.count <= 1) {
+        if (initial) add_state(acc, initial + ((size_t)slot * h.H + head) * size, 1.0f, transposed, h.D, v0, wave, n, g);
         return;
     }
-    int t0, t1;
-    rows_of(h, b, t0, t1);
-    const size_t at = (((size_t)slot * h.H + head) * D + c) * D;
-    const bool live = c < D;
-    const float lam = expf(-h.w[head]), u = live ? h.u[head * D + c] : 0.0f;
-    float S[DP], Z[DP], dw = 0.0f, du = 0.0f;
-#pragma unroll
-    for (int j = 0; j < DP; ++j) { S[j] = live && j < D && h.state ? h.state[at + j] : 0.0f; Z[j] = 0.0f; }
-    for (int t = t0; t < t1; ++t) {
-        float r = 0.0f, k = 0.0f, v = 0.0f, d = 0.0f;
-        if (live) {
-            r = widen16<BF16>(h.r[t * h.r_stride + head * D + c]);
-            k = widen16<BF16>(h.k[t * h.k_stride + head * D + c]);
-            v = widen16<BF16>(h.v[t * h.v_stride + head * D + c]);
-            d = widen16<BF16>(h.dout[t * h.out_stride + head * D + c]);
-        }
-        __syncthreads();
-        vs[c] = v; ds[c] = d;
-        __syncthreads();
-        float g = 0.0f, z = 0.0f, now = 0.0f;
-#pragma unroll
-        for (int j = 0; j < DP; ++j) {
-            g = fmaf(ds[j], S[j], g);
-            z = fmaf(ds[j], Z[j], z);
-            now = fmaf(ds[j], vs[j], now);
-            Z[j] = lam * (Z[j] + S[j]);
-            S[j] = fmaf(lam, S[j], k * vs[j]);
-        }
-        dw = fmaf(r, z, dw);
-        du = fmaf(r * k, now, du);
-        if (live) h.dr[t * h.r_stride + head * D + c] = narrow16<BF16>(fmaf(u * k, now, g));
-    }
-    if (live && h.dstate)
-#pragma unroll
-        for (int j = 0; j < DP; ++j)
-            if (j < D) dw = fmaf(h.dstate[at + j], Z[j], dw);
-    sum[c] = dw;
-    __syncthreads();
-    if (c == 0) {
-        for (int i = 1; i < DP; ++i) dw += sum[i];
-        part[D] = -dw;
-    }
-    if (live) part[c] = du;
+    auto part = [&](int idx) { return parts + ((size_t)(s.first_slot + idx) * h.H + head) * size; };
+    const int away = reverse ? s.t1 - s.a1 : s.a0 - s.t0, held = reverse ? 0 : s.count - 1;
+    if (initial) add_state(acc, part(held), expf(-(float)away * w), transposed, h.D, v0, wave, n, g);
+    if (reverse)
+        for (int m = s.idx + 1; m < s.count; ++m) add_state(acc, part(m), expf(-(float)((m - s.idx - 1) * cut) * w), transposed, h.D, v0, wave, n, g);
+    else
+        for (int m = 0; m < s.idx; ++m) add_state(acc, part(m), expf(-(float)((s.idx - 1 - m) * cut) * w), transposed, h.D, v0, wave, n, g);
 }
 
-// dk, dv and the gradient of the state in front: backwards, thread j with row j and with column j of G.
+// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes per thread, rows of PER such chunks.
+template <int COUNT, int PER>
+__device__ __forceinline__ void fetch(uint4_t (&to)[COUNT], const uint16_t* base, long long stride, int col, int D, int first, int step, int nt) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const int c = threadIdx.x + 256 * i, row = c / PER, at = col + 8 * (c % PER);
+        to[i] = uint4_t{0, 0, 0, 0};
+        if (row < nt && at < D) to[i] = *(const uint4_t*)(base + (long long)(first + step * row) * stride + at);
+    }
+}
+template <int COUNT, int PER>
+__device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const int c = threadIdx.x + 256 * i;
+        *(uint4_t*)(tile + (c / PER) * row_bytes + 16 * (c % PER)) = from[i];
+    }
+}
+template <int COUNT, int PER>
+__device__ __forceinline__ void stage_split(const uint4_t (&from)[COUNT], char* hi, char* lo, int row_bytes) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const int c = threadIdx.x + 256 * i;
+        uint4_t a, b;
+        split_f16(from[i], a, b);
+        *(uint4_t*)(hi + (c / PER) * row_bytes + 16 * (c % PER)) = a;
+        *(uint4_t*)(lo + (c / PER) * row_bytes + 16 * (c % PER)) = b;
+    }
+}
+
+// Weights exp(-(nt - 1 - i) w) of a chunk's tokens i in the state behind it, in the order of column_frag.
+__device__ __forceinline__ void key_weights(float (&kw)[2][8], int nt, float w, int g) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
+            kw[ks][e] = i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
+        }
+}
+// A fragment of 16-bit keys times its weights as three bf16 parts.
+template <bool BF16>
+__device__ __forceinline__ void weighted_keys(const uint4_t& k, const float (&kw)[8], uint4_t (&out)[3]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t pair = k[i];
+        float a = widen16<BF16>((uint16_t)pair) * kw[2 * i], b = widen16<BF16>((uint16_t)(pair >> 16)) * kw[2 * i + 1];
+        out[0][i] = split2(a, b);
+        out[1][i] = split2(a, b);
+        out[2][i] = Elem<true>::pack(a, b);
+    }
+}
+
+// S = decay S + (weighted keys)^T val over a staged chunk; `parts`: of the weighted keys (3, or 2 where 17 bits do).
+template <int DP, bool BF16, class L, int KT>
+__device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const char* lds, const float (&kw)[2][8], const uint4_t (&vf)[2][4], const uint4_t (&vl)[2][4],
+                                             int wave, int n, int g) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+            uint4_t kp[3];
+            weighted_keys<BF16>(column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g), kw[ks], kp);
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+#pragma unroll
+                for (int part = 2; part >= 0; --part) S[x][vt] = mfma_bits<true>(kp[part], vf[ks][vt], S[x][vt]);
+                if (!BF16)
+#pragma unroll
+                    for (int part = 1; part >= 0; --part) S[x][vt] = mfma_bits<true>(kp[part], vl[ks][vt], S[x][vt]);
+            }
+        }
+}
+
+// What the segments of a direction add to a state, before their sweep; the segment whose part nobody needs keeps the initial state.
+struct LocalDev { const uint16_t *key, *val; long long key_stride, val_stride; const float* initial; float* parts; bool reverse; };
+struct LocalsDev { LocalDev dir[2]; };
+
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(DP) attend_dkv_kernel(HeadsDev h) {
-    __shared__ float vs[DP], ds[DP], rs[DP], ks[DP], ru[DP];
-    const int b = blockIdx.x / h.H, head = blockIdx.x % h.H, j = threadIdx.x, D = h.D, slot = slot_of(h, b);
+__global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
+    typedef Lds<DP, BF16, false> L;
+    constexpr int KT = DP / 64;
+    __shared__ __attribute__((aligned(16))) char lds[L::state];
+    __shared__ int found;
+    const LocalDev& p = locals.dir[blockIdx.y];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int slot_at = blockIdx.x / (h.H * blocks), head = blockIdx.x / blocks % h.H, v0 = blockIdx.x % blocks * kVals;
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    const Segment s = segment_of(h, cut, slot_at, &found);
+    if (s.idx >= s.count || s.count <= 1) return;
+    const int slot = slot_of(h, s.b), D = h.D;
     if (slot < 0) return;
-    int t0, t1;
-    rows_of(h, b, t0, t1);
-    const size_t at = ((size_t)slot * h.H + head) * D * D;
-    const bool live = j < D;
-    const float lam = expf(-h.w[head]), u = live ? h.u[head * D + j] : 0.0f;
-    for (int pass = 0; pass < 2; ++pass) {                   // 0: column j, for dv; 1: row j, for dk and the state
-        float G[DP];
-#pragma unroll
-        for (int c = 0; c < DP; ++c)
-            G[c] = live && c < D && h.dstate ? h.dstate[at + (pass ? (size_t)j * D + c : (size_t)c * D + j)] : 0.0f;
-        for (int t = t1 - 1; t >= t0; --t) {
-            float r = 0.0f, k = 0.0f, v = 0.0f, d = 0.0f;
-            if (live) {
-                r = widen16<BF16>(h.r[t * h.r_stride + head * D + j]);
-                k = widen16<BF16>(h.k[t * h.k_stride + head * D + j]);
-                v = widen16<BF16>(h.v[t * h.v_stride + head * D + j]);
-                d = widen16<BF16>(h.dout[t * h.out_stride + head * D + j]);
-            }
-            __syncthreads();
-            vs[j] = v; ds[j] = d; rs[j] = r; ks[j] = k; ru[j] = r * u * k;
-            __syncthreads();
-            float g = 0.0f, now = 0.0f;
-#pragma unroll
-            for (int c = 0; c < DP; ++c) {
-                g = fmaf(pass ? vs[c] : ks[c], G[c], g);
-                now = pass ? fmaf(ds[c], vs[c], now) : now + ru[c];
-                G[c] = fmaf(lam, G[c], pass ? r * ds[c] : rs[c] * d);
-            }
-            if (live) {
-                if (pass) h.dk[t * h.k_stride + head * D + j] = narrow16<BF16>(fmaf(u * r, now, g));
-                else h.dv[t * h.v_stride + head * D + j] = narrow16<BF16>(fmaf(now, d, g));
-            }
-        }
+    const float w = h.w[head];
+    float* const to = p.parts + ((size_t)slot_at * h.H + head) * D * D;
+    float4_t S[KT][4];
+    clear(S);
+    if (s.idx == (p.reverse ? 0 : s.count - 1)) {
+        if (!p.initial) return;
+        add_state(S, p.initial + ((size_t)slot * h.H + head) * D * D, 1.0f, false, D, v0, wave, n, g);
+        store_state(S, to, D, v0, wave, n, g);
+        return;
+    }
+    const uint16_t* const key = p.key + head * D;
+    const uint16_t* const val = p.val + head * D;
+    const int len = s.a1 - s.a0, begin = p.reverse ? s.a1 - 1 : s.a0, step = p.reverse ? -1 : 1;
+    uint4_t kr[DP / 32], vr[2];
+    fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, begin, step, min(kChunk, len));
+    fetch<2, 8>(vr, val, p.val_stride, v0, D, begin, step, min(kChunk, len));
+    float kw[2][8];
+    key_weights(kw, kChunk, w, g);
+    for (int c = 0; c < len; c += kChunk) {
+        const int nt = min(kChunk, len - c);
         __syncthreads();
-        if (pass && live && h.dstate_in)
+        stage<DP / 32, DP / 8>(kr, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<2, 8>(vr, lds + L::val, L::val_row);
+        else stage_split<2, 8>(vr, lds + L::val, lds + L::val_lo, L::val_row);
+        __syncthreads();
+        if (c + kChunk < len) {
+            const int next = begin + step * (c + kChunk), left = min(kChunk, len - c - kChunk);
+            fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, next, step, left);
+            fetch<2, 8>(vr, val, p.val_stride, v0, D, next, step, left);
+        }
+        if (nt < kChunk) key_weights(kw, nt, w, g);
+        uint4_t vf[2][4], vl[2][4];
 #pragma unroll
-            for (int c = 0; c < DP; ++c)
-                if (c < D) h.dstate_in[at + (size_t)j * D + c] = G[c];
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                vf[ks][vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
+                if (!BF16) vl[ks][vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
+            }
+        const float decay = expf(-(float)nt * w);
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) S[x][vt] *= decay;
+        update_state<DP, BF16, L>(S, lds, kw, vf, vl, wave, n, g);
+    }
+    store_state(S, to, D, v0, wave, n, g);
+}
+
+// Many segments per sequence: the state at each one's front in place of its part, a thread per element.
+__global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev locals, int cut) {
+    const LocalDev& p = locals.dir[blockIdx.z];
+    const int size = h.D * h.D, at = blockIdx.y * 256 + threadIdx.x;
+    if (at >= size) return;
+    for (long long item = blockIdx.x; item < (long long)h.n_seqs * h.H; item += gridDim.x) {
+        const int b = (int)(item / h.H), head = (int)(item % h.H);
+        int t0, t1;
+        rows_of(h, b, t0, t1);
+        const int count = max(1, (t1 - t0 + cut - 1) / cut), first = h.offsets ? t0 / cut + b : b * count;
+        if (count <= 1 || slot_of(h, b) < 0) continue;
+        float* const x = p.parts + ((size_t)first * h.H + head) * size + at;
+        const size_t stride = (size_t)h.H * size;
+        const float w = h.w[head], decay = expf(-(float)cut * w);
+        const float ragged = expf(-(float)(t1 - t0 - (count - 1) * cut) * w);      // of the last segment, which may be shorter
+        float run = p.initial ? x[(p.reverse ? 0 : count - 1) * stride] : 0.0f;
+        for (int i = 0; i < count; ++i) {
+            const int m = p.reverse ? count - 1 - i : i;
+            const float own = i < count - 1 ? x[m * stride] : 0.0f;
+            x[m * stride] = run;
+            run = fmaf(m == count - 1 ? ragged : decay, run, own);
+        }
     }
 }
 
-// dw [H] and du [H][D] from their parts, [n_seqs][H][D + 1].
-__global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, int parts) {
-    const int i = blockIdx.x * 256 + threadIdx.x, wide = h.D + 1;
-    if (i >= h.H * wide) return;
-    float s = 0.0f;
-    for (int p = 0; p < parts; ++p) s += h.partial[(size_t)p * h.H * wide + i];
-    if (i % wide == h.D) h.dw[i / wide] = s;
-    else h.du[i / wide * h.D + i % wide] = s;
+struct SweepDev {
+    const uint16_t *q, *key, *val, *x;
+    long long q_stride, key_stride, val_stride, out_stride, x_stride;
+    uint16_t* out;
+    const float *initial, *parts;       // of the sweep's own state
+    float* last;                        // where the state behind the sequence goes, or nullptr
+    bool reverse, transposed, u_in_dot;
+};
+struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* sums; int count; };
+
+template <int DP, bool BF16, bool GRADW>
+__device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, int cut, bool scanned, int slot_at, int head, int v0,
+                                              char* lds, int* found) {
+    typedef Lds<DP, BF16, GRADW> L;
+    constexpr int KS = DP / 32, KT = DP / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4, D = h.D;
+    if (tid == 0) *found = -1;
+    __syncthreads();
+    const Segment s = segment_of(h, cut, slot_at, found);
+    const int slot = s.idx < s.count ? slot_of(h, s.b) : -1;
+    float* const sums = GRADW ? all.sums + ((size_t)slot_at * h.H + head) * (D + 2) : nullptr;
+    if (slot < 0) {
+        if (GRADW) {
+            if (tid < kVals && v0 + tid < D) sums[v0 + tid] = 0.0f;
+            if (tid == 0) sums[D + v0 / kVals] = 0.0f;
+            if (tid == 0 && D <= kVals) sums[D + 1] = 0.0f;
+        }
+        return;
+    }
+    const float w = h.w[head];
+    const uint16_t* const q = p.q + head * D;
+    const uint16_t* const key = p.key + head * D;
+    const uint16_t* const val = p.val + head * D;
+    const int len = s.a1 - s.a0, begin = p.reverse ? s.a1 - 1 : s.a0, step = p.reverse ? -1 : 1, a = 16 * wave + n;
+
+    uint4_t kr[DP / 32], vr[2], qr[KS];
+    uint2_t xr[4];
+    auto fetch_chunk = [&](int c) {
+        const int at = begin + step * c, nt = min(kChunk, len - c);
+        fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, at, step, nt);
+        fetch<2, 8>(vr, val, p.val_stride, v0, D, at, step, nt);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            qr[i] = uint4_t{0, 0, 0, 0};
+            if (a < nt && 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(q + (long long)(at + step * a) * p.q_stride + 32 * i + 8 * g);
+        }
+        if constexpr (GRADW)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                xr[vt] = uint2_t{0, 0};
+                if (a < nt && v0 + 16 * vt + 4 * g < D)
+                    xr[vt] = *(const uint2_t*)(p.x + (long long)(at + step * a) * p.x_stride + head * D + v0 + 16 * vt + 4 * g);
+            }
+    };
+    if (len > 0) fetch_chunk(0);
+
+    float4_t S[KT][4], Z[GRADW ? KT : 1][4];
+    if (scanned && s.count > 1) {
+        clear(S);
+        add_state(S, p.parts + ((size_t)slot_at * h.H + head) * D * D, 1.0f, p.transposed, D, v0, wave, n, g);
+    } else {
+        start_state(S, h, s, cut, p.initial, p.parts, p.reverse, p.transposed, head, slot, w, v0, wave, n, g);
+    }
+    clear(Z);
+    // u, as the bonus needs it: with the channels of the dot, or with those of val
+    if (tid < DP) *(float*)(lds + L::u_dot + 4 * tid) = tid >= D ? 0.0f : p.u_in_dot ? h.u[head * D + tid] : 1.0f;
+    if (tid < kVals) *(float*)(lds + L::u_val + 4 * tid) = v0 + tid >= D ? 0.0f : p.u_in_dot ? 1.0f : h.u[head * D + v0 + tid];
+
+    // weights of pairs (token a, token 16 (wave - d) + 4 g + j), of the state in front, of keys in the state behind
+    float pw[4][4], kw[2][8];
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pw[d][j] = expf(-(float)max(16 * d + n - 1 - 4 * g - j, 0) * w);
+    const float front = expf(-(float)a * w);
+    key_weights(kw, kChunk, w, g);
+    float du[GRADW ? 16 : 1] = {}, dw = 0.0f;
+
+    auto publish = [&](const float4_t (&st)[KT][4], int hi, int lo) {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                uint2_t a, b;
+                split4(st[x][vt], a, b);
+                const int at = (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g);
+                *(uint2_t*)(lds + hi + at) = a;
+                *(uint2_t*)(lds + lo + at) = b;
+            }
+    };
+
+    for (int c = 0; c < len; c += kChunk) {
+        const int nt = min(kChunk, len - c);
+        publish(S, L::state, L::state_lo);
+        if constexpr (GRADW) publish(Z, L::z, L::z_lo);
+        stage<DP / 32, DP / 8>(kr, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<2, 8>(vr, lds + L::val, L::val_row);
+        else stage_split<2, 8>(vr, lds + L::val, lds + L::val_lo, L::val_row);
+        __syncthreads();
+        uint4_t qf[KS], qh[KS], ql[KS];
+        uint2_t xf[4];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            qf[i] = qr[i];
+            if constexpr (BF16) qh[i] = qf[i];
+            else split_f16(qf[i], qh[i], ql[i]);
+        }
+        if constexpr (GRADW)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) xf[vt] = xr[vt];
+        if (c + kChunk < len) fetch_chunk(c + kChunk);
+
+        // the state in front
+        float4_t out[4], zo[4];
+        auto from_state = [&](float4_t (&o)[4], int hi, int lo) {
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                o[vt] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    const int at = (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g);
+                    const uint4_t sh = *(const uint4_t*)(lds + hi + at), sl = *(const uint4_t*)(lds + lo + at);
+                    o[vt] = mfma_bits<true>(sl, qh[i], o[vt]);
+                    if (!BF16) o[vt] = mfma_bits<true>(sh, ql[i], o[vt]);
+                    o[vt] = mfma_bits<true>(sh, qh[i], o[vt]);
+                }
+                o[vt] *= front;
+            }
+        };
+        from_state(out, L::state, L::state_lo);
+        if constexpr (GRADW) {
+            from_state(zo, L::z, L::z_lo);
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) zo[vt] += (float)a * out[vt];
+        }
+
+        // scores of the wavefront's tokens with those up to them, and the dot of the bonus
+        uint4_t ph[2], pl[2], zh[2], zl[2];
+        float dot = 0.0f;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            float4_t sc = {0, 0, 0, 0};
+            float4_t zs = {0, 0, 0, 0};
+            if (it <= wave) {
+                uint4_t kf[KS];
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    kf[i] = *(const uint4_t*)(lds + L::key + (16 * it + n) * L::key_row + 2 * (32 * i + 8 * g));
+                    sc = mfma_bits<BF16>(kf[i], qf[i], sc);
+                }
+                if (it == wave) {
+#pragma unroll
+                    for (int i = 0; i < KS; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2_t u = *(const float2_t*)(lds + L::u_dot + 4 * (32 * i + 8 * g + 2 * e));
+                            dot = fmaf(widen16<BF16>((uint16_t)qf[i][e]) * u.x, widen16<BF16>((uint16_t)kf[i][e]), dot);
+                            dot = fmaf(widen16<BF16>((uint16_t)(qf[i][e] >> 16)) * u.y, widen16<BF16>((uint16_t)(kf[i][e] >> 16)), dot);
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int lag = 16 * (wave - it) + n - 1 - 4 * g - j;
+                    const float weight = wave - it == 0 ? pw[0][j] : wave - it == 1 ? pw[1][j] : wave - it == 2 ? pw[2][j] : pw[3][j];
+                    sc[j] = lag >= 0 ? sc[j] * weight : 0.0f;
+                    if (GRADW) zs[j] = sc[j] * (float)lag;
+                }
+            }
+            const int ks = it >> 1, e = 2 * (it & 1);
+            uint2_t hi, lo;
+            split4(sc, hi, lo);
+            ph[ks][e] = hi.x; ph[ks][e + 1] = hi.y; pl[ks][e] = lo.x; pl[ks][e + 1] = lo.y;
+            if (GRADW) {
+                split4(zs, hi, lo);
+                zh[ks][e] = hi.x; zh[ks][e + 1] = hi.y; zl[ks][e] = lo.x; zl[ks][e + 1] = lo.y;
+            }
+        }
+        dot += __shfl_xor(dot, 16, 64);
+        dot += __shfl_xor(dot, 32, 64);
+
+        uint4_t vf[2][4], vl[2][4];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                vf[ks][vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
+                if (!BF16) vl[ks][vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
+                if (2 * ks <= wave) {
+                    out[vt] = mfma_bits<true>(vf[ks][vt], pl[ks], out[vt]);
+                    if (!BF16) out[vt] = mfma_bits<true>(vl[ks][vt], ph[ks], out[vt]);
+                    out[vt] = mfma_bits<true>(vf[ks][vt], ph[ks], out[vt]);
+                    if (GRADW) {
+                        zo[vt] = mfma_bits<true>(vf[ks][vt], zl[ks], zo[vt]);
+                        if (!BF16) zo[vt] = mfma_bits<true>(vl[ks][vt], zh[ks], zo[vt]);
+                        zo[vt] = mfma_bits<true>(vf[ks][vt], zh[ks], zo[vt]);
+                    }
+                }
+            }
+        // the bonus; outputs
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) {
+            const uint2_t vh = *(const uint2_t*)(lds + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
+            const float4_t u = *(const float4_t*)(lds + L::u_val + 4 * (16 * vt + 4 * g));
+            float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
+            if (!BF16) {
+                const uint2_t l = *(const uint2_t*)(lds + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
+                v[0] += __uint_as_float(l.x << 16); v[1] += __uint_as_float(l.x & 0xFFFF0000u);
+                v[2] += __uint_as_float(l.y << 16); v[3] += __uint_as_float(l.y & 0xFFFF0000u);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float now = dot * v[j];
+                out[vt][j] = fmaf(now, u[j], out[vt][j]);
+                if (GRADW) {
+                    const float r = widen16<BF16>((uint16_t)(xf[vt][j >> 1] >> (16 * (j & 1))));
+                    du[4 * vt + j] = fmaf(r, now, du[4 * vt + j]);
+                    dw = fmaf(r, zo[vt][j], dw);
+                }
+            }
+            if (a < nt && v0 + 16 * vt + 4 * g < D) {
+                uint2_t o;
+                o.x = Elem<BF16>::pack(out[vt][0], out[vt][1]); o.y = Elem<BF16>::pack(out[vt][2], out[vt][3]);
+                *(uint2_t*)(p.out + (long long)(begin + step * (c + a)) * p.out_stride + head * D + v0 + 16 * vt + 4 * g) = o;
+            }
+        }
+        // the state behind
+        if (nt < kChunk) key_weights(kw, nt, w, g);
+        const float decay = expf(-(float)nt * w);
+        if constexpr (GRADW) {
+            float zw[2][8];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) zw[ks][e] = kw[ks][e] * (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
+#pragma unroll
+            for (int x = 0; x < KT; ++x)
+#pragma unroll
+                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + (float)nt * S[x][vt]);
+            update_state<DP, BF16, L>(Z, lds, zw, vf, vl, wave, n, g);
+        }
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) S[x][vt] *= decay;
+        update_state<DP, BF16, L>(S, lds, kw, vf, vl, wave, n, g);
+        __syncthreads();
+    }
+    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)slot * h.H + head) * D * D, D, v0, wave, n, g);
+    if constexpr (GRADW) {
+        // <G, Z> with G the gradient of the state at the segment's end, then the sums over lanes and wavefronts
+        float4_t G[KT][4];
+        if (scanned && s.count > 1) {
+            clear(G);
+            add_state(G, all.grad_parts + ((size_t)slot_at * h.H + head) * D * D, 1.0f, true, D, v0, wave, n, g);
+        } else {
+            start_state(G, h, s, cut, all.grad_initial, all.grad_parts, true, true, head, slot, w, v0, wave, n, g);
+        }
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dw = fmaf(G[x][vt][j], Z[x][vt][j], dw);
+#pragma unroll
+        for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
+        float* const across = (float*)(lds + L::sums);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+#pragma unroll
+            for (int off = 8; off; off >>= 1) du[i] += __shfl_xor(du[i], off, 64);
+            if (n == 0) across[kVals * wave + 16 * (i >> 2) + 4 * g + (i & 3)] = du[i];
+        }
+        if (lane == 0) across[4 * kVals + wave] = dw;
+        __syncthreads();
+        if (tid < kVals && v0 + tid < D) sums[v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
+        if (tid == 0) {
+            sums[D + v0 / kVals] = -(across[4 * kVals] + across[4 * kVals + 1] + across[4 * kVals + 2] + across[4 * kVals + 3]);
+            if (D <= kVals) sums[D + 1] = 0.0f;
+        }
+    }
 }
 
-size_t attention_workspace_bytes(const HeadsDev&) { return 0; }
-size_t attention_backward_workspace_bytes(const HeadsDev& h) { return (size_t)h.n_seqs * h.H * (h.D + 1) * sizeof(float); }
+template <int DP, bool BF16, bool GRADW>
+__global__ void __launch_bounds__(256) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int found;
+    const int slot_at = blockIdx.x / (h.H * blocks), head = blockIdx.x / blocks % h.H, v0 = blockIdx.x % blocks * kVals;
+    sweep_segment<DP, BF16, GRADW>(h, all.sweep[first + blockIdx.y], all, cut, scanned != 0, slot_at, head, v0, lds, &found);
+}
 
+// dw [H] and du [H][D] from their parts, [parts][H][D + 2], the gradient of w in two of them: sixteen threads an entry, in a fixed order.
+__global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float* sums, int parts) {
+    __shared__ float lds[16][17];
+    const int wide = h.D + 2, i = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4, head = i / wide, c = i % wide;
+    float s = 0.0f;
+    if (i < h.H * wide)
+        for (int p = part; p < parts; p += 16) s += sums[(size_t)p * h.H * wide + i] + (c == h.D ? sums[(size_t)p * h.H * wide + i + 1] : 0.0f);
+    lds[part][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (part != 0 || i >= h.H * wide) return;
+    for (int p = 1; p < 16; ++p) s += lds[p][threadIdx.x];
+    if (c < h.D) h.du[head * h.D + c] = s;
+    else if (c == h.D) h.dw[head] = s;
+}
+
+// How a call is cut: `cut` tokens a segment, `slots` segments at most; split: a sequence can have more than one; scan: one launch turns
+// the segments' parts into the states in front of them, otherwise each segment adds up those before it.
+struct Plan { int cut, slots, blocks; bool split, scan; size_t part_floats, sum_floats; };
+static Plan plan_of(const HeadsDev& h) {
+    Plan p;
+    p.blocks = (h.D + kVals - 1) / kVals;
+    const long long work = (long long)h.n_tokens * h.H * p.blocks;
+    p.cut = (int)std::max(128ll, (work / 512 + kChunk - 1) / kChunk * kChunk);
+    const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
+    p.split = len > p.cut;
+    p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
+    p.scan = len / p.cut > 12;
+    p.part_floats = p.split ? (size_t)p.slots * h.H * h.D * h.D : 0;
+    p.sum_floats = (size_t)p.slots * h.H * (h.D + 2);
+    return p;
+}
+static bool single_tokens(const HeadsDev& h) { return !h.offsets && h.n_tokens == h.n_seqs; }
+
+size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h).part_floats * sizeof(float); }
+size_t attention_backward_workspace_bytes(const HeadsDev& h) {
+    const Plan p = plan_of(h);
+    return (2 * p.part_floats + p.sum_floats) * sizeof(float);
+}
+
+template <int DP, bool BF16>
+static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Plan& p, int dirs, hipStream_t s) {
+    if (!p.split) return hipSuccess;
+    hipLaunchKernelGGL((attend_local_kernel<DP, BF16>), dim3((unsigned)(p.slots * h.H * p.blocks), dirs), dim3(256), 0, s, h, l, p.cut, p.blocks);
+    if (p.scan)
+        hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (h.D * h.D + 255) / 256, dirs), dim3(256), 0, s, h, l, p.cut);
+    return hipGetLastError();
+}
+template <int DP, bool BF16, bool GRADW>
+static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const Plan& p, int first, int count, hipStream_t s) {
+    static std::atomic<unsigned long long> raised{0};
+    constexpr int bytes = Lds<DP, BF16, GRADW>::bytes;
+    const hipError_t e = raise_lds((const void*)attend_sweep_kernel<DP, BF16, GRADW>, bytes, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRADW>), dim3((unsigned)(p.slots * h.H * p.blocks), count), dim3(256), bytes, s, h, all, p.cut, (int)p.scan,
+                       p.blocks, first);
+    return hipGetLastError();
+}
+
+template <int DP, bool BF16>
+static hipError_t forward(const HeadsDev& h, hipStream_t s) {
+    const Plan p = plan_of(h);
+    LocalsDev l{};
+    l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, h.partial, false};
+    const hipError_t e = launch_locals<DP, BF16>(h, l, p, 1, s);
+    if (e != hipSuccess) return e;
+    SweepsDev all{};
+    all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, true};
+    return launch_sweeps<DP, BF16, false>(h, all, p, 0, 1, s);
+}
 template <int DP, bool BF16>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
-    const dim3 grid((unsigned)(h.n_seqs * h.H));
-    hipLaunchKernelGGL((attend_dr_kernel<DP, BF16>), grid, dim3(DP), 0, s, h);
-    hipLaunchKernelGGL((attend_dkv_kernel<DP, BF16>), grid, dim3(DP), 0, s, h);
-    hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 1) + 255) / 256), dim3(256), 0, s, h, h.n_seqs);
+    const Plan p = plan_of(h);
+    float *const S = h.partial, *const G = S + p.part_floats, *const sums = G + p.part_floats;
+    LocalsDev l{};
+    l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, S, false};
+    l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true};
+    hipError_t e = launch_locals<DP, BF16>(h, l, p, 2, s);
+    if (e != hipSuccess) return e;
+    SweepsDev all{};
+    all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
+    all.sweep[1] = SweepDev{h.v, h.dout, h.r, nullptr, h.v_stride, h.out_stride, h.r_stride, h.k_stride, 0, h.dk, h.dstate, G, nullptr, true, true, false};
+    all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, true};
+    all.grad_initial = h.dstate; all.grad_parts = G; all.sums = sums;
+    if ((e = launch_sweeps<DP, BF16, true>(h, all, p, 0, 1, s)) != hipSuccess) return e;
+    if ((e = launch_sweeps<DP, BF16, false>(h, all, p, 1, 2, s)) != hipSuccess) return e;
+    hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 2) + 15) / 16), dim3(256), 0, s, h, sums, p.slots);
     return hipGetLastError();
 }
 template <bool BF16>
 static hipError_t attention(const HeadsDev& h, bool grad, hipStream_t s) {
-    const dim3 grid((unsigned)(h.n_seqs * h.H));
     if (grad) return h.D <= 64 ? backward<64, BF16>(h, s) : backward<128, BF16>(h, s);
+    if (!single_tokens(h)) return h.D <= 64 ? forward<64, BF16>(h, s) : forward<128, BF16>(h, s);
+    const dim3 grid((unsigned)(h.n_seqs * h.H));
     if (h.D <= 64) hipLaunchKernelGGL((attend_tokens_kernel<64, BF16>), grid, dim3(64), 0, s, h);
     else hipLaunchKernelGGL((attend_tokens_kernel<128, BF16>), grid, dim3(128), 0, s, h);
     return hipGetLastError();
