@@ -464,7 +464,7 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Results may not overlap inputs.
  * r, k, v, out, dout, dr, dk, dv, states, workspace 16-byte aligned; w, u, dw, du, offsets, slots 4; no call synchronises.
  * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, head_dim), RWKVQ_ERR_SHAPE (a count below 1, n_tokens not a multiple
- *   of n_seqs without offsets, a stride below n_heads * head_dim, more than 2^31 workgroups), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8),
+ *   of n_seqs without offsets, a stride below n_heads * head_dim or above 2^24, more than 2^31 workgroups), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8),
  *   RWKVQ_ERR_DEVICE. */
 typedef struct rwkvq_heads {
     int32_t n_seqs, n_tokens;

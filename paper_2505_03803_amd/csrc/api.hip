@@ -629,7 +629,7 @@ static int check_heads(const rwkvq_heads* in, HeadsDev* h) {
     long long stride[4];
     for (int i = 0; i < 4; ++i) {
         stride[i] = given[i] ? given[i] : wide;
-        if (stride[i] < wide || stride[i] > (1ll << 40) / in->n_tokens) return RWKVQ_ERR_SHAPE;
+        if (stride[i] < wide || stride[i] > (1 << 24)) return RWKVQ_ERR_SHAPE;         // byte offsets within 64 rows are 32-bit numbers
         if (stride[i] % 8 != 0) return RWKVQ_ERR_ALIGN;
     }
     if (!aligned4(in->offsets) || !aligned4(in->slots)) return RWKVQ_ERR_ALIGN;

@@ -126,24 +126,27 @@ __device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int sl
 template <int DP, bool BF16, bool GRADW> struct Lds {
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
     static constexpr int key = 0, val = key + kChunk * key_row, val_lo = val + kChunk * val_row;
-    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), state_lo = state + kVals * key_row;
-    static constexpr int z = state_lo + kVals * key_row, z_lo = z + kVals * key_row;
-    static constexpr int u_dot = GRADW ? z_lo + kVals * key_row : z, u_val = u_dot + 4 * DP, sums = u_val + 4 * kVals;
+    static constexpr int parts = GRADW ? 3 : 2, part = kVals * key_row;          // of a published state
+    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), z = state + parts * part;
+    static constexpr int u = z + (GRADW ? parts * part : 0), sums = u + 4 * DP;
     static constexpr int bytes = sums + 4 * (4 * kVals + 8);
 };
 
 // Two values as packed bf16 and what is left of them.
 __device__ __forceinline__ uint32_t split2(float& a, float& b) {
-    const uint32_t h = Elem<true>::pack(a, b);
+    uint32_t h = Elem<true>::pack(a, b);
+    asm("" : "+v"(h));                            // the compiler would convert a once more for its own half
     a -= __uint_as_float(h << 16);
     b -= __uint_as_float(h & 0xFFFF0000u);
     return h;
 }
-// Four values as two bf16 parts, 17 bits.
-__device__ __forceinline__ void split4(const float4_t& x, uint2_t& hi, uint2_t& lo) {
+// Four values as two or three bf16 parts, 17 or 24 bits.
+template <int PARTS>
+__device__ __forceinline__ void split4(const float4_t& x, uint2_t (&out)[PARTS]) {
     float v[4] = {x[0], x[1], x[2], x[3]};
-    hi = uint2_t{split2(v[0], v[1]), split2(v[2], v[3])};
-    lo = uint2_t{Elem<true>::pack(v[0], v[1]), Elem<true>::pack(v[2], v[3])};
+#pragma unroll
+    for (int i = 0; i < PARTS - 1; ++i) out[i] = uint2_t{split2(v[0], v[1]), split2(v[2], v[3])};
+    out[PARTS - 1] = uint2_t{Elem<true>::pack(v[0], v[1]), Elem<true>::pack(v[2], v[3])};
 }
 // Eight fp16 values as two bf16 parts, exact.
 __device__ __forceinline__ void split_f16(const uint4_t& x, uint4_t& hi, uint4_t& lo) {
@@ -166,20 +169,35 @@ __device__ __forceinline__ uint4_t column_frag(const char* tile, int ks, int c, 
     return uint4_t{a.x, a.y, b.x, b.y};
 }
 
-// acc += weight * a state in memory; element (x, vt)[j] is key 16 (KT wave + x) + 4 g + j, val v0 + 16 vt + n.
+// acc += weight * a state in memory; element (x, vt)[j] is key 16 (KT wave + x) + 4 g + j, val v0 + 16 vt + n.  All loads before the first use.
 template <int KT>
 __device__ __forceinline__ void add_state(float4_t (&acc)[KT][4], const float* from, float weight, bool transposed, int D, int v0, int wave, int n, int g) {
+    float4_t in[KT][4];
+    if (transposed) {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                const int key = 16 * (KT * wave + x) + 4 * g, val = v0 + 16 * vt + n;
+                in[x][vt] = *(const float4_t*)(from + (val < D && key < D ? val * D + key : 0));
+            }
+    } else {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                const int key = 16 * (KT * wave + x) + 4 * g, val = v0 + 16 * vt + n, at = val < D && key < D ? key * D + val : 0, row = val < D && key < D ? D : 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) in[x][vt][j] = from[at + j * row];
+            }
+    }
 #pragma unroll
     for (int x = 0; x < KT; ++x)
 #pragma unroll
         for (int vt = 0; vt < 4; ++vt) {
-            const int key = 16 * (KT * wave + x) + 4 * g, val = v0 + 16 * vt + n;
-            if (val < D && key < D) {
-                if (transposed) acc[x][vt] += weight * *(const float4_t*)(from + (size_t)val * D + key);
-                else
+            const bool live = 16 * (KT * wave + x) + 4 * g < D && v0 + 16 * vt + n < D;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[x][vt][j] = fmaf(weight, from[(size_t)(key + j) * D + val], acc[x][vt][j]);
-            }
+            for (int j = 0; j < 4; ++j) acc[x][vt][j] += live ? weight * in[x][vt][j] : 0.0f;
         }
 }
 template <int KT>
@@ -222,16 +240,37 @@ __device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsD
         for (int m = 0; m < s.idx; ++m) add_state(acc, part(m), expf(-(float)((s.idx - 1 - m) * cut) * w), transposed, h.D, v0, wave, n, g);
 }
 
-// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes per thread, rows of PER such chunks.
-template <int COUNT, int PER>
-__device__ __forceinline__ void fetch(uint4_t (&to)[COUNT], const uint16_t* base, long long stride, int col, int D, int first, int step, int nt) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        const int c = threadIdx.x + 256 * i, row = c / PER, at = col + 8 * (c % PER);
-        to[i] = uint4_t{0, 0, 0, 0};
-        if (row < nt && at < D) to[i] = *(const uint4_t*)(base + (long long)(first + step * row) * stride + at);
-    }
+// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes per thread, rows of PER such chunks.  Addresses are 32-bit offsets from
+// the chunk's lowest row.  What hangs over an end is loaded from inside instead (a chunk's last row, a head's first channels): later
+// tokens reach no output that is stored and have the weight 0 in the state (x is 0 there, which ends in sums over tokens), channels of
+// keys behind a head's last meet zeros of q.
+__device__ __forceinline__ uint32_t row_offset(int row, int nt, bool reverse, long long stride, int col) {
+    row = min(row, nt - 1);
+    return 2 * ((uint32_t)(reverse ? nt - 1 - row : row) * (uint32_t)stride + (uint32_t)col);
 }
+template <int COUNT, int PER>
+struct Rows {
+    uint4_t data[COUNT];
+    uint32_t offset[COUNT];                       // of a whole chunk
+    __device__ __forceinline__ void begin(long long stride, int width, bool reverse) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = threadIdx.x + 256 * i, col = 8 * (c % PER);
+            offset[i] = row_offset(c / PER, kChunk, reverse, stride, col < width ? col : 0);
+        }
+    }
+    __device__ __forceinline__ void fetch(const uint16_t* lowest, int nt, long long stride, int width, bool reverse) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            uint32_t at = offset[i];
+            if (nt < kChunk) {
+                const int c = threadIdx.x + 256 * i, col = 8 * (c % PER);
+                at = row_offset(c / PER, nt, reverse, stride, col < width ? col : 0);
+            }
+            data[i] = *(const uint4_t*)((const char*)lowest + at);
+        }
+    }
+};
 template <int COUNT, int PER>
 __device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
 #pragma unroll
@@ -252,14 +291,29 @@ __device__ __forceinline__ void stage_split(const uint4_t (&from)[COUNT], char* 
     }
 }
 
-// Weights exp(-(nt - 1 - i) w) of a chunk's tokens i in the state behind it, in the order of column_frag.
-__device__ __forceinline__ void key_weights(float (&kw)[2][8], int nt, float w, int g) {
+// Powers of exp(-w) from which a chunk's weights are made.  A lane meets tokens 16 it + 4 g + j: their weights are near[j] times a
+// power that the whole wavefront shares, so that four registers and a few scalars stand for them all.
+struct Powers {
+    float near[4];                                // 15 - 4 g - j
+    float far[4], whole;                          // 16 i; kChunk (uniform)
+    __device__ __forceinline__ void set(float w, int g) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+        for (int j = 0; j < 4; ++j) near[j] = expf(-(float)(15 - 4 * g - j) * w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) far[i] = uniform(expf(-(float)(16 * i) * w));
+        whole = uniform(expf(-(float)kChunk * w));
+    }
+    static __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+};
+// Weights exp(-(nt - 1 - i) w) of tokens i = 32 ks .. + 31 of a chunk in the state behind it, in the order of column_frag.
+__device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, int ks, int nt, float w, int g) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) kw[e] = pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)];
+    if (nt < kChunk)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
-            kw[ks][e] = i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
+            kw[e] = i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
         }
 }
 // A fragment of 16-bit keys times its weights as three bf16 parts.
@@ -275,25 +329,39 @@ __device__ __forceinline__ void weighted_keys(const uint4_t& k, const float (&kw
     }
 }
 
-// S = decay S + (weighted keys)^T val over a staged chunk; `parts`: of the weighted keys (3, or 2 where 17 bits do).
-template <int DP, bool BF16, class L, int KT>
-__device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const char* lds, const float (&kw)[2][8], const uint4_t (&vf)[2][4], const uint4_t (&vl)[2][4],
-                                             int wave, int n, int g) {
+// S += (weighted keys)^T val over 32 tokens of a staged chunk, the weighted keys as PARTS bf16 parts.
+template <bool BF16, class L, int PARTS, int KT>
+__device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const uint4_t (&keys)[KT], const float (&kw)[8], const uint4_t (&vf)[4], const uint4_t (&vl)[4]) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int x = 0; x < KT; ++x) {
+        uint4_t kp[3];
+        weighted_keys<BF16>(keys[x], kw, kp);
 #pragma unroll
-        for (int x = 0; x < KT; ++x) {
-            uint4_t kp[3];
-            weighted_keys<BF16>(column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g), kw[ks], kp);
+        for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
-#pragma unroll
-                for (int part = 2; part >= 0; --part) S[x][vt] = mfma_bits<true>(kp[part], vf[ks][vt], S[x][vt]);
-                if (!BF16)
-#pragma unroll
-                    for (int part = 1; part >= 0; --part) S[x][vt] = mfma_bits<true>(kp[part], vl[ks][vt], S[x][vt]);
+                S[x][vt] = mfma_bits<true>(kp[part], vf[vt], S[x][vt]);
+                if (!BF16 && part < PARTS - 1) S[x][vt] = mfma_bits<true>(kp[part], vl[vt], S[x][vt]);
             }
-        }
+    }
+}
+// The operands of 32 staged tokens: columns of val (fp16: two parts) and of the wavefront's share of the keys.
+template <bool BF16, class L, int KT>
+__device__ __forceinline__ void columns(const char* lds, int ks, int wave, int n, int g, uint4_t (&vf)[4], uint4_t (&vl)[4], uint4_t (&keys)[KT]) {
+#pragma unroll
+    for (int vt = 0; vt < 4; ++vt) {
+        vf[vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
+        if (!BF16) vl[vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
+    }
+#pragma unroll
+    for (int x = 0; x < KT; ++x) keys[x] = column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g);
+}
+template <int KT>
+__device__ __forceinline__ void scale(float4_t (&S)[KT][4], float by) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) S[x][vt] *= by;
 }
 
 // What the segments of a direction add to a state, before their sweep; the segment whose part nobody needs keeps the initial state.
@@ -325,41 +393,37 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
         store_state(S, to, D, v0, wave, n, g);
         return;
     }
-    const uint16_t* const key = p.key + head * D;
-    const uint16_t* const val = p.val + head * D;
-    const int len = s.a1 - s.a0, begin = p.reverse ? s.a1 - 1 : s.a0, step = p.reverse ? -1 : 1;
-    uint4_t kr[DP / 32], vr[2];
-    fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, begin, step, min(kChunk, len));
-    fetch<2, 8>(vr, val, p.val_stride, v0, D, begin, step, min(kChunk, len));
-    float kw[2][8];
-    key_weights(kw, kChunk, w, g);
+    const int len = s.a1 - s.a0;
+    Rows<DP / 32, DP / 8> kr;
+    Rows<2, 8> vr;
+    kr.begin(p.key_stride, D, p.reverse);
+    vr.begin(p.val_stride, D - v0, p.reverse);
+    auto fetch_chunk = [&](int c) {
+        const int nt = min(kChunk, len - c);
+        const long long lowest = p.reverse ? s.a1 - c - nt : s.a0 + c;
+        kr.fetch(p.key + head * D + lowest * p.key_stride, nt, p.key_stride, D, p.reverse);
+        vr.fetch(p.val + head * D + v0 + lowest * p.val_stride, nt, p.val_stride, D - v0, p.reverse);
+    };
+    fetch_chunk(0);
+    Powers pow;
+    pow.set(w, g);
     for (int c = 0; c < len; c += kChunk) {
         const int nt = min(kChunk, len - c);
         __syncthreads();
-        stage<DP / 32, DP / 8>(kr, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<2, 8>(vr, lds + L::val, L::val_row);
-        else stage_split<2, 8>(vr, lds + L::val, lds + L::val_lo, L::val_row);
+        stage<DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<2, 8>(vr.data, lds + L::val, L::val_row);
+        else stage_split<2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
-        if (c + kChunk < len) {
-            const int next = begin + step * (c + kChunk), left = min(kChunk, len - c - kChunk);
-            fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, next, step, left);
-            fetch<2, 8>(vr, val, p.val_stride, v0, D, next, step, left);
+        if (c + kChunk < len) fetch_chunk(c + kChunk);
+        scale(S, nt < kChunk ? expf(-(float)nt * w) : pow.whole);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            uint4_t vf[4], vl[4], keys[KT];
+            float kw[8];
+            key_weights(kw, pow, ks, nt, w, g);
+            columns<BF16, L>(lds, ks, wave, n, g, vf, vl, keys);
+            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
         }
-        if (nt < kChunk) key_weights(kw, nt, w, g);
-        uint4_t vf[2][4], vl[2][4];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int vt = 0; vt < 4; ++vt) {
-                vf[ks][vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
-                if (!BF16) vl[ks][vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
-            }
-        const float decay = expf(-(float)nt * w);
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int vt = 0; vt < 4; ++vt) S[x][vt] *= decay;
-        update_state<DP, BF16, L>(S, lds, kw, vf, vl, wave, n, g);
     }
     store_state(S, to, D, v0, wave, n, g);
 }
@@ -387,6 +451,13 @@ __global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev 
             run = fmaf(m == count - 1 ? ragged : decay, run, own);
         }
     }
+}
+
+// Value j of four packed 16-bit ones.
+template <bool BF16>
+__device__ __forceinline__ float half_of(const uint2_t& v, int j) {
+    const uint32_t pair = v[j >> 1];
+    return widen16<BF16>((uint16_t)(pair >> (16 * (j & 1))));
 }
 
 struct SweepDev {
@@ -419,29 +490,43 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
         return;
     }
     const float w = h.w[head];
-    const uint16_t* const q = p.q + head * D;
-    const uint16_t* const key = p.key + head * D;
-    const uint16_t* const val = p.val + head * D;
-    const int len = s.a1 - s.a0, begin = p.reverse ? s.a1 - 1 : s.a0, step = p.reverse ? -1 : 1, a = 16 * wave + n;
+    const int len = s.a1 - s.a0, a = 16 * wave + n;
+    auto lowest_row = [&](int c, int nt) { return (long long)(p.reverse ? s.a1 - c - nt : s.a0 + c); };
 
-    uint4_t kr[DP / 32], vr[2], qr[KS];
-    uint2_t xr[4];
+    Rows<DP / 32, DP / 8> kr;
+    Rows<2, 8> vr;
+    kr.begin(p.key_stride, D, p.reverse);
+    vr.begin(p.val_stride, D - v0, p.reverse);
+    uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
+    uint2_t xdr[4];
+    const uint32_t q_whole = row_offset(a, kChunk, p.reverse, p.q_stride, 8 * g), x_whole = GRADW ? row_offset(a, kChunk, p.reverse, p.x_stride, 0) : 0,
+                   o_whole = row_offset(a, kChunk, p.reverse, p.out_stride, 4 * g);
     auto fetch_chunk = [&](int c) {
-        const int at = begin + step * c, nt = min(kChunk, len - c);
-        fetch<DP / 32, DP / 8>(kr, key, p.key_stride, 0, D, at, step, nt);
-        fetch<2, 8>(vr, val, p.val_stride, v0, D, at, step, nt);
+        const int nt = min(kChunk, len - c);
+        const long long lowest = lowest_row(c, nt);
+        kr.fetch(p.key + head * D + lowest * p.key_stride, nt, p.key_stride, D, p.reverse);
+        vr.fetch(p.val + head * D + v0 + lowest * p.val_stride, nt, p.val_stride, D - v0, p.reverse);
+        const char* const qa = (const char*)(p.q + head * D + lowest * p.q_stride);
+        const uint32_t q_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.q_stride, 8 * g) : q_whole;
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             qr[i] = uint4_t{0, 0, 0, 0};
-            if (a < nt && 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(q + (long long)(at + step * a) * p.q_stride + 32 * i + 8 * g);
+            if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(qa + q_off + 64 * i);
         }
-        if constexpr (GRADW)
+        if constexpr (GRADW) {
+            const char* const xa = (const char*)(p.x + head * D + v0 + lowest * p.x_stride);
+            const uint32_t x_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.x_stride, 0) : x_whole;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                xr[i] = uint4_t{0, 0, 0, 0};
+                if (a < nt && (D == DP || v0 + 32 * i + 8 * g < D)) xr[i] = *(const uint4_t*)(xa + x_off + 16 * g + 64 * i);
+            }
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
-                xr[vt] = uint2_t{0, 0};
-                if (a < nt && v0 + 16 * vt + 4 * g < D)
-                    xr[vt] = *(const uint2_t*)(p.x + (long long)(at + step * a) * p.x_stride + head * D + v0 + 16 * vt + 4 * g);
+                xdr[vt] = uint2_t{0, 0};
+                if (a < nt && (D == DP || v0 + 16 * vt + 4 * g < D)) xdr[vt] = *(const uint2_t*)(xa + x_off + 8 * g + 32 * vt);
             }
+        }
     };
     if (len > 0) fetch_chunk(0);
 
@@ -453,187 +538,208 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
         start_state(S, h, s, cut, p.initial, p.parts, p.reverse, p.transposed, head, slot, w, v0, wave, n, g);
     }
     clear(Z);
-    // u, as the bonus needs it: with the channels of the dot, or with those of val
-    if (tid < DP) *(float*)(lds + L::u_dot + 4 * tid) = tid >= D ? 0.0f : p.u_in_dot ? h.u[head * D + tid] : 1.0f;
-    if (tid < kVals) *(float*)(lds + L::u_val + 4 * tid) = v0 + tid >= D ? 0.0f : p.u_in_dot ? 1.0f : h.u[head * D + v0 + tid];
+    // u, where the bonus needs it: with the channels of the dot, or with those of val
+    const int u0 = p.u_in_dot ? 0 : v0;
+    if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[head * D + u0 + tid] : 0.0f;
 
-    // weights of pairs (token a, token 16 (wave - d) + 4 g + j), of the state in front, of keys in the state behind
-    float pw[4][4], kw[2][8];
+    // weights of pairs of a tile's tokens a > i, and of those with an earlier tile's; of the state in front
+    Powers pow;
+    pow.set(w, g);
+    float same[4], earlier[4];
+    const float front = expf(-(float)a * w), in_tile = expf(-(float)n * w);
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) pw[d][j] = expf(-(float)max(16 * d + n - 1 - 4 * g - j, 0) * w);
-    const float front = expf(-(float)a * w);
-    key_weights(kw, kChunk, w, g);
+    for (int j = 0; j < 4; ++j) {
+        same[j] = expf(-(float)max(n - 1 - 4 * g - j, 0) * w);
+        earlier[j] = pow.near[j] * in_tile;
+    }
     float du[GRADW ? 16 : 1] = {}, dw = 0.0f;
 
-    auto publish = [&](const float4_t (&st)[KT][4], int hi, int lo) {
+    auto publish = [&](const float4_t (&st)[KT][4], int to) {
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
-                uint2_t a, b;
-                split4(st[x][vt], a, b);
-                const int at = (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g);
-                *(uint2_t*)(lds + hi + at) = a;
-                *(uint2_t*)(lds + lo + at) = b;
+                uint2_t v[L::parts];
+                split4(st[x][vt], v);
+#pragma unroll
+                for (int i = 0; i < L::parts; ++i) *(uint2_t*)(lds + to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
             }
     };
 
     for (int c = 0; c < len; c += kChunk) {
         const int nt = min(kChunk, len - c);
-        publish(S, L::state, L::state_lo);
-        if constexpr (GRADW) publish(Z, L::z, L::z_lo);
-        stage<DP / 32, DP / 8>(kr, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<2, 8>(vr, lds + L::val, L::val_row);
-        else stage_split<2, 8>(vr, lds + L::val, lds + L::val_lo, L::val_row);
+        publish(S, L::state);
+        if constexpr (GRADW) publish(Z, L::z);
+        stage<DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<2, 8>(vr.data, lds + L::val, L::val_row);
+        else stage_split<2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
-        uint4_t qf[KS], qh[KS], ql[KS];
-        uint2_t xf[4];
+        uint4_t qf[KS], qh[KS], ql[KS], xf[2], xl[2];
+        uint2_t xd[4];
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             qf[i] = qr[i];
             if constexpr (BF16) qh[i] = qf[i];
             else split_f16(qf[i], qh[i], ql[i]);
         }
-        if constexpr (GRADW)
+        if constexpr (GRADW) {
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) xf[vt] = xr[vt];
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (BF16) xf[i] = xr[i];
+                else split_f16(xr[i], xf[i], xl[i]);
+            }
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) xd[vt] = xdr[vt];
+        }
         if (c + kChunk < len) fetch_chunk(c + kChunk);
 
-        // the state in front
-        float4_t out[4], zo[4];
-        auto from_state = [&](float4_t (&o)[4], int hi, int lo) {
+        // the state in front, and its derivative
+        float4_t out[4];
+        auto from_state = [&](int vt, int from) {
+            float4_t o = {0, 0, 0, 0};
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) {
-                o[vt] = float4_t{0, 0, 0, 0};
+            for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const int at = (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g);
-                    const uint4_t sh = *(const uint4_t*)(lds + hi + at), sl = *(const uint4_t*)(lds + lo + at);
-                    o[vt] = mfma_bits<true>(sl, qh[i], o[vt]);
-                    if (!BF16) o[vt] = mfma_bits<true>(sh, ql[i], o[vt]);
-                    o[vt] = mfma_bits<true>(sh, qh[i], o[vt]);
+                for (int part = L::parts - 1; part >= 0; --part) {
+                    const uint4_t st = *(const uint4_t*)(lds + from + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                    o = mfma_bits<true>(st, qh[i], o);
+                    if (!BF16 && part < L::parts - 1) o = mfma_bits<true>(st, ql[i], o);
                 }
-                o[vt] *= front;
-            }
+            return front * o;
         };
-        from_state(out, L::state, L::state_lo);
-        if constexpr (GRADW) {
-            from_state(zo, L::z, L::z_lo);
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) zo[vt] += (float)a * out[vt];
+        for (int vt = 0; vt < 4; ++vt) {
+            out[vt] = from_state(vt, L::state);
+            if constexpr (GRADW) {
+                const float4_t z = from_state(vt, L::z) + (float)a * out[vt];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dw = fmaf(half_of<BF16>(xd[vt], j), z[j], dw);
+            }
         }
 
-        // scores of the wavefront's tokens with those up to them, and the dot of the bonus
-        uint4_t ph[2], pl[2], zh[2], zl[2];
+        // scores of the wavefront's tokens with those up to them; the bonus' dot is on their diagonal, or (with u) takes its place
+        uint4_t ph[2], pl[2];
         float dot = 0.0f;
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
-            float4_t sc = {0, 0, 0, 0};
-            float4_t zs = {0, 0, 0, 0};
+            const int ks = it >> 1, e = 2 * (it & 1);
+            uint2_t sp[2] = {{0, 0}, {0, 0}};
             if (it <= wave) {
+                float4_t sc = {0, 0, 0, 0};
                 uint4_t kf[KS];
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
                     kf[i] = *(const uint4_t*)(lds + L::key + (16 * it + n) * L::key_row + 2 * (32 * i + 8 * g));
                     sc = mfma_bits<BF16>(kf[i], qf[i], sc);
                 }
-                if (it == wave) {
+                if (it < wave) {
+                    const float far = wave - it == 1 ? pow.far[0] : wave - it == 2 ? pow.far[1] : pow.far[2];
 #pragma unroll
-                    for (int i = 0; i < KS; ++i)
+                    for (int j = 0; j < 4; ++j) sc[j] *= earlier[j] * far;
+                } else {
+                    if (p.u_in_dot) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2_t u = *(const float2_t*)(lds + L::u_dot + 4 * (32 * i + 8 * g + 2 * e));
-                            dot = fmaf(widen16<BF16>((uint16_t)qf[i][e]) * u.x, widen16<BF16>((uint16_t)kf[i][e]), dot);
-                            dot = fmaf(widen16<BF16>((uint16_t)(qf[i][e] >> 16)) * u.y, widen16<BF16>((uint16_t)(kf[i][e] >> 16)), dot);
-                        }
-                }
+                        for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int lag = 16 * (wave - it) + n - 1 - 4 * g - j;
-                    const float weight = wave - it == 0 ? pw[0][j] : wave - it == 1 ? pw[1][j] : wave - it == 2 ? pw[2][j] : pw[3][j];
-                    sc[j] = lag >= 0 ? sc[j] * weight : 0.0f;
-                    if (GRADW) zs[j] = sc[j] * (float)lag;
-                }
-            }
-            const int ks = it >> 1, e = 2 * (it & 1);
-            uint2_t hi, lo;
-            split4(sc, hi, lo);
-            ph[ks][e] = hi.x; ph[ks][e + 1] = hi.y; pl[ks][e] = lo.x; pl[ks][e + 1] = lo.y;
-            if (GRADW) {
-                split4(zs, hi, lo);
-                zh[ks][e] = hi.x; zh[ks][e + 1] = hi.y; zl[ks][e] = lo.x; zl[ks][e + 1] = lo.y;
-            }
-        }
-        dot += __shfl_xor(dot, 16, 64);
-        dot += __shfl_xor(dot, 32, 64);
-
-        uint4_t vf[2][4], vl[2][4];
+                            for (int c2 = 0; c2 < 2; ++c2) {
+                                const float4_t u = *(const float4_t*)(lds + L::u + 4 * (32 * i + 8 * g + 4 * c2));
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+                                for (int c4 = 0; c4 < 4; ++c4) {
+                                    const uint32_t qq = qf[i][2 * c2 + (c4 >> 1)], kk = kf[i][2 * c2 + (c4 >> 1)];
+                                    dot = fmaf(widen16<BF16>((uint16_t)(qq >> (16 * (c4 & 1)))) * u[c4], widen16<BF16>((uint16_t)(kk >> (16 * (c4 & 1)))), dot);
+                                }
+                            }
+                    } else {
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) {
-                vf[ks][vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
-                if (!BF16) vl[ks][vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
-                if (2 * ks <= wave) {
-                    out[vt] = mfma_bits<true>(vf[ks][vt], pl[ks], out[vt]);
-                    if (!BF16) out[vt] = mfma_bits<true>(vl[ks][vt], ph[ks], out[vt]);
-                    out[vt] = mfma_bits<true>(vf[ks][vt], ph[ks], out[vt]);
-                    if (GRADW) {
-                        zo[vt] = mfma_bits<true>(vf[ks][vt], zl[ks], zo[vt]);
-                        if (!BF16) zo[vt] = mfma_bits<true>(vl[ks][vt], zh[ks], zo[vt]);
-                        zo[vt] = mfma_bits<true>(vf[ks][vt], zh[ks], zo[vt]);
+                        for (int j = 0; j < 4; ++j) dot = 4 * g + j == n ? sc[j] : dot;
+                    }
+                    dot += __shfl_xor(dot, 16, 64);
+                    dot += __shfl_xor(dot, 32, 64);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sc[j] = 4 * g + j < n ? sc[j] * same[j] : 0.0f;
+                        if (!GRADW && p.u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
                     }
                 }
-            }
-        // the bonus; outputs
+                split4(sc, sp);
+                if constexpr (GRADW) {                                  // x . val of the same pairs, weighted with their lags
+                    float4_t xv = {0, 0, 0, 0};
 #pragma unroll
-        for (int vt = 0; vt < 4; ++vt) {
-            const uint2_t vh = *(const uint2_t*)(lds + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
-            const float4_t u = *(const float4_t*)(lds + L::u_val + 4 * (16 * vt + 4 * g));
-            float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
-            if (!BF16) {
-                const uint2_t l = *(const uint2_t*)(lds + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
-                v[0] += __uint_as_float(l.x << 16); v[1] += __uint_as_float(l.x & 0xFFFF0000u);
-                v[2] += __uint_as_float(l.y << 16); v[3] += __uint_as_float(l.y & 0xFFFF0000u);
-            }
+                    for (int i = 0; i < 2; ++i) {
+                        const int at = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
+                        const uint4_t v = *(const uint4_t*)(lds + L::val + at);
+                        if (!BF16) {
+                            const uint4_t vl = *(const uint4_t*)(lds + L::val_lo + at);
+                            xv = mfma_bits<true>(vl, xl[i], xv);
+                            xv = mfma_bits<true>(vl, xf[i], xv);
+                            xv = mfma_bits<true>(v, xl[i], xv);
+                        }
+                        xv = mfma_bits<true>(v, xf[i], xv);
+                    }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float now = dot * v[j];
-                out[vt][j] = fmaf(now, u[j], out[vt][j]);
-                if (GRADW) {
-                    const float r = widen16<BF16>((uint16_t)(xf[vt][j >> 1] >> (16 * (j & 1))));
-                    du[4 * vt + j] = fmaf(r, now, du[4 * vt + j]);
-                    dw = fmaf(r, zo[vt][j], dw);
+                    for (int j = 0; j < 4; ++j) dw = fmaf(sc[j] * (float)(a - 1 - (16 * it + 4 * g + j)), xv[j], dw);
                 }
             }
-            if (a < nt && v0 + 16 * vt + 4 * g < D) {
-                uint2_t o;
-                o.x = Elem<BF16>::pack(out[vt][0], out[vt][1]); o.y = Elem<BF16>::pack(out[vt][2], out[vt][3]);
-                *(uint2_t*)(p.out + (long long)(begin + step * (c + a)) * p.out_stride + head * D + v0 + 16 * vt + 4 * g) = o;
-            }
+            ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
         }
-        // the state behind
-        if (nt < kChunk) key_weights(kw, nt, w, g);
-        const float decay = expf(-(float)nt * w);
+
+        // what the scores weigh, and the state behind
+        const float decay = nt < kChunk ? expf(-(float)nt * w) : pow.whole;
         if constexpr (GRADW) {
-            float zw[2][8];
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) zw[ks][e] = kw[ks][e] * (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
 #pragma unroll
             for (int x = 0; x < KT; ++x)
 #pragma unroll
                 for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + (float)nt * S[x][vt]);
-            update_state<DP, BF16, L>(Z, lds, zw, vf, vl, wave, n, g);
         }
+        scale(S, decay);
 #pragma unroll
-        for (int x = 0; x < KT; ++x)
+        for (int ks = 0; ks < 2; ++ks) {
+            uint4_t vf[4], vl[4], keys[KT];
+            float kw[8];
+            key_weights(kw, pow, ks, nt, w, g);
+            columns<BF16, L>(lds, ks, wave, n, g, vf, vl, keys);
+            if (2 * ks <= wave) {
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) S[x][vt] *= decay;
-        update_state<DP, BF16, L>(S, lds, kw, vf, vl, wave, n, g);
+                for (int vt = 0; vt < 4; ++vt) {
+                    out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
+                    if (!BF16) out[vt] = mfma_bits<true>(vl[vt], ph[ks], out[vt]);
+                    out[vt] = mfma_bits<true>(vf[vt], ph[ks], out[vt]);
+                }
+            }
+            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
+            if constexpr (GRADW) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) kw[e] *= (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
+                update_state<BF16, L, 3>(Z, keys, kw, vf, vl);
+            }
+        }
+        // the bonus with u at the channels of val; the gradients of u and w
+        if (GRADW || !p.u_in_dot) {
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                const uint2_t vh = *(const uint2_t*)(lds + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
+                const float4_t u = *(const float4_t*)(lds + L::u + 4 * (16 * vt + 4 * g));
+                float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
+                if (!BF16) {
+                    const uint2_t l = *(const uint2_t*)(lds + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
+                    v[0] += __uint_as_float(l.x << 16); v[1] += __uint_as_float(l.x & 0xFFFF0000u);
+                    v[2] += __uint_as_float(l.y << 16); v[3] += __uint_as_float(l.y & 0xFFFF0000u);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float now = dot * v[j];
+                    out[vt][j] = fmaf(now, u[j], out[vt][j]);
+                    if (GRADW) du[4 * vt + j] = fmaf(half_of<BF16>(xd[vt], j), now, du[4 * vt + j]);
+                }
+            }
+        }
+        if (a < nt) {
+            char* const to = (char*)(p.out + head * D + v0 + lowest_row(c, nt) * p.out_stride) + (nt < kChunk ? row_offset(a, nt, p.reverse, p.out_stride, 4 * g) : o_whole);
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt)
+                if (D == DP || v0 + 16 * vt + 4 * g < D)
+                    *(uint2_t*)(to + 32 * vt) = uint2_t{Elem<BF16>::pack(out[vt][0], out[vt][1]), Elem<BF16>::pack(out[vt][2], out[vt][3])};
+        }
         __syncthreads();
     }
     if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)slot * h.H + head) * D * D, D, v0, wave, n, g);
@@ -672,7 +778,7 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
 }
 
 template <int DP, bool BF16, bool GRADW>
-__global__ void __launch_bounds__(256) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
+__global__ void __launch_bounds__(256, GRADW && DP > 64 ? 1 : 2) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     const int slot_at = blockIdx.x / (h.H * blocks), head = blockIdx.x / blocks % h.H, v0 = blockIdx.x % blocks * kVals;

@@ -261,7 +261,7 @@ def test_offsets_out_of_order_stay_inside():
 def test_rows_beyond_32_bits():
     """Rows that begin more than 2^31 elements behind the first: r, k, v and out are columns of one wide buffer."""
     torch = G.torch_()
-    T, H, D, stride = 67, 1, 64, 1 << 25
+    T, H, D, stride = 131, 1, 64, 1 << 24
     c = Case([T], H, D, "bf16", seed=9, offsets=False)
     buf = torch.empty(stride * (T - 1) + 8 * D, dtype=torch.int16, device="cuda")
     view = lambda i: torch.as_strided(buf, (T, D), (stride, 1), i * D)
