@@ -240,7 +240,7 @@ __device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsD
         for (int m = 0; m < s.idx; ++m) add_state(acc, part(m), expf(-(float)((s.idx - 1 - m) * cut) * w), transposed, h.D, v0, wave, n, g);
 }
 
-// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes per thread, rows of PER such chunks.  Addresses are 32-bit offsets from
+// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes for each of NT threads, rows of PER such chunks.  Addresses are 32-bit offsets from
 // the chunk's lowest row.  What hangs over an end is loaded from inside instead (a chunk's last row, a head's first channels): later
 // tokens reach no output that is stored and have the weight 0 in the state (x is 0 there, which ends in sums over tokens), channels of
 // keys behind a head's last meet zeros of q.
@@ -248,14 +248,14 @@ __device__ __forceinline__ uint32_t row_offset(int row, int nt, bool reverse, lo
     row = min(row, nt - 1);
     return 2 * ((uint32_t)(reverse ? nt - 1 - row : row) * (uint32_t)stride + (uint32_t)col);
 }
-template <int COUNT, int PER>
+template <int NT, int COUNT, int PER>
 struct Rows {
     uint4_t data[COUNT];
     uint32_t offset[COUNT];                       // of a whole chunk
     __device__ __forceinline__ void begin(long long stride, int width, bool reverse) {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int c = threadIdx.x + 256 * i, col = 8 * (c % PER);
+            const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
             offset[i] = row_offset(c / PER, kChunk, reverse, stride, col < width ? col : 0);
         }
     }
@@ -264,26 +264,26 @@ struct Rows {
         for (int i = 0; i < COUNT; ++i) {
             uint32_t at = offset[i];
             if (nt < kChunk) {
-                const int c = threadIdx.x + 256 * i, col = 8 * (c % PER);
+                const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
                 at = row_offset(c / PER, nt, reverse, stride, col < width ? col : 0);
             }
             data[i] = *(const uint4_t*)((const char*)lowest + at);
         }
     }
 };
-template <int COUNT, int PER>
+template <int NT, int COUNT, int PER>
 __device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
-        const int c = threadIdx.x + 256 * i;
+        const int c = threadIdx.x + NT * i;
         *(uint4_t*)(tile + (c / PER) * row_bytes + 16 * (c % PER)) = from[i];
     }
 }
-template <int COUNT, int PER>
+template <int NT, int COUNT, int PER>
 __device__ __forceinline__ void stage_split(const uint4_t (&from)[COUNT], char* hi, char* lo, int row_bytes) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
-        const int c = threadIdx.x + 256 * i;
+        const int c = threadIdx.x + NT * i;
         uint4_t a, b;
         split_f16(from[i], a, b);
         *(uint4_t*)(hi + (c / PER) * row_bytes + 16 * (c % PER)) = a;
@@ -345,14 +345,17 @@ __device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const uint4_t
             }
     }
 }
-// The operands of 32 staged tokens: columns of val (fp16: two parts) and of the wavefront's share of the keys.
-template <bool BF16, class L, int KT>
-__device__ __forceinline__ void columns(const char* lds, int ks, int wave, int n, int g, uint4_t (&vf)[4], uint4_t (&vl)[4], uint4_t (&keys)[KT]) {
+// The operands of 32 staged tokens: columns of val (fp16: two parts), and of a wavefront's share of the keys.
+template <bool BF16, class L>
+__device__ __forceinline__ void val_columns(const char* lds, int ks, int n, int g, uint4_t (&vf)[4], uint4_t (&vl)[4]) {
 #pragma unroll
     for (int vt = 0; vt < 4; ++vt) {
         vf[vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
         if (!BF16) vl[vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
     }
+}
+template <class L, int KT>
+__device__ __forceinline__ void key_columns(const char* lds, int ks, int wave, int n, int g, uint4_t (&keys)[KT]) {
 #pragma unroll
     for (int x = 0; x < KT; ++x) keys[x] = column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g);
 }
@@ -394,8 +397,8 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
         return;
     }
     const int len = s.a1 - s.a0;
-    Rows<DP / 32, DP / 8> kr;
-    Rows<2, 8> vr;
+    Rows<256, DP / 32, DP / 8> kr;
+    Rows<256, 2, 8> vr;
     kr.begin(p.key_stride, D, p.reverse);
     vr.begin(p.val_stride, D - v0, p.reverse);
     auto fetch_chunk = [&](int c) {
@@ -410,9 +413,9 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
     for (int c = 0; c < len; c += kChunk) {
         const int nt = min(kChunk, len - c);
         __syncthreads();
-        stage<DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<2, 8>(vr.data, lds + L::val, L::val_row);
-        else stage_split<2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
+        stage<256, DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<256, 2, 8>(vr.data, lds + L::val, L::val_row);
+        else stage_split<256, 2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
         if (c + kChunk < len) fetch_chunk(c + kChunk);
         scale(S, nt < kChunk ? expf(-(float)nt * w) : pow.whole);
@@ -421,7 +424,8 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
             uint4_t vf[4], vl[4], keys[KT];
             float kw[8];
             key_weights(kw, pow, ks, nt, w, g);
-            columns<BF16, L>(lds, ks, wave, n, g, vf, vl, keys);
+            val_columns<BF16, L>(lds, ks, n, g, vf, vl);
+            key_columns<L>(lds, ks, wave, n, g, keys);
             update_state<BF16, L, 3>(S, keys, kw, vf, vl);
         }
     }
@@ -470,43 +474,134 @@ struct SweepDev {
 };
 struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* sums; int count; };
 
-template <int DP, bool BF16, bool GRADW>
-__device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, int cut, bool scanned, int slot_at, int head, int v0,
-                                              char* lds, int* found) {
-    typedef Lds<DP, BF16, GRADW> L;
-    constexpr int KS = DP / 32, KT = DP / 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4, D = h.D;
-    if (tid == 0) *found = -1;
-    __syncthreads();
-    const Segment s = segment_of(h, cut, slot_at, found);
-    const int slot = s.idx < s.count ? slot_of(h, s.b) : -1;
-    float* const sums = GRADW ? all.sums + ((size_t)slot_at * h.H + head) * (D + 2) : nullptr;
-    if (slot < 0) {
-        if (GRADW) {
-            if (tid < kVals && v0 + tid < D) sums[v0 + tid] = 0.0f;
-            if (tid == 0) sums[D + v0 / kVals] = 0.0f;
-            if (tid == 0 && D <= kVals) sums[D + 1] = 0.0f;
-        }
-        return;
+// What both kinds of wavefront know of their segment.
+struct Place {
+    Segment s;
+    int slot_at, slot, head, v0, D, len, lane, wave, n, g;
+    float w;
+};
+// A thread's share of the staging of a sweep's chunks.
+template <int DP, bool BF16, class L>
+struct Staging {
+    Rows<512, DP / 64, DP / 8> key;
+    Rows<512, 1, 8> val;
+    __device__ __forceinline__ void begin(const SweepDev& p, const Place& at) {
+        key.begin(p.key_stride, at.D, p.reverse);
+        val.begin(p.val_stride, at.D - at.v0, p.reverse);
     }
-    const float w = h.w[head];
-    const int len = s.a1 - s.a0, a = 16 * wave + n;
-    auto lowest_row = [&](int c, int nt) { return (long long)(p.reverse ? s.a1 - c - nt : s.a0 + c); };
+    __device__ __forceinline__ void fetch(const SweepDev& p, const Place& at, int nt, long long lowest) {
+        key.fetch(p.key + at.head * at.D + lowest * p.key_stride, nt, p.key_stride, at.D, p.reverse);
+        val.fetch(p.val + at.head * at.D + at.v0 + lowest * p.val_stride, nt, p.val_stride, at.D - at.v0, p.reverse);
+    }
+    __device__ __forceinline__ void store(char* lds) const {
+        stage<512, DP / 64, DP / 8>(key.data, lds + L::key, L::key_row);
+        if constexpr (BF16) stage<512, 1, 8>(val.data, lds + L::val, L::val_row);
+        else stage_split<512, 1, 8>(val.data, lds + L::val, lds + L::val_lo, L::val_row);
+    }
+};
+__device__ __forceinline__ long long lowest_row(const SweepDev& p, const Place& at, int c, int nt) { return p.reverse ? at.s.a1 - c - nt : at.s.a0 + c; }
 
-    Rows<DP / 32, DP / 8> kr;
-    Rows<2, 8> vr;
-    kr.begin(p.key_stride, D, p.reverse);
-    vr.begin(p.val_stride, D - v0, p.reverse);
+// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of <G, Z>.
+template <int DP, bool BF16, bool GRADW>
+__device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
+    typedef Lds<DP, BF16, GRADW> L;
+    constexpr int KT = DP / 64;
+    const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
+    const float w = at.w;
+    const Segment& s = at.s;
+    Staging<DP, BF16, L> rows;
+    rows.begin(p, at);
+    if (at.len > 0) rows.fetch(p, at, min(kChunk, at.len), lowest_row(p, at, 0, min(kChunk, at.len)));
+    float4_t S[KT][4], Z[GRADW ? KT : 1][4];
+    auto load = [&](float4_t (&to)[KT][4], const float* initial, const float* parts, bool reverse, bool transposed) {
+        if (scanned && s.count > 1) {
+            clear(to);
+            add_state(to, parts + ((size_t)at.slot_at * h.H + at.head) * D * D, 1.0f, transposed, D, at.v0, wave, n, g);
+        } else {
+            start_state(to, h, s, cut, initial, parts, reverse, transposed, at.head, at.slot, w, at.v0, wave, n, g);
+        }
+    };
+    load(S, p.initial, p.parts, p.reverse, p.transposed);
+    clear(Z);
+    Powers pow;
+    pow.set(w, g);
+    auto publish = [&](const float4_t (&st)[KT][4], int to) {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                uint2_t v[L::parts];
+                split4(st[x][vt], v);
+#pragma unroll
+                for (int i = 0; i < L::parts; ++i) *(uint2_t*)(lds + to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
+            }
+    };
+    for (int c = 0; c < at.len; c += kChunk) {
+        const int nt = min(kChunk, at.len - c);
+        publish(S, L::state);
+        if constexpr (GRADW) publish(Z, L::z);
+        rows.store(lds);
+        __syncthreads();
+        if (c + kChunk < at.len) {
+            const int next = min(kChunk, at.len - c - kChunk);
+            rows.fetch(p, at, next, lowest_row(p, at, c + kChunk, next));
+        }
+        const float decay = nt < kChunk ? expf(-(float)nt * w) : pow.whole;
+        if constexpr (GRADW) {
+#pragma unroll
+            for (int x = 0; x < KT; ++x)
+#pragma unroll
+                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + (float)nt * S[x][vt]);
+        }
+        scale(S, decay);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            uint4_t vf[4], vl[4], keys[KT];
+            float kw[8];
+            key_weights(kw, pow, ks, nt, w, g);
+            val_columns<BF16, L>(lds, ks, n, g, vf, vl);
+            key_columns<L>(lds, ks, wave, n, g, keys);
+            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
+            if constexpr (GRADW) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) kw[e] *= (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
+                update_state<BF16, L, 3>(Z, keys, kw, vf, vl);
+            }
+        }
+        __syncthreads();
+    }
+    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
+    float dw = 0.0f;
+    if constexpr (GRADW) {                        // G: the gradient of the state at the segment's end
+        load(S, all.grad_initial, all.grad_parts, true, true);
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dw = fmaf(S[x][vt][j], Z[x][vt][j], dw);
+    }
+    return dw;
+}
+
+// The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
+template <int DP, bool BF16, bool GRADW>
+__device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRADW ? 16 : 1], char* lds) {
+    typedef Lds<DP, BF16, GRADW> L;
+    constexpr int KS = DP / 32;
+    const int wave = at.wave, n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
+    const float w = at.w;
+    Staging<DP, BF16, L> rows;
+    rows.begin(p, at);
     uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
     uint2_t xdr[4];
     const uint32_t q_whole = row_offset(a, kChunk, p.reverse, p.q_stride, 8 * g), x_whole = GRADW ? row_offset(a, kChunk, p.reverse, p.x_stride, 0) : 0,
                    o_whole = row_offset(a, kChunk, p.reverse, p.out_stride, 4 * g);
     auto fetch_chunk = [&](int c) {
-        const int nt = min(kChunk, len - c);
-        const long long lowest = lowest_row(c, nt);
-        kr.fetch(p.key + head * D + lowest * p.key_stride, nt, p.key_stride, D, p.reverse);
-        vr.fetch(p.val + head * D + v0 + lowest * p.val_stride, nt, p.val_stride, D - v0, p.reverse);
-        const char* const qa = (const char*)(p.q + head * D + lowest * p.q_stride);
+        const int nt = min(kChunk, at.len - c);
+        const long long lowest = lowest_row(p, at, c, nt);
+        rows.fetch(p, at, nt, lowest);
+        const char* const qa = (const char*)(p.q + at.head * D + lowest * p.q_stride);
         const uint32_t q_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.q_stride, 8 * g) : q_whole;
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
@@ -514,7 +609,7 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
             if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(qa + q_off + 64 * i);
         }
         if constexpr (GRADW) {
-            const char* const xa = (const char*)(p.x + head * D + v0 + lowest * p.x_stride);
+            const char* const xa = (const char*)(p.x + at.head * D + v0 + lowest * p.x_stride);
             const uint32_t x_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.x_stride, 0) : x_whole;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -528,51 +623,26 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
             }
         }
     };
-    if (len > 0) fetch_chunk(0);
-
-    float4_t S[KT][4], Z[GRADW ? KT : 1][4];
-    if (scanned && s.count > 1) {
-        clear(S);
-        add_state(S, p.parts + ((size_t)slot_at * h.H + head) * D * D, 1.0f, p.transposed, D, v0, wave, n, g);
-    } else {
-        start_state(S, h, s, cut, p.initial, p.parts, p.reverse, p.transposed, head, slot, w, v0, wave, n, g);
-    }
-    clear(Z);
+    if (at.len > 0) fetch_chunk(0);
     // u, where the bonus needs it: with the channels of the dot, or with those of val
-    const int u0 = p.u_in_dot ? 0 : v0;
-    if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[head * D + u0 + tid] : 0.0f;
+    const int u0 = p.u_in_dot ? 0 : v0, tid = threadIdx.x;
+    if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
 
     // weights of pairs of a tile's tokens a > i, and of those with an earlier tile's; of the state in front
-    Powers pow;
-    pow.set(w, g);
-    float same[4], earlier[4];
+    float same[4], earlier[4], far[3];
     const float front = expf(-(float)a * w), in_tile = expf(-(float)n * w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         same[j] = expf(-(float)max(n - 1 - 4 * g - j, 0) * w);
-        earlier[j] = pow.near[j] * in_tile;
+        earlier[j] = expf(-(float)(15 - 4 * g - j) * w) * in_tile;
     }
-    float du[GRADW ? 16 : 1] = {}, dw = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) far[i] = Powers::uniform(expf(-(float)(16 * i) * w));
+    float dw = 0.0f;
 
-    auto publish = [&](const float4_t (&st)[KT][4], int to) {
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int vt = 0; vt < 4; ++vt) {
-                uint2_t v[L::parts];
-                split4(st[x][vt], v);
-#pragma unroll
-                for (int i = 0; i < L::parts; ++i) *(uint2_t*)(lds + to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
-            }
-    };
-
-    for (int c = 0; c < len; c += kChunk) {
-        const int nt = min(kChunk, len - c);
-        publish(S, L::state);
-        if constexpr (GRADW) publish(Z, L::z);
-        stage<DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<2, 8>(vr.data, lds + L::val, L::val_row);
-        else stage_split<2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
+    for (int c = 0; c < at.len; c += kChunk) {
+        const int nt = min(kChunk, at.len - c);
+        rows.store(lds);
         __syncthreads();
         uint4_t qf[KS], qh[KS], ql[KS], xf[2], xl[2];
         uint2_t xd[4];
@@ -591,7 +661,7 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) xd[vt] = xdr[vt];
         }
-        if (c + kChunk < len) fetch_chunk(c + kChunk);
+        if (c + kChunk < at.len) fetch_chunk(c + kChunk);
 
         // the state in front, and its derivative
         float4_t out[4];
@@ -633,9 +703,9 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
                     sc = mfma_bits<BF16>(kf[i], qf[i], sc);
                 }
                 if (it < wave) {
-                    const float far = wave - it == 1 ? pow.far[0] : wave - it == 2 ? pow.far[1] : pow.far[2];
+                    const float tiles = wave - it == 1 ? far[0] : wave - it == 2 ? far[1] : far[2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sc[j] *= earlier[j] * far;
+                    for (int j = 0; j < 4; ++j) sc[j] *= earlier[j] * tiles;
                 } else {
                     if (p.u_in_dot) {
 #pragma unroll
@@ -666,10 +736,10 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
                     float4_t xv = {0, 0, 0, 0};
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int at = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
-                        const uint4_t v = *(const uint4_t*)(lds + L::val + at);
+                        const int from = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
+                        const uint4_t v = *(const uint4_t*)(lds + L::val + from);
                         if (!BF16) {
-                            const uint4_t vl = *(const uint4_t*)(lds + L::val_lo + at);
+                            const uint4_t vl = *(const uint4_t*)(lds + L::val_lo + from);
                             xv = mfma_bits<true>(vl, xl[i], xv);
                             xv = mfma_bits<true>(vl, xf[i], xv);
                             xv = mfma_bits<true>(v, xl[i], xv);
@@ -682,23 +752,11 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
             }
             ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
         }
-
-        // what the scores weigh, and the state behind
-        const float decay = nt < kChunk ? expf(-(float)nt * w) : pow.whole;
-        if constexpr (GRADW) {
-#pragma unroll
-            for (int x = 0; x < KT; ++x)
-#pragma unroll
-                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + (float)nt * S[x][vt]);
-        }
-        scale(S, decay);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uint4_t vf[4], vl[4], keys[KT];
-            float kw[8];
-            key_weights(kw, pow, ks, nt, w, g);
-            columns<BF16, L>(lds, ks, wave, n, g, vf, vl, keys);
             if (2 * ks <= wave) {
+                uint4_t vf[4], vl[4];
+                val_columns<BF16, L>(lds, ks, n, g, vf, vl);
 #pragma unroll
                 for (int vt = 0; vt < 4; ++vt) {
                     out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
@@ -706,14 +764,8 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
                     out[vt] = mfma_bits<true>(vf[vt], ph[ks], out[vt]);
                 }
             }
-            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
-            if constexpr (GRADW) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kw[e] *= (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
-                update_state<BF16, L, 3>(Z, keys, kw, vf, vl);
-            }
         }
-        // the bonus with u at the channels of val; the gradients of u and w
+        // the bonus with u at the channels of val; the gradient of u
         if (GRADW || !p.u_in_dot) {
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
@@ -734,7 +786,8 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
             }
         }
         if (a < nt) {
-            char* const to = (char*)(p.out + head * D + v0 + lowest_row(c, nt) * p.out_stride) + (nt < kChunk ? row_offset(a, nt, p.reverse, p.out_stride, 4 * g) : o_whole);
+            char* const to = (char*)(p.out + at.head * D + v0 + lowest_row(p, at, c, nt) * p.out_stride) +
+                             (nt < kChunk ? row_offset(a, nt, p.reverse, p.out_stride, 4 * g) : o_whole);
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
                 if (D == DP || v0 + 16 * vt + 4 * g < D)
@@ -742,47 +795,58 @@ __device__ __forceinline__ void sweep_segment(const HeadsDev& h, const SweepDev&
         }
         __syncthreads();
     }
-    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)slot * h.H + head) * D * D, D, v0, wave, n, g);
-    if constexpr (GRADW) {
-        // <G, Z> with G the gradient of the state at the segment's end, then the sums over lanes and wavefronts
-        float4_t G[KT][4];
-        if (scanned && s.count > 1) {
-            clear(G);
-            add_state(G, all.grad_parts + ((size_t)slot_at * h.H + head) * D * D, 1.0f, true, D, v0, wave, n, g);
-        } else {
-            start_state(G, h, s, cut, all.grad_initial, all.grad_parts, true, true, head, slot, w, v0, wave, n, g);
-        }
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int vt = 0; vt < 4; ++vt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) dw = fmaf(G[x][vt][j], Z[x][vt][j], dw);
-#pragma unroll
-        for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
-        float* const across = (float*)(lds + L::sums);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-#pragma unroll
-            for (int off = 8; off; off >>= 1) du[i] += __shfl_xor(du[i], off, 64);
-            if (n == 0) across[kVals * wave + 16 * (i >> 2) + 4 * g + (i & 3)] = du[i];
-        }
-        if (lane == 0) across[4 * kVals + wave] = dw;
-        __syncthreads();
-        if (tid < kVals && v0 + tid < D) sums[v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
-        if (tid == 0) {
-            sums[D + v0 / kVals] = -(across[4 * kVals] + across[4 * kVals + 1] + across[4 * kVals + 2] + across[4 * kVals + 3]);
-            if (D <= kVals) sums[D + 1] = 0.0f;
-        }
-    }
+    return dw;
 }
 
 template <int DP, bool BF16, bool GRADW>
-__global__ void __launch_bounds__(256, GRADW && DP > 64 ? 1 : 2) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
+__global__ void __launch_bounds__(512, GRADW || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
+    typedef Lds<DP, BF16, GRADW> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
-    const int slot_at = blockIdx.x / (h.H * blocks), head = blockIdx.x / blocks % h.H, v0 = blockIdx.x % blocks * kVals;
-    sweep_segment<DP, BF16, GRADW>(h, all.sweep[first + blockIdx.y], all, cut, scanned != 0, slot_at, head, v0, lds, &found);
+    const SweepDev& p = all.sweep[first + blockIdx.y];
+    const int tid = threadIdx.x, D = h.D;
+    Place at;
+    at.slot_at = blockIdx.x / (h.H * blocks); at.head = blockIdx.x / blocks % h.H; at.v0 = blockIdx.x % blocks * kVals; at.D = D;
+    at.lane = tid & 63; at.wave = __builtin_amdgcn_readfirstlane(tid >> 6); at.n = at.lane & 15; at.g = at.lane >> 4;
+    if (tid == 0) found = -1;
+    __syncthreads();
+    at.s = segment_of(h, cut, at.slot_at, &found);
+    at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
+    float* const sums = GRADW ? all.sums + ((size_t)at.slot_at * h.H + at.head) * (D + 2) : nullptr;
+    if (at.slot < 0) {
+        if (GRADW) {
+            if (tid < kVals && at.v0 + tid < D) sums[at.v0 + tid] = 0.0f;
+            if (tid == 0) sums[D + at.v0 / kVals] = 0.0f;
+            if (tid == 0 && D <= kVals) sums[D + 1] = 0.0f;
+        }
+        return;
+    }
+    at.len = at.s.a1 - at.s.a0;
+    at.w = h.w[at.head];
+    // the two kinds of wavefront meet at the same barriers: two for each chunk
+    float du[GRADW ? 16 : 1] = {};
+    float dw = at.wave < 4 ? outputs<DP, BF16, GRADW>(h, p, at, du, lds) : carry_state<DP, BF16, GRADW>(h, p, all, at, cut, scanned != 0, lds);
+    if constexpr (GRADW) {
+        float* const across = (float*)(lds + L::sums);
+#pragma unroll
+        for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
+        if (at.lane == 0) across[4 * kVals + at.wave] = dw;
+        if (at.wave < 4)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+#pragma unroll
+                for (int off = 8; off; off >>= 1) du[i] += __shfl_xor(du[i], off, 64);
+                if (at.n == 0) across[kVals * at.wave + 16 * (i >> 2) + 4 * at.g + (i & 3)] = du[i];
+            }
+        __syncthreads();
+        if (tid < kVals && at.v0 + tid < D) sums[at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
+        if (tid == 0) {
+            float sum = 0.0f;
+            for (int i = 0; i < 8; ++i) sum += across[4 * kVals + i];
+            sums[D + at.v0 / kVals] = -sum;
+            if (D <= kVals) sums[D + 1] = 0.0f;
+        }
+    }
 }
 
 // dw [H] and du [H][D] from their parts, [parts][H][D + 2], the gradient of w in two of them: sixteen threads an entry, in a fixed order.
@@ -838,7 +902,7 @@ static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const P
     constexpr int bytes = Lds<DP, BF16, GRADW>::bytes;
     const hipError_t e = raise_lds((const void*)attend_sweep_kernel<DP, BF16, GRADW>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRADW>), dim3((unsigned)(p.slots * h.H * p.blocks), count), dim3(256), bytes, s, h, all, p.cut, (int)p.scan,
+    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRADW>), dim3((unsigned)(p.slots * h.H * p.blocks), count), dim3(512), bytes, s, h, all, p.cut, (int)p.scan,
                        p.blocks, first);
     return hipGetLastError();
 }
