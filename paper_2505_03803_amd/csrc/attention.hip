@@ -123,13 +123,17 @@ __device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int sl
     return s;
 }
 
+// LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
+// published beside the one that the outputs still read.
 template <int DP, bool BF16, bool GRADW> struct Lds {
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
     static constexpr int key = 0, val = key + kChunk * key_row, val_lo = val + kChunk * val_row;
     static constexpr int parts = GRADW ? 3 : 2, part = kVals * key_row;          // of a published state
     static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), z = state + parts * part;
-    static constexpr int u = z + (GRADW ? parts * part : 0), sums = u + 4 * DP;
-    static constexpr int bytes = sums + 4 * (4 * kVals + 8);
+    static constexpr int buffer = z + (GRADW ? parts * part : 0);
+    static constexpr bool two = 2 * buffer + 4 * DP + 1056 <= 160 * 1024 && (BF16 || DP > 64);
+    static constexpr int u = two ? 2 * buffer : buffer, sums = u + 4 * DP;
+    static constexpr int bytes = sums + (GRADW ? 4 * (4 * kVals + 8) : 0);
 };
 
 // Two values as packed bf16 and what is left of them.
@@ -240,13 +244,12 @@ __device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsD
         for (int m = 0; m < s.idx; ++m) add_state(acc, part(m), expf(-(float)((s.idx - 1 - m) * cut) * w), transposed, h.D, v0, wave, n, g);
 }
 
-// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes for each of NT threads, rows of PER such chunks.  Addresses are 32-bit offsets from
-// the chunk's lowest row.  What hangs over an end is loaded from inside instead (a chunk's last row, a head's first channels): later
-// tokens reach no output that is stored and have the weight 0 in the state (x is 0 there, which ends in sums over tokens), channels of
-// keys behind a head's last meet zeros of q.
-__device__ __forceinline__ uint32_t row_offset(int row, int nt, bool reverse, long long stride, int col) {
-    row = min(row, nt - 1);
-    return 2 * ((uint32_t)(reverse ? nt - 1 - row : row) * (uint32_t)stride + (uint32_t)col);
+// A chunk's rows on their way into LDS: COUNT chunks of 16 bytes for each of NT threads, rows of PER such chunks.  Addresses are 32-bit
+// offsets from the lowest of the chunk's 64 rows.  What hangs over an end is loaded from inside instead (a chunk's last row, a head's first
+// channels): later tokens reach no output that is stored and have the weight 0 in the state (x is 0 there, which ends in sums over
+// tokens), channels of keys behind a head's last meet zeros of q.
+__device__ __forceinline__ uint32_t row_offset(int row, bool reverse, long long stride, int col) {
+    return 2 * ((uint32_t)(reverse ? kChunk - 1 - row : row) * (uint32_t)stride + (uint32_t)col);
 }
 template <int NT, int COUNT, int PER>
 struct Rows {
@@ -256,20 +259,29 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
             const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
-            offset[i] = row_offset(c / PER, kChunk, reverse, stride, col < width ? col : 0);
+            offset[i] = row_offset(c / PER, reverse, stride, col < width ? col : 0);
         }
     }
-    __device__ __forceinline__ void fetch(const uint16_t* lowest, int nt, long long stride, int width, bool reverse) {
+    __device__ __forceinline__ void fetch(const char* lowest) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) data[i] = *(const uint4_t*)(lowest + offset[i]);
+    }
+    // the last nt < kChunk rows of a segment
+    __device__ __forceinline__ void fetch_tail(const char* lowest, int nt, long long stride, int width, bool reverse) {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            uint32_t at = offset[i];
-            if (nt < kChunk) {
-                const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
-                at = row_offset(c / PER, nt, reverse, stride, col < width ? col : 0);
-            }
-            data[i] = *(const uint4_t*)((const char*)lowest + at);
+            const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
+            data[i] = *(const uint4_t*)(lowest + row_offset(min(c / PER, nt - 1), reverse, stride, col < width ? col : 0));
         }
     }
+};
+// Where a tensor's chunks begin: the first one's lowest row of 64 (which need not all be the segment's), and the way to the next.
+struct Walk {
+    const char* at;
+    long long step;
+    __device__ __forceinline__ Walk(const uint16_t* base, long long stride, int a0, int a1, bool reverse)
+        : at((const char*)base + 2 * stride * (reverse ? a1 - kChunk : a0)), step(2 * stride * (reverse ? -kChunk : kChunk)) {}
+    __device__ __forceinline__ void next() { at += step; }
 };
 template <int NT, int COUNT, int PER>
 __device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
@@ -306,16 +318,16 @@ struct Powers {
     static __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 };
 // Weights exp(-(nt - 1 - i) w) of tokens i = 32 ks .. + 31 of a chunk in the state behind it, in the order of column_frag.
+template <bool TAIL>
 __device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, int ks, int nt, float w, int g) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) kw[e] = pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)];
-    if (nt < kChunk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
-            kw[e] = i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
-        }
+    for (int e = 0; e < 8; ++e) {
+        const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
+        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
+    }
 }
+struct Whole { static constexpr bool tail = false; };
+struct Tail { static constexpr bool tail = true; };
 // A fragment of 16-bit keys times its weights as three bf16 parts.
 template <bool BF16>
 __device__ __forceinline__ void weighted_keys(const uint4_t& k, const float (&kw)[8], uint4_t (&out)[3]) {
@@ -401,34 +413,39 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
     Rows<256, 2, 8> vr;
     kr.begin(p.key_stride, D, p.reverse);
     vr.begin(p.val_stride, D - v0, p.reverse);
-    auto fetch_chunk = [&](int c) {
-        const int nt = min(kChunk, len - c);
-        const long long lowest = p.reverse ? s.a1 - c - nt : s.a0 + c;
-        kr.fetch(p.key + head * D + lowest * p.key_stride, nt, p.key_stride, D, p.reverse);
-        vr.fetch(p.val + head * D + v0 + lowest * p.val_stride, nt, p.val_stride, D - v0, p.reverse);
+    Walk key_at(p.key + head * D, p.key_stride, s.a0, s.a1, p.reverse), val_at(p.val + head * D + v0, p.val_stride, s.a0, s.a1, p.reverse);
+    const long long key_stride = p.key_stride, val_stride = p.val_stride;
+    const bool reverse = p.reverse;
+    auto fetch = [&](int left) {
+        if (left >= kChunk) { kr.fetch(key_at.at); vr.fetch(val_at.at); }
+        else if (left > 0) { kr.fetch_tail(key_at.at, left, key_stride, D, reverse); vr.fetch_tail(val_at.at, left, val_stride, D - v0, reverse); }
+        key_at.next(); val_at.next();
     };
-    fetch_chunk(0);
+    fetch(len);
     Powers pow;
     pow.set(w, g);
-    for (int c = 0; c < len; c += kChunk) {
-        const int nt = min(kChunk, len - c);
+    auto chunk = [&](auto kind, int left) {
+        constexpr bool tail = decltype(kind)::tail;
         __syncthreads();
         stage<256, DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
         if constexpr (BF16) stage<256, 2, 8>(vr.data, lds + L::val, L::val_row);
         else stage_split<256, 2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
-        if (c + kChunk < len) fetch_chunk(c + kChunk);
-        scale(S, nt < kChunk ? expf(-(float)nt * w) : pow.whole);
+        if (!tail) fetch(left - kChunk);
+        scale(S, tail ? expf(-(float)left * w) : pow.whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT];
             float kw[8];
-            key_weights(kw, pow, ks, nt, w, g);
+            key_weights<tail>(kw, pow, ks, left, w, g);
             val_columns<BF16, L>(lds, ks, n, g, vf, vl);
             key_columns<L>(lds, ks, wave, n, g, keys);
             update_state<BF16, L, 3>(S, keys, kw, vf, vl);
         }
-    }
+    };
+    int left = len;
+    for (; left >= kChunk; left -= kChunk) chunk(Whole{}, left);
+    if (left > 0) chunk(Tail{}, left);
     store_state(S, to, D, v0, wave, n, g);
 }
 
@@ -485,13 +502,22 @@ template <int DP, bool BF16, class L>
 struct Staging {
     Rows<512, DP / 64, DP / 8> key;
     Rows<512, 1, 8> val;
-    __device__ __forceinline__ void begin(const SweepDev& p, const Place& at) {
-        key.begin(p.key_stride, at.D, p.reverse);
-        val.begin(p.val_stride, at.D - at.v0, p.reverse);
+    Walk key_at, val_at;
+    long long key_stride, val_stride;
+    int D, width;
+    bool reverse;
+    __device__ __forceinline__ Staging(const SweepDev& p, const Place& at)
+        : key_at(p.key + at.head * at.D, p.key_stride, at.s.a0, at.s.a1, p.reverse),
+          val_at(p.val + at.head * at.D + at.v0, p.val_stride, at.s.a0, at.s.a1, p.reverse),
+          key_stride(p.key_stride), val_stride(p.val_stride), D(at.D), width(at.D - at.v0), reverse(p.reverse) {
+        key.begin(key_stride, D, reverse);
+        val.begin(val_stride, width, reverse);
     }
-    __device__ __forceinline__ void fetch(const SweepDev& p, const Place& at, int nt, long long lowest) {
-        key.fetch(p.key + at.head * at.D + lowest * p.key_stride, nt, p.key_stride, at.D, p.reverse);
-        val.fetch(p.val + at.head * at.D + at.v0 + lowest * p.val_stride, nt, p.val_stride, at.D - at.v0, p.reverse);
+    // the next chunk, of which `left` rows and what comes behind are left
+    __device__ __forceinline__ void fetch(int left) {
+        if (left >= kChunk) { key.fetch(key_at.at); val.fetch(val_at.at); }
+        else if (left > 0) { key.fetch_tail(key_at.at, left, key_stride, D, reverse); val.fetch_tail(val_at.at, left, val_stride, width, reverse); }
+        key_at.next(); val_at.next();
     }
     __device__ __forceinline__ void store(char* lds) const {
         stage<512, DP / 64, DP / 8>(key.data, lds + L::key, L::key_row);
@@ -499,7 +525,6 @@ struct Staging {
         else stage_split<512, 1, 8>(val.data, lds + L::val, lds + L::val_lo, L::val_row);
     }
 };
-__device__ __forceinline__ long long lowest_row(const SweepDev& p, const Place& at, int c, int nt) { return p.reverse ? at.s.a1 - c - nt : at.s.a0 + c; }
 
 // The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of <G, Z>.
 template <int DP, bool BF16, bool GRADW>
@@ -509,9 +534,8 @@ __device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& 
     const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
     const float w = at.w;
     const Segment& s = at.s;
-    Staging<DP, BF16, L> rows;
-    rows.begin(p, at);
-    if (at.len > 0) rows.fetch(p, at, min(kChunk, at.len), lowest_row(p, at, 0, min(kChunk, at.len)));
+    Staging<DP, BF16, L> rows(p, at);
+    rows.fetch(at.len);
     float4_t S[KT][4], Z[GRADW ? KT : 1][4];
     auto load = [&](float4_t (&to)[KT][4], const float* initial, const float* parts, bool reverse, bool transposed) {
         if (scanned && s.count > 1) {
@@ -525,7 +549,7 @@ __device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& 
     clear(Z);
     Powers pow;
     pow.set(w, g);
-    auto publish = [&](const float4_t (&st)[KT][4], int to) {
+    auto publish = [&](const float4_t (&st)[KT][4], char* to) {
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
@@ -533,43 +557,46 @@ __device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& 
                 uint2_t v[L::parts];
                 split4(st[x][vt], v);
 #pragma unroll
-                for (int i = 0; i < L::parts; ++i) *(uint2_t*)(lds + to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
+                for (int i = 0; i < L::parts; ++i) *(uint2_t*)(to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
             }
     };
-    for (int c = 0; c < at.len; c += kChunk) {
-        const int nt = min(kChunk, at.len - c);
-        publish(S, L::state);
-        if constexpr (GRADW) publish(Z, L::z);
-        rows.store(lds);
+    char* buffer = lds;
+    auto chunk = [&](auto kind, int left) {
+        constexpr bool tail = decltype(kind)::tail;
+        publish(S, buffer + L::state);
+        if constexpr (GRADW) publish(Z, buffer + L::z);
+        rows.store(buffer);
         __syncthreads();
-        if (c + kChunk < at.len) {
-            const int next = min(kChunk, at.len - c - kChunk);
-            rows.fetch(p, at, next, lowest_row(p, at, c + kChunk, next));
-        }
-        const float decay = nt < kChunk ? expf(-(float)nt * w) : pow.whole;
+        if (!tail) rows.fetch(left - kChunk);
+        const float decay = tail ? expf(-(float)left * w) : pow.whole;
         if constexpr (GRADW) {
+            const float nt = tail ? (float)left : (float)kChunk;
 #pragma unroll
             for (int x = 0; x < KT; ++x)
 #pragma unroll
-                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + (float)nt * S[x][vt]);
+                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + nt * S[x][vt]);
         }
         scale(S, decay);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT];
             float kw[8];
-            key_weights(kw, pow, ks, nt, w, g);
-            val_columns<BF16, L>(lds, ks, n, g, vf, vl);
-            key_columns<L>(lds, ks, wave, n, g, keys);
+            key_weights<tail>(kw, pow, ks, left, w, g);
+            val_columns<BF16, L>(buffer, ks, n, g, vf, vl);
+            key_columns<L>(buffer, ks, wave, n, g, keys);
             update_state<BF16, L, 3>(S, keys, kw, vf, vl);
             if constexpr (GRADW) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) kw[e] *= (float)(nt - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
+                for (int e = 0; e < 8; ++e) kw[e] *= (float)((tail ? left : kChunk) - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
                 update_state<BF16, L, 3>(Z, keys, kw, vf, vl);
             }
         }
-        __syncthreads();
-    }
+        if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
+        else __syncthreads();
+    };
+    int left = at.len;
+    for (; left >= kChunk; left -= kChunk) chunk(Whole{}, left);
+    if (left > 0) chunk(Tail{}, left);
     if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
     float dw = 0.0f;
     if constexpr (GRADW) {                        // G: the gradient of the state at the segment's end
@@ -591,41 +618,44 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
     constexpr int KS = DP / 32;
     const int wave = at.wave, n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
-    Staging<DP, BF16, L> rows;
-    rows.begin(p, at);
+    Staging<DP, BF16, L> rows(p, at);
+    const bool reverse = p.reverse, u_in_dot = p.u_in_dot;
+    const long long q_stride = p.q_stride, x_stride = p.x_stride, out_stride = p.out_stride;
+    Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRADW ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
+        out_at(p.out + at.head * D + v0, out_stride, at.s.a0, at.s.a1, reverse);
     uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
     uint2_t xdr[4];
-    const uint32_t q_whole = row_offset(a, kChunk, p.reverse, p.q_stride, 8 * g), x_whole = GRADW ? row_offset(a, kChunk, p.reverse, p.x_stride, 0) : 0,
-                   o_whole = row_offset(a, kChunk, p.reverse, p.out_stride, 4 * g);
-    auto fetch_chunk = [&](int c) {
-        const int nt = min(kChunk, at.len - c);
-        const long long lowest = lowest_row(p, at, c, nt);
-        rows.fetch(p, at, nt, lowest);
-        const char* const qa = (const char*)(p.q + at.head * D + lowest * p.q_stride);
-        const uint32_t q_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.q_stride, 8 * g) : q_whole;
+    const uint32_t q_off = row_offset(a, reverse, q_stride, 8 * g), x_off = GRADW ? row_offset(a, reverse, x_stride, 0) : 0,
+                   out_off = row_offset(a, reverse, out_stride, 4 * g);
+    auto fetch = [&](int left) {
+        rows.fetch(left);
+        if (left > 0) {
+            const int row = min(a, left - 1);
+            const char* const from = q_at.at + (left < kChunk ? row_offset(row, reverse, q_stride, 8 * g) : q_off);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            qr[i] = uint4_t{0, 0, 0, 0};
-            if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(qa + q_off + 64 * i);
-        }
-        if constexpr (GRADW) {
-            const char* const xa = (const char*)(p.x + at.head * D + v0 + lowest * p.x_stride);
-            const uint32_t x_off = nt < kChunk ? row_offset(a, nt, p.reverse, p.x_stride, 0) : x_whole;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                xr[i] = uint4_t{0, 0, 0, 0};
-                if (a < nt && (D == DP || v0 + 32 * i + 8 * g < D)) xr[i] = *(const uint4_t*)(xa + x_off + 16 * g + 64 * i);
+            for (int i = 0; i < KS; ++i) {
+                qr[i] = uint4_t{0, 0, 0, 0};
+                if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(from + 64 * i);
             }
+            if constexpr (GRADW) {
+                const char* const xf = x_at.at + (left < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
 #pragma unroll
-            for (int vt = 0; vt < 4; ++vt) {
-                xdr[vt] = uint2_t{0, 0};
-                if (a < nt && (D == DP || v0 + 16 * vt + 4 * g < D)) xdr[vt] = *(const uint2_t*)(xa + x_off + 8 * g + 32 * vt);
+                for (int i = 0; i < 2; ++i) {
+                    xr[i] = uint4_t{0, 0, 0, 0};
+                    if (a < left && (D == DP || v0 + 32 * i + 8 * g < D)) xr[i] = *(const uint4_t*)(xf + 16 * g + 64 * i);
+                }
+#pragma unroll
+                for (int vt = 0; vt < 4; ++vt) {
+                    xdr[vt] = uint2_t{0, 0};
+                    if (a < left && (D == DP || v0 + 16 * vt + 4 * g < D)) xdr[vt] = *(const uint2_t*)(xf + 8 * g + 32 * vt);
+                }
             }
         }
+        q_at.next(); x_at.next();
     };
-    if (at.len > 0) fetch_chunk(0);
+    fetch(at.len);
     // u, where the bonus needs it: with the channels of the dot, or with those of val
-    const int u0 = p.u_in_dot ? 0 : v0, tid = threadIdx.x;
+    const int u0 = u_in_dot ? 0 : v0, tid = threadIdx.x;
     if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
 
     // weights of pairs of a tile's tokens a > i, and of those with an earlier tile's; of the state in front
@@ -640,9 +670,9 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
     for (int i = 0; i < 3; ++i) far[i] = Powers::uniform(expf(-(float)(16 * i) * w));
     float dw = 0.0f;
 
-    for (int c = 0; c < at.len; c += kChunk) {
-        const int nt = min(kChunk, at.len - c);
-        rows.store(lds);
+    char* buffer = lds;
+    auto chunk = [&](int left) {
+        rows.store(buffer);
         __syncthreads();
         uint4_t qf[KS], qh[KS], ql[KS], xf[2], xl[2];
         uint2_t xd[4];
@@ -661,7 +691,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) xd[vt] = xdr[vt];
         }
-        if (c + kChunk < at.len) fetch_chunk(c + kChunk);
+        fetch(left - kChunk);
 
         // the state in front, and its derivative
         float4_t out[4];
@@ -671,7 +701,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
             for (int i = 0; i < KS; ++i)
 #pragma unroll
                 for (int part = L::parts - 1; part >= 0; --part) {
-                    const uint4_t st = *(const uint4_t*)(lds + from + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                    const uint4_t st = *(const uint4_t*)(buffer + from + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
                     o = mfma_bits<true>(st, qh[i], o);
                     if (!BF16 && part < L::parts - 1) o = mfma_bits<true>(st, ql[i], o);
                 }
@@ -699,7 +729,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
                 uint4_t kf[KS];
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
-                    kf[i] = *(const uint4_t*)(lds + L::key + (16 * it + n) * L::key_row + 2 * (32 * i + 8 * g));
+                    kf[i] = *(const uint4_t*)(buffer + L::key + (16 * it + n) * L::key_row + 2 * (32 * i + 8 * g));
                     sc = mfma_bits<BF16>(kf[i], qf[i], sc);
                 }
                 if (it < wave) {
@@ -707,7 +737,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
 #pragma unroll
                     for (int j = 0; j < 4; ++j) sc[j] *= earlier[j] * tiles;
                 } else {
-                    if (p.u_in_dot) {
+                    if (u_in_dot) {
 #pragma unroll
                         for (int i = 0; i < KS; ++i)
 #pragma unroll
@@ -728,7 +758,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         sc[j] = 4 * g + j < n ? sc[j] * same[j] : 0.0f;
-                        if (!GRADW && p.u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
+                        if (!GRADW && u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
                     }
                 }
                 split4(sc, sp);
@@ -737,9 +767,9 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int from = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
-                        const uint4_t v = *(const uint4_t*)(lds + L::val + from);
+                        const uint4_t v = *(const uint4_t*)(buffer + L::val + from);
                         if (!BF16) {
-                            const uint4_t vl = *(const uint4_t*)(lds + L::val_lo + from);
+                            const uint4_t vl = *(const uint4_t*)(buffer + L::val_lo + from);
                             xv = mfma_bits<true>(vl, xl[i], xv);
                             xv = mfma_bits<true>(vl, xf[i], xv);
                             xv = mfma_bits<true>(v, xl[i], xv);
@@ -756,7 +786,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
         for (int ks = 0; ks < 2; ++ks) {
             if (2 * ks <= wave) {
                 uint4_t vf[4], vl[4];
-                val_columns<BF16, L>(lds, ks, n, g, vf, vl);
+                val_columns<BF16, L>(buffer, ks, n, g, vf, vl);
 #pragma unroll
                 for (int vt = 0; vt < 4; ++vt) {
                     out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
@@ -766,14 +796,14 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
             }
         }
         // the bonus with u at the channels of val; the gradient of u
-        if (GRADW || !p.u_in_dot) {
+        if (GRADW || !u_in_dot) {
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
-                const uint2_t vh = *(const uint2_t*)(lds + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
+                const uint2_t vh = *(const uint2_t*)(buffer + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
                 const float4_t u = *(const float4_t*)(lds + L::u + 4 * (16 * vt + 4 * g));
                 float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
                 if (!BF16) {
-                    const uint2_t l = *(const uint2_t*)(lds + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
+                    const uint2_t l = *(const uint2_t*)(buffer + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
                     v[0] += __uint_as_float(l.x << 16); v[1] += __uint_as_float(l.x & 0xFFFF0000u);
                     v[2] += __uint_as_float(l.y << 16); v[3] += __uint_as_float(l.y & 0xFFFF0000u);
                 }
@@ -785,16 +815,18 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
                 }
             }
         }
-        if (a < nt) {
-            char* const to = (char*)(p.out + at.head * D + v0 + lowest_row(p, at, c, nt) * p.out_stride) +
-                             (nt < kChunk ? row_offset(a, nt, p.reverse, p.out_stride, 4 * g) : o_whole);
+        if (a < left) {
+            char* const to = (char*)out_at.at + out_off;
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
                 if (D == DP || v0 + 16 * vt + 4 * g < D)
                     *(uint2_t*)(to + 32 * vt) = uint2_t{Elem<BF16>::pack(out[vt][0], out[vt][1]), Elem<BF16>::pack(out[vt][2], out[vt][3])};
         }
-        __syncthreads();
-    }
+        out_at.next();
+        if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
+        else __syncthreads();
+    };
+    for (int left = at.len; left > 0; left -= kChunk) chunk(left);
     return dw;
 }
 
