@@ -78,10 +78,16 @@ __global__ void __launch_bounds__(DP) attend_tokens_kernel(HeadsDev h) {
 //   dr:   q = dout, key = v,    val = k,    bonus (dout . v) u k,    the state transposed
 //   dk:   q = v,    key = dout, val = r,    bonus (v . dout) u r,    backwards, state G transposed
 //   dv:   q = k,    key = r,    val = dout, bonus (sum_c k u r) dout, backwards, state G.
-// The gradient of w comes out of the sweep for dr, which also carries Z, the derivative of its state by -w, within a segment:
-//   Z' = l^n (Z + n S) + sum_i (n-1-i) l^(n-1-i) key_i^T val_i,
-//   dw = -sum_a r_a . (l^a (Z^T + a S^T) dout_a + sum_{i<a} (a-1-i) l^(a-1-i) (dout_a . v_i) k_i) - <G, Z> at the segment's end:
-// every lag enters with its weight, nothing cancels.
+// The gradient of w.  Its definition weighs every pair of tokens i < t, with X_ti = l^(t-1-i) (r_t . k_i) (dout_t . v_i), by the lag t - 1 - i
+// (-w's exponent).  Pairs of one chunk are summed so.  The lag of any other pair is the place a of t in its chunk, plus what follows i in its
+// own chunk, plus 64 for each whole chunk between, so that with R_t the dot of r_t with the state's part of dr_t and K_i that of k_i
+// with the state's part of dk_i
+//   -dw = (pairs of one chunk) + sum_t a_t R_t + sum_i (n - 1 - a_i) K_i + sum over chunks of n <G, l^n S>,  G behind a chunk, S in front of it.
+// The last sum needs both states of every chunk at once; but what passes by a chunk is what passes its end less what its keys add, so
+// over a segment of L tokens it is L <G, S> (both at its end) + sum_t o_t R_t - sum_i (o_i + n_i) K_i with o the place of a token's chunk in
+// the segment.  That cancels for heads that forget within a chunk: where n w >= 20 (l^n < 2.1e-9) a chunk is left out of the sum, below the
+// rounding of the rest; of a fast head that leaves at most the segment's last chunk, n (<G, S> - sum of its K_i).  For the others these products have 24-bit operands, their sums over a chunk are carried on in binary64, and
+// a segment of the backward pass is at most 2048 tokens.
 //
 // A workgroup of four wavefronts takes a segment of a sequence, one head and 64 channels of val.  Wavefront `wave` owns tokens
 // 16 wave .. + 15 of a chunk for scores and outputs (computed transposed: a lane holds one token and four consecutive channels or
@@ -125,15 +131,14 @@ __device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int sl
 
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
 // published beside the one that the outputs still read.
-template <int DP, bool BF16, bool GRADW> struct Lds {
+template <int DP, bool BF16, int GRAD> struct Lds {
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
     static constexpr int key = 0, val = key + kChunk * key_row, val_lo = val + kChunk * val_row;
-    static constexpr int parts = GRADW ? 3 : 2, part = kVals * key_row;          // of a published state
-    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), z = state + parts * part;
-    static constexpr int buffer = z + (GRADW ? parts * part : 0);
-    static constexpr bool two = 2 * buffer + 4 * DP + 1056 <= 160 * 1024 && (BF16 || DP > 64);
+    static constexpr int parts = GRAD ? 3 : 2, part = kVals * key_row;          // of a published state
+    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), buffer = state + parts * part;
+    static constexpr bool two = 2 * buffer + 4 * DP + 1088 <= 160 * 1024 && (BF16 || DP > 64);
     static constexpr int u = two ? 2 * buffer : buffer, sums = u + 4 * DP;
-    static constexpr int bytes = sums + (GRADW ? 4 * (4 * kVals + 8) : 0);
+    static constexpr int bytes = sums + (GRAD ? 4 * 4 * kVals + 8 * 8 : 0);
 };
 
 // Two values as packed bf16 and what is left of them.
@@ -275,14 +280,16 @@ struct Rows {
         }
     }
 };
-// Where a tensor's chunks begin: the first one's lowest row of 64 (which need not all be the segment's), and the way to the next.
+// Where the rows of a tensor's next chunk begin: its lowest row of 64, not all of which need be the segment's.
 struct Walk {
     const char* at;
-    long long step;
+    long long row;
     __device__ __forceinline__ Walk(const uint16_t* base, long long stride, int a0, int a1, bool reverse)
-        : at((const char*)base + 2 * stride * (reverse ? a1 - kChunk : a0)), step(2 * stride * (reverse ? -kChunk : kChunk)) {}
-    __device__ __forceinline__ void next() { at += step; }
+        : at((const char*)base + 2 * stride * (reverse ? a1 - kChunk : a0)), row(reverse ? -2 * stride : 2 * stride) {}
+    __device__ __forceinline__ void pass(int rows) { at += row * rows; }
 };
+// Chunks of both directions meet at multiples of 64 tokens from a segment's front: backwards, a shorter one comes first.
+__device__ __forceinline__ int first_chunk(int len, bool reverse) { return reverse ? len - (len - 1) / kChunk * kChunk : min(kChunk, len); }
 template <int NT, int COUNT, int PER>
 __device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
 #pragma unroll
@@ -385,7 +392,7 @@ struct LocalsDev { LocalDev dir[2]; };
 
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
-    typedef Lds<DP, BF16, false> L;
+    typedef Lds<DP, BF16, 0> L;
     constexpr int KT = DP / 64;
     __shared__ __attribute__((aligned(16))) char lds[L::state];
     __shared__ int found;
@@ -416,36 +423,41 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
     Walk key_at(p.key + head * D, p.key_stride, s.a0, s.a1, p.reverse), val_at(p.val + head * D + v0, p.val_stride, s.a0, s.a1, p.reverse);
     const long long key_stride = p.key_stride, val_stride = p.val_stride;
     const bool reverse = p.reverse;
-    auto fetch = [&](int left) {
-        if (left >= kChunk) { kr.fetch(key_at.at); vr.fetch(val_at.at); }
-        else if (left > 0) { kr.fetch_tail(key_at.at, left, key_stride, D, reverse); vr.fetch_tail(val_at.at, left, val_stride, D - v0, reverse); }
-        key_at.next(); val_at.next();
+    auto fetch = [&](int nt) {
+        if (nt >= kChunk) { kr.fetch(key_at.at); vr.fetch(val_at.at); }
+        else if (nt > 0) { kr.fetch_tail(key_at.at, nt, key_stride, D, reverse); vr.fetch_tail(val_at.at, nt, val_stride, D - v0, reverse); }
+        key_at.pass(nt); val_at.pass(nt);
     };
-    fetch(len);
+    int nt = first_chunk(len, reverse);
+    fetch(nt);
     Powers pow;
     pow.set(w, g);
-    auto chunk = [&](auto kind, int left) {
+    auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         __syncthreads();
         stage<256, DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
         if constexpr (BF16) stage<256, 2, 8>(vr.data, lds + L::val, L::val_row);
         else stage_split<256, 2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
-        if (!tail) fetch(left - kChunk);
-        scale(S, tail ? expf(-(float)left * w) : pow.whole);
+        fetch(next);
+        scale(S, tail ? expf(-(float)nt * w) : pow.whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT];
             float kw[8];
-            key_weights<tail>(kw, pow, ks, left, w, g);
+            key_weights<tail>(kw, pow, ks, nt, w, g);
             val_columns<BF16, L>(lds, ks, n, g, vf, vl);
             key_columns<L>(lds, ks, wave, n, g, keys);
             update_state<BF16, L, 3>(S, keys, kw, vf, vl);
         }
     };
-    int left = len;
-    for (; left >= kChunk; left -= kChunk) chunk(Whole{}, left);
-    if (left > 0) chunk(Tail{}, left);
+    for (int left = len; left > 0;) {
+        const int next = min(kChunk, left - nt);
+        if (nt < kChunk) chunk(Tail{}, nt, next);
+        else chunk(Whole{}, nt, next);
+        left -= nt;
+        nt = next;
+    }
     store_state(S, to, D, v0, wave, n, g);
 }
 
@@ -489,7 +501,10 @@ struct SweepDev {
     float* last;                        // where the state behind the sequence goes, or nullptr
     bool reverse, transposed, u_in_dot;
 };
-struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* sums; int count; };
+struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* du_parts; double* dw_parts; };   // dw_parts: [slots][H][4]
+
+// Whether a head remembers more than rounding leaves over a chunk of n tokens (see the gradient of w).
+__device__ __forceinline__ bool passes(float w, int n) { return w * (float)n < 20.0f; }
 
 // What both kinds of wavefront know of their segment.
 struct Place {
@@ -513,11 +528,11 @@ struct Staging {
         key.begin(key_stride, D, reverse);
         val.begin(val_stride, width, reverse);
     }
-    // the next chunk, of which `left` rows and what comes behind are left
-    __device__ __forceinline__ void fetch(int left) {
-        if (left >= kChunk) { key.fetch(key_at.at); val.fetch(val_at.at); }
-        else if (left > 0) { key.fetch_tail(key_at.at, left, key_stride, D, reverse); val.fetch_tail(val_at.at, left, val_stride, width, reverse); }
-        key_at.next(); val_at.next();
+    // the next chunk, of nt rows
+    __device__ __forceinline__ void fetch(int nt) {
+        if (nt >= kChunk) { key.fetch(key_at.at); val.fetch(val_at.at); }
+        else if (nt > 0) { key.fetch_tail(key_at.at, nt, key_stride, D, reverse); val.fetch_tail(val_at.at, nt, val_stride, width, reverse); }
+        key_at.pass(nt); val_at.pass(nt);
     }
     __device__ __forceinline__ void store(char* lds) const {
         stage<512, DP / 64, DP / 8>(key.data, lds + L::key, L::key_row);
@@ -526,17 +541,18 @@ struct Staging {
     }
 };
 
-// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of <G, Z>.
-template <int DP, bool BF16, bool GRADW>
-__device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
-    typedef Lds<DP, BF16, GRADW> L;
+// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of L <G, S>.
+template <int DP, bool BF16, int GRAD>
+__device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
+    typedef Lds<DP, BF16, GRAD> L;
     constexpr int KT = DP / 64;
     const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
     const float w = at.w;
     const Segment& s = at.s;
     Staging<DP, BF16, L> rows(p, at);
-    rows.fetch(at.len);
-    float4_t S[KT][4], Z[GRADW ? KT : 1][4];
+    int nt = first_chunk(at.len, p.reverse);
+    rows.fetch(nt);
+    float4_t S[KT][4];
     auto load = [&](float4_t (&to)[KT][4], const float* initial, const float* parts, bool reverse, bool transposed) {
         if (scanned && s.count > 1) {
             clear(to);
@@ -546,7 +562,6 @@ __device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& 
         }
     };
     load(S, p.initial, p.parts, p.reverse, p.transposed);
-    clear(Z);
     Powers pow;
     pow.set(w, g);
     auto publish = [&](const float4_t (&st)[KT][4], char* to) {
@@ -561,99 +576,94 @@ __device__ __forceinline__ float carry_state(const HeadsDev& h, const SweepDev& 
             }
     };
     char* buffer = lds;
-    auto chunk = [&](auto kind, int left) {
+    auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         publish(S, buffer + L::state);
-        if constexpr (GRADW) publish(Z, buffer + L::z);
         rows.store(buffer);
         __syncthreads();
-        if (!tail) rows.fetch(left - kChunk);
-        const float decay = tail ? expf(-(float)left * w) : pow.whole;
-        if constexpr (GRADW) {
-            const float nt = tail ? (float)left : (float)kChunk;
-#pragma unroll
-            for (int x = 0; x < KT; ++x)
-#pragma unroll
-                for (int vt = 0; vt < 4; ++vt) Z[x][vt] = decay * (Z[x][vt] + nt * S[x][vt]);
-        }
-        scale(S, decay);
+        rows.fetch(next);
+        scale(S, tail ? expf(-(float)nt * w) : pow.whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT];
             float kw[8];
-            key_weights<tail>(kw, pow, ks, left, w, g);
+            key_weights<tail>(kw, pow, ks, nt, w, g);
             val_columns<BF16, L>(buffer, ks, n, g, vf, vl);
             key_columns<L>(buffer, ks, wave, n, g, keys);
             update_state<BF16, L, 3>(S, keys, kw, vf, vl);
-            if constexpr (GRADW) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kw[e] *= (float)((tail ? left : kChunk) - 1 - (32 * ks + 16 * (e >> 2) + 4 * g + (e & 3)));
-                update_state<BF16, L, 3>(Z, keys, kw, vf, vl);
-            }
         }
         if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
         else __syncthreads();
     };
-    int left = at.len;
-    for (; left >= kChunk; left -= kChunk) chunk(Whole{}, left);
-    if (left > 0) chunk(Tail{}, left);
+    for (int left = at.len; left > 0;) {
+        const int next = min(kChunk, left - nt);
+        if (nt < kChunk) chunk(Tail{}, nt, next);
+        else chunk(Whole{}, nt, next);
+        left -= nt;
+        nt = next;
+    }
     if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
-    float dw = 0.0f;
-    if constexpr (GRADW) {                        // G: the gradient of the state at the segment's end
-        load(S, all.grad_initial, all.grad_parts, true, true);
+    double dw = 0.0;
+    if constexpr (GRAD == 1) {                    // G: the gradient of the state at the segment's end
+        float4_t G[KT][4];
+        load(G, all.grad_initial, all.grad_parts, true, true);
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) dw = fmaf(S[x][vt][j], Z[x][vt][j], dw);
+                for (int j = 0; j < 4; ++j) dw += (double)G[x][vt][j] * (double)S[x][vt][j];
+        const int last = at.len % kChunk;
+        dw *= (double)(passes(w, kChunk) ? at.len : passes(w, last) ? last : 0);
     }
     return dw;
 }
 
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
-template <int DP, bool BF16, bool GRADW>
-__device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRADW ? 16 : 1], char* lds) {
-    typedef Lds<DP, BF16, GRADW> L;
+template <int DP, bool BF16, int GRAD>
+__device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRAD == 1 ? 16 : 1], char* lds) {
+    typedef Lds<DP, BF16, GRAD> L;
     constexpr int KS = DP / 32;
     const int wave = at.wave, n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
     Staging<DP, BF16, L> rows(p, at);
     const bool reverse = p.reverse, u_in_dot = p.u_in_dot;
     const long long q_stride = p.q_stride, x_stride = p.x_stride, out_stride = p.out_stride;
-    Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRADW ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
+    Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRAD ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
         out_at(p.out + at.head * D + v0, out_stride, at.s.a0, at.s.a1, reverse);
     uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
     uint2_t xdr[4];
-    const uint32_t q_off = row_offset(a, reverse, q_stride, 8 * g), x_off = GRADW ? row_offset(a, reverse, x_stride, 0) : 0,
+    const uint32_t q_off = row_offset(a, reverse, q_stride, 8 * g), x_off = GRAD ? row_offset(a, reverse, x_stride, 0) : 0,
                    out_off = row_offset(a, reverse, out_stride, 4 * g);
-    auto fetch = [&](int left) {
-        rows.fetch(left);
-        if (left > 0) {
-            const int row = min(a, left - 1);
-            const char* const from = q_at.at + (left < kChunk ? row_offset(row, reverse, q_stride, 8 * g) : q_off);
+    auto fetch = [&](int nt) {
+        rows.fetch(nt);
+        if (nt > 0) {
+            const int row = min(a, nt - 1);
+            const char* const from = q_at.at + (nt < kChunk ? row_offset(row, reverse, q_stride, 8 * g) : q_off);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 qr[i] = uint4_t{0, 0, 0, 0};
                 if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(from + 64 * i);
             }
-            if constexpr (GRADW) {
-                const char* const xf = x_at.at + (left < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
+            if constexpr (GRAD) {
+                const char* const xf = x_at.at + (nt < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
+                if constexpr (GRAD == 1)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    xr[i] = uint4_t{0, 0, 0, 0};
-                    if (a < left && (D == DP || v0 + 32 * i + 8 * g < D)) xr[i] = *(const uint4_t*)(xf + 16 * g + 64 * i);
-                }
+                    for (int i = 0; i < 2; ++i) {
+                        xr[i] = uint4_t{0, 0, 0, 0};
+                        if (a < nt && (D == DP || v0 + 32 * i + 8 * g < D)) xr[i] = *(const uint4_t*)(xf + 16 * g + 64 * i);
+                    }
 #pragma unroll
                 for (int vt = 0; vt < 4; ++vt) {
                     xdr[vt] = uint2_t{0, 0};
-                    if (a < left && (D == DP || v0 + 16 * vt + 4 * g < D)) xdr[vt] = *(const uint2_t*)(xf + 8 * g + 32 * vt);
+                    if (a < nt && (D == DP || v0 + 16 * vt + 4 * g < D)) xdr[vt] = *(const uint2_t*)(xf + 8 * g + 32 * vt);
                 }
             }
         }
-        q_at.next(); x_at.next();
+        q_at.pass(nt); x_at.pass(nt);
     };
-    fetch(at.len);
+    int nt = first_chunk(at.len, reverse);
+    fetch(nt);
     // u, where the bonus needs it: with the channels of the dot, or with those of val
     const int u0 = u_in_dot ? 0 : v0, tid = threadIdx.x;
     if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
@@ -668,10 +678,11 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
     }
 #pragma unroll
     for (int i = 0; i < 3; ++i) far[i] = Powers::uniform(expf(-(float)(16 * i) * w));
-    float dw = 0.0f;
+    double dw = 0.0;
+    const bool slow = GRAD && passes(w, kChunk);
 
     char* buffer = lds;
-    auto chunk = [&](int left) {
+    auto chunk = [&](int nt, int next, int left) {
         rows.store(buffer);
         __syncthreads();
         uint4_t qf[KS], qh[KS], ql[KS], xf[2], xl[2];
@@ -682,39 +693,43 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
             if constexpr (BF16) qh[i] = qf[i];
             else split_f16(qf[i], qh[i], ql[i]);
         }
-        if constexpr (GRADW) {
+        if constexpr (GRAD) {
+            if constexpr (GRAD == 1)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if constexpr (BF16) xf[i] = xr[i];
-                else split_f16(xr[i], xf[i], xl[i]);
-            }
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (BF16) xf[i] = xr[i];
+                    else split_f16(xr[i], xf[i], xl[i]);
+                }
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) xd[vt] = xdr[vt];
         }
-        fetch(left - kChunk);
+        fetch(next);
 
-        // the state in front, and its derivative
+        // the state in front; for the gradient of w its part of the outputs with x, weighted by the token's place in the segment
         float4_t out[4];
-        auto from_state = [&](int vt, int from) {
+        double state_dot = 0.0;
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) {
             float4_t o = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
                 for (int part = L::parts - 1; part >= 0; --part) {
-                    const uint4_t st = *(const uint4_t*)(buffer + from + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                    const uint4_t st = *(const uint4_t*)(buffer + L::state + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
                     o = mfma_bits<true>(st, qh[i], o);
                     if (!BF16 && part < L::parts - 1) o = mfma_bits<true>(st, ql[i], o);
                 }
-            return front * o;
-        };
+            out[vt] = front * o;
+            if constexpr (GRAD) {
+                float sum = 0.0f;
 #pragma unroll
-        for (int vt = 0; vt < 4; ++vt) {
-            out[vt] = from_state(vt, L::state);
-            if constexpr (GRADW) {
-                const float4_t z = from_state(vt, L::z) + (float)a * out[vt];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) dw = fmaf(half_of<BF16>(xd[vt], j), z[j], dw);
+                for (int j = 0; j < 4; ++j) sum = fmaf(half_of<BF16>(xd[vt], j), out[vt][j], sum);
+                state_dot += (double)sum;
             }
+        }
+        if constexpr (GRAD) {
+            const int before = GRAD == 1 ? (slow ? at.len - left : 0) : slow ? left : passes(w, nt) && nt < kChunk ? nt : 0;
+            dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;
         }
 
         // scores of the wavefront's tokens with those up to them; the bonus' dot is on their diagonal, or (with u) takes its place
@@ -758,11 +773,11 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         sc[j] = 4 * g + j < n ? sc[j] * same[j] : 0.0f;
-                        if (!GRADW && u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
+                        if (GRAD == 0 && u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
                     }
                 }
                 split4(sc, sp);
-                if constexpr (GRADW) {                                  // x . val of the same pairs, weighted with their lags
+                if constexpr (GRAD == 1) {                             // x . val of the same pairs, weighted with their lags
                     float4_t xv = {0, 0, 0, 0};
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -776,8 +791,10 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
                         }
                         xv = mfma_bits<true>(v, xf[i], xv);
                     }
+                    float sum = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) dw = fmaf(sc[j] * (float)(a - 1 - (16 * it + 4 * g + j)), xv[j], dw);
+                    for (int j = 0; j < 4; ++j) sum = fmaf(sc[j] * (float)(a - 1 - (16 * it + 4 * g + j)), xv[j], sum);
+                    dw += (double)sum;
                 }
             }
             ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
@@ -796,7 +813,7 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
             }
         }
         // the bonus with u at the channels of val; the gradient of u
-        if (GRADW || !u_in_dot) {
+        if (GRAD || !u_in_dot) {
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
                 const uint2_t vh = *(const uint2_t*)(buffer + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
@@ -811,31 +828,36 @@ __device__ __forceinline__ float outputs(const HeadsDev& h, const SweepDev& p, c
                 for (int j = 0; j < 4; ++j) {
                     const float now = dot * v[j];
                     out[vt][j] = fmaf(now, u[j], out[vt][j]);
-                    if (GRADW) du[4 * vt + j] = fmaf(half_of<BF16>(xd[vt], j), now, du[4 * vt + j]);
+                    if (GRAD == 1) du[4 * vt + j] = fmaf(half_of<BF16>(xd[vt], j), now, du[4 * vt + j]);
                 }
             }
         }
-        if (a < left) {
+        if (a < nt) {
             char* const to = (char*)out_at.at + out_off;
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
                 if (D == DP || v0 + 16 * vt + 4 * g < D)
                     *(uint2_t*)(to + 32 * vt) = uint2_t{Elem<BF16>::pack(out[vt][0], out[vt][1]), Elem<BF16>::pack(out[vt][2], out[vt][3])};
         }
-        out_at.next();
+        out_at.pass(nt);
         if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
         else __syncthreads();
     };
-    for (int left = at.len; left > 0; left -= kChunk) chunk(left);
+    for (int left = at.len; left > 0;) {
+        const int next = min(kChunk, left - nt);
+        chunk(nt, next, left);
+        left -= nt;
+        nt = next;
+    }
     return dw;
 }
 
-template <int DP, bool BF16, bool GRADW>
-__global__ void __launch_bounds__(512, GRADW || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int first) {
-    typedef Lds<DP, BF16, GRADW> L;
+template <int DP, bool BF16, int GRAD>
+__global__ void __launch_bounds__(512, GRAD == 1 || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int which) {
+    typedef Lds<DP, BF16, GRAD> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
-    const SweepDev& p = all.sweep[first + blockIdx.y];
+    const SweepDev& p = all.sweep[which];
     const int tid = threadIdx.x, D = h.D;
     Place at;
     at.slot_at = blockIdx.x / (h.H * blocks); at.head = blockIdx.x / blocks % h.H; at.v0 = blockIdx.x % blocks * kVals; at.D = D;
@@ -844,80 +866,91 @@ __global__ void __launch_bounds__(512, GRADW || DP > 64 ? 2 : 4) attend_sweep_ke
     __syncthreads();
     at.s = segment_of(h, cut, at.slot_at, &found);
     at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
-    float* const sums = GRADW ? all.sums + ((size_t)at.slot_at * h.H + at.head) * (D + 2) : nullptr;
+    float* const du_part = GRAD == 1 ? all.du_parts + ((size_t)at.slot_at * h.H + at.head) * D : nullptr;
+    double* const dw_part = GRAD ? all.dw_parts + ((size_t)at.slot_at * h.H + at.head) * 4 + 2 * (GRAD - 1) + at.v0 / kVals : nullptr;
     if (at.slot < 0) {
-        if (GRADW) {
-            if (tid < kVals && at.v0 + tid < D) sums[at.v0 + tid] = 0.0f;
-            if (tid == 0) sums[D + at.v0 / kVals] = 0.0f;
-            if (tid == 0 && D <= kVals) sums[D + 1] = 0.0f;
-        }
+        if (GRAD == 1 && tid < kVals && at.v0 + tid < D) du_part[at.v0 + tid] = 0.0f;
+        if (GRAD && tid == 0) *dw_part = 0.0;
         return;
     }
     at.len = at.s.a1 - at.s.a0;
     at.w = h.w[at.head];
-    // the two kinds of wavefront meet at the same barriers: two for each chunk
-    float du[GRADW ? 16 : 1] = {};
-    float dw = at.wave < 4 ? outputs<DP, BF16, GRADW>(h, p, at, du, lds) : carry_state<DP, BF16, GRADW>(h, p, all, at, cut, scanned != 0, lds);
-    if constexpr (GRADW) {
-        float* const across = (float*)(lds + L::sums);
+    // the two kinds of wavefront meet at the same barriers
+    float du[GRAD == 1 ? 16 : 1] = {};
+    double dw = at.wave < 4 ? outputs<DP, BF16, GRAD>(h, p, at, du, lds) : carry_state<DP, BF16, GRAD>(h, p, all, at, cut, scanned != 0, lds);
+    if constexpr (GRAD) {
+        double* const each = (double*)(lds + L::sums);
+        float* const across = (float*)(each + 8);
 #pragma unroll
         for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
-        if (at.lane == 0) across[4 * kVals + at.wave] = dw;
-        if (at.wave < 4)
+        if (at.lane == 0) each[at.wave] = dw;
+        if (GRAD == 1 && at.wave < 4)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
+                float sum = du[GRAD == 1 ? i : 0];
 #pragma unroll
-                for (int off = 8; off; off >>= 1) du[i] += __shfl_xor(du[i], off, 64);
-                if (at.n == 0) across[kVals * at.wave + 16 * (i >> 2) + 4 * at.g + (i & 3)] = du[i];
+                for (int off = 8; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
+                if (at.n == 0) across[kVals * at.wave + 16 * (i >> 2) + 4 * at.g + (i & 3)] = sum;
             }
         __syncthreads();
-        if (tid < kVals && at.v0 + tid < D) sums[at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
+        if (GRAD == 1 && tid < kVals && at.v0 + tid < D)
+            du_part[at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
         if (tid == 0) {
-            float sum = 0.0f;
-            for (int i = 0; i < 8; ++i) sum += across[4 * kVals + i];
-            sums[D + at.v0 / kVals] = -sum;
-            if (D <= kVals) sums[D + 1] = 0.0f;
+            double sum = 0.0;
+            for (int i = 0; i < 8; ++i) sum += each[i];
+            *dw_part = -sum;
         }
     }
 }
 
-// dw [H] and du [H][D] from their parts, [parts][H][D + 2], the gradient of w in two of them: sixteen threads an entry, in a fixed order.
-__global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float* sums, int parts) {
-    __shared__ float lds[16][17];
-    const int wide = h.D + 2, i = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4, head = i / wide, c = i % wide;
-    float s = 0.0f;
-    if (i < h.H * wide)
-        for (int p = part; p < parts; p += 16) s += sums[(size_t)p * h.H * wide + i] + (c == h.D ? sums[(size_t)p * h.H * wide + i + 1] : 0.0f);
+// du [H][D] from its parts [slots][H][D], dw [H] from [slots][H][4], of which `blocks` are used in each half: sixteen threads an entry, in a
+// fixed order.
+__global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float* du_parts, const double* dw_parts, int slots, int blocks) {
+    __shared__ double lds[16][17];
+    const int i = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4, n_du = h.H * h.D;
+    double s = 0.0;
+    if (i < n_du) {
+        float f = 0.0f;
+        for (int p = part; p < slots; p += 16) f += du_parts[(size_t)p * n_du + i];
+        s = (double)f;
+    } else if (i < n_du + h.H) {
+        for (int p = part; p < slots; p += 16) {
+            const double* const at = dw_parts + ((size_t)p * h.H + i - n_du) * 4;
+            for (int b = 0; b < blocks; ++b) s += at[b] + at[2 + b];
+        }
+    }
     lds[part][threadIdx.x & 15] = s;
     __syncthreads();
-    if (part != 0 || i >= h.H * wide) return;
+    if (part != 0) return;
     for (int p = 1; p < 16; ++p) s += lds[p][threadIdx.x];
-    if (c < h.D) h.du[head * h.D + c] = s;
-    else if (c == h.D) h.dw[head] = s;
+    if (i < n_du) h.du[i] = (float)s;
+    else if (i < n_du + h.H) h.dw[i - n_du] = (float)s;
 }
 
 // How a call is cut: `cut` tokens a segment, `slots` segments at most; split: a sequence can have more than one; scan: one launch turns
 // the segments' parts into the states in front of them, otherwise each segment adds up those before it.
-struct Plan { int cut, slots, blocks; bool split, scan; size_t part_floats, sum_floats; };
-static Plan plan_of(const HeadsDev& h) {
+struct Plan { int cut, slots, blocks; bool split, scan; size_t part_floats, du_floats, dw_doubles; };
+static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
     const long long work = (long long)h.n_tokens * h.H * p.blocks;
     p.cut = (int)std::max(128ll, (work / 512 + kChunk - 1) / kChunk * kChunk);
+    if (grad) p.cut = std::min(p.cut, 2048);
     const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
     p.split = len > p.cut;
     p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
     p.scan = len / p.cut > 12;
     p.part_floats = p.split ? (size_t)p.slots * h.H * h.D * h.D : 0;
-    p.sum_floats = (size_t)p.slots * h.H * (h.D + 2);
+    p.dw_doubles = (size_t)p.slots * h.H * 4;
+    p.du_floats = (size_t)p.slots * h.H * h.D;
     return p;
 }
 static bool single_tokens(const HeadsDev& h) { return !h.offsets && h.n_tokens == h.n_seqs; }
 
-size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h).part_floats * sizeof(float); }
+size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h, false).part_floats * sizeof(float); }
 size_t attention_backward_workspace_bytes(const HeadsDev& h) {
-    const Plan p = plan_of(h);
-    return (2 * p.part_floats + p.sum_floats) * sizeof(float);
+    const Plan p = plan_of(h, true);
+    return (2 * p.part_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
 }
 
 template <int DP, bool BF16>
@@ -928,32 +961,33 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
         hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (h.D * h.D + 255) / 256, dirs), dim3(256), 0, s, h, l, p.cut);
     return hipGetLastError();
 }
-template <int DP, bool BF16, bool GRADW>
-static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const Plan& p, int first, int count, hipStream_t s) {
+template <int DP, bool BF16, int GRAD>
+static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const Plan& p, int which, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
-    constexpr int bytes = Lds<DP, BF16, GRADW>::bytes;
-    const hipError_t e = raise_lds((const void*)attend_sweep_kernel<DP, BF16, GRADW>, bytes, raised);
+    constexpr int bytes = Lds<DP, BF16, GRAD>::bytes;
+    const hipError_t e = raise_lds((const void*)attend_sweep_kernel<DP, BF16, GRAD>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRADW>), dim3((unsigned)(p.slots * h.H * p.blocks), count), dim3(512), bytes, s, h, all, p.cut, (int)p.scan,
-                       p.blocks, first);
+    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRAD>), dim3((unsigned)(p.slots * h.H * p.blocks)), dim3(512), bytes, s, h, all, p.cut, (int)p.scan,
+                       p.blocks, which);
     return hipGetLastError();
 }
 
 template <int DP, bool BF16>
 static hipError_t forward(const HeadsDev& h, hipStream_t s) {
-    const Plan p = plan_of(h);
+    const Plan p = plan_of(h, false);
     LocalsDev l{};
     l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, h.partial, false};
     const hipError_t e = launch_locals<DP, BF16>(h, l, p, 1, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
     all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, true};
-    return launch_sweeps<DP, BF16, false>(h, all, p, 0, 1, s);
+    return launch_sweeps<DP, BF16, 0>(h, all, p, 0, s);
 }
 template <int DP, bool BF16>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
-    const Plan p = plan_of(h);
-    float *const S = h.partial, *const G = S + p.part_floats, *const sums = G + p.part_floats;
+    const Plan p = plan_of(h, true);
+    double* const dw_parts = (double*)h.partial;
+    float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const du_parts = G + p.part_floats;
     LocalsDev l{};
     l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, S, false};
     l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true};
@@ -961,12 +995,13 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     if (e != hipSuccess) return e;
     SweepsDev all{};
     all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
-    all.sweep[1] = SweepDev{h.v, h.dout, h.r, nullptr, h.v_stride, h.out_stride, h.r_stride, h.k_stride, 0, h.dk, h.dstate, G, nullptr, true, true, false};
+    all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, false};
     all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, true};
-    all.grad_initial = h.dstate; all.grad_parts = G; all.sums = sums;
-    if ((e = launch_sweeps<DP, BF16, true>(h, all, p, 0, 1, s)) != hipSuccess) return e;
-    if ((e = launch_sweeps<DP, BF16, false>(h, all, p, 1, 2, s)) != hipSuccess) return e;
-    hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 2) + 15) / 16), dim3(256), 0, s, h, sums, p.slots);
+    all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
+    if ((e = launch_sweeps<DP, BF16, 1>(h, all, p, 0, s)) != hipSuccess) return e;
+    if ((e = launch_sweeps<DP, BF16, 2>(h, all, p, 1, s)) != hipSuccess) return e;
+    if ((e = launch_sweeps<DP, BF16, 0>(h, all, p, 2, s)) != hipSuccess) return e;
+    hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 1) + 15) / 16), dim3(256), 0, s, h, du_parts, dw_parts, p.slots, p.blocks);
     return hipGetLastError();
 }
 template <bool BF16>
