@@ -621,7 +621,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
 
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
 template <int DP, bool BF16, int GRAD>
-__device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRAD == 1 ? 16 : 1], char* lds) {
+__device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
     typedef Lds<DP, BF16, GRAD> L;
     constexpr int KS = DP / 32;
     const int wave = at.wave, n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
@@ -828,7 +828,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 for (int j = 0; j < 4; ++j) {
                     const float now = dot * v[j];
                     out[vt][j] = fmaf(now, u[j], out[vt][j]);
-                    if (GRAD == 1) du[4 * vt + j] = fmaf(half_of<BF16>(xd[vt], j), now, du[4 * vt + j]);
+                    if (GRAD == 2) du[4 * vt + j] = fmaf(half_of<BF16>(xd[vt], j), now, du[4 * vt + j]);
                 }
             }
         }
@@ -853,7 +853,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 }
 
 template <int DP, bool BF16, int GRAD>
-__global__ void __launch_bounds__(512, GRAD == 1 || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int which) {
+__global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int which) {
     typedef Lds<DP, BF16, GRAD> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
@@ -866,17 +866,17 @@ __global__ void __launch_bounds__(512, GRAD == 1 || DP > 64 ? 2 : 4) attend_swee
     __syncthreads();
     at.s = segment_of(h, cut, at.slot_at, &found);
     at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
-    float* const du_part = GRAD == 1 ? all.du_parts + ((size_t)at.slot_at * h.H + at.head) * D : nullptr;
+    float* const du_part = GRAD == 2 ? all.du_parts + ((size_t)at.slot_at * h.H + at.head) * D : nullptr;
     double* const dw_part = GRAD ? all.dw_parts + ((size_t)at.slot_at * h.H + at.head) * 4 + 2 * (GRAD - 1) + at.v0 / kVals : nullptr;
     if (at.slot < 0) {
-        if (GRAD == 1 && tid < kVals && at.v0 + tid < D) du_part[at.v0 + tid] = 0.0f;
+        if (GRAD == 2 && tid < kVals && at.v0 + tid < D) du_part[at.v0 + tid] = 0.0f;
         if (GRAD && tid == 0) *dw_part = 0.0;
         return;
     }
     at.len = at.s.a1 - at.s.a0;
     at.w = h.w[at.head];
     // the two kinds of wavefront meet at the same barriers
-    float du[GRAD == 1 ? 16 : 1] = {};
+    float du[GRAD == 2 ? 16 : 1] = {};
     double dw = at.wave < 4 ? outputs<DP, BF16, GRAD>(h, p, at, du, lds) : carry_state<DP, BF16, GRAD>(h, p, all, at, cut, scanned != 0, lds);
     if constexpr (GRAD) {
         double* const each = (double*)(lds + L::sums);
@@ -884,16 +884,16 @@ __global__ void __launch_bounds__(512, GRAD == 1 || DP > 64 ? 2 : 4) attend_swee
 #pragma unroll
         for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
         if (at.lane == 0) each[at.wave] = dw;
-        if (GRAD == 1 && at.wave < 4)
+        if (GRAD == 2 && at.wave < 4)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float sum = du[GRAD == 1 ? i : 0];
+                float sum = du[GRAD == 2 ? i : 0];
 #pragma unroll
                 for (int off = 8; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
                 if (at.n == 0) across[kVals * at.wave + 16 * (i >> 2) + 4 * at.g + (i & 3)] = sum;
             }
         __syncthreads();
-        if (GRAD == 1 && tid < kVals && at.v0 + tid < D)
+        if (GRAD == 2 && tid < kVals && at.v0 + tid < D)
             du_part[at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
         if (tid == 0) {
             double sum = 0.0;
