@@ -57,16 +57,28 @@ template <int DT_> struct Piece<DT_, 8> {
         *(uint4_t*)((uint16_t*)p + i) = o;
     }
 };
-// V floats of a weight, or what stands for it.
+// V floats of a weight, or what stands for it; `whole`: 16 bytes at a time.
 template <int V>
-__device__ __forceinline__ void load_floats(float (&f)[V], const float* p, long long i, bool live, float otherwise) {
+__device__ __forceinline__ void load_floats(float (&f)[V], const float* p, long long i, bool live, float otherwise, bool whole) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = p && live ? p[i + j] : otherwise;
+    for (int j = 0; j < V; ++j) f[j] = otherwise;
+    if (!p || !live) return;
+    if constexpr (V >= 4)
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const float4_t v = *(const float4_t*)(p + i + j);
+                f[j] = v[0]; f[j + 1] = v[1]; f[j + 2] = v[2]; f[j + 3] = v[3];
+            }
+            return;
+        }
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = p[i + j];
 }
 
 // Which part of a call a thread has.  A team of `size` lanes (a power of two up to 64, or the workgroup) takes a group of a row, lane l the
 // pieces l, l + size, ..; the teams of a workgroup share out `groups` neighbouring groups and, where there are more teams, `rows` rows.
-struct Teams { int size, groups, rows; };
+struct Teams { int size, groups, rows; bool whole; };      // whole: weight and bias at multiples of 16 bytes
 struct Seat {
     int lane, g, row;                             // row: -1 for a lane without work
     __device__ __forceinline__ Seat(const Teams& t, const NormDev& p, bool block) {
@@ -104,8 +116,8 @@ __global__ void __launch_bounds__(256) norm_kernel(NormDev p, Teams teams) {
     if constexpr (keep)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            load_floats<V>(w[e], p.weight, g0 + at(e), live(e), 1.0f);
-            load_floats<V>(b[e], p.bias, g0 + at(e), live(e), 0.0f);
+            load_floats<V>(w[e], p.weight, g0 + at(e), live(e), 1.0f, teams.whole);
+            load_floats<V>(b[e], p.bias, g0 + at(e), live(e), 0.0f, teams.whole);
         }
     Piece<DT_, V> next[E];
     auto fetch = [&](long long m) {
@@ -144,8 +156,8 @@ __global__ void __launch_bounds__(256) norm_kernel(NormDev p, Teams teams) {
                 if (live(e)) {
                     float we[V], be[V], y[V];
                     if constexpr (!keep) {
-                        load_floats<V>(we, p.weight, g0 + at(e), true, 1.0f);
-                        load_floats<V>(be, p.bias, g0 + at(e), true, 0.0f);
+                        load_floats<V>(we, p.weight, g0 + at(e), true, 1.0f, teams.whole);
+                        load_floats<V>(be, p.bias, g0 + at(e), true, 0.0f, teams.whole);
                     }
 #pragma unroll
                     for (int j = 0; j < V; ++j) y[j] = fmaf(x[e][j] * rstd, keep ? w[keep ? e : 0][j] : we[j], keep ? b[keep ? e : 0][j] : be[j]);
@@ -170,7 +182,7 @@ __global__ void __launch_bounds__(256) norm_backward_kernel(NormDev p, Teams tea
     float w[E][V], dw[E][V], db[E][V];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        load_floats<V>(w[e], p.weight, g0 + at(e), live(e), 1.0f);
+        load_floats<V>(w[e], p.weight, g0 + at(e), live(e), 1.0f, teams.whole);
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[e][j] = db[e][j] = 0.0f;
     }
@@ -319,6 +331,7 @@ __global__ void __launch_bounds__(1024) sum_partials_kernel(const float* partial
     const int c = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
     float s = 0.0f;
     if (c < width)
+#pragma unroll 8
         for (int i = part; i < count; i += 16) s += partial[(size_t)i * width + c];
     lds[part][threadIdx.x & 63] = s;
     __syncthreads();
@@ -361,10 +374,12 @@ static Pick pick(const NormDev& p, int dt, bool backward) {
         k.teams.groups = std::min(p.groups, per);
         k.teams.rows = per / k.teams.groups;
     } else {
-        k.teams = Teams{256, 1, 1};
+        k.teams.size = 256; k.teams.groups = k.teams.rows = 1;
     }
+    k.teams.whole = (((uintptr_t)p.weight | (uintptr_t)p.bias) & 15) == 0;
     const int each = (pieces + k.teams.size - 1) / k.teams.size;
-    for (k.E = 1; k.E < each; k.E *= 2) {}
+    for (int E : {1, 2, 3, 4, 6, 8, 16, 32, 64})
+        if (k.E < each) k.E = E;
     k.loop = k.E * k.V > (k.block ? block_values(k.V, backward) : kWaveValues);
     k.grid_y = (p.groups + k.teams.groups - 1) / k.teams.groups;
     const long long row_sets = (p.M + k.teams.rows - 1) / k.teams.rows;
@@ -402,7 +417,9 @@ static void launch_rows(const NormDev& p, const Pick& k, bool backward, hipStrea
     switch (k.E) {
         case 1: launch_rows<DT_, V, 1, BLOCK>(p, k, backward, s); break;
         case 2: launch_rows<DT_, V, 2, BLOCK>(p, k, backward, s); break;
+        case 3: launch_rows<DT_, V, 3, BLOCK>(p, k, backward, s); break;
         case 4: launch_rows<DT_, V, 4, BLOCK>(p, k, backward, s); break;
+        case 6: launch_rows<DT_, V, 6, BLOCK>(p, k, backward, s); break;
         case 8: launch_rows<DT_, V, 8, BLOCK>(p, k, backward, s); break;
         case 16: launch_rows<DT_, V, 16, BLOCK>(p, k, backward, s); break;
         case 32: launch_rows<DT_, V, 32, BLOCK>(p, k, backward, s); break;
