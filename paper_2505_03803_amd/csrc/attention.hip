@@ -8,11 +8,6 @@ namespace rwkvq {
 
 template <bool BF16>
 __device__ __forceinline__ float widen16(uint16_t v) { return BF16 ? bf16_bits_to_f32(v) : f16_bits_to_f32(v); }
-template <bool BF16>
-__device__ __forceinline__ uint16_t narrow16(float v) {
-    return BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : f32_to_f16_bits(v);
-}
-
 // Rows of sequence b, within 0 .. n_tokens whatever the offsets hold.
 __device__ __forceinline__ void rows_of(const HeadsDev& h, int b, int& t0, int& t1) {
     if (h.offsets) {
@@ -30,43 +25,63 @@ __device__ __forceinline__ int slot_of(const HeadsDev& h, int b) {
     return s >= 0 && s < h.n_slots ? s : -1;
 }
 
-// A workgroup per sequence and head, token by token; thread j holds column j of the state.
-template <int DP, bool BF16>
-__global__ void __launch_bounds__(DP) attend_tokens_kernel(HeadsDev h) {
-    __shared__ float rs[DP], ks[DP], ru[DP];
-    const int b = blockIdx.x / h.H, head = blockIdx.x % h.H, j = threadIdx.x, D = h.D, slot = slot_of(h, b);
+// One token for each sequence: a workgroup per sequence and head.  LANES lanes hold a row of the state, four columns each, a thread
+// ROWS rows; all of a state is on its way before any of it is used, and is written back where it is.  What bounds it: HBM
+// bandwidth (the state read and written once), for few sequences a launch and two ways to memory.
+template <int LANES, int ROWS, bool BF16>
+__global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
+    constexpr int per = 256 / LANES;              // rows at a time
+    __shared__ float4_t sums[4][LANES];
+    const int b = blockIdx.x / h.H, head = blockIdx.x % h.H, lane = threadIdx.x % LANES, first = threadIdx.x / LANES, D = h.D, slot = slot_of(h, b);
     if (slot < 0) return;
-    int t0, t1;
-    rows_of(h, b, t0, t1);
     const size_t at = ((size_t)slot * h.H + head) * D * D;
-    const bool live = j < D;
-    const float lam = expf(-h.w[head]), u = live ? h.u[head * D + j] : 0.0f;
-    float S[DP];
+    const int col = 4 * lane;
+    const bool live = col < D;
+    const uint16_t* const r = h.r + b * h.r_stride + head * D;
+    const uint16_t* const k = h.k + b * h.k_stride + head * D;
+    const float* const u = h.u + head * D;
+    float4_t S[ROWS];
+    uint16_t rr[ROWS], kk[ROWS];
+    float uu[ROWS];
+    uint2_t vv = {0, 0};
 #pragma unroll
-    for (int c = 0; c < DP; ++c) S[c] = live && c < D && h.state ? h.state[at + (size_t)c * D + j] : 0.0f;
-    for (int t = t0; t < t1; ++t) {
-        float r = 0.0f, k = 0.0f, v = 0.0f;
-        if (live) {
-            r = widen16<BF16>(h.r[t * h.r_stride + head * D + j]);
-            k = widen16<BF16>(h.k[t * h.k_stride + head * D + j]);
-            v = widen16<BF16>(h.v[t * h.v_stride + head * D + j]);
-        }
-        __syncthreads();
-        rs[j] = r; ks[j] = k; ru[j] = r * u * k;
-        __syncthreads();
-        float o = 0.0f, now = 0.0f;
-#pragma unroll
-        for (int c = 0; c < DP; ++c) {
-            o = fmaf(rs[c], S[c], o);
-            now += ru[c];
-            S[c] = fmaf(lam, S[c], ks[c] * v);
-        }
-        if (live) h.out[t * h.out_stride + head * D + j] = narrow16<BF16>(fmaf(now, v, o));
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = first + per * i;
+        S[i] = float4_t{0, 0, 0, 0};
+        if (live && row < D && h.state) S[i] = *(const float4_t*)(h.state + at + (size_t)row * D + col);
     }
-    if (live && h.state_out)
+    if (live) vv = *(const uint2_t*)(h.v + b * h.v_stride + head * D + col);
 #pragma unroll
-        for (int c = 0; c < DP; ++c)
-            if (c < D) h.state_out[at + (size_t)c * D + j] = S[c];
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = first + per * i;
+        rr[i] = kk[i] = 0; uu[i] = 0.0f;
+        if (row < D) { rr[i] = r[row]; kk[i] = k[row]; uu[i] = u[row]; }
+    }
+    const float lam = expf(-h.w[head]);
+    const float v[4] = {widen16<BF16>((uint16_t)vv.x), widen16<BF16>((uint16_t)(vv.x >> 16)), widen16<BF16>((uint16_t)vv.y), widen16<BF16>((uint16_t)(vv.y >> 16))};
+    float4_t o = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int row = first + per * i;
+        const float rf = widen16<BF16>(rr[i]), kf = widen16<BF16>(kk[i]), uk = uu[i] * kf;
+        float4_t next;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            o[j] = fmaf(rf, fmaf(uk, v[j], S[i][j]), o[j]);
+            next[j] = fmaf(lam, S[i][j], kf * v[j]);
+        }
+        if (live && row < D && h.state_out) *(float4_t*)(h.state_out + at + (size_t)row * D + col) = next;
+    }
+#pragma unroll
+    for (int off = LANES; off < 64; off <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], off, 64);
+    if ((threadIdx.x & 63) < LANES) sums[threadIdx.x >> 6][lane] = o;
+    __syncthreads();
+    if (threadIdx.x < LANES && live) {
+        o = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        *(uint2_t*)(h.out + b * h.out_stride + head * D + col) = uint2_t{Elem<BF16>::pack(o[0], o[1]), Elem<BF16>::pack(o[2], o[3])};
+    }
 }
 
 // ---- chunks of 64 tokens on the matrix cores ---------------------------------------------------------------------------
@@ -1008,9 +1023,10 @@ template <bool BF16>
 static hipError_t attention(const HeadsDev& h, bool grad, hipStream_t s) {
     if (grad) return h.D <= 64 ? backward<64, BF16>(h, s) : backward<128, BF16>(h, s);
     if (!single_tokens(h)) return h.D <= 64 ? forward<64, BF16>(h, s) : forward<128, BF16>(h, s);
-    const dim3 grid((unsigned)(h.n_seqs * h.H));
-    if (h.D <= 64) hipLaunchKernelGGL((attend_tokens_kernel<64, BF16>), grid, dim3(64), 0, s, h);
-    else hipLaunchKernelGGL((attend_tokens_kernel<128, BF16>), grid, dim3(128), 0, s, h);
+    const dim3 grid((unsigned)(h.n_seqs * h.H)), block(256);
+    if (h.D <= 32) hipLaunchKernelGGL((attend_step_kernel<8, 1, BF16>), grid, block, 0, s, h);
+    else if (h.D <= 64) hipLaunchKernelGGL((attend_step_kernel<16, 4, BF16>), grid, block, 0, s, h);
+    else hipLaunchKernelGGL((attend_step_kernel<32, 16, BF16>), grid, block, 0, s, h);
     return hipGetLastError();
 }
 hipError_t launch_attention(const HeadsDev& h, int dt, hipStream_t s) {
