@@ -244,24 +244,70 @@ __device__ __forceinline__ void clear(float4_t (&acc)[KT][4]) {
         for (int vt = 0; vt < 4; ++vt) acc[x][vt] = float4_t{0, 0, 0, 0};
 }
 
-// The state at a segment's front, in the order of the sweep.  `parts`: for each segment what it adds to a state; the one whose own
-// part nobody needs (the last one of the sweep) holds the state that the sequence begins with.
+// Parts: what the segments of a direction add to a state, in the order in which lanes hold one, [slot][head][64 channels of val][x][vt][wave][lane]
+// of float4.  The segment whose own part nobody needs (the last one of the sweep) has there the state that the sequence begins with.
 template <int KT>
-__device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsDev& h, const Segment& s, int cut, const float* initial, const float* parts,
-                                            bool reverse, bool transposed, int head, int slot, float w, int v0, int wave, int n, int g) {
+__device__ __forceinline__ size_t part_size(int D) { return (size_t)(64 * KT) * kVals * ((D + kVals - 1) / kVals); }
+template <int KT>
+__device__ __forceinline__ size_t part_place(int block, int x, int vt, int wave, int lane) { return 4 * (size_t)((((block * KT + x) * 4 + vt) * 4 + wave) * 64 + lane); }
+template <int KT>
+__device__ __forceinline__ void store_part(const float4_t (&acc)[KT][4], float* to, int v0, int wave, int lane) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) *(float4_t*)(to + part_place<KT>(v0 / kVals, x, vt, wave, lane)) = acc[x][vt];
+}
+template <int KT>
+__device__ __forceinline__ void load_part(float4_t (&in)[KT][4], const float* from, bool transposed, int v0, int wave, int lane) {
+    const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) {
+            if (!transposed) {
+                in[x][vt] = *(const float4_t*)(from + part_place<KT>(v0 / kVals, x, vt, wave, lane));
+            } else {                              // key and val exchange their roles: four lanes of another tile have the lane's four values
+                const int key = 16 * (KT * wave + x), tile = v0 / 16 + vt;
+                const float* const at = from + part_place<KT>(key / kVals, tile % KT, key % kVals / 16, tile / KT, 16 * (n >> 2) + 4 * g) + (n & 3);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) in[x][vt][j] = at[4 * j];
+            }
+        }
+}
+template <int KT>
+__device__ __forceinline__ void add(float4_t (&acc)[KT][4], const float4_t (&in)[KT][4], float weight) {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int vt = 0; vt < 4; ++vt) acc[x][vt] += weight * in[x][vt];
+}
+
+// The state at a segment's front, in the order of the sweep.
+template <int KT>
+__device__ __forceinline__ void start_state(float4_t (&acc)[KT][4], const HeadsDev& h, const Segment& s, int cut, bool scanned, const float* initial, const float* parts,
+                                            bool reverse, bool transposed, bool parts_transposed, int head, int slot, float w, int v0, int wave, int lane) {
     clear(acc);
-    const size_t size = (size_t)h.D * h.D;
+    const size_t size = part_size<KT>(h.D);
     if (s.count <= 1) {
-        if (initial) add_state(acc, initial + ((size_t)slot * h.H + head) * size, 1.0f, transposed, h.D, v0, wave, n, g);
+        if (initial) add_state(acc, initial + ((size_t)slot * h.H + head) * h.D * h.D, 1.0f, transposed, h.D, v0, wave, lane & 15, lane >> 4);
         return;
     }
     auto part = [&](int idx) { return parts + ((size_t)(s.first_slot + idx) * h.H + head) * size; };
-    const int away = reverse ? s.t1 - s.a1 : s.a0 - s.t0, held = reverse ? 0 : s.count - 1;
-    if (initial) add_state(acc, part(held), expf(-(float)away * w), transposed, h.D, v0, wave, n, g);
-    if (reverse)
-        for (int m = s.idx + 1; m < s.count; ++m) add_state(acc, part(m), expf(-(float)((m - s.idx - 1) * cut) * w), transposed, h.D, v0, wave, n, g);
-    else
-        for (int m = 0; m < s.idx; ++m) add_state(acc, part(m), expf(-(float)((s.idx - 1 - m) * cut) * w), transposed, h.D, v0, wave, n, g);
+    if (scanned) {
+        load_part(acc, part(s.idx), parts_transposed, v0, wave, lane);
+        return;
+    }
+    // those in front of the segment, nearest first, then what the sequence begins with: loads of two at a time before their use
+    const int before = reverse ? s.count - 1 - s.idx : s.idx, away = reverse ? s.t1 - s.a1 : s.a0 - s.t0, count = before + (initial ? 1 : 0);
+    auto which = [&](int i) { return part(i == before ? (reverse ? 0 : s.count - 1) : reverse ? s.idx + 1 + i : s.idx - 1 - i); };
+    auto weight = [&](int i) { return expf(-(float)(i == before ? away : i * cut) * w); };
+    float4_t a[KT][4], b[KT][4];
+    for (int i = 0; i < count; i += 2) {
+        load_part(a, which(i), parts_transposed, v0, wave, lane);
+        if (i + 1 < count) load_part(b, which(i + 1), parts_transposed, v0, wave, lane);
+        add(acc, a, weight(i));
+        if (i + 1 < count) add(acc, b, weight(i + 1));
+    }
 }
 
 // A chunk's rows on their way into LDS: COUNT chunks of 16 bytes for each of NT threads, rows of PER such chunks.  Addresses are 32-bit
@@ -401,15 +447,15 @@ __device__ __forceinline__ void scale(float4_t (&S)[KT][4], float by) {
         for (int vt = 0; vt < 4; ++vt) S[x][vt] *= by;
 }
 
-// What the segments of a direction add to a state, before their sweep; the segment whose part nobody needs keeps the initial state.
-struct LocalDev { const uint16_t *key, *val; long long key_stride, val_stride; const float* initial; float* parts; bool reverse; };
+// The parts of one direction, before the sweeps; transposed: key is what the state in memory calls val.
+struct LocalDev { const uint16_t *key, *val; long long key_stride, val_stride; const float* initial; float* parts; bool reverse, transposed; };
 struct LocalsDev { LocalDev dir[2]; };
 
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
+__global__ void __launch_bounds__(256, DP > 64 ? 2 : 4) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
     typedef Lds<DP, BF16, 0> L;
     constexpr int KT = DP / 64;
-    __shared__ __attribute__((aligned(16))) char lds[L::state];
+    __shared__ __attribute__((aligned(16))) char both[2][L::state];
     __shared__ int found;
     const LocalDev& p = locals.dir[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -421,13 +467,13 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
     const int slot = slot_of(h, s.b), D = h.D;
     if (slot < 0) return;
     const float w = h.w[head];
-    float* const to = p.parts + ((size_t)slot_at * h.H + head) * D * D;
+    float* const to = p.parts + ((size_t)slot_at * h.H + head) * part_size<KT>(D);
     float4_t S[KT][4];
     clear(S);
     if (s.idx == (p.reverse ? 0 : s.count - 1)) {
         if (!p.initial) return;
-        add_state(S, p.initial + ((size_t)slot * h.H + head) * D * D, 1.0f, false, D, v0, wave, n, g);
-        store_state(S, to, D, v0, wave, n, g);
+        add_state(S, p.initial + ((size_t)slot * h.H + head) * D * D, 1.0f, p.transposed, D, v0, wave, n, g);
+        store_part(S, to, v0, wave, lane);
         return;
     }
     const int len = s.a1 - s.a0;
@@ -447,13 +493,15 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
     fetch(nt);
     Powers pow;
     pow.set(w, g);
+    int turn = 0;                                 // two tiles: a barrier a chunk
     auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
-        __syncthreads();
+        char* const lds = both[turn];
         stage<256, DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
         if constexpr (BF16) stage<256, 2, 8>(vr.data, lds + L::val, L::val_row);
         else stage_split<256, 2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
+        turn ^= 1;
         fetch(next);
         scale(S, tail ? expf(-(float)nt * w) : pow.whole);
 #pragma unroll
@@ -473,13 +521,13 @@ __global__ void __launch_bounds__(256) attend_local_kernel(HeadsDev h, LocalsDev
         left -= nt;
         nt = next;
     }
-    store_state(S, to, D, v0, wave, n, g);
+    store_part(S, to, v0, wave, lane);
 }
 
 // Many segments per sequence: the state at each one's front in place of its part, a thread per element.
-__global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev locals, int cut) {
+__global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev locals, int cut, int size) {
     const LocalDev& p = locals.dir[blockIdx.z];
-    const int size = h.D * h.D, at = blockIdx.y * 256 + threadIdx.x;
+    const int at = blockIdx.y * 256 + threadIdx.x;
     if (at >= size) return;
     for (long long item = blockIdx.x; item < (long long)h.n_seqs * h.H; item += gridDim.x) {
         const int b = (int)(item / h.H), head = (int)(item % h.H);
@@ -514,7 +562,7 @@ struct SweepDev {
     uint16_t* out;
     const float *initial, *parts;       // of the sweep's own state
     float* last;                        // where the state behind the sequence goes, or nullptr
-    bool reverse, transposed, u_in_dot;
+    bool reverse, transposed, parts_transposed, u_in_dot;       // transposed: key is what the state in memory calls val; and what the parts do
 };
 struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* du_parts; double* dw_parts; };   // dw_parts: [slots][H][4]
 
@@ -568,15 +616,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     int nt = first_chunk(at.len, p.reverse);
     rows.fetch(nt);
     float4_t S[KT][4];
-    auto load = [&](float4_t (&to)[KT][4], const float* initial, const float* parts, bool reverse, bool transposed) {
-        if (scanned && s.count > 1) {
-            clear(to);
-            add_state(to, parts + ((size_t)at.slot_at * h.H + at.head) * D * D, 1.0f, transposed, D, at.v0, wave, n, g);
-        } else {
-            start_state(to, h, s, cut, initial, parts, reverse, transposed, at.head, at.slot, w, at.v0, wave, n, g);
-        }
-    };
-    load(S, p.initial, p.parts, p.reverse, p.transposed);
+    start_state(S, h, s, cut, scanned, p.initial, p.parts, p.reverse, p.transposed, p.parts_transposed, at.head, at.slot, w, at.v0, wave, at.lane);
     Powers pow;
     pow.set(w, g);
     auto publish = [&](const float4_t (&st)[KT][4], char* to) {
@@ -621,13 +661,14 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     double dw = 0.0;
     if constexpr (GRAD == 1) {                    // G: the gradient of the state at the segment's end
         float4_t G[KT][4];
-        load(G, all.grad_initial, all.grad_parts, true, true);
+        start_state(G, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) dw += (double)G[x][vt][j] * (double)S[x][vt][j];
+                for (int j = 0; j < 4; ++j)       // places behind a head's last channels hold whatever was loaded for them
+                    if (16 * (KT * wave + x) + 4 * g < D && at.v0 + 16 * vt + n < D) dw += (double)G[x][vt][j] * (double)S[x][vt][j];
         const int last = at.len % kChunk;
         dw *= (double)(passes(w, kChunk) ? at.len : passes(w, last) ? last : 0);
     }
@@ -944,7 +985,7 @@ __global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float
 
 // How a call is cut: `cut` tokens a segment, `slots` segments at most; split: a sequence can have more than one; scan: one launch turns
 // the segments' parts into the states in front of them, otherwise each segment adds up those before it.
-struct Plan { int cut, slots, blocks; bool split, scan; size_t part_floats, du_floats, dw_doubles; };
+struct Plan { int cut, slots, blocks, part_size; bool split, scan; size_t part_floats, du_floats, dw_doubles; };
 static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
@@ -955,7 +996,8 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
     p.split = len > p.cut;
     p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
     p.scan = len / p.cut > 12;
-    p.part_floats = p.split ? (size_t)p.slots * h.H * h.D * h.D : 0;
+    p.part_size = (h.D <= 64 ? 64 : 128) * kVals * p.blocks;
+    p.part_floats = p.split ? (size_t)p.slots * h.H * p.part_size : 0;
     p.dw_doubles = (size_t)p.slots * h.H * 4;
     p.du_floats = (size_t)p.slots * h.H * h.D;
     return p;
@@ -973,7 +1015,7 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
     if (!p.split) return hipSuccess;
     hipLaunchKernelGGL((attend_local_kernel<DP, BF16>), dim3((unsigned)(p.slots * h.H * p.blocks), dirs), dim3(256), 0, s, h, l, p.cut, p.blocks);
     if (p.scan)
-        hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (h.D * h.D + 255) / 256, dirs), dim3(256), 0, s, h, l, p.cut);
+        hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, dirs), dim3(256), 0, s, h, l, p.cut, p.part_size);
     return hipGetLastError();
 }
 template <int DP, bool BF16, int GRAD>
@@ -991,11 +1033,11 @@ template <int DP, bool BF16>
 static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, false);
     LocalsDev l{};
-    l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, h.partial, false};
+    l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, h.partial, false, false};
     const hipError_t e = launch_locals<DP, BF16>(h, l, p, 1, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
-    all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, true};
+    all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, false, true};
     return launch_sweeps<DP, BF16, 0>(h, all, p, 0, s);
 }
 template <int DP, bool BF16>
@@ -1004,14 +1046,14 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     double* const dw_parts = (double*)h.partial;
     float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const du_parts = G + p.part_floats;
     LocalsDev l{};
-    l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, S, false};
-    l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true};
+    l.dir[0] = LocalDev{h.v, h.k, h.v_stride, h.k_stride, h.state, S, false, true};
+    l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true, false};
     hipError_t e = launch_locals<DP, BF16>(h, l, p, 2, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
-    all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
-    all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, false};
-    all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, true};
+    all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false, false};
+    all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true, false};
+    all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false, true};
     all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
     if ((e = launch_sweeps<DP, BF16, 1>(h, all, p, 0, s)) != hipSuccess) return e;
     if ((e = launch_sweeps<DP, BF16, 2>(h, all, p, 1, s)) != hipSuccess) return e;
