@@ -146,14 +146,16 @@ __device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int sl
 
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
 // published beside the one that the outputs still read.
-template <int DP, bool BF16, int GRAD> struct Lds {
+template <int DP, bool BF16, int GRAD, bool PAIR = false> struct Lds {
+    static constexpr int threads = PAIR ? 768 : 512;
+    static constexpr bool split_keys = PAIR && !BF16;                            // fp16 keys as two bf16 parts too: they are somebody's val
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
-    static constexpr int key = 0, val = key + kChunk * key_row, val_lo = val + kChunk * val_row;
-    static constexpr int parts = GRAD ? 3 : 2, part = kVals * key_row;          // of a published state
+    static constexpr int key = 0, key_lo = key + kChunk * key_row, val = key_lo + (split_keys ? kChunk * key_row : 0), val_lo = val + kChunk * val_row;
+    static constexpr int parts = GRAD || PAIR ? 3 : 2, part = kVals * key_row;   // of a published state
     static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), buffer = state + parts * part;
-    static constexpr bool two = 2 * buffer + 4 * DP + 1088 <= 160 * 1024 && (BF16 || DP > 64);
+    static constexpr bool two = 2 * buffer + 4 * DP + 1152 <= 160 * 1024 && (BF16 || DP > 64 || PAIR);
     static constexpr int u = two ? 2 * buffer : buffer, sums = u + 4 * DP;
-    static constexpr int bytes = sums + (GRAD ? 4 * 4 * kVals + 8 * 8 : 0);
+    static constexpr int bytes = sums + (GRAD || PAIR ? 12 * 8 + 4 * 4 * kVals : 0);
 };
 
 // Two values as packed bf16 and what is left of them.
@@ -321,23 +323,44 @@ template <int NT, int COUNT, int PER>
 struct Rows {
     uint4_t data[COUNT];
     uint32_t offset[COUNT];                       // of a whole chunk
-    __device__ __forceinline__ void begin(long long stride, int width, bool reverse) {
+    int id;                                       // the thread's number among the NT
+    __device__ __forceinline__ void begin(int thread, long long stride, int width, bool reverse) {
+        id = thread;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
+            const int c = id + NT * i, col = 8 * (c % PER);
             offset[i] = row_offset(c / PER, reverse, stride, col < width ? col : 0);
         }
     }
-    __device__ __forceinline__ void fetch(const char* lowest) {
+    // the next nt rows: a whole chunk, or what a segment has beyond whole ones
+    __device__ __forceinline__ void fetch(const char* lowest, int nt, long long stride, int width, bool reverse) {
+        if (nt >= kChunk) {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) data[i] = *(const uint4_t*)(lowest + offset[i]);
+            for (int i = 0; i < COUNT; ++i) data[i] = *(const uint4_t*)(lowest + offset[i]);
+        } else if (nt > 0) {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int c = id + NT * i, col = 8 * (c % PER);
+                data[i] = *(const uint4_t*)(lowest + row_offset(min(c / PER, nt - 1), reverse, stride, col < width ? col : 0));
+            }
+        }
     }
-    // the last nt < kChunk rows of a segment
-    __device__ __forceinline__ void fetch_tail(const char* lowest, int nt, long long stride, int width, bool reverse) {
+    __device__ __forceinline__ void store(char* tile, int row_bytes) const {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int c = threadIdx.x + NT * i, col = 8 * (c % PER);
-            data[i] = *(const uint4_t*)(lowest + row_offset(min(c / PER, nt - 1), reverse, stride, col < width ? col : 0));
+            const int c = id + NT * i;
+            *(uint4_t*)(tile + (c / PER) * row_bytes + 16 * (c % PER)) = data[i];
+        }
+    }
+    // fp16 values as two bf16 parts
+    __device__ __forceinline__ void store_split(char* hi, char* lo, int row_bytes) const {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = id + NT * i;
+            uint4_t x, y;
+            split_f16(data[i], x, y);
+            *(uint4_t*)(hi + (c / PER) * row_bytes + 16 * (c % PER)) = x;
+            *(uint4_t*)(lo + (c / PER) * row_bytes + 16 * (c % PER)) = y;
         }
     }
 };
@@ -351,26 +374,6 @@ struct Walk {
 };
 // Chunks of both directions meet at multiples of 64 tokens from a segment's front: backwards, a shorter one comes first.
 __device__ __forceinline__ int first_chunk(int len, bool reverse) { return reverse ? len - (len - 1) / kChunk * kChunk : min(kChunk, len); }
-template <int NT, int COUNT, int PER>
-__device__ __forceinline__ void stage(const uint4_t (&from)[COUNT], char* tile, int row_bytes) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        const int c = threadIdx.x + NT * i;
-        *(uint4_t*)(tile + (c / PER) * row_bytes + 16 * (c % PER)) = from[i];
-    }
-}
-template <int NT, int COUNT, int PER>
-__device__ __forceinline__ void stage_split(const uint4_t (&from)[COUNT], char* hi, char* lo, int row_bytes) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        const int c = threadIdx.x + NT * i;
-        uint4_t a, b;
-        split_f16(from[i], a, b);
-        *(uint4_t*)(hi + (c / PER) * row_bytes + 16 * (c % PER)) = a;
-        *(uint4_t*)(lo + (c / PER) * row_bytes + 16 * (c % PER)) = b;
-    }
-}
-
 // Powers of exp(-w) from which a chunk's weights are made.  A lane meets tokens 16 it + 4 g + j: their weights are near[j] times a
 // power that the whole wavefront shares, so that four registers and a few scalars stand for them all.
 struct Powers {
@@ -396,13 +399,18 @@ __device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, i
 }
 struct Whole { static constexpr bool tail = false; };
 struct Tail { static constexpr bool tail = true; };
-// A fragment of 16-bit keys times its weights as three bf16 parts.
-template <bool BF16>
-__device__ __forceinline__ void weighted_keys(const uint4_t& k, const float (&kw)[8], uint4_t (&out)[3]) {
+// A fragment of keys (16-bit ones, or two bf16 parts of fp16 ones) times its weights as three bf16 parts.
+template <bool BF16, bool SPLIT>
+__device__ __forceinline__ void weighted_keys(const uint4_t& k, const uint4_t& low, const float (&kw)[8], uint4_t (&out)[3]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t pair = k[i];
-        float a = widen16<BF16>((uint16_t)pair) * kw[2 * i], b = widen16<BF16>((uint16_t)(pair >> 16)) * kw[2 * i + 1];
+        float a = widen16<BF16 || SPLIT>((uint16_t)pair), b = widen16<BF16 || SPLIT>((uint16_t)(pair >> 16));
+        if (SPLIT) {
+            const uint32_t rest = low[i];
+            a += widen16<true>((uint16_t)rest); b += widen16<true>((uint16_t)(rest >> 16));
+        }
+        a *= kw[2 * i]; b *= kw[2 * i + 1];
         out[0][i] = split2(a, b);
         out[1][i] = split2(a, b);
         out[2][i] = Elem<true>::pack(a, b);
@@ -411,11 +419,11 @@ __device__ __forceinline__ void weighted_keys(const uint4_t& k, const float (&kw
 
 // S += (weighted keys)^T val over 32 tokens of a staged chunk, the weighted keys as PARTS bf16 parts.
 template <bool BF16, class L, int PARTS, int KT>
-__device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const uint4_t (&keys)[KT], const float (&kw)[8], const uint4_t (&vf)[4], const uint4_t (&vl)[4]) {
+__device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const uint4_t (&keys)[KT], const uint4_t (&low)[KT], const float (&kw)[8], const uint4_t (&vf)[4], const uint4_t (&vl)[4]) {
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
         uint4_t kp[3];
-        weighted_keys<BF16>(keys[x], kw, kp);
+        weighted_keys<BF16, L::split_keys>(keys[x], low[x], kw, kp);
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
@@ -426,18 +434,21 @@ __device__ __forceinline__ void update_state(float4_t (&S)[KT][4], const uint4_t
     }
 }
 // The operands of 32 staged tokens: columns of val (fp16: two parts), and of a wavefront's share of the keys.
-template <bool BF16, class L>
-__device__ __forceinline__ void val_columns(const char* lds, int ks, int n, int g, uint4_t (&vf)[4], uint4_t (&vl)[4]) {
+template <bool BF16>
+__device__ __forceinline__ void val_columns(const char* hi, const char* lo, int ks, int n, int g, uint4_t (&vf)[4], uint4_t (&vl)[4]) {
 #pragma unroll
     for (int vt = 0; vt < 4; ++vt) {
-        vf[vt] = column_frag<L::val_row>(lds + L::val, ks, vt, n, g);
-        if (!BF16) vl[vt] = column_frag<L::val_row>(lds + L::val_lo, ks, vt, n, g);
+        vf[vt] = column_frag<2 * kVals + 16>(hi, ks, vt, n, g);
+        if (!BF16) vl[vt] = column_frag<2 * kVals + 16>(lo, ks, vt, n, g);
     }
 }
 template <class L, int KT>
-__device__ __forceinline__ void key_columns(const char* lds, int ks, int wave, int n, int g, uint4_t (&keys)[KT]) {
+__device__ __forceinline__ void key_columns(const char* lds, int ks, int wave, int n, int g, uint4_t (&keys)[KT], uint4_t (&low)[KT]) {
 #pragma unroll
-    for (int x = 0; x < KT; ++x) keys[x] = column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g);
+    for (int x = 0; x < KT; ++x) {
+        keys[x] = column_frag<L::key_row>(lds + L::key, ks, KT * wave + x, n, g);
+        if (L::split_keys) low[x] = column_frag<L::key_row>(lds + L::key_lo, ks, KT * wave + x, n, g);
+    }
 }
 template <int KT>
 __device__ __forceinline__ void scale(float4_t (&S)[KT][4], float by) {
@@ -479,14 +490,14 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 4) attend_local_kernel(Head
     const int len = s.a1 - s.a0;
     Rows<256, DP / 32, DP / 8> kr;
     Rows<256, 2, 8> vr;
-    kr.begin(p.key_stride, D, p.reverse);
-    vr.begin(p.val_stride, D - v0, p.reverse);
+    kr.begin(threadIdx.x, p.key_stride, D, p.reverse);
+    vr.begin(threadIdx.x, p.val_stride, D - v0, p.reverse);
     Walk key_at(p.key + head * D, p.key_stride, s.a0, s.a1, p.reverse), val_at(p.val + head * D + v0, p.val_stride, s.a0, s.a1, p.reverse);
     const long long key_stride = p.key_stride, val_stride = p.val_stride;
     const bool reverse = p.reverse;
     auto fetch = [&](int nt) {
-        if (nt >= kChunk) { kr.fetch(key_at.at); vr.fetch(val_at.at); }
-        else if (nt > 0) { kr.fetch_tail(key_at.at, nt, key_stride, D, reverse); vr.fetch_tail(val_at.at, nt, val_stride, D - v0, reverse); }
+        kr.fetch(key_at.at, nt, key_stride, D, reverse);
+        vr.fetch(val_at.at, nt, val_stride, D - v0, reverse);
         key_at.pass(nt); val_at.pass(nt);
     };
     int nt = first_chunk(len, reverse);
@@ -497,21 +508,21 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 4) attend_local_kernel(Head
     auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         char* const lds = both[turn];
-        stage<256, DP / 32, DP / 8>(kr.data, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<256, 2, 8>(vr.data, lds + L::val, L::val_row);
-        else stage_split<256, 2, 8>(vr.data, lds + L::val, lds + L::val_lo, L::val_row);
+        kr.store(lds + L::key, L::key_row);
+        if constexpr (BF16) vr.store(lds + L::val, L::val_row);
+        else vr.store_split(lds + L::val, lds + L::val_lo, L::val_row);
         __syncthreads();
         turn ^= 1;
         fetch(next);
         scale(S, tail ? expf(-(float)nt * w) : pow.whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uint4_t vf[4], vl[4], keys[KT];
+            uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
             key_weights<tail>(kw, pow, ks, nt, w, g);
-            val_columns<BF16, L>(lds, ks, n, g, vf, vl);
-            key_columns<L>(lds, ks, wave, n, g, keys);
-            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
+            val_columns<BF16>(lds + L::val, lds + L::val_lo, ks, n, g, vf, vl);
+            key_columns<L>(lds, ks, wave, n, g, keys, low);
+            update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
         }
     };
     for (int left = len; left > 0;) {
@@ -563,6 +574,11 @@ struct SweepDev {
     const float *initial, *parts;       // of the sweep's own state
     float* last;                        // where the state behind the sequence goes, or nullptr
     bool reverse, transposed, parts_transposed, u_in_dot;       // transposed: key is what the state in memory calls val; and what the parts do
+    __device__ __forceinline__ SweepDev swapped() const {
+        SweepDev s = *this;
+        s.key = val; s.val = key; s.key_stride = val_stride; s.val_stride = key_stride;
+        return s;
+    }
 };
 struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* du_parts; double* dw_parts; };   // dw_parts: [slots][H][4]
 
@@ -575,7 +591,7 @@ struct Place {
     int slot_at, slot, head, v0, D, len, lane, wave, n, g;
     float w;
 };
-// A thread's share of the staging of a sweep's chunks.
+// A thread's share of the staging of a sweep's chunks.  Of twelve wavefronts the first eight bring the keys, the last eight val.
 template <int DP, bool BF16, class L>
 struct Staging {
     Rows<512, DP / 64, DP / 8> key;
@@ -583,31 +599,36 @@ struct Staging {
     Walk key_at, val_at;
     long long key_stride, val_stride;
     int D, width;
-    bool reverse;
+    bool reverse, keys, vals;
     __device__ __forceinline__ Staging(const SweepDev& p, const Place& at)
         : key_at(p.key + at.head * at.D, p.key_stride, at.s.a0, at.s.a1, p.reverse),
           val_at(p.val + at.head * at.D + at.v0, p.val_stride, at.s.a0, at.s.a1, p.reverse),
-          key_stride(p.key_stride), val_stride(p.val_stride), D(at.D), width(at.D - at.v0), reverse(p.reverse) {
-        key.begin(key_stride, D, reverse);
-        val.begin(val_stride, width, reverse);
+          key_stride(p.key_stride), val_stride(p.val_stride), D(at.D), width(at.D - at.v0), reverse(p.reverse),
+          keys(L::threads == 512 || at.wave < 8), vals(L::threads == 512 || at.wave >= 4) {
+        if (keys) key.begin(threadIdx.x, key_stride, D, reverse);
+        if (vals) val.begin(threadIdx.x - (L::threads - 512), val_stride, width, reverse);
     }
     // the next chunk, of nt rows
     __device__ __forceinline__ void fetch(int nt) {
-        if (nt >= kChunk) { key.fetch(key_at.at); val.fetch(val_at.at); }
-        else if (nt > 0) { key.fetch_tail(key_at.at, nt, key_stride, D, reverse); val.fetch_tail(val_at.at, nt, val_stride, width, reverse); }
+        if (keys) key.fetch(key_at.at, nt, key_stride, D, reverse);
+        if (vals) val.fetch(val_at.at, nt, val_stride, width, reverse);
         key_at.pass(nt); val_at.pass(nt);
     }
     __device__ __forceinline__ void store(char* lds) const {
-        stage<512, DP / 64, DP / 8>(key.data, lds + L::key, L::key_row);
-        if constexpr (BF16) stage<512, 1, 8>(val.data, lds + L::val, L::val_row);
-        else stage_split<512, 1, 8>(val.data, lds + L::val, lds + L::val_lo, L::val_row);
+        if (keys) {
+            if constexpr (L::split_keys) key.store_split(lds + L::key, lds + L::key_lo, L::key_row);
+            else key.store(lds + L::key, L::key_row);
+        }
+        if (vals) {
+            if constexpr (BF16) val.store(lds + L::val, L::val_row);
+            else val.store_split(lds + L::val, lds + L::val_lo, L::val_row);
+        }
     }
 };
 
 // The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of L <G, S>.
-template <int DP, bool BF16, int GRAD>
+template <int DP, bool BF16, class L, bool MEETS_G>
 __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
-    typedef Lds<DP, BF16, GRAD> L;
     constexpr int KT = DP / 64;
     const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
     const float w = at.w;
@@ -640,12 +661,12 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
         scale(S, tail ? expf(-(float)nt * w) : pow.whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uint4_t vf[4], vl[4], keys[KT];
+            uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
             key_weights<tail>(kw, pow, ks, nt, w, g);
-            val_columns<BF16, L>(buffer, ks, n, g, vf, vl);
-            key_columns<L>(buffer, ks, wave, n, g, keys);
-            update_state<BF16, L, 3>(S, keys, kw, vf, vl);
+            val_columns<BF16>(buffer + L::val, buffer + L::val_lo, ks, n, g, vf, vl);
+            key_columns<L>(buffer, ks, wave, n, g, keys, low);
+            update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
         }
         if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
         else __syncthreads();
@@ -659,7 +680,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     }
     if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
     double dw = 0.0;
-    if constexpr (GRAD == 1) {                    // G: the gradient of the state at the segment's end
+    if constexpr (MEETS_G) {                      // G: the gradient of the state at the segment's end
         float4_t G[KT][4];
         start_state(G, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
 #pragma unroll
@@ -676,30 +697,40 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
 }
 
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
-template <int DP, bool BF16, int GRAD>
-__device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
-    typedef Lds<DP, BF16, GRAD> L;
-    constexpr int KS = DP / 32;
-    const int wave = at.wave, n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
+//   GRAD 1: the shares of dw that dr's sweep has, with x = r;  2: those of dk's and du, with x = k;  0: neither.  STORE: the outputs.
+//   SWAP: the tiles and the state are those of the sweep for dv, whose key and val exchange their roles in the one for dk.
+template <int DP, bool BF16, class L, int GRAD, bool STORE, bool SWAP>
+__device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, int wave, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
+    constexpr int KS = DP / 32, parts = GRAD ? L::parts : 2;
+    constexpr int key_tile = SWAP ? L::val : L::key, key_low = SWAP ? L::val_lo : L::key_lo, val_tile = SWAP ? L::key : L::val, val_low = SWAP ? L::key_lo : L::val_lo;
+    const int n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
-    Staging<DP, BF16, L> rows(p, at);
+    Staging<DP, BF16, L> rows(SWAP ? p.swapped() : p, at);
     const bool reverse = p.reverse, u_in_dot = p.u_in_dot;
     const long long q_stride = p.q_stride, x_stride = p.x_stride, out_stride = p.out_stride;
     Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRAD ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
         out_at(p.out + at.head * D + v0, out_stride, at.s.a0, at.s.a1, reverse);
     uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
     uint2_t xdr[4];
-    const uint32_t q_off = row_offset(a, reverse, q_stride, 8 * g), x_off = GRAD ? row_offset(a, reverse, x_stride, 0) : 0,
+    const int q_col = SWAP ? 4 * g : 8 * g;
+    const uint32_t q_off = row_offset(a, reverse, q_stride, q_col), x_off = GRAD ? row_offset(a, reverse, x_stride, 0) : 0,
                    out_off = row_offset(a, reverse, out_stride, 4 * g);
     auto fetch = [&](int nt) {
         rows.fetch(nt);
         if (nt > 0) {
             const int row = min(a, nt - 1);
-            const char* const from = q_at.at + (nt < kChunk ? row_offset(row, reverse, q_stride, 8 * g) : q_off);
+            const char* const from = q_at.at + (nt < kChunk ? row_offset(row, reverse, q_stride, q_col) : q_off);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 qr[i] = uint4_t{0, 0, 0, 0};
-                if (D == DP || 32 * i + 8 * g < D) qr[i] = *(const uint4_t*)(from + 64 * i);
+                if constexpr (SWAP) {             // in the order of column_frag
+                    uint2_t a = {0, 0}, b = {0, 0};
+                    if (D == DP || 32 * i + 4 * g < D) a = *(const uint2_t*)(from + 64 * i);
+                    if (D == DP || 32 * i + 16 + 4 * g < D) b = *(const uint2_t*)(from + 64 * i + 32);
+                    qr[i] = uint4_t{a.x, a.y, b.x, b.y};
+                } else if (D == DP || 32 * i + 8 * g < D) {
+                    qr[i] = *(const uint4_t*)(from + 64 * i);
+                }
             }
             if constexpr (GRAD) {
                 const char* const xf = x_at.at + (nt < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
@@ -721,7 +752,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     int nt = first_chunk(at.len, reverse);
     fetch(nt);
     // u, where the bonus needs it: with the channels of the dot, or with those of val
-    const int u0 = u_in_dot ? 0 : v0, tid = threadIdx.x;
+    const int u0 = u_in_dot ? 0 : v0, tid = 64 * wave + at.lane;
     if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
 
     // weights of pairs of a tile's tokens a > i, and of those with an earlier tile's; of the state in front
@@ -770,10 +801,11 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int part = L::parts - 1; part >= 0; --part) {
-                    const uint4_t st = *(const uint4_t*)(buffer + L::state + part * L::part + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                for (int part = parts - 1; part >= 0; --part) {
+                    const char* const from = buffer + L::state + part * L::part;
+                    const uint4_t st = SWAP ? column_frag<L::key_row>(from, i, vt, n, g) : *(const uint4_t*)(from + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
                     o = mfma_bits<true>(st, qh[i], o);
-                    if (!BF16 && part < L::parts - 1) o = mfma_bits<true>(st, ql[i], o);
+                    if (!BF16 && part < parts - 1) o = mfma_bits<true>(st, ql[i], o);
                 }
             out[vt] = front * o;
             if constexpr (GRAD) {
@@ -797,11 +829,24 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             uint2_t sp[2] = {{0, 0}, {0, 0}};
             if (it <= wave) {
                 float4_t sc = {0, 0, 0, 0};
-                uint4_t kf[KS];
+                uint4_t kf[KS], kl[KS];
+                auto key_frag = [&](int tile, int i) {
+                    const char* const from = buffer + tile + (16 * it + n) * L::key_row + 64 * i;
+                    if (!SWAP) return *(const uint4_t*)(from + 16 * g);
+                    const uint2_t a = *(const uint2_t*)(from + 8 * g), b = *(const uint2_t*)(from + 32 + 8 * g);
+                    return uint4_t{a.x, a.y, b.x, b.y};
+                };
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
-                    kf[i] = *(const uint4_t*)(buffer + L::key + (16 * it + n) * L::key_row + 2 * (32 * i + 8 * g));
-                    sc = mfma_bits<BF16>(kf[i], qf[i], sc);
+                    kf[i] = key_frag(key_tile, i);
+                    if constexpr (L::split_keys) {
+                        kl[i] = key_frag(key_low, i);
+                        sc = mfma_bits<true>(kl[i], qh[i], sc);
+                        sc = mfma_bits<true>(kf[i], ql[i], sc);
+                        sc = mfma_bits<true>(kf[i], qh[i], sc);
+                    } else {
+                        sc = mfma_bits<BF16>(kf[i], qf[i], sc);
+                    }
                 }
                 if (it < wave) {
                     const float tiles = wave - it == 1 ? far[0] : wave - it == 2 ? far[1] : far[2];
@@ -817,7 +862,12 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 #pragma unroll
                                 for (int c4 = 0; c4 < 4; ++c4) {
                                     const uint32_t qq = qf[i][2 * c2 + (c4 >> 1)], kk = kf[i][2 * c2 + (c4 >> 1)];
-                                    dot = fmaf(widen16<BF16>((uint16_t)(qq >> (16 * (c4 & 1)))) * u[c4], widen16<BF16>((uint16_t)(kk >> (16 * (c4 & 1)))), dot);
+                                    float k = widen16<BF16 || L::split_keys>((uint16_t)(kk >> (16 * (c4 & 1))));
+                                    if constexpr (L::split_keys) {
+                                        const uint32_t rest = kl[i][2 * c2 + (c4 >> 1)];
+                                        k += widen16<true>((uint16_t)(rest >> (16 * (c4 & 1))));
+                                    }
+                                    dot = fmaf(widen16<BF16>((uint16_t)(qq >> (16 * (c4 & 1)))) * u[c4], k, dot);
                                 }
                             }
                     } else {
@@ -832,15 +882,15 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                         if (GRAD == 0 && u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
                     }
                 }
-                split4(sc, sp);
+                if constexpr (STORE) split4(sc, sp);
                 if constexpr (GRAD == 1) {                             // x . val of the same pairs, weighted with their lags
                     float4_t xv = {0, 0, 0, 0};
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int from = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
-                        const uint4_t v = *(const uint4_t*)(buffer + L::val + from);
+                        const uint4_t v = *(const uint4_t*)(buffer + val_tile + from);
                         if (!BF16) {
-                            const uint4_t vl = *(const uint4_t*)(buffer + L::val_lo + from);
+                            const uint4_t vl = *(const uint4_t*)(buffer + val_low + from);
                             xv = mfma_bits<true>(vl, xl[i], xv);
                             xv = mfma_bits<true>(vl, xf[i], xv);
                             xv = mfma_bits<true>(v, xl[i], xv);
@@ -855,11 +905,12 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             }
             ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
         }
+        if constexpr (STORE) {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (2 * ks <= wave) {
                 uint4_t vf[4], vl[4];
-                val_columns<BF16, L>(buffer, ks, n, g, vf, vl);
+                val_columns<BF16>(buffer + val_tile, buffer + val_low, ks, n, g, vf, vl);
 #pragma unroll
                 for (int vt = 0; vt < 4; ++vt) {
                     out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
@@ -872,11 +923,11 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
         if (GRAD || !u_in_dot) {
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
-                const uint2_t vh = *(const uint2_t*)(buffer + L::val + a * L::val_row + 2 * (16 * vt + 4 * g));
+                const uint2_t vh = *(const uint2_t*)(buffer + val_tile + a * L::val_row + 2 * (16 * vt + 4 * g));
                 const float4_t u = *(const float4_t*)(lds + L::u + 4 * (16 * vt + 4 * g));
                 float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
                 if (!BF16) {
-                    const uint2_t l = *(const uint2_t*)(buffer + L::val_lo + a * L::val_row + 2 * (16 * vt + 4 * g));
+                    const uint2_t l = *(const uint2_t*)(buffer + val_low + a * L::val_row + 2 * (16 * vt + 4 * g));
                     v[0] += __uint_as_float(l.x << 16); v[1] += __uint_as_float(l.x & 0xFFFF0000u);
                     v[2] += __uint_as_float(l.y << 16); v[3] += __uint_as_float(l.y & 0xFFFF0000u);
                 }
@@ -895,6 +946,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 if (D == DP || v0 + 16 * vt + 4 * g < D)
                     *(uint2_t*)(to + 32 * vt) = uint2_t{Elem<BF16>::pack(out[vt][0], out[vt][1]), Elem<BF16>::pack(out[vt][2], out[vt][3])};
         }
+        }
         out_at.pass(nt);
         if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
         else __syncthreads();
@@ -908,55 +960,93 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     return dw;
 }
 
+// Where a workgroup is; false if it has nothing to do.
+__device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut, int blocks, int* found) {
+    const int tid = threadIdx.x;
+    at.slot_at = blockIdx.x / (h.H * blocks); at.head = blockIdx.x / blocks % h.H; at.v0 = blockIdx.x % blocks * kVals; at.D = h.D;
+    at.lane = tid & 63; at.wave = __builtin_amdgcn_readfirstlane(tid >> 6); at.n = at.lane & 15; at.g = at.lane >> 4;
+    if (tid == 0) *found = -1;
+    __syncthreads();
+    at.s = segment_of(h, cut, at.slot_at, found);
+    at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
+    if (at.slot < 0) return false;
+    at.len = at.s.a1 - at.s.a0;
+    at.w = h.w[at.head];
+    return true;
+}
+// A workgroup's parts of dw, and of du from four of its wavefronts (`which`: 0 .. 3, or -1).
+template <int WAVES, bool DU>
+__device__ __forceinline__ void leave_sums(const HeadsDev& h, const SweepsDev& all, const Place& at, int half, double dw, const float* du, int which, char* lds) {
+    double* const each = (double*)lds;
+    float* const across = (float*)(each + 12);
+#pragma unroll
+    for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
+    if (at.lane == 0) each[at.wave] = dw;
+    if constexpr (DU) {
+        if (which >= 0)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float sum = du[i];
+#pragma unroll
+                for (int off = 8; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
+                if (at.n == 0) across[kVals * which + 16 * (i >> 2) + 4 * at.g + (i & 3)] = sum;
+            }
+    }
+    __syncthreads();
+    const int tid = threadIdx.x;
+    if (DU && tid < kVals && at.v0 + tid < at.D)
+        all.du_parts[((size_t)at.slot_at * h.H + at.head) * at.D + at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
+    if (tid == 0) {
+        double sum = 0.0;
+        for (int i = 0; i < WAVES; ++i) sum += each[i];
+        all.dw_parts[((size_t)at.slot_at * h.H + at.head) * 4 + 2 * half + at.v0 / kVals] = -sum;
+    }
+}
+// The same of one that has nothing to do.
+template <bool DU>
+__device__ __forceinline__ void leave_zeros(const HeadsDev& h, const SweepsDev& all, const Place& at, int half) {
+    const int tid = threadIdx.x;
+    if (DU && tid < kVals && at.v0 + tid < at.D) all.du_parts[((size_t)at.slot_at * h.H + at.head) * at.D + at.v0 + tid] = 0.0f;
+    if (tid == 0) all.dw_parts[((size_t)at.slot_at * h.H + at.head) * 4 + 2 * half + at.v0 / kVals] = 0.0;
+}
+
+// One sweep: four wavefronts for the outputs, four for the state, which meet at the same barriers.
 template <int DP, bool BF16, int GRAD>
 __global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int which) {
     typedef Lds<DP, BF16, GRAD> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
-    const SweepDev& p = all.sweep[which];
-    const int tid = threadIdx.x, D = h.D;
     Place at;
-    at.slot_at = blockIdx.x / (h.H * blocks); at.head = blockIdx.x / blocks % h.H; at.v0 = blockIdx.x % blocks * kVals; at.D = D;
-    at.lane = tid & 63; at.wave = __builtin_amdgcn_readfirstlane(tid >> 6); at.n = at.lane & 15; at.g = at.lane >> 4;
-    if (tid == 0) found = -1;
-    __syncthreads();
-    at.s = segment_of(h, cut, at.slot_at, &found);
-    at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
-    float* const du_part = GRAD == 2 ? all.du_parts + ((size_t)at.slot_at * h.H + at.head) * D : nullptr;
-    double* const dw_part = GRAD ? all.dw_parts + ((size_t)at.slot_at * h.H + at.head) * 4 + 2 * (GRAD - 1) + at.v0 / kVals : nullptr;
-    if (at.slot < 0) {
-        if (GRAD == 2 && tid < kVals && at.v0 + tid < D) du_part[at.v0 + tid] = 0.0f;
-        if (GRAD && tid == 0) *dw_part = 0.0;
+    if (!find_place(at, h, cut, blocks, &found)) {
+        if constexpr (GRAD != 0) leave_zeros<GRAD == 2>(h, all, at, GRAD - 1);
         return;
     }
-    at.len = at.s.a1 - at.s.a0;
-    at.w = h.w[at.head];
-    // the two kinds of wavefront meet at the same barriers
     float du[GRAD == 2 ? 16 : 1] = {};
-    double dw = at.wave < 4 ? outputs<DP, BF16, GRAD>(h, p, at, du, lds) : carry_state<DP, BF16, GRAD>(h, p, all, at, cut, scanned != 0, lds);
-    if constexpr (GRAD) {
-        double* const each = (double*)(lds + L::sums);
-        float* const across = (float*)(each + 8);
-#pragma unroll
-        for (int off = 32; off; off >>= 1) dw += __shfl_xor(dw, off, 64);
-        if (at.lane == 0) each[at.wave] = dw;
-        if (GRAD == 2 && at.wave < 4)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float sum = du[GRAD == 2 ? i : 0];
-#pragma unroll
-                for (int off = 8; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-                if (at.n == 0) across[kVals * at.wave + 16 * (i >> 2) + 4 * at.g + (i & 3)] = sum;
-            }
-        __syncthreads();
-        if (GRAD == 2 && tid < kVals && at.v0 + tid < D)
-            du_part[at.v0 + tid] = across[tid] + across[kVals + tid] + across[2 * kVals + tid] + across[3 * kVals + tid];
-        if (tid == 0) {
-            double sum = 0.0;
-            for (int i = 0; i < 8; ++i) sum += each[i];
-            *dw_part = -sum;
-        }
+    const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false>(h, all.sweep[which], at, at.wave, du, lds)
+                                  : carry_state<DP, BF16, L, GRAD == 1>(h, all.sweep[which], all, at, cut, scanned != 0, lds);
+    if constexpr (GRAD != 0) leave_sums<8, GRAD == 2>(h, all, at, GRAD - 1, dw, du, at.wave < 4 ? at.wave : -1, lds + L::sums);
+}
+
+// Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
+// in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
+// dw, which need the state in more bits, computed apart from its outputs.
+template <bool BF16, bool DK>
+__global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+    typedef Lds<64, BF16, 0, true> L;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int found;
+    Place at;
+    if (!find_place(at, h, cut, 1, &found)) {
+        leave_zeros<DK>(h, all, at, DK);
+        return;
     }
+    float du[DK ? 16 : 1] = {}, none[1];
+    const SweepDev& p = all.sweep[DK ? 2 : 0];
+    const double dw = at.wave < 4   ? outputs<64, BF16, L, 0, true, false>(h, p, at, at.wave, none, lds)
+                      : at.wave < 8 ? carry_state<64, BF16, L, !DK>(h, p, all, at, cut, scanned != 0, lds)
+                      : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK>(h, all.sweep[1], at, at.wave - 8, du, lds)
+                                    : outputs<64, BF16, L, DK ? 2 : 1, DK, DK>(h, p, at, at.wave - 8, du, lds);
+    leave_sums<12, DK>(h, all, at, DK, dw, du, at.wave >= 8 ? at.wave - 8 : -1, lds + L::sums);
 }
 
 // du [H][D] from its parts [slots][H][D], dw [H] from [slots][H][4], of which `blocks` are used in each half: sixteen threads an entry, in a
@@ -1029,6 +1119,16 @@ static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const P
     return hipGetLastError();
 }
 
+template <bool BF16, bool DK>
+static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
+    static std::atomic<unsigned long long> raised{0};
+    constexpr int bytes = Lds<64, BF16, 0, true>::bytes;
+    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, DK>, bytes, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, DK>), dim3((unsigned)(p.slots * h.H)), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
+    return hipGetLastError();
+}
+
 template <int DP, bool BF16>
 static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, false);
@@ -1055,9 +1155,14 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true, false};
     all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false, true};
     all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
-    if ((e = launch_sweeps<DP, BF16, 1>(h, all, p, 0, s)) != hipSuccess) return e;
-    if ((e = launch_sweeps<DP, BF16, 2>(h, all, p, 1, s)) != hipSuccess) return e;
-    if ((e = launch_sweeps<DP, BF16, 0>(h, all, p, 2, s)) != hipSuccess) return e;
+    if constexpr (DP == 64) {
+        if ((e = launch_pair<BF16, false>(h, all, p, s)) != hipSuccess) return e;
+        if ((e = launch_pair<BF16, true>(h, all, p, s)) != hipSuccess) return e;
+    } else {
+        if ((e = launch_sweeps<DP, BF16, 1>(h, all, p, 0, s)) != hipSuccess) return e;
+        if ((e = launch_sweeps<DP, BF16, 2>(h, all, p, 1, s)) != hipSuccess) return e;
+        if ((e = launch_sweeps<DP, BF16, 0>(h, all, p, 2, s)) != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 1) + 15) / 16), dim3(256), 0, s, h, du_parts, dw_parts, p.slots, p.blocks);
     return hipGetLastError();
 }
