@@ -573,7 +573,7 @@ struct SweepDev {
     uint16_t* out;
     const float *initial, *parts;       // of the sweep's own state
     float* last;                        // where the state behind the sequence goes, or nullptr
-    bool reverse, transposed, parts_transposed, u_in_dot;       // transposed: key is what the state in memory calls val; and what the parts do
+    bool reverse, transposed, parts_transposed;        // transposed: key is what the state in memory calls val; and what the parts do
     __device__ __forceinline__ SweepDev swapped() const {
         SweepDev s = *this;
         s.key = val; s.val = key; s.key_stride = val_stride; s.val_stride = key_stride;
@@ -696,17 +696,19 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     return dw;
 }
 
+__device__ __forceinline__ float weighted(float w, float x) { return w != 0.0f ? w * x : 0.0f; }
+
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
 //   GRAD 1: the shares of dw that dr's sweep has, with x = r;  2: those of dk's and du, with x = k;  0: neither.  STORE: the outputs.
 //   SWAP: the tiles and the state are those of the sweep for dv, whose key and val exchange their roles in the one for dk.
-template <int DP, bool BF16, class L, int GRAD, bool STORE, bool SWAP>
+template <int DP, bool BF16, class L, int GRAD, bool STORE, bool SWAP, bool U_IN_DOT>
 __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, int wave, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
     constexpr int KS = DP / 32, parts = GRAD ? L::parts : 2;
     constexpr int key_tile = SWAP ? L::val : L::key, key_low = SWAP ? L::val_lo : L::key_lo, val_tile = SWAP ? L::key : L::val, val_low = SWAP ? L::key_lo : L::val_lo;
     const int n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
     Staging<DP, BF16, L> rows(SWAP ? p.swapped() : p, at);
-    const bool reverse = p.reverse, u_in_dot = p.u_in_dot;
+    const bool reverse = p.reverse;
     const long long q_stride = p.q_stride, x_stride = p.x_stride, out_stride = p.out_stride;
     Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRAD ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
         out_at(p.out + at.head * D + v0, out_stride, at.s.a0, at.s.a1, reverse);
@@ -751,20 +753,24 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     };
     int nt = first_chunk(at.len, reverse);
     fetch(nt);
-    // u, where the bonus needs it: with the channels of the dot, or with those of val
-    const int u0 = u_in_dot ? 0 : v0, tid = 64 * wave + at.lane;
+    const int u0 = U_IN_DOT ? 0 : v0, tid = 64 * wave + at.lane;
     if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
 
-    // weights of pairs of a tile's tokens a > i, and of those with an earlier tile's; of the state in front
-    float same[4], earlier[4], far[3];
-    const float front = expf(-(float)a * w), in_tile = expf(-(float)n * w);
+    // weights of pairs (token a, token 16 it + 4 g + j), 0 where i >= a; of the state in front; which of a tile's tokens is the lane's own.
+    // Every wavefront takes all four tiles: without branches their loads and products overlap, and the last wavefront has four anyway.
+    float pw[4][4], own[4], mine[4];
+    const float front = expf(-(float)a * w);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        same[j] = expf(-(float)max(n - 1 - 4 * g - j, 0) * w);
-        earlier[j] = expf(-(float)(15 - 4 * g - j) * w) * in_tile;
+    for (int it = 0; it < 4; ++it) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int lag = a - 1 - (16 * it + 4 * g + j);
+            pw[it][j] = lag >= 0 ? expf(-(float)lag * w) : 0.0f;
+        }
+        mine[it] = it == wave ? 1.0f : 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < 3; ++i) far[i] = Powers::uniform(expf(-(float)(16 * i) * w));
+    for (int j = 0; j < 4; ++j) own[j] = 4 * g + j == n ? 1.0f : 0.0f;
     double dw = 0.0;
     const bool slow = GRAD && passes(w, kChunk);
 
@@ -792,6 +798,12 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
         }
         fetch(next);
 
+        auto key_frag = [&](int tile, int row, int i) {
+            const char* const from = buffer + tile + row * L::key_row + 64 * i;
+            if (!SWAP) return *(const uint4_t*)(from + 16 * g);
+            const uint2_t x = *(const uint2_t*)(from + 8 * g), y = *(const uint2_t*)(from + 32 + 8 * g);
+            return uint4_t{x.x, x.y, y.x, y.y};
+        };
         // the state in front; for the gradient of w its part of the outputs with x, weighted by the token's place in the segment
         float4_t out[4];
         double state_dot = 0.0;
@@ -820,111 +832,98 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;
         }
 
-        // scores of the wavefront's tokens with those up to them; the bonus' dot is on their diagonal, or (with u) takes its place
+        // scores of the wavefront's tokens with those before them.  A weight of 0 leaves out also a score
+        // that left binary32
         uint4_t ph[2], pl[2];
-        float dot = 0.0f;
+        float dot = 0.0f;                         // of the bonus: a token's score with itself, or that with u
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
             const int ks = it >> 1, e = 2 * (it & 1);
-            uint2_t sp[2] = {{0, 0}, {0, 0}};
-            if (it <= wave) {
-                float4_t sc = {0, 0, 0, 0};
-                uint4_t kf[KS], kl[KS];
-                auto key_frag = [&](int tile, int i) {
-                    const char* const from = buffer + tile + (16 * it + n) * L::key_row + 64 * i;
-                    if (!SWAP) return *(const uint4_t*)(from + 16 * g);
-                    const uint2_t a = *(const uint2_t*)(from + 8 * g), b = *(const uint2_t*)(from + 32 + 8 * g);
-                    return uint4_t{a.x, a.y, b.x, b.y};
-                };
+            float4_t sc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    kf[i] = key_frag(key_tile, i);
-                    if constexpr (L::split_keys) {
-                        kl[i] = key_frag(key_low, i);
-                        sc = mfma_bits<true>(kl[i], qh[i], sc);
-                        sc = mfma_bits<true>(kf[i], ql[i], sc);
-                        sc = mfma_bits<true>(kf[i], qh[i], sc);
-                    } else {
-                        sc = mfma_bits<BF16>(kf[i], qf[i], sc);
-                    }
-                }
-                if (it < wave) {
-                    const float tiles = wave - it == 1 ? far[0] : wave - it == 2 ? far[1] : far[2];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sc[j] *= earlier[j] * tiles;
+            for (int i = 0; i < KS; ++i) {
+                const uint4_t kf = key_frag(key_tile, 16 * it + n, i);
+                if constexpr (L::split_keys) {
+                    sc = mfma_bits<true>(key_frag(key_low, 16 * it + n, i), qh[i], sc);
+                    sc = mfma_bits<true>(kf, ql[i], sc);
+                    sc = mfma_bits<true>(kf, qh[i], sc);
                 } else {
-                    if (u_in_dot) {
-#pragma unroll
-                        for (int i = 0; i < KS; ++i)
-#pragma unroll
-                            for (int c2 = 0; c2 < 2; ++c2) {
-                                const float4_t u = *(const float4_t*)(lds + L::u + 4 * (32 * i + 8 * g + 4 * c2));
-#pragma unroll
-                                for (int c4 = 0; c4 < 4; ++c4) {
-                                    const uint32_t qq = qf[i][2 * c2 + (c4 >> 1)], kk = kf[i][2 * c2 + (c4 >> 1)];
-                                    float k = widen16<BF16 || L::split_keys>((uint16_t)(kk >> (16 * (c4 & 1))));
-                                    if constexpr (L::split_keys) {
-                                        const uint32_t rest = kl[i][2 * c2 + (c4 >> 1)];
-                                        k += widen16<true>((uint16_t)(rest >> (16 * (c4 & 1))));
-                                    }
-                                    dot = fmaf(widen16<BF16>((uint16_t)(qq >> (16 * (c4 & 1)))) * u[c4], k, dot);
-                                }
-                            }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) dot = 4 * g + j == n ? sc[j] : dot;
-                    }
-                    dot += __shfl_xor(dot, 16, 64);
-                    dot += __shfl_xor(dot, 32, 64);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sc[j] = 4 * g + j < n ? sc[j] * same[j] : 0.0f;
-                        if (GRAD == 0 && u_in_dot) sc[j] = 4 * g + j == n ? dot : sc[j];
-                    }
-                }
-                if constexpr (STORE) split4(sc, sp);
-                if constexpr (GRAD == 1) {                             // x . val of the same pairs, weighted with their lags
-                    float4_t xv = {0, 0, 0, 0};
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int from = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
-                        const uint4_t v = *(const uint4_t*)(buffer + val_tile + from);
-                        if (!BF16) {
-                            const uint4_t vl = *(const uint4_t*)(buffer + val_low + from);
-                            xv = mfma_bits<true>(vl, xl[i], xv);
-                            xv = mfma_bits<true>(vl, xf[i], xv);
-                            xv = mfma_bits<true>(v, xl[i], xv);
-                        }
-                        xv = mfma_bits<true>(v, xf[i], xv);
-                    }
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum = fmaf(sc[j] * (float)(a - 1 - (16 * it + 4 * g + j)), xv[j], sum);
-                    dw += (double)sum;
+                    sc = mfma_bits<BF16>(kf, qf[i], sc);
                 }
             }
-            ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
+            if constexpr (STORE && !U_IN_DOT) {
+                float self = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) self += weighted(own[j], sc[j]);
+                dot += weighted(mine[it], self);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[j] = weighted(pw[it][j], sc[j]);
+            if constexpr (GRAD == 1) {                                 // x . val of the same pairs, weighted with their lags
+                float4_t xv = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int from = (16 * it + n) * L::val_row + 2 * (32 * i + 8 * g);
+                    const uint4_t v = *(const uint4_t*)(buffer + val_tile + from);
+                    if (!BF16) {
+                        const uint4_t vl = *(const uint4_t*)(buffer + val_low + from);
+                        xv = mfma_bits<true>(vl, xl[i], xv);
+                        xv = mfma_bits<true>(vl, xf[i], xv);
+                        xv = mfma_bits<true>(v, xl[i], xv);
+                    }
+                    xv = mfma_bits<true>(v, xf[i], xv);
+                }
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += weighted(sc[j], (float)(a - 1 - (16 * it + 4 * g + j)) * xv[j]);
+                dw += (double)sum;
+            }
+            if constexpr (STORE) {
+                uint2_t sp[2];
+                split4(sc, sp);
+                ph[ks][e] = sp[0].x; ph[ks][e + 1] = sp[0].y; pl[ks][e] = sp[1].x; pl[ks][e + 1] = sp[1].y;
+            }
         }
         if constexpr (STORE) {
+        if constexpr (U_IN_DOT) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            if (2 * ks <= wave) {
-                uint4_t vf[4], vl[4];
-                val_columns<BF16>(buffer + val_tile, buffer + val_low, ks, n, g, vf, vl);
+            for (int i = 0; i < KS; ++i) {
+                const uint4_t kf = key_frag(key_tile, a, i), kl = L::split_keys ? key_frag(key_low, a, i) : kf;
 #pragma unroll
-                for (int vt = 0; vt < 4; ++vt) {
-                    out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
-                    if (!BF16) out[vt] = mfma_bits<true>(vl[vt], ph[ks], out[vt]);
-                    out[vt] = mfma_bits<true>(vf[vt], ph[ks], out[vt]);
+                for (int c2 = 0; c2 < 2; ++c2) {
+                    const float4_t u = *(const float4_t*)(lds + L::u + 4 * (32 * i + 8 * g + 4 * c2));
+#pragma unroll
+                    for (int c4 = 0; c4 < 4; ++c4) {
+                        const uint32_t qq = qf[i][2 * c2 + (c4 >> 1)], kk = kf[2 * c2 + (c4 >> 1)];
+                        float k = widen16<BF16 || L::split_keys>((uint16_t)(kk >> (16 * (c4 & 1))));
+                        if constexpr (L::split_keys) {
+                            const uint32_t rest = kl[2 * c2 + (c4 >> 1)];
+                            k += widen16<true>((uint16_t)(rest >> (16 * (c4 & 1))));
+                        }
+                        dot = fmaf(widen16<BF16>((uint16_t)(qq >> (16 * (c4 & 1)))) * u[c4], k, dot);
+                    }
                 }
             }
         }
-        // the bonus with u at the channels of val; the gradient of u
-        if (GRAD || !u_in_dot) {
+        dot += __shfl_xor(dot, 16, 64);
+        dot += __shfl_xor(dot, 32, 64);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            uint4_t vf[4], vl[4];
+            val_columns<BF16>(buffer + val_tile, buffer + val_low, ks, n, g, vf, vl);
+#pragma unroll
+            for (int vt = 0; vt < 4; ++vt) {
+                out[vt] = mfma_bits<true>(vf[vt], pl[ks], out[vt]);
+                if (!BF16) out[vt] = mfma_bits<true>(vl[vt], ph[ks], out[vt]);
+                out[vt] = mfma_bits<true>(vf[vt], ph[ks], out[vt]);
+            }
+        }
+        // the bonus, with u at the channels of val unless the dot has it; the gradient of u
+        {
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt) {
                 const uint2_t vh = *(const uint2_t*)(buffer + val_tile + a * L::val_row + 2 * (16 * vt + 4 * g));
-                const float4_t u = *(const float4_t*)(lds + L::u + 4 * (16 * vt + 4 * g));
+                const float4_t u = U_IN_DOT ? float4_t{1, 1, 1, 1} : *(const float4_t*)(lds + L::u + 4 * (16 * vt + 4 * g));
                 float v[4] = {__uint_as_float(vh.x << 16), __uint_as_float(vh.x & 0xFFFF0000u), __uint_as_float(vh.y << 16), __uint_as_float(vh.y & 0xFFFF0000u)};
                 if (!BF16) {
                     const uint2_t l = *(const uint2_t*)(buffer + val_low + a * L::val_row + 2 * (16 * vt + 4 * g));
@@ -1022,7 +1021,7 @@ __global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_ker
         return;
     }
     float du[GRAD == 2 ? 16 : 1] = {};
-    const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false>(h, all.sweep[which], at, at.wave, du, lds)
+    const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false, GRAD == 0>(h, all.sweep[which], at, at.wave, du, lds)
                                   : carry_state<DP, BF16, L, GRAD == 1>(h, all.sweep[which], all, at, cut, scanned != 0, lds);
     if constexpr (GRAD != 0) leave_sums<8, GRAD == 2>(h, all, at, GRAD - 1, dw, du, at.wave < 4 ? at.wave : -1, lds + L::sums);
 }
@@ -1042,10 +1041,10 @@ __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsD
     }
     float du[DK ? 16 : 1] = {}, none[1];
     const SweepDev& p = all.sweep[DK ? 2 : 0];
-    const double dw = at.wave < 4   ? outputs<64, BF16, L, 0, true, false>(h, p, at, at.wave, none, lds)
+    const double dw = at.wave < 4   ? outputs<64, BF16, L, 0, true, false, DK>(h, p, at, at.wave, none, lds)
                       : at.wave < 8 ? carry_state<64, BF16, L, !DK>(h, p, all, at, cut, scanned != 0, lds)
-                      : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK>(h, all.sweep[1], at, at.wave - 8, du, lds)
-                                    : outputs<64, BF16, L, DK ? 2 : 1, DK, DK>(h, p, at, at.wave - 8, du, lds);
+                      : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, all.sweep[1], at, at.wave - 8, du, lds)
+                                    : outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, p, at, at.wave - 8, du, lds);
     leave_sums<12, DK>(h, all, at, DK, dw, du, at.wave >= 8 ? at.wave - 8 : -1, lds + L::sums);
 }
 
@@ -1137,7 +1136,7 @@ static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     const hipError_t e = launch_locals<DP, BF16>(h, l, p, 1, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
-    all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, false, true};
+    all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, false};
     return launch_sweeps<DP, BF16, 0>(h, all, p, 0, s);
 }
 template <int DP, bool BF16>
@@ -1151,9 +1150,9 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     hipError_t e = launch_locals<DP, BF16>(h, l, p, 2, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
-    all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false, false};
-    all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true, false};
-    all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false, true};
+    all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
+    all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true};
+    all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false};
     all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
     if constexpr (DP == 64) {
         if ((e = launch_pair<BF16, false>(h, all, p, s)) != hipSuccess) return e;
