@@ -6,7 +6,8 @@ used without the GPU library being present):
 
   synth    seeded synthetic workloads (no arithmetic of the method in it)
   binding  ctypes binding of librwkvq.so (same names as include/rwkvq.h)
+  time_mix a multi-head time-mixing block made of the library's calls: prompts, tokens, gradients
   build    hipcc driver that compiles csrc/ into librwkvq.so
 """
 
-__all__ = ["synth", "binding", "build"]
+__all__ = ["synth", "binding", "build", "time_mix"]
