@@ -456,7 +456,8 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  *   of each sequence in both; a sequence whose slot is not in 0 .. n_slots - 1 is left out: nothing of it is written.
  *   w: DEVICE [n_heads] (positive forgets), u: DEVICE [n_heads][head_dim].  head_dim: a multiple of 8 up to 128.
  *   Products of 16-bit values are exact and every sum is binary32; where a state or a weight that was computed meets the matrix cores it goes in
- *   as a sum of two or three bf16 parts (17 bits for an output, 24 for a state).  The same bits every time.
+ *   as a sum of two or three bf16 parts (17 bits for an output, 24 for a state).  The same bits every time.  An
+ *   infinity or NaN among r, k, v, dout reaches what its formula makes of it, at times as NaN for an infinity, and no other result.
  *   workspace: DEVICE, rwkvq_linear_attention_workspace_size(heads) bytes (0 is possible: NULL then allowed).
  * rwkvq_linear_attention_backward: the gradients.  dout like out (out_stride); dstate: gradient for the states behind the
  *   sequences (NULL: zeros); dr, dk, dv like r, k, v with their strides; dw [n_heads] and du [n_heads][head_dim] floats,

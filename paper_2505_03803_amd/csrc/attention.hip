@@ -144,18 +144,39 @@ __device__ __forceinline__ Segment segment_of(const HeadsDev& h, int cut, int sl
     return s;
 }
 
+// Infinities and NaN.  On the matrix cores a weight of 0 times a later token's infinity would reach the earlier tokens of its chunk, so val
+// is staged with 0 in the place of either, and the token and channel are marked: outputs of that channel from that token on, and
+// its column of the state, are made NaN instead (so is what an infinity would have made infinite).  Keys only meet scores, which are masked
+// after their product, unless they are the val of another sweep over the same tiles.  A mark is 64 times the chunk's number and 63 less the
+// token, so that the largest is the latest chunk's first; nothing needs clearing.
+struct Marks {
+    static constexpr int bytes = 2 * 4 * (2 * kVals + 1) + 8;      // for each buffer: channels of val, channels of keys, whether there is any
+    int* at;
+    __device__ __forceinline__ Marks(char* lds) : at((int*)lds) {}
+    __device__ __forceinline__ int* channel(int turn, bool key) const { return at + (2 * turn + key) * kVals; }
+    __device__ __forceinline__ int& any(int turn) const { return at[4 * kVals + turn]; }
+    __device__ __forceinline__ void clear(int tid) const {
+        if (tid < 4 * kVals + 2) at[tid] = -1;
+    }
+    // the first marked token of a channel, or kChunk
+    static __device__ __forceinline__ int first(int mark, int number) { return mark >> 6 == number ? 63 - (mark & 63) : kChunk; }
+    static __device__ __forceinline__ float nan() { return __uint_as_float(0x7FC00000u); }
+};
+
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
 // published beside the one that the outputs still read.
-template <int DP, bool BF16, int GRAD, bool PAIR = false> struct Lds {
+// swaps: there is a sweep whose val are the keys.
+template <int DP, bool BF16, int GRAD, bool PAIR = false, bool SWAPS = false> struct Lds {
+    static constexpr bool swaps = SWAPS;
     static constexpr int threads = PAIR ? 768 : 512;
     static constexpr bool split_keys = PAIR && !BF16;                            // fp16 keys as two bf16 parts too: they are somebody's val
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
     static constexpr int key = 0, key_lo = key + kChunk * key_row, val = key_lo + (split_keys ? kChunk * key_row : 0), val_lo = val + kChunk * val_row;
     static constexpr int parts = GRAD || PAIR ? 3 : 2, part = kVals * key_row;   // of a published state
     static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), buffer = state + parts * part;
-    static constexpr bool two = 2 * buffer + 4 * DP + 1152 <= 160 * 1024 && (BF16 || DP > 64 || PAIR);
+    static constexpr bool two = 2 * buffer + 4 * DP + 1152 + Marks::bytes <= 160 * 1024 && (BF16 || DP > 64 || PAIR);
     static constexpr int u = two ? 2 * buffer : buffer, sums = u + 4 * DP;
-    static constexpr int bytes = sums + (GRAD || PAIR ? 12 * 8 + 4 * 4 * kVals : 0);
+    static constexpr int marks = sums + (GRAD || PAIR ? 12 * 8 + 4 * 4 * kVals : 0), bytes = marks + Marks::bytes;
 };
 
 // Two values as packed bf16 and what is left of them.
@@ -323,6 +344,32 @@ template <int NT, int COUNT, int PER>
 struct Rows {
     uint4_t data[COUNT];
     uint32_t offset[COUNT];                       // of a whole chunk
+    // infinities and NaN, whose exponents of all ones carry into the sign's place, to zeros and marks
+    template <bool BF16>
+    __device__ __forceinline__ void mark(const Marks& marks, int turn, bool is_key, int number) {
+        constexpr uint32_t exponent = BF16 ? 0x7F807F80u : 0x7C007C00u, one = BF16 ? 0x00800080u : 0x04000400u;
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) any |= (data[i][c] & exponent) + one;
+        if ((any & 0x80008000u) == 0) return;
+        marks.any(turn) = number;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int c = id + NT * i, row = c / PER, col = 8 * (c % PER);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t half = 0xFFFFu << (16 * (e & 1));
+                uint32_t word = data[i][e >> 1];
+                if (((word & exponent & half) ^ (exponent & half)) == 0) {
+                    word &= ~half;
+                    atomicMax(marks.channel(turn, is_key) + col + e, 64 * number + 63 - row);
+                }
+                data[i][e >> 1] = word;
+            }
+        }
+    }
     int id;                                       // the thread's number among the NT
     __device__ __forceinline__ void begin(int thread, long long stride, int width, bool reverse) {
         id = thread;
@@ -614,7 +661,10 @@ struct Staging {
         if (vals) val.fetch(val_at.at, nt, val_stride, width, reverse);
         key_at.pass(nt); val_at.pass(nt);
     }
-    __device__ __forceinline__ void store(char* lds) const {
+    // into buffer `turn` at `lds`, as the segment's chunk `number`
+    __device__ __forceinline__ void store(char* lds, const Marks& marks, int turn, int number) {
+        if (vals) val.template mark<BF16>(marks, turn, false, number);
+        if (L::swaps && keys) key.template mark<BF16>(marks, turn, true, number);
         if (keys) {
             if constexpr (L::split_keys) key.store_split(lds + L::key, lds + L::key_lo, L::key_row);
             else key.store(lds + L::key, L::key_row);
@@ -625,6 +675,24 @@ struct Staging {
         }
     }
 };
+
+template <class L, int KT>
+__device__ __forceinline__ void mark_state(float4_t (&S)[KT][4], const Marks& marks, int turn, int number, int wave, int n, int g) {
+    bool row[KT][4] = {};
+    if constexpr (L::swaps)
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) row[x][j] = Marks::first(marks.channel(turn, true)[16 * (KT * wave + x) + 4 * g + j], number) < kChunk;
+#pragma unroll
+    for (int vt = 0; vt < 4; ++vt) {
+        const bool col = Marks::first(marks.channel(turn, false)[16 * vt + n], number) < kChunk;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[x][vt][j] = col || row[x][j] ? Marks::nan() : S[x][vt][j];
+    }
+}
 
 // The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of L <G, S>.
 template <int DP, bool BF16, class L, bool MEETS_G>
@@ -651,11 +719,13 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
                 for (int i = 0; i < L::parts; ++i) *(uint2_t*)(to + i * L::part + (16 * vt + n) * L::key_row + 2 * (16 * (KT * wave + x) + 4 * g)) = v[i];
             }
     };
+    const Marks marks(lds + L::marks);
     char* buffer = lds;
+    int turn = 0, number = 0;
     auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         publish(S, buffer + L::state);
-        rows.store(buffer);
+        rows.store(buffer, marks, turn, number);
         __syncthreads();
         rows.fetch(next);
         scale(S, tail ? expf(-(float)nt * w) : pow.whole);
@@ -668,8 +738,10 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
             key_columns<L>(buffer, ks, wave, n, g, keys, low);
             update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
         }
-        if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
+        if (__builtin_amdgcn_readfirstlane(marks.any(turn)) == number) mark_state<L>(S, marks, turn, number, wave, n, g);
+        if (L::two) turn ^= 1, buffer = lds + turn * L::buffer;
         else __syncthreads();
+        ++number;
     };
     for (int left = at.len; left > 0;) {
         const int next = min(kChunk, left - nt);
@@ -696,7 +768,13 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     return dw;
 }
 
-__device__ __forceinline__ float weighted(float w, float x) { return w != 0.0f ? w * x : 0.0f; }
+// x, in a scalar register, as something that changes with `by`: conditions on it are made where they are used, not kept for each lane in
+// more scalar registers than there are.
+template <bool YES>
+__device__ __forceinline__ int per_chunk(int x, int by) {
+    if (YES) asm("" : "+s"(x) : "s"(by));
+    return x;
+}
 
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
 //   GRAD 1: the shares of dw that dr's sweep has, with x = r;  2: those of dk's and du, with x = k;  0: neither.  STORE: the outputs.
@@ -705,19 +783,20 @@ template <int DP, bool BF16, class L, int GRAD, bool STORE, bool SWAP, bool U_IN
 __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, int wave, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
     constexpr int KS = DP / 32, parts = GRAD ? L::parts : 2;
     constexpr int key_tile = SWAP ? L::val : L::key, key_low = SWAP ? L::val_lo : L::key_lo, val_tile = SWAP ? L::key : L::val, val_low = SWAP ? L::key_lo : L::val_lo;
-    const int n = at.n, g = at.g, D = at.D, v0 = at.v0, a = 16 * wave + n;
+    const int n = at.n, g = at.g, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
     Staging<DP, BF16, L> rows(SWAP ? p.swapped() : p, at);
     const bool reverse = p.reverse;
     const long long q_stride = p.q_stride, x_stride = p.x_stride, out_stride = p.out_stride;
-    Walk q_at(p.q + at.head * D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRAD ? p.x + at.head * D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
-        out_at(p.out + at.head * D + v0, out_stride, at.s.a0, at.s.a1, reverse);
+    Walk q_at(p.q + at.head * at.D, q_stride, at.s.a0, at.s.a1, reverse), x_at(GRAD ? p.x + at.head * at.D + v0 : p.q, x_stride, at.s.a0, at.s.a1, reverse),
+        out_at(p.out + at.head * at.D + v0, out_stride, at.s.a0, at.s.a1, reverse);
     uint4_t qr[KS], xr[2];                        // x as an operand, and where the lane's outputs are
     uint2_t xdr[4];
     const int q_col = SWAP ? 4 * g : 8 * g;
     const uint32_t q_off = row_offset(a, reverse, q_stride, q_col), x_off = GRAD ? row_offset(a, reverse, x_stride, 0) : 0,
                    out_off = row_offset(a, reverse, out_stride, 4 * g);
     auto fetch = [&](int nt) {
+        const int D = per_chunk<L::threads == 768 && !L::swaps>(at.D, nt);
         rows.fetch(nt);
         if (nt > 0) {
             const int row = min(a, nt - 1);
@@ -754,11 +833,12 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     int nt = first_chunk(at.len, reverse);
     fetch(nt);
     const int u0 = U_IN_DOT ? 0 : v0, tid = 64 * wave + at.lane;
-    if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < D ? h.u[at.head * D + u0 + tid] : 0.0f;
+    if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < at.D ? h.u[at.head * at.D + u0 + tid] : 0.0f;
 
-    // weights of pairs (token a, token 16 it + 4 g + j), 0 where i >= a; of the state in front; which of a tile's tokens is the lane's own.
+    // weights of pairs (token a, token 16 it + 4 g + j), and of the state in front.
     // Every wavefront takes all four tiles: without branches their loads and products overlap, and the last wavefront has four anyway.
-    float pw[4][4], own[4], mine[4];
+    float pw[4][4];
+    bool lower[4], own[4];                        // of the lane's own tile: earlier tokens, and the lane's
     const float front = expf(-(float)a * w);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
@@ -767,16 +847,18 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             const int lag = a - 1 - (16 * it + 4 * g + j);
             pw[it][j] = lag >= 0 ? expf(-(float)lag * w) : 0.0f;
         }
-        mine[it] = it == wave ? 1.0f : 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) own[j] = 4 * g + j == n ? 1.0f : 0.0f;
+    for (int j = 0; j < 4; ++j) { lower[j] = 4 * g + j < n; own[j] = 4 * g + j == n; }
     double dw = 0.0;
     const bool slow = GRAD && passes(w, kChunk);
 
+    const Marks marks(lds + L::marks);
     char* buffer = lds;
+    int turn = 0, number = 0;
     auto chunk = [&](int nt, int next, int left) {
-        rows.store(buffer);
+        const int tile = per_chunk<L::threads == 768 && !L::swaps>(wave, left), D = per_chunk<L::threads == 768 && !L::swaps>(at.D, left);
+        rows.store(buffer, marks, turn, number);
         __syncthreads();
         uint4_t qf[KS], qh[KS], ql[KS], xf[2], xl[2];
         uint2_t xd[4];
@@ -832,8 +914,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;
         }
 
-        // scores of the wavefront's tokens with those before them.  A weight of 0 leaves out also a score
-        // that left binary32
+        // scores of the wavefront's tokens with those before them
         uint4_t ph[2], pl[2];
         float dot = 0.0f;                         // of the bonus: a token's score with itself, or that with u
 #pragma unroll
@@ -854,11 +935,11 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             if constexpr (STORE && !U_IN_DOT) {
                 float self = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) self += weighted(own[j], sc[j]);
-                dot += weighted(mine[it], self);
+                for (int j = 0; j < 4; ++j) self += own[j] ? sc[j] : 0.0f;
+                dot += it == tile ? self : 0.0f;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[j] = weighted(pw[it][j], sc[j]);
+            for (int j = 0; j < 4; ++j) sc[j] = (it < tile) | ((it == tile) & lower[j]) ? pw[it][j] * sc[j] : 0.0f;
             if constexpr (GRAD == 1) {                                 // x . val of the same pairs, weighted with their lags
                 float4_t xv = {0, 0, 0, 0};
 #pragma unroll
@@ -875,7 +956,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 }
                 float sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += weighted(sc[j], (float)(a - 1 - (16 * it + 4 * g + j)) * xv[j]);
+                for (int j = 0; j < 4; ++j) sum += (it < tile) | ((it == tile) & lower[j]) ? sc[j] * ((float)(a - 1 - (16 * it + 4 * g + j)) * xv[j]) : 0.0f;
                 dw += (double)sum;
             }
             if constexpr (STORE) {
@@ -946,9 +1027,27 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                     *(uint2_t*)(to + 32 * vt) = uint2_t{Elem<BF16>::pack(out[vt][0], out[vt][1]), Elem<BF16>::pack(out[vt][2], out[vt][3])};
         }
         }
+        if (__builtin_amdgcn_readfirstlane(marks.any(turn)) == number) {
+            if constexpr (STORE) {
+                int first = kChunk;               // of the keys, in any channel
+                if constexpr (L::swaps) {
+                    first = Marks::first(marks.channel(turn, !SWAP)[at.lane], number);
+#pragma unroll
+                    for (int off = 32; off; off >>= 1) first = min(first, __shfl_xor(first, off, 64));
+                }
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const int channel = 16 * (c >> 2) + 4 * g + (c & 3), from = min(first, Marks::first(marks.channel(turn, SWAP)[channel], number));
+                    if (a < nt && a >= from && v0 + channel < D) *(uint16_t*)((char*)out_at.at + out_off + 32 * (c >> 2) + 2 * (c & 3)) = 0x7FC0;      // NaN in both types
+                    if (GRAD == 2 && from < kChunk) du[c] = Marks::nan();
+                }
+            }
+            if (GRAD) dw = (double)Marks::nan();
+        }
         out_at.pass(nt);
-        if (L::two) buffer = buffer == lds ? lds + L::buffer : lds;
+        if (L::two) turn ^= 1, buffer = lds + turn * L::buffer;
         else __syncthreads();
+        ++number;
     };
     for (int left = at.len; left > 0;) {
         const int next = min(kChunk, left - nt);
@@ -960,11 +1059,12 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 }
 
 // Where a workgroup is; false if it has nothing to do.
-__device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut, int blocks, int* found) {
+__device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut, int blocks, int* found, const Marks& marks) {
     const int tid = threadIdx.x;
     at.slot_at = blockIdx.x / (h.H * blocks); at.head = blockIdx.x / blocks % h.H; at.v0 = blockIdx.x % blocks * kVals; at.D = h.D;
     at.lane = tid & 63; at.wave = __builtin_amdgcn_readfirstlane(tid >> 6); at.n = at.lane & 15; at.g = at.lane >> 4;
     if (tid == 0) *found = -1;
+    marks.clear(tid);
     __syncthreads();
     at.s = segment_of(h, cut, at.slot_at, found);
     at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
@@ -1016,7 +1116,7 @@ __global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_ker
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     Place at;
-    if (!find_place(at, h, cut, blocks, &found)) {
+    if (!find_place(at, h, cut, blocks, &found, Marks(lds + L::marks))) {
         if constexpr (GRAD != 0) leave_zeros<GRAD == 2>(h, all, at, GRAD - 1);
         return;
     }
@@ -1031,11 +1131,11 @@ __global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_ker
 // dw, which need the state in more bits, computed apart from its outputs.
 template <bool BF16, bool DK>
 __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
-    typedef Lds<64, BF16, 0, true> L;
+    typedef Lds<64, BF16, 0, true, DK> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     Place at;
-    if (!find_place(at, h, cut, 1, &found)) {
+    if (!find_place(at, h, cut, 1, &found, Marks(lds + L::marks))) {
         leave_zeros<DK>(h, all, at, DK);
         return;
     }
@@ -1121,7 +1221,7 @@ static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const P
 template <bool BF16, bool DK>
 static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
-    constexpr int bytes = Lds<64, BF16, 0, true>::bytes;
+    constexpr int bytes = Lds<64, BF16, 0, true, DK>::bytes;
     const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, DK>, bytes, raised);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_pair_kernel<BF16, DK>), dim3((unsigned)(p.slots * h.H)), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);

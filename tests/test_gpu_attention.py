@@ -346,3 +346,47 @@ def test_gradients_against_differences():
         terms = g * d
         bar = 2.0 ** -15 * np.abs(A[i] * d).sum() + 1e-6 * abs(want) + (4 * 2.0 ** -8 * np.sqrt((terms ** 2).sum()) if i < 3 else 0.0)
         assert abs(terms.sum() - want) <= bar, (i, terms.sum(), want, bar)
+
+
+@pytest.mark.parametrize("bad", ["inf", "nan"])
+@pytest.mark.parametrize("dt,H,D,T,t0", [("f16", 2, 64, 150, 70), ("bf16", 2, 64, 150, 70), ("bf16", 3, 40, 90, 87), ("f16", 2, 24, 50, 0), ("f16", 2, 128, 150, 70),
+                                         ("bf16", 2, 104, 70, 63), ("bf16", 2, 64, 300, 64)])
+def test_infinities_reach_only_what_they_should(dt, H, D, T, t0, bad):
+    """One infinity or NaN in r, k, v or dout of token t0, head 1, channel c: what the formulas make of it is not finite, and every other
+    number keeps its bits (earlier tokens of the same chunk among them)."""
+    print(f"attention {bad} in {dt} D={D} T={T}", flush=True)
+    torch = G.torch_()
+    w, c = [0.1] * H, D - 3
+    value = {"f16": dict(inf=0x7C00, nan=0x7E00), "bf16": dict(inf=0xFF80, nan=0x7FC0)}[dt][bad]
+
+    def run(case):
+        so = torch.full((1, H, D, D), 7.0, device="cuda")
+        got = dict(out=case.forward(so), so=so.cpu().numpy())
+        got.update(case.backward())
+        got["dw"], got["du"] = got["dw"][:-1], got["du"][:-1].reshape(H, D)
+        return {p: widen(a.view(np.uint16), dt).reshape(T, H, D) if p in ("out", "dr", "dk", "dv") else a for p, a in got.items()}
+
+    clean = run(Case([T], H, D, dt, seed=5, w=w, offsets=False))
+    all_ = slice(None)
+    reached = dict(                                # result: (tokens or none, channels)
+        v=dict(out=(slice(t0, None), c), so=(all_, c), dr=(slice(t0, None), all_), dk=(t0, all_), du=(all_,), dw=()),
+        k=dict(out=(slice(t0, None), all_), so=(c, all_), dr=(slice(t0, None), c), dv=(t0, all_), du=(c,), dw=()),
+        r=dict(out=(t0, all_), di=(c, all_), dk=(slice(0, t0 + 1), c), dv=(slice(0, t0 + 1), all_), du=(c,), dw=()),
+        dout=dict(di=(all_, c), dr=(t0, all_), dk=(slice(0, t0 + 1), all_), dv=(slice(0, t0 + 1), c), du=(all_,), dw=()))
+    for p, where in reached.items():
+        case = Case([T], H, D, dt, seed=5, w=w, offsets=False)
+        case.bits[p][t0, D + c] = value
+        case.d[p] = dev(case.bits[p])
+        got = run(case)
+        for name, a in got.items():
+            want = np.zeros(a.shape, dtype=bool)
+            if name in where:
+                at = where[name]
+                if name in ("out", "dr", "dk", "dv"):
+                    want[at[0], 1, at[1]] = True
+                elif name in ("so", "di"):
+                    want[0, 1, at[0], at[1]] = True
+                else:
+                    want[(1, *at)] = True
+            assert not np.isfinite(a[want]).any(), (p, name)
+            assert np.array_equal(a[~want], clean[name][~want]), (p, name)
