@@ -509,8 +509,8 @@ __device__ __forceinline__ void scale(float4_t (&S)[KT][4], float by) {
 struct LocalDev { const uint16_t *key, *val; long long key_stride, val_stride; const float* initial; float* parts; bool reverse, transposed; };
 struct LocalsDev { LocalDev dir[2]; };
 
-template <int DP, bool BF16>
-__global__ void __launch_bounds__(256, DP > 64 ? 2 : 4) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
+template <int DP, bool BF16, int DIRS>
+__global__ void __launch_bounds__(256, DP > 64 ? 2 : 2 * DIRS) attend_local_kernel(HeadsDev h, LocalsDev locals, int cut, int blocks) {
     typedef Lds<DP, BF16, 0> L;
     constexpr int KT = DP / 64;
     __shared__ __attribute__((aligned(16))) char both[2][L::state];
@@ -1199,12 +1199,12 @@ size_t attention_backward_workspace_bytes(const HeadsDev& h) {
     return (2 * p.part_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
 }
 
-template <int DP, bool BF16>
-static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Plan& p, int dirs, hipStream_t s) {
+template <int DP, bool BF16, int DIRS>
+static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Plan& p, hipStream_t s) {
     if (!p.split) return hipSuccess;
-    hipLaunchKernelGGL((attend_local_kernel<DP, BF16>), dim3((unsigned)(p.slots * h.H * p.blocks), dirs), dim3(256), 0, s, h, l, p.cut, p.blocks);
+    hipLaunchKernelGGL((attend_local_kernel<DP, BF16, DIRS>), dim3((unsigned)(p.slots * h.H * p.blocks), DIRS), dim3(256), 0, s, h, l, p.cut, p.blocks);
     if (p.scan)
-        hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, dirs), dim3(256), 0, s, h, l, p.cut, p.part_size);
+        hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, DIRS), dim3(256), 0, s, h, l, p.cut, p.part_size);
     return hipGetLastError();
 }
 template <int DP, bool BF16, int GRAD>
@@ -1233,7 +1233,7 @@ static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, false);
     LocalsDev l{};
     l.dir[0] = LocalDev{h.k, h.v, h.k_stride, h.v_stride, h.state, h.partial, false, false};
-    const hipError_t e = launch_locals<DP, BF16>(h, l, p, 1, s);
+    const hipError_t e = launch_locals<DP, BF16, 1>(h, l, p, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
     all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, false};
@@ -1247,7 +1247,7 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     LocalsDev l{};
     l.dir[0] = LocalDev{h.v, h.k, h.v_stride, h.k_stride, h.state, S, false, true};
     l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true, false};
-    hipError_t e = launch_locals<DP, BF16>(h, l, p, 2, s);
+    hipError_t e = launch_locals<DP, BF16, 2>(h, l, p, s);
     if (e != hipSuccess) return e;
     SweepsDev all{};
     all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
