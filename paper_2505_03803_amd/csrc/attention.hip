@@ -1111,31 +1111,33 @@ __device__ __forceinline__ void leave_zeros(const HeadsDev& h, const SweepsDev& 
 
 // One sweep: four wavefronts for the outputs, four for the state, which meet at the same barriers.
 template <int DP, bool BF16, int GRAD>
-__global__ void __launch_bounds__(512, GRAD || DP > 64 ? 2 : 4) attend_sweep_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks, int which) {
+__device__ __forceinline__ void sweep(const HeadsDev& h, const SweepsDev& all, const SweepDev& p, int cut, int scanned, int blocks, int* found, char* lds) {
     typedef Lds<DP, BF16, GRAD> L;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ int found;
     Place at;
-    if (!find_place(at, h, cut, blocks, &found, Marks(lds + L::marks))) {
+    if (!find_place(at, h, cut, blocks, found, Marks(lds + L::marks))) {
         if constexpr (GRAD != 0) leave_zeros<GRAD == 2>(h, all, at, GRAD - 1);
         return;
     }
     float du[GRAD == 2 ? 16 : 1] = {};
-    const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false, GRAD == 0>(h, all.sweep[which], at, at.wave, du, lds)
-                                  : carry_state<DP, BF16, L, GRAD == 1>(h, all.sweep[which], all, at, cut, scanned != 0, lds);
+    const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false, GRAD == 0>(h, p, at, at.wave, du, lds)
+                                  : carry_state<DP, BF16, L, GRAD == 1>(h, p, all, at, cut, scanned != 0, lds);
     if constexpr (GRAD != 0) leave_sums<8, GRAD == 2>(h, all, at, GRAD - 1, dw, du, at.wave < 4 ? at.wave : -1, lds + L::sums);
+}
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(HeadsDev h, SweepsDev all, int cut, int scanned, int blocks) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int found;
+    sweep<DP, BF16, 0>(h, all, all.sweep[0], cut, scanned, blocks, &found, lds);
 }
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
 // dw, which need the state in more bits, computed apart from its outputs.
 template <bool BF16, bool DK>
-__global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+__device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
     typedef Lds<64, BF16, 0, true, DK> L;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ int found;
     Place at;
-    if (!find_place(at, h, cut, 1, &found, Marks(lds + L::marks))) {
+    if (!find_place(at, h, cut, 1, found, Marks(lds + L::marks))) {
         leave_zeros<DK>(h, all, at, DK);
         return;
     }
@@ -1146,6 +1148,24 @@ __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsD
                       : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, all.sweep[1], at, at.wave - 8, du, lds)
                                     : outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, p, at, at.wave - 8, du, lds);
     leave_sums<12, DK>(h, all, at, DK, dw, du, at.wave >= 8 ? at.wave - 8 : -1, lds + L::sums);
+}
+
+// The sweeps of the backward pass need nothing of each other: KIND says which, or blockIdx.y, the longest first.
+constexpr int kEach = 3;
+template <bool BF16, int KIND>
+__global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int found;
+    if (KIND == 1 || (KIND == kEach && blockIdx.y == 0)) pair<BF16, true>(h, all, cut, scanned, &found, lds);
+    else pair<BF16, false>(h, all, cut, scanned, &found, lds);
+}
+template <bool BF16>
+__global__ void __launch_bounds__(512, 2) attend_backward_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ int found;
+    if (blockIdx.y == 0) sweep<128, BF16, 1>(h, all, all.sweep[0], cut, scanned, 2, &found, lds);
+    else if (blockIdx.y == 1) sweep<128, BF16, 2>(h, all, all.sweep[1], cut, scanned, 2, &found, lds);
+    else sweep<128, BF16, 0>(h, all, all.sweep[2], cut, scanned, 2, &found, lds);
 }
 
 // du [H][D] from its parts [slots][H][D], dw [H] from [slots][H][4], of which `blocks` are used in each half: sixteen threads an entry, in a
@@ -1207,27 +1227,15 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
         hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, DIRS), dim3(256), 0, s, h, l, p.cut, p.part_size);
     return hipGetLastError();
 }
-template <int DP, bool BF16, int GRAD>
-static hipError_t launch_sweeps(const HeadsDev& h, const SweepsDev& all, const Plan& p, int which, hipStream_t s) {
-    static std::atomic<unsigned long long> raised{0};
-    constexpr int bytes = Lds<DP, BF16, GRAD>::bytes;
-    const hipError_t e = raise_lds((const void*)attend_sweep_kernel<DP, BF16, GRAD>, bytes, raised);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_sweep_kernel<DP, BF16, GRAD>), dim3((unsigned)(p.slots * h.H * p.blocks)), dim3(512), bytes, s, h, all, p.cut, (int)p.scan,
-                       p.blocks, which);
-    return hipGetLastError();
-}
-
-template <bool BF16, bool DK>
+template <bool BF16, int KIND>
 static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
-    constexpr int bytes = Lds<64, BF16, 0, true, DK>::bytes;
-    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, DK>, bytes, raised);
+    constexpr int bytes = Lds<64, BF16, 0, true, true>::bytes;
+    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_pair_kernel<BF16, DK>), dim3((unsigned)(p.slots * h.H)), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
     return hipGetLastError();
 }
-
 template <int DP, bool BF16>
 static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, false);
@@ -1237,7 +1245,12 @@ static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     if (e != hipSuccess) return e;
     SweepsDev all{};
     all.sweep[0] = SweepDev{h.r, h.k, h.v, nullptr, h.r_stride, h.k_stride, h.v_stride, h.out_stride, 0, h.out, h.state, h.partial, h.state_out, false, false, false};
-    return launch_sweeps<DP, BF16, 0>(h, all, p, 0, s);
+    static std::atomic<unsigned long long> raised{0};
+    constexpr int bytes = Lds<DP, BF16, 0>::bytes;
+    const hipError_t r = raise_lds((const void*)attend_forward_kernel<DP, BF16>, bytes, raised);
+    if (r != hipSuccess) return r;
+    hipLaunchKernelGGL((attend_forward_kernel<DP, BF16>), dim3((unsigned)(p.slots * h.H * p.blocks)), dim3(512), bytes, s, h, all, p.cut, (int)p.scan, p.blocks);
+    return hipGetLastError();
 }
 template <int DP, bool BF16>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
@@ -1255,12 +1268,18 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false};
     all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
     if constexpr (DP == 64) {
-        if ((e = launch_pair<BF16, false>(h, all, p, s)) != hipSuccess) return e;
-        if ((e = launch_pair<BF16, true>(h, all, p, s)) != hipSuccess) return e;
+        if (p.slots * h.H <= 128) {               // both kinds find room on the 256 units at once; the kernel that has both is 7 % slower
+            e = launch_pair<BF16, kEach>(h, all, p, s);
+        } else {
+            e = launch_pair<BF16, 0>(h, all, p, s);
+            if (e == hipSuccess) e = launch_pair<BF16, 1>(h, all, p, s);
+        }
+        if (e != hipSuccess) return e;
     } else {
-        if ((e = launch_sweeps<DP, BF16, 1>(h, all, p, 0, s)) != hipSuccess) return e;
-        if ((e = launch_sweeps<DP, BF16, 2>(h, all, p, 1, s)) != hipSuccess) return e;
-        if ((e = launch_sweeps<DP, BF16, 0>(h, all, p, 2, s)) != hipSuccess) return e;
+        static std::atomic<unsigned long long> raised{0};
+        constexpr int bytes = Lds<128, BF16, 1>::bytes;
+        if ((e = raise_lds((const void*)attend_backward_kernel<BF16>, bytes, raised)) != hipSuccess) return e;
+        hipLaunchKernelGGL((attend_backward_kernel<BF16>), dim3((unsigned)(p.slots * h.H * 2), 3), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
     }
     hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 1) + 15) / 16), dim3(256), 0, s, h, du_parts, dw_parts, p.slots, p.blocks);
     return hipGetLastError();
