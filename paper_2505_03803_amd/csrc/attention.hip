@@ -1277,7 +1277,7 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         if (e != hipSuccess) return e;
     } else {
         static std::atomic<unsigned long long> raised{0};
-        constexpr int bytes = Lds<128, BF16, 1>::bytes;
+        constexpr int bytes = std::max(std::max(Lds<128, BF16, 0>::bytes, Lds<128, BF16, 1>::bytes), Lds<128, BF16, 2>::bytes);
         if ((e = raise_lds((const void*)attend_backward_kernel<BF16>, bytes, raised)) != hipSuccess) return e;
         hipLaunchKernelGGL((attend_backward_kernel<BF16>), dim3((unsigned)(p.slots * h.H * 2), 3), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
     }
