@@ -1199,7 +1199,7 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
     const long long work = (long long)h.n_tokens * h.H * p.blocks;
-    p.cut = (int)std::max(128ll, (work / (grad ? 256 : 512) + kChunk - 1) / kChunk * kChunk);
+    p.cut = (int)std::max(128ll, (work / (!grad ? 512 : h.D > 64 ? 128 : 256) + kChunk - 1) / kChunk * kChunk);
     if (grad) p.cut = std::min(p.cut, 2048);
     const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
     p.split = len > p.cut;
