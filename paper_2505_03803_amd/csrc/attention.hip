@@ -598,11 +598,19 @@ __global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev 
         const float w = h.w[head], decay = expf(-(float)cut * w);
         const float ragged = expf(-(float)(t1 - t0 - (count - 1) * cut) * w);      // of the last segment, which may be shorter
         float run = p.initial ? x[(p.reverse ? 0 : count - 1) * stride] : 0.0f;
-        for (int i = 0; i < count; ++i) {
-            const int m = p.reverse ? count - 1 - i : i;
-            const float own = i < count - 1 ? x[m * stride] : 0.0f;
-            x[m * stride] = run;
-            run = fmaf(m == count - 1 ? ragged : decay, run, own);
+        for (int from = 0; from < count; from += 8) {        // eight loads in flight
+            float own[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int m = p.reverse ? count - 1 - from - i : from + i;
+                own[i] = from + i < count - 1 ? x[m * stride] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int m = p.reverse ? count - 1 - from - i : from + i;
+                if (from + i < count) x[m * stride] = run;
+                run = fmaf(m == count - 1 ? ragged : decay, run, own[i]);
+            }
         }
     }
 }
@@ -1199,12 +1207,12 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
     const long long work = (long long)h.n_tokens * h.H * p.blocks;
-    p.cut = (int)std::max(128ll, (work / (!grad ? 512 : h.D > 64 ? 128 : 256) + kChunk - 1) / kChunk * kChunk);
+    p.cut = (int)std::max(128ll, (work / (!grad ? (h.offsets && (long long)h.n_seqs * h.H * p.blocks > 512 ? 1024 : 512) : h.D > 64 ? 128 : 256) + kChunk - 1) / kChunk * kChunk);
     if (grad) p.cut = std::min(p.cut, 2048);
     const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
     p.split = len > p.cut;
     p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
-    p.scan = len / p.cut > 12;
+    p.scan = len / p.cut > 16;
     p.part_size = (h.D <= 64 ? 64 : 128) * kVals * p.blocks;
     p.part_floats = p.split ? (size_t)p.slots * h.H * p.part_size : 0;
     p.dw_doubles = (size_t)p.slots * h.H * 4;
