@@ -390,3 +390,12 @@ def test_infinities_reach_only_what_they_should(dt, H, D, T, t0, bad):
                     want[(1, *at)] = True
             assert not np.isfinite(a[want]).any(), (p, name)
             assert np.array_equal(a[~want], clean[name][~want]), (p, name)
+
+
+@pytest.mark.parametrize("lens,H,D,dt", [([2305], 1, 64, "bf16"), ([70, 2500, 0, 129], 2, 32, "f16"), ([2200, 1], 1, 128, "bf16"), ([2177], 1, 104, "f16")])
+def test_long_sequences(lens, H, D, dt):
+    """More segments than a workgroup adds up by itself."""
+    print(f"attention lens={lens} D={D} {dt}", flush=True)
+    c = Case(lens, H, D, dt, seed=sum(lens), w=[0.003, 0.3][:H], offsets=len(lens) > 1)
+    c.check_forward()
+    c.check_backward()
