@@ -98,11 +98,13 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // own chunk, plus 64 for each whole chunk between, so that with R_t the dot of r_t with the state's part of dr_t and K_i that of k_i
 // with the state's part of dk_i
 //   -dw = (pairs of one chunk) + sum_t a_t R_t + sum_i (n - 1 - a_i) K_i + sum over chunks of n <G, l^n S>,  G behind a chunk, S in front of it.
-// The last sum needs both states of every chunk at once; but what passes by a chunk is what passes its end less what its keys add, so
-// over a segment of L tokens it is L <G, S> (both at its end) + sum_t o_t R_t - sum_i (o_i + n_i) K_i with o the place of a token's chunk in
-// the segment.  That cancels for heads that forget within a chunk: where n w >= 20 (l^n < 2.1e-9) a chunk is left out of the sum, below the
-// rounding of the rest; of a fast head that leaves at most the segment's last chunk, n (<G, S> - sum of its K_i).  For the others these products have 24-bit operands, their sums over a chunk are carried on in binary64, and
-// a segment of the backward pass is at most 2048 tokens.
+// The last sum needs both states of every chunk at once; but what passes by a chunk is what passes its end less what its keys add, and what is
+// at a block's front less what is at its end is sum_t R_t - sum_i K_i.  So over a block of L tokens, with o the place of a token's chunk in it and any c,
+// it is (L - c) <G, S> (both at its end) + c <G, S> (at its front) + sum_t (o_t - c) R_t - sum_i (o_i + n_i - c) K_i.  The rounding of R and K grows with
+// |o - c|, so that blocks are short (256 or 512 tokens, c half of it: as exact as the recurrence in binary32; over 2048 tokens at once the error was eight times
+// that): the sweep for dr leaves S at the blocks' boundaries for the one for dk.  For heads that forget within a chunk the rest cancels: where
+// n w >= 20 (l^n < 2.1e-9) a chunk is left out of the sum, below the rounding of the rest; of a fast head that leaves at most the segment's last
+// chunk, n (<G, S> - sum of its K_i).  These products have 24-bit operands, their sums over a chunk are carried on in binary64.
 //
 // A workgroup of four wavefronts takes a segment of a sequence, one head and 64 channels of val.  Wavefront `wave` owns tokens
 // 16 wave .. + 15 of a chunk for scores and outputs (computed transposed: a lane holds one token and four consecutive channels or
@@ -114,6 +116,7 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 constexpr int kChunk = 64;                    // tokens
 constexpr int kVals = 64;                     // channels of val of a workgroup
+constexpr int reach_of(int D) { return D > 64 ? 256 : 512; }     // tokens of a block, between the states that both directions meet at
 
 struct Segment { int b, idx, count, first_slot, t0, t1, a0, a1; };     // sequence, its place in it of how many; rows of both
 
@@ -433,6 +436,9 @@ struct Powers {
         for (int i = 0; i < 4; ++i) far[i] = uniform(expf(-(float)(16 * i) * w));
         whole = uniform(expf(-(float)kChunk * w));
     }
+    // The same for any lag below 64, to the same bits: what a state takes in and what is read from it have to agree for the gradient of w, where
+    // they cancel.
+    static __device__ __forceinline__ float of(int lag, float w) { return expf(-(float)(lag & 15) * w) * expf(-(float)(lag & ~15) * w); }
     static __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 };
 // Weights exp(-(nt - 1 - i) w) of tokens i = 32 ks .. + 31 of a chunk in the state behind it, in the order of column_frag.
@@ -441,7 +447,7 @@ __device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, i
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
-        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
+        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? Powers::of(nt - 1 - i, w) : 0.0f;
     }
 }
 struct Whole { static constexpr bool tail = false; };
@@ -635,7 +641,13 @@ struct SweepDev {
         return s;
     }
 };
-struct SweepsDev { SweepDev sweep[3]; const float *grad_initial, *grad_parts; float* du_parts; double* dw_parts; };   // dw_parts: [slots][H][4]
+struct SweepsDev {
+    SweepDev sweep[3];
+    const float *state_initial, *state_parts, *grad_initial, *grad_parts;
+    float *posts, *du_parts;            // posts: S at the boundaries of blocks, [slots][H][n_posts] parts
+    double* dw_parts;                   // [slots][H][4]
+    int n_posts;
+};
 
 // Whether a head remembers more than rounding leaves over a chunk of n tokens (see the gradient of w).
 __device__ __forceinline__ bool passes(float w, int n) { return w * (float)n < 20.0f; }
@@ -643,7 +655,7 @@ __device__ __forceinline__ bool passes(float w, int n) { return w * (float)n < 2
 // What both kinds of wavefront know of their segment.
 struct Place {
     Segment s;
-    int slot_at, slot, head, v0, D, len, lane, wave, n, g;
+    int slot_at, slot, head, v0, D, len, middle, lane, wave, n, g;       // middle: c of the gradient of w
     float w;
 };
 // A thread's share of the staging of a sweep's chunks.  Of twelve wavefronts the first eight bring the keys, the last eight val.
@@ -702,8 +714,10 @@ __device__ __forceinline__ void mark_state(float4_t (&S)[KT][4], const Marks& ma
     }
 }
 
-// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of L <G, S>.
-template <int DP, bool BF16, class L, bool MEETS_G>
+// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of
+// the <G, S>.  MEETS 1: the state is S, which meets G at the segment's end and is left at the boundaries of blocks;  2: it is G, which meets S there
+// and at the segment's front.
+template <int DP, bool BF16, class L, int MEETS>
 __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
     constexpr int KT = DP / 64;
     const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
@@ -751,27 +765,44 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
         else __syncthreads();
         ++number;
     };
-    for (int left = at.len; left > 0;) {
-        const int next = min(kChunk, left - nt);
-        if (nt < kChunk) chunk(Tail{}, nt, next);
-        else chunk(Whole{}, nt, next);
-        left -= nt;
-        nt = next;
-    }
-    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
     double dw = 0.0;
-    if constexpr (MEETS_G) {                      // G: the gradient of the state at the segment's end
-        float4_t G[KT][4];
-        start_state(G, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
+    auto meet = [&](const float4_t (&other)[KT][4], int weight) {
+        double sum = 0.0;
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)       // places behind a head's last channels hold whatever was loaded for them
-                    if (16 * (KT * wave + x) + 4 * g < D && at.v0 + 16 * vt + n < D) dw += (double)G[x][vt][j] * (double)S[x][vt][j];
-        const int last = at.len % kChunk;
-        dw *= (double)(passes(w, kChunk) ? at.len : passes(w, last) ? last : 0);
+                    if (16 * (KT * wave + x) + 4 * g < D && at.v0 + 16 * vt + n < D) sum += (double)other[x][vt][j] * (double)S[x][vt][j];
+        dw += (double)weight * sum;
+    };
+    const bool slow = MEETS && at.len > 0 && passes(w, kChunk);
+    float* const posts = MEETS ? all.posts + ((size_t)at.slot_at * h.H + at.head) * all.n_posts * part_size<KT>(D) : nullptr;
+    for (int left = at.len; left > 0;) {
+        const int next = min(kChunk, left - nt);
+        if (MEETS == 1 && slow && left < at.len && ((at.len - left) & (reach_of(DP) - 1)) == 0)
+            store_part(S, posts + ((at.len - left) / reach_of(DP) - 1) * part_size<KT>(D), at.v0, wave, at.lane);
+        float4_t other[KT][4];                    // on its way during the chunk in front
+        const bool boundary = MEETS == 2 && slow && next > 0 && ((left - nt) & (reach_of(DP) - 1)) == 0;
+        if (boundary) load_part(other, posts + ((left - nt) / reach_of(DP) - 1) * part_size<KT>(D), !p.transposed, at.v0, wave, at.lane);
+        if (nt < kChunk) chunk(Tail{}, nt, next);
+        else chunk(Whole{}, nt, next);
+        if (boundary) meet(other, reach_of(DP));
+        left -= nt;
+        nt = next;
+    }
+    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
+    if constexpr (MEETS != 0) {
+        float4_t other[KT][4];
+        if (MEETS == 1) {
+            start_state(other, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
+            const int last = at.len % kChunk;
+            meet(other, slow ? at.len - (at.len - 1) / reach_of(DP) * reach_of(DP) - at.middle : passes(w, last) ? last : 0);
+        } else if (slow) {
+            start_state(other, h, s, cut, scanned, all.state_initial, all.state_parts, false, p.transposed, !p.transposed, at.head, at.slot, w, at.v0, wave, at.lane);
+            meet(other, at.middle);
+        }
     }
     return dw;
 }
@@ -847,7 +878,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     // Every wavefront takes all four tiles: without branches their loads and products overlap, and the last wavefront has four anyway.
     float pw[4][4];
     bool lower[4], own[4];                        // of the lane's own tile: earlier tokens, and the lane's
-    const float front = expf(-(float)a * w);
+    const float front = Powers::of(a, w);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
 #pragma unroll
@@ -918,7 +949,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             }
         }
         if constexpr (GRAD) {
-            const int before = GRAD == 1 ? (slow ? at.len - left : 0) : slow ? left : passes(w, nt) && nt < kChunk ? nt : 0;
+            const int before = GRAD == 1 ? (slow ? ((at.len - left) & (reach_of(DP) - 1)) - at.middle : 0) : slow ? ((left - nt) & (reach_of(DP) - 1)) + nt - at.middle : passes(w, nt) && nt < kChunk ? nt : 0;
             dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;
         }
 
@@ -933,7 +964,9 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             for (int i = 0; i < KS; ++i) {
                 const uint4_t kf = key_frag(key_tile, 16 * it + n, i);
                 if constexpr (L::split_keys) {
-                    sc = mfma_bits<true>(key_frag(key_low, 16 * it + n, i), qh[i], sc);
+                    const uint4_t kl = key_frag(key_low, 16 * it + n, i);
+                    sc = mfma_bits<true>(kl, ql[i], sc);
+                    sc = mfma_bits<true>(kl, qh[i], sc);
                     sc = mfma_bits<true>(kf, ql[i], sc);
                     sc = mfma_bits<true>(kf, qh[i], sc);
                 } else {
@@ -1078,6 +1111,7 @@ __device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut
     at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
     if (at.slot < 0) return false;
     at.len = at.s.a1 - at.s.a0;
+    at.middle = min(at.len, reach_of(h.D)) / 2;
     at.w = h.w[at.head];
     return true;
 }
@@ -1128,7 +1162,7 @@ __device__ __forceinline__ void sweep(const HeadsDev& h, const SweepsDev& all, c
     }
     float du[GRAD == 2 ? 16 : 1] = {};
     const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false, GRAD == 0>(h, p, at, at.wave, du, lds)
-                                  : carry_state<DP, BF16, L, GRAD == 1>(h, p, all, at, cut, scanned != 0, lds);
+                                  : carry_state<DP, BF16, L, GRAD>(h, p, all, at, cut, scanned != 0, lds);
     if constexpr (GRAD != 0) leave_sums<8, GRAD == 2>(h, all, at, GRAD - 1, dw, du, at.wave < 4 ? at.wave : -1, lds + L::sums);
 }
 template <int DP, bool BF16>
@@ -1152,13 +1186,14 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
     float du[DK ? 16 : 1] = {}, none[1];
     const SweepDev& p = all.sweep[DK ? 2 : 0];
     const double dw = at.wave < 4   ? outputs<64, BF16, L, 0, true, false, DK>(h, p, at, at.wave, none, lds)
-                      : at.wave < 8 ? carry_state<64, BF16, L, !DK>(h, p, all, at, cut, scanned != 0, lds)
+                      : at.wave < 8 ? carry_state<64, BF16, L, DK ? 2 : 1>(h, p, all, at, cut, scanned != 0, lds)
                       : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, all.sweep[1], at, at.wave - 8, du, lds)
                                     : outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, p, at, at.wave - 8, du, lds);
     leave_sums<12, DK>(h, all, at, DK, dw, du, at.wave >= 8 ? at.wave - 8 : -1, lds + L::sums);
 }
 
-// The sweeps of the backward pass need nothing of each other: KIND says which, or blockIdx.y, the longest first.
+// The sweeps of the backward pass need nothing of each other but the states that dr's leaves between blocks, where a segment has several.  KIND 0: dr;
+// 1: dk and dv; kEach: all, the longest first.
 constexpr int kEach = 3;
 template <bool BF16, int KIND>
 __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
@@ -1167,12 +1202,12 @@ __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsD
     if (KIND == 1 || (KIND == kEach && blockIdx.y == 0)) pair<BF16, true>(h, all, cut, scanned, &found, lds);
     else pair<BF16, false>(h, all, cut, scanned, &found, lds);
 }
-template <bool BF16>
+template <bool BF16, int KIND>
 __global__ void __launch_bounds__(512, 2) attend_backward_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
-    if (blockIdx.y == 0) sweep<128, BF16, 1>(h, all, all.sweep[0], cut, scanned, 2, &found, lds);
-    else if (blockIdx.y == 1) sweep<128, BF16, 2>(h, all, all.sweep[1], cut, scanned, 2, &found, lds);
+    if (KIND == 0 || (KIND == kEach && blockIdx.y == 0)) sweep<128, BF16, 1>(h, all, all.sweep[0], cut, scanned, 2, &found, lds);
+    else if (blockIdx.y == (KIND == kEach)) sweep<128, BF16, 2>(h, all, all.sweep[1], cut, scanned, 2, &found, lds);
     else sweep<128, BF16, 0>(h, all, all.sweep[2], cut, scanned, 2, &found, lds);
 }
 
@@ -1202,7 +1237,7 @@ __global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float
 
 // How a call is cut: `cut` tokens a segment, `slots` segments at most; split: a sequence can have more than one; scan: one launch turns
 // the segments' parts into the states in front of them, otherwise each segment adds up those before it.
-struct Plan { int cut, slots, blocks, part_size; bool split, scan; size_t part_floats, du_floats, dw_doubles; };
+struct Plan { int cut, slots, blocks, part_size, n_posts; bool split, scan; size_t part_floats, post_floats, du_floats, dw_doubles; };
 static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
@@ -1215,6 +1250,8 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
     p.scan = len / p.cut > 16;
     p.part_size = (h.D <= 64 ? 64 : 128) * kVals * p.blocks;
     p.part_floats = p.split ? (size_t)p.slots * h.H * p.part_size : 0;
+    p.n_posts = (std::min(len, p.cut) - 1) / reach_of(h.D);
+    p.post_floats = (size_t)p.slots * h.H * p.n_posts * p.part_size;
     p.dw_doubles = (size_t)p.slots * h.H * 4;
     p.du_floats = (size_t)p.slots * h.H * h.D;
     return p;
@@ -1224,7 +1261,7 @@ static bool single_tokens(const HeadsDev& h) { return !h.offsets && h.n_tokens =
 size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h, false).part_floats * sizeof(float); }
 size_t attention_backward_workspace_bytes(const HeadsDev& h) {
     const Plan p = plan_of(h, true);
-    return (2 * p.part_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
+    return (2 * p.part_floats + p.post_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
 }
 
 template <int DP, bool BF16, int DIRS>
@@ -1242,6 +1279,15 @@ static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Pla
     const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND>, bytes, raised);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
+    return hipGetLastError();
+}
+template <bool BF16, int KIND>
+static hipError_t launch_wide(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
+    static std::atomic<unsigned long long> raised{0};
+    constexpr int bytes = std::max(std::max(Lds<128, BF16, 0>::bytes, Lds<128, BF16, 1>::bytes), Lds<128, BF16, 2>::bytes);
+    const hipError_t e = raise_lds((const void*)attend_backward_kernel<BF16, KIND>, bytes, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((attend_backward_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H * 2), KIND == kEach ? 3 : KIND + 1), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
     return hipGetLastError();
 }
 template <int DP, bool BF16>
@@ -1264,7 +1310,7 @@ template <int DP, bool BF16>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, true);
     double* const dw_parts = (double*)h.partial;
-    float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const du_parts = G + p.part_floats;
+    float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const posts = G + p.part_floats, *const du_parts = posts + p.post_floats;
     LocalsDev l{};
     l.dir[0] = LocalDev{h.v, h.k, h.v_stride, h.k_stride, h.state, S, false, true};
     l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true, false};
@@ -1274,9 +1320,11 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
     all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true};
     all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false};
-    all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
+    all.state_initial = h.state; all.state_parts = S; all.grad_initial = h.dstate; all.grad_parts = G;
+    all.posts = posts; all.n_posts = p.n_posts; all.du_parts = du_parts; all.dw_parts = dw_parts;
+    const bool at_once = p.n_posts == 0;          // otherwise dk's kernel waits for what dr's leaves
     if constexpr (DP == 64) {
-        if (p.slots * h.H <= 128) {               // both kinds find room on the 256 units at once; the kernel that has both is 7 % slower
+        if (at_once && p.slots * h.H <= 128) {               // both kinds find room on the 256 units at once; the kernel that has both is 7 % slower
             e = launch_pair<BF16, kEach>(h, all, p, s);
         } else {
             e = launch_pair<BF16, 0>(h, all, p, s);
@@ -1284,10 +1332,13 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         }
         if (e != hipSuccess) return e;
     } else {
-        static std::atomic<unsigned long long> raised{0};
-        constexpr int bytes = std::max(std::max(Lds<128, BF16, 0>::bytes, Lds<128, BF16, 1>::bytes), Lds<128, BF16, 2>::bytes);
-        if ((e = raise_lds((const void*)attend_backward_kernel<BF16>, bytes, raised)) != hipSuccess) return e;
-        hipLaunchKernelGGL((attend_backward_kernel<BF16>), dim3((unsigned)(p.slots * h.H * 2), 3), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
+        if (at_once) {
+            e = launch_wide<BF16, kEach>(h, all, p, s);
+        } else {
+            e = launch_wide<BF16, 0>(h, all, p, s);
+            if (e == hipSuccess) e = launch_wide<BF16, 1>(h, all, p, s);
+        }
+        if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL(attend_sum_kernel, dim3((h.H * (h.D + 1) + 15) / 16), dim3(256), 0, s, h, du_parts, dw_parts, p.slots, p.blocks);
     return hipGetLastError();
