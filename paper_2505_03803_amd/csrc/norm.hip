@@ -383,8 +383,10 @@ static Pick pick(const NormDev& p, int dt, bool backward) {
     k.loop = k.E * k.V > (k.block ? block_values(k.V, backward) : kWaveValues);
     k.grid_y = (p.groups + k.teams.groups - 1) / k.teams.groups;
     const long long row_sets = (p.M + k.teams.rows - 1) / k.teams.rows;
-    // workgroups that stay for several rows: eight to a compute unit forwards; backwards fewer, each leaves 8 bytes a column
-    const int wanted = std::max(1, (backward ? 512 : 2048) / k.grid_y);
+    // workgroups that stay for several rows: eight to a compute unit forwards; backwards, where each leaves 8 bytes a column, as many only if
+    // they stay for 16 rows, and two otherwise (8192 rows of 4096 bf16: 256 in all take 68 us, 512 50, 768 53, 1024 62)
+    const long long all = std::min(std::max(row_sets * k.grid_y / 16, 512ll), 2048ll);
+    const int wanted = (int)std::max(1ll, (backward ? all : 2048) / k.grid_y);
     k.grid_x = (int)std::min<long long>(row_sets, wanted);
     k.partials = k.grid_x * k.teams.rows;
     if (k.grid_y > 65535) k.loop = true;
