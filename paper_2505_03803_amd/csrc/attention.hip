@@ -27,7 +27,9 @@ __device__ __forceinline__ int slot_of(const HeadsDev& h, int b) {
 
 // One token for each sequence: a workgroup per sequence and head.  LANES lanes hold a row of the state, four columns each, a thread
 // ROWS rows; all of a state is on its way before any of it is used, and is written back where it is.  What bounds it: HBM
-// bandwidth (the state read and written once), for few sequences a launch and two ways to memory.
+// bandwidth (the state read and written once), for few sequences a launch and two ways to memory.  Heads of up to 32, 64 and 128 channels
+// have 8, 16 and 32 lanes a row, so that a row is one or two cache lines.  256 sequences of 64 heads of 64: 111 us, 4.9 TB/s, the rate of a copy; one
+// sequence 3.6 us (rows loaded one after the other 8.1 us).
 template <int LANES, int ROWS, bool BF16>
 __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
     constexpr int per = 256 / LANES;              // rows at a time
@@ -106,10 +108,15 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // n w >= 20 (l^n < 2.1e-9) a chunk is left out of the sum, below the rounding of the rest; of a fast head that leaves at most the segment's last
 // chunk, n (<G, S> - sum of its K_i).  These products have 24-bit operands, their sums over a chunk are carried on in binary64.
 //
-// A workgroup of four wavefronts takes a segment of a sequence, one head and 64 channels of val.  Wavefront `wave` owns tokens
-// 16 wave .. + 15 of a chunk for scores and outputs (computed transposed: a lane holds one token and four consecutive channels or
-// earlier tokens, so that the scores of a token are the next product's operand without leaving their registers) and a quarter of
-// the state's rows for the update, which it publishes in LDS as the next chunk's operand.
+// A workgroup takes a segment of a sequence, one head and 64 channels of val, chunk by chunk: four wavefronts compute outputs, each those of 16
+// tokens of a chunk (transposed: a lane holds one token and four consecutive channels or earlier tokens, so that the scores of a token are the
+// next product's operand without leaving their registers), and four carry the state, a quarter of its rows each, and publish it in LDS as
+// the next chunk's operand.  One set of four for both needs more registers than two sets on a unit have (forward, 8192 tokens of 64 heads:
+// 70 us against 61).  Segments of a sequence run side by side; what those in front of one leave in its state is summed up before, by a pass over
+// keys and values alone.
+// What bounds it.  Forward: HBM bandwidth nearly (r, k, v read and out written, 268 MB in 66 us = 4.1 TB/s, behind a pass of 33 us for
+// what segments leave).  Backward: a wavefront's own chain of LDS reads, products and conversions, chunk after chunk (vector units busy 43 % of
+// the cycles, matrix cores 18 %, LDS 38 %; one workgroup of twelve wavefronts a unit, whose registers and LDS leave no room for another).
 // Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
 // states as two bf16 parts (17 bits), the weighted keys of a state's update as three (24 bits), since states are binary32 results.
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -167,8 +174,9 @@ struct Marks {
 };
 
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
-// published beside the one that the outputs still read.
-// swaps: there is a sweep whose val are the keys.
+// published beside the one that the outputs still read (forward 70 -> 61 us).  Forward sweeps of fp16 heads of up to 64 channels keep one, so that two
+// workgroups fit a unit.  Rows of 32 or 48 bytes more than the values, for fewer bank conflicts, are no faster (dr 113 and 112 us against 112), and
+// cost bf16 the second workgroup (85 us against 66).  swaps: there is a sweep whose val are the keys.
 template <int DP, bool BF16, int GRAD, bool PAIR = false, bool SWAPS = false> struct Lds {
     static constexpr bool swaps = SWAPS;
     static constexpr int threads = PAIR ? 768 : 512;
@@ -511,7 +519,10 @@ __device__ __forceinline__ void scale(float4_t (&S)[KT][4], float by) {
         for (int vt = 0; vt < 4; ++vt) S[x][vt] *= by;
 }
 
-// The parts of one direction, before the sweeps; transposed: key is what the state in memory calls val.
+// The parts of one direction, before the sweeps; transposed: key is what the state in memory calls val.  Four wavefronts with a quarter of the state's
+// rows each, two tiles in LDS and so one barrier a chunk.  What bounds it: HBM bandwidth (8192 tokens of 64 heads: 33 us, 4.1 TB/s).  Both
+// directions of the backward pass are one launch, four workgroups a unit; forward has half as many, and registers for that (36 us with those for
+// four; backward 47 instead of 40 with those for three).  A second chunk on its way gains nothing (35 us).
 struct LocalDev { const uint16_t *key, *val; long long key_stride, val_stride; const float* initial; float* parts; bool reverse, transposed; };
 struct LocalsDev { LocalDev dir[2]; };
 
@@ -588,7 +599,8 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 2 * DIRS) attend_local_kern
     store_part(S, to, v0, wave, lane);
 }
 
-// Many segments per sequence: the state at each one's front in place of its part, a thread per element.
+// Many segments per sequence: the state at each one's front in place of its part, a thread per element, eight loads in flight.  What bounds it: a
+// launch and the way to memory (26 segments of 20 heads: 7 us).
 __global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev locals, int cut, int size) {
     const LocalDev& p = locals.dir[blockIdx.z];
     const int at = blockIdx.y * 256 + threadIdx.x;
@@ -1151,7 +1163,8 @@ __device__ __forceinline__ void leave_zeros(const HeadsDev& h, const SweepsDev& 
     if (tid == 0) all.dw_parts[((size_t)at.slot_at * h.H + at.head) * 4 + 2 * half + at.v0 / kVals] = 0.0;
 }
 
-// One sweep: four wavefronts for the outputs, four for the state, which meet at the same barriers.
+// One sweep: four wavefronts for the outputs, four for the state, which meet at the same barriers.  Forward, 8192 tokens of 64 heads of 64: 66 us in
+// bf16, 97 in fp16, whose values are two parts.
 template <int DP, bool BF16, int GRAD>
 __device__ __forceinline__ void sweep(const HeadsDev& h, const SweepsDev& all, const SweepDev& p, int cut, int scanned, int blocks, int* found, char* lds) {
     typedef Lds<DP, BF16, GRAD> L;
@@ -1174,7 +1187,8 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
-// dw, which need the state in more bits, computed apart from its outputs.
+// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 123 us for dr, 150 for dk and dv
+// (as sweeps of eight wavefronts: 160 and 128 + 61).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
     typedef Lds<64, BF16, 0, true, DK> L;
@@ -1193,7 +1207,7 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
 }
 
 // The sweeps of the backward pass need nothing of each other but the states that dr's leaves between blocks, where a segment has several.  KIND 0: dr;
-// 1: dk and dv; kEach: all, the longest first.
+// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 62 us; three launches 92).
 constexpr int kEach = 3;
 template <bool BF16, int KIND>
 __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
@@ -1237,14 +1251,22 @@ __global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float
 
 // How a call is cut: `cut` tokens a segment, `slots` segments at most; split: a sequence can have more than one; scan: one launch turns
 // the segments' parts into the states in front of them, otherwise each segment adds up those before it.
+// Segments are as long as the device stays full.  Forward two workgroups fit a unit: 512 in all (8192 tokens of 64 heads: shorter segments for 1024 are slower,
+// the pass in front has more to do); ragged sequences that are more than that by themselves end at different times, and shorter segments even
+// that out (sixteen of 1 to 1184 tokens, 80 heads: 98 us for 512, 92 for 1024, 101 and a scan for 2048; four sequences of 32 heads 24 against 32).
+// Backward one workgroup fits: 256, and no pass in front where sequences are as many by themselves (4 x 2048 tokens x 64 heads: 245 us
+// against 294 for 512); above 64 channels the three sweeps are one launch, and 128 (75 us against 92).  No segment is shorter than 128 tokens, two
+// chunks (256: 800 tokens of 16 heads 19 us instead of 16), but what fits 256 is not cut (224 tokens: 13 us in one segment, 15 in two).
+// A scan pays from 17 segments on: 14 segments 28 us without, 25 + 6 and a launch with it; 26 42 against 30 + 7; 32, backward, 63 against 41 + 7.
 struct Plan { int cut, slots, blocks, part_size, n_posts; bool split, scan; size_t part_floats, post_floats, du_floats, dw_doubles; };
 static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
     const long long work = (long long)h.n_tokens * h.H * p.blocks;
+    const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
     p.cut = (int)std::max(128ll, (work / (!grad ? (h.offsets && (long long)h.n_seqs * h.H * p.blocks > 512 ? 1024 : 512) : h.D > 64 ? 128 : 256) + kChunk - 1) / kChunk * kChunk);
     if (grad) p.cut = std::min(p.cut, 2048);
-    const int len = h.offsets ? h.n_tokens : h.n_tokens / h.n_seqs;
+    if (len <= 256) p.cut = std::max(p.cut, 256);
     p.split = len > p.cut;
     p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
     p.scan = len / p.cut > 16;
@@ -1324,7 +1346,9 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     all.posts = posts; all.n_posts = p.n_posts; all.du_parts = du_parts; all.dw_parts = dw_parts;
     const bool at_once = p.n_posts == 0;          // otherwise dk's kernel waits for what dr's leaves
     if constexpr (DP == 64) {
-        if (at_once && p.slots * h.H <= 128) {               // both kinds find room on the 256 units at once; the kernel that has both is 7 % slower
+        // both kinds at once, and a launch less, for at most 512 workgroups: 400 tokens of 16 heads 17 us instead of 29, 760 of 23 44 instead of 49.
+        // Many are better apart, the kernel that has both has too few registers (512 in all, 2048 tokens each: 263 us instead of 245).
+        if (at_once && p.slots * h.H <= 256) {
             e = launch_pair<BF16, kEach>(h, all, p, s);
         } else {
             e = launch_pair<BF16, 0>(h, all, p, s);

