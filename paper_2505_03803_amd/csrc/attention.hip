@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // 70 us against 61).  Segments of a sequence run side by side; what those in front of one leave in its state is summed up before, by a pass over
 // keys and values alone.
 // What bounds it.  Forward: HBM bandwidth nearly (r, k, v read and out written, 268 MB in 66 us = 4.1 TB/s, behind a pass of 33 us for
-// what segments leave).  Backward: a wavefront's own chain of LDS reads, products and conversions, chunk after chunk (vector units busy 43 % of
-// the cycles, matrix cores 18 %, LDS 38 %; one workgroup of twelve wavefronts a unit, whose registers and LDS leave no room for another).
+// what segments leave).  Backward: a wavefront's own chain of LDS reads, products and conversions, chunk after chunk (dk and dv: matrix cores
+// busy 22 % of the cycles, LDS 47 %, 0.14 vector instructions a cycle and SIMD; one workgroup of twelve wavefronts a unit, whose registers and LDS leave no
+// room for another).
 // Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
 // states as two bf16 parts (17 bits), the weighted keys of a state's update as three (24 bits), since states are binary32 results.
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -1187,7 +1188,7 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
-// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 123 us for dr, 150 for dk and dv
+// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 142 for dk and dv
 // (as sweeps of eight wavefronts: 160 and 128 + 61).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
