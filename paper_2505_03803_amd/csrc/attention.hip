@@ -18,6 +18,11 @@ __device__ __forceinline__ void rows_of(const HeadsDev& h, int b, int& t0, int& 
         t0 = b * len; t1 = t0 + len;
     }
 }
+// A head's decay; an infinite one forgets all but the token in front, which 0 times it would make NaN.
+__device__ __forceinline__ float decay_of(const HeadsDev& h, int head) {
+    const uint32_t w = __builtin_amdgcn_readfirstlane(__float_as_uint(h.w[head]));
+    return __uint_as_float(w == 0x7F800000u ? 0x7F7FFFFFu : w);      // the largest finite one, without leaving scalar registers
+}
 // Slot of sequence b's states, -1 if it is to be left out.
 __device__ __forceinline__ int slot_of(const HeadsDev& h, int b) {
     if (!h.slots) return b;
@@ -451,12 +456,12 @@ struct Powers {
     static __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 };
 // Weights exp(-(nt - 1 - i) w) of tokens i = 32 ks .. + 31 of a chunk in the state behind it, in the order of column_frag.
-template <bool TAIL>
+template <bool TAIL, bool AGREE>
 __device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, int ks, int nt, float w, int g) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
-        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? Powers::of(nt - 1 - i, w) : 0.0f;
+        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? (AGREE ? Powers::of(nt - 1 - i, w) : expf(-(float)(nt - 1 - i) * w)) : 0.0f;
     }
 }
 struct Whole { static constexpr bool tail = false; };
@@ -542,7 +547,7 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 2 * DIRS) attend_local_kern
     if (s.idx >= s.count || s.count <= 1) return;
     const int slot = slot_of(h, s.b), D = h.D;
     if (slot < 0) return;
-    const float w = h.w[head];
+    const float w = decay_of(h, head);
     float* const to = p.parts + ((size_t)slot_at * h.H + head) * part_size<KT>(D);
     float4_t S[KT][4];
     clear(S);
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 2 * DIRS) attend_local_kern
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
-            key_weights<tail>(kw, pow, ks, nt, w, g);
+            key_weights<tail, DIRS == 2>(kw, pow, ks, nt, w, g);
             val_columns<BF16>(lds + L::val, lds + L::val_lo, ks, n, g, vf, vl);
             key_columns<L>(lds, ks, wave, n, g, keys, low);
             update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
@@ -614,7 +619,7 @@ __global__ void __launch_bounds__(256) attend_scan_kernel(HeadsDev h, LocalsDev 
         if (count <= 1 || slot_of(h, b) < 0) continue;
         float* const x = p.parts + ((size_t)first * h.H + head) * size + at;
         const size_t stride = (size_t)h.H * size;
-        const float w = h.w[head], decay = expf(-(float)cut * w);
+        const float w = decay_of(h, head), decay = expf(-(float)cut * w);
         const float ragged = expf(-(float)(t1 - t0 - (count - 1) * cut) * w);      // of the last segment, which may be shorter
         float run = p.initial ? x[(p.reverse ? 0 : count - 1) * stride] : 0.0f;
         for (int from = 0; from < count; from += 8) {        // eight loads in flight
@@ -768,7 +773,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
-            key_weights<tail>(kw, pow, ks, nt, w, g);
+            key_weights<tail, MEETS != 0>(kw, pow, ks, nt, w, g);
             val_columns<BF16>(buffer + L::val, buffer + L::val_lo, ks, n, g, vf, vl);
             key_columns<L>(buffer, ks, wave, n, g, keys, low);
             update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
@@ -824,7 +829,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
 // more scalar registers than there are.
 template <bool YES>
 __device__ __forceinline__ int per_chunk(int x, int by) {
-    if (YES) asm("" : "+s"(x) : "s"(by));
+    if (YES && !__builtin_constant_p(x)) asm("" : "+s"(x) : "s"(by));
     return x;
 }
 
@@ -891,7 +896,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     // Every wavefront takes all four tiles: without branches their loads and products overlap, and the last wavefront has four anyway.
     float pw[4][4];
     bool lower[4], own[4];                        // of the lane's own tile: earlier tokens, and the lane's
-    const float front = Powers::of(a, w);
+    const float front = GRAD ? Powers::of(a, w) : expf(-(float)a * w);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
 #pragma unroll
@@ -1125,7 +1130,7 @@ __device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut
     if (at.slot < 0) return false;
     at.len = at.s.a1 - at.s.a0;
     at.middle = min(at.len, reach_of(h.D)) / 2;
-    at.w = h.w[at.head];
+    at.w = decay_of(h, at.head);
     return true;
 }
 // A workgroup's parts of dw, and of du from four of its wavefronts (`which`: 0 .. 3, or -1).
@@ -1188,7 +1193,7 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
-// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 142 for dk and dv
+// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 131 for dk and dv
 // (as sweeps of eight wavefronts: 160 and 128 + 61).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
@@ -1208,17 +1213,20 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
 }
 
 // The sweeps of the backward pass need nothing of each other but the states that dr's leaves between blocks, where a segment has several.  KIND 0: dr;
-// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 62 us; three launches 92).
+// 1: dk and dv; WHOLE: heads of exactly 64 or 128 channels, whose places are all in use, which takes conditions out of the kernels that have too
+// few registers (dk and dv of 64 channels 142 -> 131 us; dr's alone gains nothing, the forward sweep of fp16 loses, 97 -> 110).  kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 58 us; three launches 92).
 constexpr int kEach = 3;
-template <bool BF16, int KIND>
+template <bool BF16, int KIND, bool WHOLE>
 __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+    if (WHOLE) h.D = 64;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     if (KIND == 1 || (KIND == kEach && blockIdx.y == 0)) pair<BF16, true>(h, all, cut, scanned, &found, lds);
     else pair<BF16, false>(h, all, cut, scanned, &found, lds);
 }
-template <bool BF16, int KIND>
+template <bool BF16, int KIND, bool WHOLE>
 __global__ void __launch_bounds__(512, 2) attend_backward_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
+    if (WHOLE) h.D = 128;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     if (KIND == 0 || (KIND == kEach && blockIdx.y == 0)) sweep<128, BF16, 1>(h, all, all.sweep[0], cut, scanned, 2, &found, lds);
@@ -1295,22 +1303,22 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
         hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, DIRS), dim3(256), 0, s, h, l, p.cut, p.part_size);
     return hipGetLastError();
 }
-template <bool BF16, int KIND>
+template <bool BF16, int KIND, bool WHOLE>
 static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
     constexpr int bytes = Lds<64, BF16, 0, true, true>::bytes;
-    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND>, bytes, raised);
+    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND, WHOLE>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND, WHOLE>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
     return hipGetLastError();
 }
-template <bool BF16, int KIND>
+template <bool BF16, int KIND, bool WHOLE>
 static hipError_t launch_wide(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
     constexpr int bytes = std::max(std::max(Lds<128, BF16, 0>::bytes, Lds<128, BF16, 1>::bytes), Lds<128, BF16, 2>::bytes);
-    const hipError_t e = raise_lds((const void*)attend_backward_kernel<BF16, KIND>, bytes, raised);
+    const hipError_t e = raise_lds((const void*)attend_backward_kernel<BF16, KIND, WHOLE>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_backward_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H * 2), KIND == kEach ? 3 : KIND + 1), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
+    hipLaunchKernelGGL((attend_backward_kernel<BF16, KIND, WHOLE>), dim3((unsigned)(p.slots * h.H * 2), KIND == kEach ? 3 : KIND + 1), dim3(512), bytes, s, h, all, p.cut, (int)p.scan);
     return hipGetLastError();
 }
 template <int DP, bool BF16>
@@ -1329,7 +1337,7 @@ static hipError_t forward(const HeadsDev& h, hipStream_t s) {
     hipLaunchKernelGGL((attend_forward_kernel<DP, BF16>), dim3((unsigned)(p.slots * h.H * p.blocks)), dim3(512), bytes, s, h, all, p.cut, (int)p.scan, p.blocks);
     return hipGetLastError();
 }
-template <int DP, bool BF16>
+template <int DP, bool BF16, bool WHOLE>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, true);
     double* const dw_parts = (double*)h.partial;
@@ -1350,18 +1358,18 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         // both kinds at once, and a launch less, for at most 512 workgroups: 400 tokens of 16 heads 17 us instead of 29, 760 of 23 44 instead of 49.
         // Many are better apart, the kernel that has both has too few registers (512 in all, 2048 tokens each: 263 us instead of 245).
         if (at_once && p.slots * h.H <= 256) {
-            e = launch_pair<BF16, kEach>(h, all, p, s);
+            e = launch_pair<BF16, kEach, false>(h, all, p, s);
         } else {
-            e = launch_pair<BF16, 0>(h, all, p, s);
-            if (e == hipSuccess) e = launch_pair<BF16, 1>(h, all, p, s);
+            e = launch_pair<BF16, 0, false>(h, all, p, s);
+            if (e == hipSuccess) e = launch_pair<BF16, 1, WHOLE>(h, all, p, s);
         }
         if (e != hipSuccess) return e;
     } else {
         if (at_once) {
-            e = launch_wide<BF16, kEach>(h, all, p, s);
+            e = launch_wide<BF16, kEach, WHOLE>(h, all, p, s);
         } else {
-            e = launch_wide<BF16, 0>(h, all, p, s);
-            if (e == hipSuccess) e = launch_wide<BF16, 1>(h, all, p, s);
+            e = launch_wide<BF16, 0, WHOLE>(h, all, p, s);
+            if (e == hipSuccess) e = launch_wide<BF16, 1, WHOLE>(h, all, p, s);
         }
         if (e != hipSuccess) return e;
     }
@@ -1370,7 +1378,8 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
 }
 template <bool BF16>
 static hipError_t attention(const HeadsDev& h, bool grad, hipStream_t s) {
-    if (grad) return h.D <= 64 ? backward<64, BF16>(h, s) : backward<128, BF16>(h, s);
+    if (grad)
+        return h.D == 64 ? backward<64, BF16, true>(h, s) : h.D < 64 ? backward<64, BF16, false>(h, s) : h.D == 128 ? backward<128, BF16, true>(h, s) : backward<128, BF16, false>(h, s);
     if (!single_tokens(h)) return h.D <= 64 ? forward<64, BF16>(h, s) : forward<128, BF16>(h, s);
     const dim3 grid((unsigned)(h.n_seqs * h.H)), block(256);
     if (h.D <= 32) hipLaunchKernelGGL((attend_step_kernel<8, 1, BF16>), grid, block, 0, s, h);

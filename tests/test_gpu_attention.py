@@ -399,3 +399,16 @@ def test_long_sequences(lens, H, D, dt):
     c = Case(lens, H, D, dt, seed=sum(lens), w=[0.003, 0.3][:H], offsets=len(lens) > 1)
     c.check_forward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("dt,H,D,T", [("bf16", 2, 64, 150), ("f16", 2, 128, 70), ("f16", 2, 64, 1)])
+def test_infinite_decay(dt, H, D, T):
+    """A decay that leaves nothing: the same bits as one whose powers are 0, tokens in front still count with the weight 1."""
+    torch = G.torch_()
+    got = []
+    for w in (1e4, np.inf):
+        c = Case([T], H, D, dt, seed=11, w=[w, 0.5], offsets=False)
+        so = torch.full((1, H, D, D), 7.0, device="cuda")
+        got.append((c.forward(so), so.cpu().numpy(), c.backward()))
+    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    assert all(np.array_equal(got[0][2][p], got[1][2][p]) for p in got[0][2])
