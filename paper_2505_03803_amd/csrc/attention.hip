@@ -1193,7 +1193,7 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
-// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 131 for dk and dv
+// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 140 for dk and dv
 // (as sweeps of eight wavefronts: 160 and 128 + 61).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
@@ -1213,12 +1213,12 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
 }
 
 // The sweeps of the backward pass need nothing of each other but the states that dr's leaves between blocks, where a segment has several.  KIND 0: dr;
-// 1: dk and dv; WHOLE: heads of exactly 64 or 128 channels, whose places are all in use, which takes conditions out of the kernels that have too
-// few registers (dk and dv of 64 channels 142 -> 131 us; dr's alone gains nothing, the forward sweep of fp16 loses, 97 -> 110).  kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 58 us; three launches 92).
+// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 61 us; three launches 92).  WHOLE: heads of
+// exactly 128 channels, whose places are all in use, which takes conditions out of a kernel that has too few registers (65 -> 61 us; that of 64 channels
+// gains nothing by it, 138 to 158 us with and without, the forward sweep neither).
 constexpr int kEach = 3;
-template <bool BF16, int KIND, bool WHOLE>
+template <bool BF16, int KIND>
 __global__ void __launch_bounds__(768, 3) attend_pair_kernel(HeadsDev h, SweepsDev all, int cut, int scanned) {
-    if (WHOLE) h.D = 64;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ int found;
     if (KIND == 1 || (KIND == kEach && blockIdx.y == 0)) pair<BF16, true>(h, all, cut, scanned, &found, lds);
@@ -1303,13 +1303,13 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
         hipLaunchKernelGGL(attend_scan_kernel, dim3((unsigned)std::min(65536ll, (long long)h.n_seqs * h.H), (p.part_size + 255) / 256, DIRS), dim3(256), 0, s, h, l, p.cut, p.part_size);
     return hipGetLastError();
 }
-template <bool BF16, int KIND, bool WHOLE>
+template <bool BF16, int KIND>
 static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
     constexpr int bytes = Lds<64, BF16, 0, true, true>::bytes;
-    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND, WHOLE>, bytes, raised);
+    const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND>, bytes, raised);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND, WHOLE>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
     return hipGetLastError();
 }
 template <bool BF16, int KIND, bool WHOLE>
@@ -1358,10 +1358,10 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         // both kinds at once, and a launch less, for at most 512 workgroups: 400 tokens of 16 heads 17 us instead of 29, 760 of 23 44 instead of 49.
         // Many are better apart, the kernel that has both has too few registers (512 in all, 2048 tokens each: 263 us instead of 245).
         if (at_once && p.slots * h.H <= 256) {
-            e = launch_pair<BF16, kEach, false>(h, all, p, s);
+            e = launch_pair<BF16, kEach>(h, all, p, s);
         } else {
-            e = launch_pair<BF16, 0, false>(h, all, p, s);
-            if (e == hipSuccess) e = launch_pair<BF16, 1, WHOLE>(h, all, p, s);
+            e = launch_pair<BF16, 0>(h, all, p, s);
+            if (e == hipSuccess) e = launch_pair<BF16, 1>(h, all, p, s);
         }
         if (e != hipSuccess) return e;
     } else {
@@ -1379,7 +1379,7 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
 template <bool BF16>
 static hipError_t attention(const HeadsDev& h, bool grad, hipStream_t s) {
     if (grad)
-        return h.D == 64 ? backward<64, BF16, true>(h, s) : h.D < 64 ? backward<64, BF16, false>(h, s) : h.D == 128 ? backward<128, BF16, true>(h, s) : backward<128, BF16, false>(h, s);
+        return h.D <= 64 ? backward<64, BF16, false>(h, s) : h.D == 128 ? backward<128, BF16, true>(h, s) : backward<128, BF16, false>(h, s);
     if (!single_tokens(h)) return h.D <= 64 ? forward<64, BF16>(h, s) : forward<128, BF16>(h, s);
     const dim3 grid((unsigned)(h.n_seqs * h.H)), block(256);
     if (h.D <= 32) hipLaunchKernelGGL((attend_step_kernel<8, 1, BF16>), grid, block, 0, s, h);
