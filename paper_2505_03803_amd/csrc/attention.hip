@@ -968,7 +968,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
         }
         if constexpr (GRAD) {
             const int before = GRAD == 1 ? (slow ? ((at.len - left) & (reach_of(DP) - 1)) - at.middle : 0) : slow ? ((left - nt) & (reach_of(DP) - 1)) + nt - at.middle : passes(w, nt) && nt < kChunk ? nt : 0;
-            dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;
+            if (a < nt) dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;      // weights of places behind the last token may be infinite
         }
 
         // scores of the wavefront's tokens with those before them
@@ -1016,7 +1016,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 float sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum += (it < tile) | ((it == tile) & lower[j]) ? sc[j] * ((float)(a - 1 - (16 * it + 4 * g + j)) * xv[j]) : 0.0f;
-                dw += (double)sum;
+                if (a < nt) dw += (double)sum;
             }
             if constexpr (STORE) {
                 uint2_t sp[2];
