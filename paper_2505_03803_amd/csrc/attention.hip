@@ -102,16 +102,12 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 //   dv:   q = k,    key = r,    val = dout, bonus (sum_c k u r) dout, backwards, state G.
 // The gradient of w.  Its definition weighs every pair of tokens i < t, with X_ti = l^(t-1-i) (r_t . k_i) (dout_t . v_i), by the lag t - 1 - i
 // (-w's exponent).  Pairs of one chunk are summed so.  The lag of any other pair is the place a of t in its chunk, plus what follows i in its
-// own chunk, plus 64 for each whole chunk between, so that with R_t the dot of r_t with the state's part of dr_t and K_i that of k_i
-// with the state's part of dk_i
-//   -dw = (pairs of one chunk) + sum_t a_t R_t + sum_i (n - 1 - a_i) K_i + sum over chunks of n <G, l^n S>,  G behind a chunk, S in front of it.
-// The last sum needs both states of every chunk at once; but what passes by a chunk is what passes its end less what its keys add, and what is
-// at a block's front less what is at its end is sum_t R_t - sum_i K_i.  So over a block of L tokens, with o the place of a token's chunk in it and any c,
-// it is (L - c) <G, S> (both at its end) + c <G, S> (at its front) + sum_t (o_t - c) R_t - sum_i (o_i + n_i - c) K_i.  The rounding of R and K grows with
-// |o - c|, so that blocks are short (256 or 512 tokens, c half of it: as exact as the recurrence in binary32; over 2048 tokens at once the error was eight times
-// that): the sweep for dr leaves S at the blocks' boundaries for the one for dk.  For heads that forget within a chunk the rest cancels: where
-// n w >= 20 (l^n < 2.1e-9) a chunk is left out of the sum, below the rounding of the rest; of a fast head that leaves at most the segment's last
-// chunk, n (<G, S> - sum of its K_i).  These products have 24-bit operands, their sums over a chunk are carried on in binary64.
+// own chunk, plus the chunks between.  With R_t the dot of r_t with the state's part of dr_t, K_i that of k_i with the state's part of dk_i, and
+// a second state N that counts the tokens of whole chunks that what is in S has passed since the segment's front, N' = l^n (N + n S),
+//   -dw = (pairs of one chunk) + sum_t (a_t R_t + l^a r_t N dout_t) + sum_i (n - 1 - a_i) K_i + sum over segments <G, N>, both behind the segment.
+// Each term has its own lag as its weight and nothing cancels, so that the error is one of dw's terms and of nothing else in the sequences.  (Without
+// N, from differences of R, K and <G, S> at the ends of blocks of tokens, a large score without a lag leaves its rounding times the block's length.)
+// The sweep for dr carries N; S and N meet x in 24 bits there, as G does in the one for dk, and sums over a chunk are carried on in binary64.
 //
 // A workgroup takes a segment of a sequence, one head and 64 channels of val, chunk by chunk: four wavefronts compute outputs, each those of 16
 // tokens of a chunk (transposed: a lane holds one token and four consecutive channels or earlier tokens, so that the scores of a token are the
@@ -129,7 +125,6 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 constexpr int kChunk = 64;                    // tokens
 constexpr int kVals = 64;                     // channels of val of a workgroup
-constexpr int reach_of(int D) { return D > 64 ? 256 : 512; }     // tokens of a block, between the states that both directions meet at
 
 struct Segment { int b, idx, count, first_slot, t0, t1, a0, a1; };     // sequence, its place in it of how many; rows of both
 
@@ -181,19 +176,21 @@ struct Marks {
 
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
 // published beside the one that the outputs still read (forward 70 -> 61 us).  Forward sweeps of fp16 heads of up to 64 channels keep one, so that two
-// workgroups fit a unit.  Rows of 32 or 48 bytes more than the values, for fewer bank conflicts, are no faster (dr 113 and 112 us against 112), and
+// workgroups fit a unit; dr's of fp16 heads and of heads above 64 channels have room for one beside N.  Rows of 32 or 48 bytes more than the values, for fewer bank conflicts, are no faster (dr 113 and 112 us against 112), and
 // cost bf16 the second workgroup (85 us against 66).  swaps: there is a sweep whose val are the keys.
 template <int DP, bool BF16, int GRAD, bool PAIR = false, bool SWAPS = false> struct Lds {
     static constexpr bool swaps = SWAPS;
     static constexpr int threads = PAIR ? 768 : 512;
-    static constexpr bool split_keys = PAIR && !BF16;                            // fp16 keys as two bf16 parts too: they are somebody's val
+    static constexpr bool split_keys = SWAPS && !BF16;                           // fp16 keys as two bf16 parts too: they are somebody's val
+    static constexpr bool passed_too = GRAD == 1 || (PAIR && !SWAPS);            // N beside the state, for the gradient of w
     static constexpr int key_row = 2 * DP + 16, val_row = 2 * kVals + 16;       // bytes; 16 more than the values: rows begin at different banks
     static constexpr int key = 0, key_lo = key + kChunk * key_row, val = key_lo + (split_keys ? kChunk * key_row : 0), val_lo = val + kChunk * val_row;
     static constexpr int parts = GRAD || PAIR ? 3 : 2, part = kVals * key_row;   // of a published state
-    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), buffer = state + parts * part;
+    static constexpr int state = val_lo + (BF16 ? 0 : kChunk * val_row), passed = state + parts * part, buffer = passed + (passed_too ? parts * part : 0);
     static constexpr bool two = 2 * buffer + 4 * DP + 1152 + Marks::bytes <= 160 * 1024 && (BF16 || DP > 64 || PAIR);
     static constexpr int u = two ? 2 * buffer : buffer, sums = u + 4 * DP;
     static constexpr int marks = sums + (GRAD || PAIR ? 12 * 8 + 4 * 4 * kVals : 0), bytes = marks + Marks::bytes;
+    static_assert(bytes <= 160 * 1024, "a unit's LDS");
 };
 
 // Two values as packed bf16 and what is left of them.
@@ -450,18 +447,15 @@ struct Powers {
         for (int i = 0; i < 4; ++i) far[i] = uniform(expf(-(float)(16 * i) * w));
         whole = uniform(expf(-(float)kChunk * w));
     }
-    // The same for any lag below 64, to the same bits: what a state takes in and what is read from it have to agree for the gradient of w, where
-    // they cancel.
-    static __device__ __forceinline__ float of(int lag, float w) { return expf(-(float)(lag & 15) * w) * expf(-(float)(lag & ~15) * w); }
     static __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 };
 // Weights exp(-(nt - 1 - i) w) of tokens i = 32 ks .. + 31 of a chunk in the state behind it, in the order of column_frag.
-template <bool TAIL, bool AGREE>
+template <bool TAIL>
 __device__ __forceinline__ void key_weights(float (&kw)[8], const Powers& pow, int ks, int nt, float w, int g) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 32 * ks + 16 * (e >> 2) + 4 * g + (e & 3);
-        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? (AGREE ? Powers::of(nt - 1 - i, w) : expf(-(float)(nt - 1 - i) * w)) : 0.0f;
+        kw[e] = !TAIL ? pow.near[e & 3] * pow.far[3 - 2 * ks - (e >> 2)] : i < nt ? expf(-(float)(nt - 1 - i) * w) : 0.0f;
     }
 }
 struct Whole { static constexpr bool tail = false; };
@@ -589,7 +583,7 @@ __global__ void __launch_bounds__(256, DP > 64 ? 2 : 2 * DIRS) attend_local_kern
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
-            key_weights<tail, DIRS == 2>(kw, pow, ks, nt, w, g);
+            key_weights<tail>(kw, pow, ks, nt, w, g);
             val_columns<BF16>(lds + L::val, lds + L::val_lo, ks, n, g, vf, vl);
             key_columns<L>(lds, ks, wave, n, g, keys, low);
             update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
@@ -661,19 +655,15 @@ struct SweepDev {
 };
 struct SweepsDev {
     SweepDev sweep[3];
-    const float *state_initial, *state_parts, *grad_initial, *grad_parts;
-    float *posts, *du_parts;            // posts: S at the boundaries of blocks, [slots][H][n_posts] parts
+    const float *grad_initial, *grad_parts;
+    float* du_parts;
     double* dw_parts;                   // [slots][H][4]
-    int n_posts;
 };
-
-// Whether a head remembers more than rounding leaves over a chunk of n tokens (see the gradient of w).
-__device__ __forceinline__ bool passes(float w, int n) { return w * (float)n < 20.0f; }
 
 // What both kinds of wavefront know of their segment.
 struct Place {
     Segment s;
-    int slot_at, slot, head, v0, D, len, middle, lane, wave, n, g;       // middle: c of the gradient of w
+    int slot_at, slot, head, v0, D, len, lane, wave, n, g;
     float w;
 };
 // A thread's share of the staging of a sweep's chunks.  Of twelve wavefronts the first eight bring the keys, the last eight val.
@@ -732,10 +722,9 @@ __device__ __forceinline__ void mark_state(float4_t (&S)[KT][4], const Marks& ma
     }
 }
 
-// The state of a sweep: four wavefronts, each with a quarter of the rows.  Returns the lane's share of
-// the <G, S>.  MEETS 1: the state is S, which meets G at the segment's end and is left at the boundaries of blocks;  2: it is G, which meets S there
-// and at the segment's front.
-template <int DP, bool BF16, class L, int MEETS>
+// The state of a sweep: four wavefronts, each with a quarter of the rows; where the sweep has shares of the gradient of w for it (L::passed_too) N
+// as well, which meets G at the segment's end.  Returns the lane's share of that.
+template <int DP, bool BF16, class L>
 __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev& p, const SweepsDev& all, const Place& at, int cut, bool scanned, char* lds) {
     constexpr int KT = DP / 64;
     const int wave = at.wave - 4, n = at.n, g = at.g, D = at.D;
@@ -744,7 +733,8 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     Staging<DP, BF16, L> rows(p, at);
     int nt = first_chunk(at.len, p.reverse);
     rows.fetch(nt);
-    float4_t S[KT][4];
+    float4_t S[KT][4], N[L::passed_too ? KT : 1][4];
+    clear(N);
     start_state(S, h, s, cut, scanned, p.initial, p.parts, p.reverse, p.transposed, p.parts_transposed, at.head, at.slot, w, at.v0, wave, at.lane);
     Powers pow;
     pow.set(w, g);
@@ -765,15 +755,21 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         publish(S, buffer + L::state);
+        if constexpr (L::passed_too) publish(N, buffer + L::passed);
         rows.store(buffer, marks, turn, number);
         __syncthreads();
         rows.fetch(next);
-        scale(S, tail ? expf(-(float)nt * w) : pow.whole);
+        const float whole = tail ? expf(-(float)nt * w) : pow.whole;
+        if constexpr (L::passed_too) {
+            add(N, S, (float)nt);
+            scale(N, whole);
+        }
+        scale(S, whole);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4_t vf[4], vl[4], keys[KT], low[KT];
             float kw[8];
-            key_weights<tail, MEETS != 0>(kw, pow, ks, nt, w, g);
+            key_weights<tail>(kw, pow, ks, nt, w, g);
             val_columns<BF16>(buffer + L::val, buffer + L::val_lo, ks, n, g, vf, vl);
             key_columns<L>(buffer, ks, wave, n, g, keys, low);
             update_state<BF16, L, 3>(S, keys, low, kw, vf, vl);
@@ -783,44 +779,24 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
         else __syncthreads();
         ++number;
     };
+    for (int left = at.len; left > 0;) {
+        const int next = min(kChunk, left - nt);
+        if (nt < kChunk) chunk(Tail{}, nt, next);
+        else chunk(Whole{}, nt, next);
+        left -= nt;
+        nt = next;
+    }
+    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
     double dw = 0.0;
-    auto meet = [&](const float4_t (&other)[KT][4], int weight) {
-        double sum = 0.0;
+    if constexpr (L::passed_too) {
+        start_state(S, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
 #pragma unroll
         for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int vt = 0; vt < 4; ++vt)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)       // places behind a head's last channels hold whatever was loaded for them
-                    if (16 * (KT * wave + x) + 4 * g < D && at.v0 + 16 * vt + n < D) sum += (double)other[x][vt][j] * (double)S[x][vt][j];
-        dw += (double)weight * sum;
-    };
-    const bool slow = MEETS && at.len > 0 && passes(w, kChunk);
-    float* const posts = MEETS ? all.posts + ((size_t)at.slot_at * h.H + at.head) * all.n_posts * part_size<KT>(D) : nullptr;
-    for (int left = at.len; left > 0;) {
-        const int next = min(kChunk, left - nt);
-        if (MEETS == 1 && slow && left < at.len && ((at.len - left) & (reach_of(DP) - 1)) == 0)
-            store_part(S, posts + ((at.len - left) / reach_of(DP) - 1) * part_size<KT>(D), at.v0, wave, at.lane);
-        float4_t other[KT][4];                    // on its way during the chunk in front
-        const bool boundary = MEETS == 2 && slow && next > 0 && ((left - nt) & (reach_of(DP) - 1)) == 0;
-        if (boundary) load_part(other, posts + ((left - nt) / reach_of(DP) - 1) * part_size<KT>(D), !p.transposed, at.v0, wave, at.lane);
-        if (nt < kChunk) chunk(Tail{}, nt, next);
-        else chunk(Whole{}, nt, next);
-        if (boundary) meet(other, reach_of(DP));
-        left -= nt;
-        nt = next;
-    }
-    if (p.last && s.idx == (p.reverse ? 0 : s.count - 1)) store_state(S, p.last + ((size_t)at.slot * h.H + at.head) * D * D, D, at.v0, wave, n, g);
-    if constexpr (MEETS != 0) {
-        float4_t other[KT][4];
-        if (MEETS == 1) {
-            start_state(other, h, s, cut, scanned, all.grad_initial, all.grad_parts, true, true, true, at.head, at.slot, w, at.v0, wave, at.lane);
-            const int last = at.len % kChunk;
-            meet(other, slow ? at.len - (at.len - 1) / reach_of(DP) * reach_of(DP) - at.middle : passes(w, last) ? last : 0);
-        } else if (slow) {
-            start_state(other, h, s, cut, scanned, all.state_initial, all.state_parts, false, p.transposed, !p.transposed, at.head, at.slot, w, at.v0, wave, at.lane);
-            meet(other, at.middle);
-        }
+                for (int j = 0; j < 4; ++j)           // places behind a head's last channels hold whatever was loaded for them
+                    if (16 * (KT * wave + x) + 4 * g < D && at.v0 + 16 * vt + n < D) dw += (double)S[x][vt][j] * (double)N[x][vt][j];
     }
     return dw;
 }
@@ -834,11 +810,13 @@ __device__ __forceinline__ int per_chunk(int x, int by) {
 }
 
 // The outputs of a sweep: four wavefronts with sixteen tokens of each chunk.  Returns the lane's share of dw, and those of du.
-//   GRAD 1: the shares of dw that dr's sweep has, with x = r;  2: those of dk's and du, with x = k;  0: neither.  STORE: the outputs.
+//   GRAD 1: the shares of dw that dr's sweep has, with x = r;  2: those of dk's and du, with x = k;  0: neither.  STORE: the outputs; where two sets of
+//   wavefronts share dr's sweep the one that stores has the state's shares of dw, the other N's and those of pairs of one chunk.
 //   SWAP: the tiles and the state are those of the sweep for dv, whose key and val exchange their roles in the one for dk.
 template <int DP, bool BF16, class L, int GRAD, bool STORE, bool SWAP, bool U_IN_DOT>
 __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, const Place& at, int wave, float (&du)[GRAD == 2 ? 16 : 1], char* lds) {
     constexpr int KS = DP / 32, parts = GRAD ? L::parts : 2;
+    constexpr bool passed = GRAD == 1 && (L::threads == 512 || !STORE);
     constexpr int key_tile = SWAP ? L::val : L::key, key_low = SWAP ? L::val_lo : L::key_lo, val_tile = SWAP ? L::key : L::val, val_low = SWAP ? L::key_lo : L::val_lo;
     const int n = at.n, g = at.g, v0 = at.v0, a = 16 * wave + n;
     const float w = at.w;
@@ -872,7 +850,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             }
             if constexpr (GRAD) {
                 const char* const xf = x_at.at + (nt < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
-                if constexpr (GRAD == 1)
+                if constexpr (passed)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         xr[i] = uint4_t{0, 0, 0, 0};
@@ -896,7 +874,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
     // Every wavefront takes all four tiles: without branches their loads and products overlap, and the last wavefront has four anyway.
     float pw[4][4];
     bool lower[4], own[4];                        // of the lane's own tile: earlier tokens, and the lane's
-    const float front = GRAD ? Powers::of(a, w) : expf(-(float)a * w);
+    const float front = expf(-(float)a * w);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
 #pragma unroll
@@ -908,7 +886,6 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) { lower[j] = 4 * g + j < n; own[j] = 4 * g + j == n; }
     double dw = 0.0;
-    const bool slow = GRAD && passes(w, kChunk);
 
     const Marks marks(lds + L::marks);
     char* buffer = lds;
@@ -926,7 +903,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             else split_f16(qf[i], qh[i], ql[i]);
         }
         if constexpr (GRAD) {
-            if constexpr (GRAD == 1)
+            if constexpr (passed)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if constexpr (BF16) xf[i] = xr[i];
@@ -943,33 +920,36 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             const uint2_t x = *(const uint2_t*)(from + 8 * g), y = *(const uint2_t*)(from + 32 + 8 * g);
             return uint4_t{x.x, x.y, y.x, y.y};
         };
-        // the state in front; for the gradient of w its part of the outputs with x, weighted by the token's place in the segment
+        // the state in front; for the gradient of w its part of the outputs with x, weighted by the token's place in the chunk, and N's
         float4_t out[4];
         double state_dot = 0.0;
 #pragma unroll
         for (int vt = 0; vt < 4; ++vt) {
-            float4_t o = {0, 0, 0, 0};
+            auto product = [&](int state) {
+                float4_t o = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < KS; ++i)
+                for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int part = parts - 1; part >= 0; --part) {
-                    const char* const from = buffer + L::state + part * L::part;
-                    const uint4_t st = SWAP ? column_frag<L::key_row>(from, i, vt, n, g) : *(const uint4_t*)(from + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
-                    o = mfma_bits<true>(st, qh[i], o);
-                    if (!BF16 && part < parts - 1) o = mfma_bits<true>(st, ql[i], o);
-                }
-            out[vt] = front * o;
+                    for (int part = parts - 1; part >= 0; --part) {
+                        const char* const from = buffer + state + part * L::part;
+                        const uint4_t st = SWAP ? column_frag<L::key_row>(from, i, vt, n, g) : *(const uint4_t*)(from + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                        o = mfma_bits<true>(st, qh[i], o);
+                        if (!BF16 && part < parts - 1) o = mfma_bits<true>(st, ql[i], o);
+                    }
+                return o;
+            };
+            out[vt] = float4_t{0, 0, 0, 0};
+            if constexpr (STORE) out[vt] = front * product(L::state);
             if constexpr (GRAD) {
+                float4_t weighted = (float)a * out[vt];
+                if constexpr (passed) weighted += front * product(L::passed);
                 float sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum = fmaf(half_of<BF16>(xd[vt], j), out[vt][j], sum);
+                for (int j = 0; j < 4; ++j) sum = fmaf(half_of<BF16>(xd[vt], j), weighted[j], sum);
                 state_dot += (double)sum;
             }
         }
-        if constexpr (GRAD) {
-            const int before = GRAD == 1 ? (slow ? ((at.len - left) & (reach_of(DP) - 1)) - at.middle : 0) : slow ? ((left - nt) & (reach_of(DP) - 1)) + nt - at.middle : passes(w, nt) && nt < kChunk ? nt : 0;
-            if (a < nt) dw += (double)(GRAD == 1 ? a + before : a - before) * state_dot;      // weights of places behind the last token may be infinite
-        }
+        if (GRAD && a < nt) dw += state_dot;      // weights of places behind the last token may be infinite
 
         // scores of the wavefront's tokens with those before them
         uint4_t ph[2], pl[2];
@@ -999,7 +979,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) sc[j] = (it < tile) | ((it == tile) & lower[j]) ? pw[it][j] * sc[j] : 0.0f;
-            if constexpr (GRAD == 1) {                                 // x . val of the same pairs, weighted with their lags
+            if constexpr (passed) {                                    // x . val of the same pairs, weighted with their lags
                 float4_t xv = {0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -1129,7 +1109,6 @@ __device__ __forceinline__ bool find_place(Place& at, const HeadsDev& h, int cut
     at.slot = at.s.idx < at.s.count ? slot_of(h, at.s.b) : -1;
     if (at.slot < 0) return false;
     at.len = at.s.a1 - at.s.a0;
-    at.middle = min(at.len, reach_of(h.D)) / 2;
     at.w = decay_of(h, at.head);
     return true;
 }
@@ -1181,7 +1160,7 @@ __device__ __forceinline__ void sweep(const HeadsDev& h, const SweepsDev& all, c
     }
     float du[GRAD == 2 ? 16 : 1] = {};
     const double dw = at.wave < 4 ? outputs<DP, BF16, L, GRAD, true, false, GRAD == 0>(h, p, at, at.wave, du, lds)
-                                  : carry_state<DP, BF16, L, GRAD>(h, p, all, at, cut, scanned != 0, lds);
+                                  : carry_state<DP, BF16, L>(h, p, all, at, cut, scanned != 0, lds);
     if constexpr (GRAD != 0) leave_sums<8, GRAD == 2>(h, all, at, GRAD - 1, dw, du, at.wave < 4 ? at.wave : -1, lds + L::sums);
 }
 template <int DP, bool BF16>
@@ -1192,9 +1171,9 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 }
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
-// in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, with its shares of
-// dw, which need the state in more bits, computed apart from its outputs.  4 sequences of 2048 tokens, 64 heads of 64, bf16: 116 us for dr, 140 for dk and dv
-// (as sweeps of eight wavefronts: 160 and 128 + 61).
+// in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, whose second set of
+// wavefronts has N's shares of dw and those of pairs of one chunk (all shares in one set: dr 133 us instead of 122).  4 sequences of 2048 tokens, 64 heads
+// of 64, bf16: 122 us for dr, 130 for dk and dv (fp16: 180 and 170).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
     typedef Lds<64, BF16, 0, true, DK> L;
@@ -1205,15 +1184,15 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
     }
     float du[DK ? 16 : 1] = {}, none[1];
     const SweepDev& p = all.sweep[DK ? 2 : 0];
-    const double dw = at.wave < 4   ? outputs<64, BF16, L, 0, true, false, DK>(h, p, at, at.wave, none, lds)
-                      : at.wave < 8 ? carry_state<64, BF16, L, DK ? 2 : 1>(h, p, all, at, cut, scanned != 0, lds)
+    const double dw = at.wave < 4   ? outputs<64, BF16, L, DK ? 0 : 1, true, false, DK>(h, p, at, at.wave, none, lds)
+                      : at.wave < 8 ? carry_state<64, BF16, L>(h, p, all, at, cut, scanned != 0, lds)
                       : DK          ? outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, all.sweep[1], at, at.wave - 8, du, lds)
                                     : outputs<64, BF16, L, DK ? 2 : 1, DK, DK, false>(h, p, at, at.wave - 8, du, lds);
     leave_sums<12, DK>(h, all, at, DK, dw, du, at.wave >= 8 ? at.wave - 8 : -1, lds + L::sums);
 }
 
-// The sweeps of the backward pass need nothing of each other but the states that dr's leaves between blocks, where a segment has several.  KIND 0: dr;
-// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 61 us; three launches 92).  WHOLE: heads of
+// The sweeps of the backward pass need nothing of each other.  KIND 0: dr;
+// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 63 us; two launches 41 + 40).  WHOLE: heads of
 // exactly 128 channels, whose places are all in use, which takes conditions out of a kernel that has too few registers (65 -> 61 us; that of 64 channels
 // gains nothing by it, 138 to 158 us with and without, the forward sweep neither).
 constexpr int kEach = 3;
@@ -1266,8 +1245,10 @@ __global__ void __launch_bounds__(256) attend_sum_kernel(HeadsDev h, const float
 // Backward one workgroup fits: 256, and no pass in front where sequences are as many by themselves (4 x 2048 tokens x 64 heads: 245 us
 // against 294 for 512); above 64 channels the three sweeps are one launch, and 128 (75 us against 92).  No segment is shorter than 128 tokens, two
 // chunks (256: 800 tokens of 16 heads 19 us instead of 16), but what fits 256 is not cut (224 tokens: 13 us in one segment, 15 in two).
+// Backward none is longer than 2048 (16384 tokens of 40 heads of 128: 1395 us against 1829 for a segment a workgroup; 32768 of 64 heads of 64: 1354
+// against 1221).
 // A scan pays from 17 segments on: 14 segments 28 us without, 25 + 6 and a launch with it; 26 42 against 30 + 7; 32, backward, 63 against 41 + 7.
-struct Plan { int cut, slots, blocks, part_size, n_posts; bool split, scan; size_t part_floats, post_floats, du_floats, dw_doubles; };
+struct Plan { int cut, slots, blocks, part_size, longest; bool split, scan; size_t part_floats, du_floats, dw_doubles; };
 static Plan plan_of(const HeadsDev& h, bool grad) {
     Plan p;
     p.blocks = (h.D + kVals - 1) / kVals;
@@ -1280,9 +1261,8 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
     p.slots = h.offsets ? h.n_tokens / p.cut + h.n_seqs : h.n_seqs * ((len + p.cut - 1) / p.cut);
     p.scan = len / p.cut > 16;
     p.part_size = (h.D <= 64 ? 64 : 128) * kVals * p.blocks;
+    p.longest = std::min(len, p.cut);
     p.part_floats = p.split ? (size_t)p.slots * h.H * p.part_size : 0;
-    p.n_posts = (std::min(len, p.cut) - 1) / reach_of(h.D);
-    p.post_floats = (size_t)p.slots * h.H * p.n_posts * p.part_size;
     p.dw_doubles = (size_t)p.slots * h.H * 4;
     p.du_floats = (size_t)p.slots * h.H * h.D;
     return p;
@@ -1292,7 +1272,7 @@ static bool single_tokens(const HeadsDev& h) { return !h.offsets && h.n_tokens =
 size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h, false).part_floats * sizeof(float); }
 size_t attention_backward_workspace_bytes(const HeadsDev& h) {
     const Plan p = plan_of(h, true);
-    return (2 * p.part_floats + p.post_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
+    return (2 * p.part_floats + p.du_floats) * sizeof(float) + p.dw_doubles * sizeof(double);
 }
 
 template <int DP, bool BF16, int DIRS>
@@ -1306,7 +1286,7 @@ static hipError_t launch_locals(const HeadsDev& h, const LocalsDev& l, const Pla
 template <bool BF16, int KIND>
 static hipError_t launch_pair(const HeadsDev& h, const SweepsDev& all, const Plan& p, hipStream_t s) {
     static std::atomic<unsigned long long> raised{0};
-    constexpr int bytes = Lds<64, BF16, 0, true, true>::bytes;
+    constexpr int bytes = std::max(Lds<64, BF16, 0, true, false>::bytes, Lds<64, BF16, 0, true, true>::bytes);
     const hipError_t e = raise_lds((const void*)attend_pair_kernel<BF16, KIND>, bytes, raised);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_pair_kernel<BF16, KIND>), dim3((unsigned)(p.slots * h.H), KIND == kEach ? 2 : 1), dim3(768), bytes, s, h, all, p.cut, (int)p.scan);
@@ -1341,7 +1321,7 @@ template <int DP, bool BF16, bool WHOLE>
 static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     const Plan p = plan_of(h, true);
     double* const dw_parts = (double*)h.partial;
-    float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const posts = G + p.part_floats, *const du_parts = posts + p.post_floats;
+    float *const S = (float*)(dw_parts + p.dw_doubles), *const G = S + p.part_floats, *const du_parts = G + p.part_floats;
     LocalsDev l{};
     l.dir[0] = LocalDev{h.v, h.k, h.v_stride, h.k_stride, h.state, S, false, true};
     l.dir[1] = LocalDev{h.r, h.dout, h.r_stride, h.out_stride, h.dstate, G, true, false};
@@ -1351,13 +1331,11 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
     all.sweep[0] = SweepDev{h.dout, h.v, h.k, h.r, h.out_stride, h.v_stride, h.k_stride, h.r_stride, h.r_stride, h.dr, h.state, S, nullptr, false, true, false};
     all.sweep[1] = SweepDev{h.v, h.dout, h.r, h.k, h.v_stride, h.out_stride, h.r_stride, h.k_stride, h.k_stride, h.dk, h.dstate, G, nullptr, true, true, true};
     all.sweep[2] = SweepDev{h.k, h.r, h.dout, nullptr, h.k_stride, h.r_stride, h.out_stride, h.v_stride, 0, h.dv, h.dstate, G, h.dstate_in, true, false, false};
-    all.state_initial = h.state; all.state_parts = S; all.grad_initial = h.dstate; all.grad_parts = G;
-    all.posts = posts; all.n_posts = p.n_posts; all.du_parts = du_parts; all.dw_parts = dw_parts;
-    const bool at_once = p.n_posts == 0;          // otherwise dk's kernel waits for what dr's leaves
+    all.grad_initial = h.dstate; all.grad_parts = G; all.du_parts = du_parts; all.dw_parts = dw_parts;
     if constexpr (DP == 64) {
-        // both kinds at once, and a launch less, for at most 512 workgroups: 400 tokens of 16 heads 17 us instead of 29, 760 of 23 44 instead of 49.
-        // Many are better apart, the kernel that has both has too few registers (512 in all, 2048 tokens each: 263 us instead of 245).
-        if (at_once && p.slots * h.H <= 256) {
+        // both kinds at once, and a launch less, for at most 512 workgroups and 512 tokens each: 400 tokens of 16 heads 17 us instead of 29.  More and
+        // longer ones are better apart, the kernel that has both has too few registers (512 in all, 2048 tokens each: 291 us instead of 258).
+        if (p.longest <= 512 && p.slots * h.H <= 256) {
             e = launch_pair<BF16, kEach>(h, all, p, s);
         } else {
             e = launch_pair<BF16, 0>(h, all, p, s);
@@ -1365,7 +1343,8 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         }
         if (e != hipSuccess) return e;
     } else {
-        if (at_once) {
+        // likewise: segments of 128 tokens 63 us instead of 81 (above), of 2048 tokens (4 sequences, 32 heads of 128) 423 instead of 413
+        if (p.longest <= 256) {
             e = launch_wide<BF16, kEach, WHOLE>(h, all, p, s);
         } else {
             e = launch_wide<BF16, 0, WHOLE>(h, all, p, s);
