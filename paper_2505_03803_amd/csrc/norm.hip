@@ -199,7 +199,9 @@ __global__ void __launch_bounds__(256) norm_backward_kernel(NormDev p, Teams tea
                 dn[e].load(p.dy, m * p.dy_stride + g0 + at(e));
             }
         }
-        if (seat.row >= 0 && m < p.M) { mean_n = p.mean[m * p.groups + seat.g]; rstd_n = p.rstd[m * p.groups + seat.g]; }
+        const bool there = seat.row >= 0 && m < p.M;
+        mean_n = there ? p.mean[m * p.groups + seat.g] : 0.0f;
+        rstd_n = there ? p.rstd[m * p.groups + seat.g] : 0.0f;
     };
     const float over_n = 1.0f / (float)p.n;
     int turn = 0;
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(256) norm_backward_kernel(NormDev p, Teams tea
             xn[e].widen(x[e]); dn[e].widen(d[e]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                x[e][j] = (x[e][j] - mean) * rstd;
+                x[e][j] = live(e) ? (x[e][j] - mean) * rstd : 0.0f;   // a mean times a rstd that binary32 does not hold is nobody's
                 const float g = d[e][j] * w[e][j];                  // 0 where dy was not read
                 c1 += g;
                 c2 = fmaf(g, x[e][j], c2);
