@@ -434,7 +434,8 @@ int rwkvq_linear_dispatch_post(const rwkvq_matrix* mats, const void* const* xs, 
  *   exit.  Sums in a fixed order: the same bits every time.
  * x, y, dx, dy, workspace 16-byte aligned, floats 4.  Rows whose n and strides are multiples of 16 bytes load and
  *   store 16 bytes at a time.  Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, eps), RWKVQ_ERR_SHAPE (M,
- *   groups or n < 1, groups * n > 2^24, a stride below groups * n, M * stride > 2^40), RWKVQ_ERR_ALIGN, RWKVQ_ERR_DEVICE. */
+ *   groups or n < 1, groups * n > 2^24, M * groups > 2^31 - 1, a stride below groups * n,
+ *   M * stride > 2^40), RWKVQ_ERR_ALIGN, RWKVQ_ERR_DEVICE. */
 int rwkvq_layer_norm(const void* x, int x_dtype, int M, int groups, int n, long long x_stride, const float* weight,
                      const float* bias, double eps, void* y, long long y_stride, float* mean, float* rstd, void* stream);
 size_t rwkvq_layer_norm_backward_workspace_size(int M, int groups, int n);

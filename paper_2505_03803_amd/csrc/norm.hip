@@ -255,33 +255,36 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float* lds) {
     team_sum2<NT, true>(a, b, 64, lds);
 }
 
-// A workgroup per row and group, one element at a time, x read three times.
+// Rows and groups by a workgroup each, one element at a time, x read three times.  A launch holds fewer than 2^32 threads, so that beyond
+// kLoops of them a workgroup takes several.
+constexpr long long kLoops = 1 << 22;
 template <int DT_>
 __global__ void __launch_bounds__(256) norm_loop_kernel(NormDev p) {
     typedef typename Type<DT_>::raw raw;
     __shared__ float lds[8];
-    const long long seg = blockIdx.x;
-    const long long m = seg / p.groups;
-    const int g0 = (int)(seg % p.groups) * p.n;
-    const raw* const x = (const raw*)p.x + m * p.x_stride + g0;
-    raw* const y = (raw*)p.y + m * p.y_stride + g0;
-    float s = 0.0f, none = 0.0f;
-    for (int c = threadIdx.x; c < p.n; c += 256) s += Type<DT_>::widen(x[c]);
-    block_sum2<256>(s, none, lds);
-    const float mean = s / (float)p.n;
-    float q = 0.0f;
-    for (int c = threadIdx.x; c < p.n; c += 256) { const float d = Type<DT_>::widen(x[c]) - mean; q = fmaf(d, d, q); }
-    block_sum2<256>(q, none, lds);
-    const float rstd = 1.0f / sqrtf(q / (float)p.n + p.eps);
-    for (int c = threadIdx.x; c < p.n; c += 256) {
-        float v = (Type<DT_>::widen(x[c]) - mean) * rstd;
-        if (p.weight) v *= p.weight[g0 + c];
-        if (p.bias) v += p.bias[g0 + c];
-        y[c] = Type<DT_>::narrow(v);
-    }
-    if (threadIdx.x == 0) {
-        if (p.mean) p.mean[seg] = mean;
-        if (p.rstd) p.rstd[seg] = rstd;
+    for (long long seg = blockIdx.x; seg < (long long)p.M * p.groups; seg += gridDim.x) {
+        const long long m = seg / p.groups;
+        const int g0 = (int)(seg % p.groups) * p.n;
+        const raw* const x = (const raw*)p.x + m * p.x_stride + g0;
+        raw* const y = (raw*)p.y + m * p.y_stride + g0;
+        float s = 0.0f, none = 0.0f;
+        for (int c = threadIdx.x; c < p.n; c += 256) s += Type<DT_>::widen(x[c]);
+        block_sum2<256>(s, none, lds);
+        const float mean = s / (float)p.n;
+        float q = 0.0f;
+        for (int c = threadIdx.x; c < p.n; c += 256) { const float d = Type<DT_>::widen(x[c]) - mean; q = fmaf(d, d, q); }
+        block_sum2<256>(q, none, lds);
+        const float rstd = 1.0f / sqrtf(q / (float)p.n + p.eps);
+        for (int c = threadIdx.x; c < p.n; c += 256) {
+            float v = (Type<DT_>::widen(x[c]) - mean) * rstd;
+            if (p.weight) v *= p.weight[g0 + c];
+            if (p.bias) v += p.bias[g0 + c];
+            y[c] = Type<DT_>::narrow(v);
+        }
+        if (threadIdx.x == 0) {
+            if (p.mean) p.mean[seg] = mean;
+            if (p.rstd) p.rstd[seg] = rstd;
+        }
     }
 }
 
@@ -289,24 +292,25 @@ template <int DT_>
 __global__ void __launch_bounds__(256) norm_dx_loop_kernel(NormDev p) {
     typedef typename Type<DT_>::raw raw;
     __shared__ float lds[8];
-    const long long seg = blockIdx.x;
-    const long long m = seg / p.groups;
-    const int g0 = (int)(seg % p.groups) * p.n;
-    const raw* const x = (const raw*)p.x + m * p.x_stride + g0;
-    const raw* const dy = (const raw*)p.dy + m * p.dy_stride + g0;
-    raw* const dx = (raw*)p.dx + m * p.dx_stride + g0;
-    const float mean = p.mean[seg], rstd = p.rstd[seg];
-    float s = 0.0f, q = 0.0f;
-    for (int c = threadIdx.x; c < p.n; c += 256) {
-        const float g = Type<DT_>::widen(dy[c]) * (p.weight ? p.weight[g0 + c] : 1.0f);
-        s += g;
-        q = fmaf(g, (Type<DT_>::widen(x[c]) - mean) * rstd, q);
-    }
-    block_sum2<256>(s, q, lds);
-    s /= (float)p.n; q /= (float)p.n;
-    for (int c = threadIdx.x; c < p.n; c += 256) {
-        const float g = Type<DT_>::widen(dy[c]) * (p.weight ? p.weight[g0 + c] : 1.0f);
-        dx[c] = Type<DT_>::narrow(rstd * (g - s - (Type<DT_>::widen(x[c]) - mean) * rstd * q));
+    for (long long seg = blockIdx.x; seg < (long long)p.M * p.groups; seg += gridDim.x) {
+        const long long m = seg / p.groups;
+        const int g0 = (int)(seg % p.groups) * p.n;
+        const raw* const x = (const raw*)p.x + m * p.x_stride + g0;
+        const raw* const dy = (const raw*)p.dy + m * p.dy_stride + g0;
+        raw* const dx = (raw*)p.dx + m * p.dx_stride + g0;
+        const float mean = p.mean[seg], rstd = p.rstd[seg];
+        float s = 0.0f, q = 0.0f;
+        for (int c = threadIdx.x; c < p.n; c += 256) {
+            const float g = Type<DT_>::widen(dy[c]) * (p.weight ? p.weight[g0 + c] : 1.0f);
+            s += g;
+            q = fmaf(g, (Type<DT_>::widen(x[c]) - mean) * rstd, q);
+        }
+        block_sum2<256>(s, q, lds);
+        s /= (float)p.n; q /= (float)p.n;
+        for (int c = threadIdx.x; c < p.n; c += 256) {
+            const float g = Type<DT_>::widen(dy[c]) * (p.weight ? p.weight[g0 + c] : 1.0f);
+            dx[c] = Type<DT_>::narrow(rstd * (g - s - (Type<DT_>::widen(x[c]) - mean) * rstd * q));
+        }
     }
 }
 
@@ -441,7 +445,7 @@ static void launch_rows(const NormDev& p, const Pick& k, bool backward, hipStrea
 template <int DT_>
 static hipError_t norm_forward(const NormDev& p, hipStream_t s) {
     const Pick k = pick(p, DT_, false);
-    if (k.loop) hipLaunchKernelGGL(norm_loop_kernel<DT_>, dim3((unsigned)((long long)p.M * p.groups)), dim3(256), 0, s, p);
+    if (k.loop) hipLaunchKernelGGL(norm_loop_kernel<DT_>, dim3((unsigned)std::min((long long)p.M * p.groups, kLoops)), dim3(256), 0, s, p);
     else launch_rows<DT_>(p, k, false, s);
     return hipGetLastError();
 }
@@ -459,7 +463,7 @@ static hipError_t norm_backward(const NormDev& p, hipStream_t s) {
     } else {
         parts = column_parts(p.M, wide);
         if (p.dweight) hipLaunchKernelGGL(norm_columns_kernel<DT_>, dim3((wide + 255) / 256, parts), dim3(256), 0, s, p);
-        if (p.dx) hipLaunchKernelGGL(norm_dx_loop_kernel<DT_>, dim3((unsigned)((long long)p.M * p.groups)), dim3(256), 0, s, p);
+        if (p.dx) hipLaunchKernelGGL(norm_dx_loop_kernel<DT_>, dim3((unsigned)std::min((long long)p.M * p.groups, kLoops)), dim3(256), 0, s, p);
     }
     if (p.dweight) return launch_sum_partials(p.partial, parts, 2 * wide, wide, p.dweight, p.dbias, s);
     return hipGetLastError();

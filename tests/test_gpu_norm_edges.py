@@ -59,3 +59,40 @@ def test_gradients_of_equal_values_of_any_size(M, groups, n, dt):
     check(dx.double().cpu().numpy(), want, bar + HALF_ULP[dt] * 1.01 * np.abs(want))
     assert float(dw.abs().max()) == 0.0
     check(wide32(db), dy64.sum(0), (M + 32) * 2.0 ** -24 * np.abs(dy64).sum(0))
+
+
+@pytest.mark.parametrize("M,groups,n", [(1, 1 << 24, 1), (3, 1 << 23, 2)])
+def test_more_groups_than_a_launch_has_workgroups(M, groups, n):
+    """2^24 groups and more, each a workgroup of 256 threads: as many as 32 bits of threads do not count."""
+    print(f"norm M={M} groups={groups} n={n}", flush=True)
+    torch = G.torch_()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    wide, eps = groups * n, 1e-5
+    x, dy = (torch.randn(M, wide, generator=gen, device="cuda").half() for _ in range(2))
+    w, b = (torch.randn(wide, generator=gen, device="cuda") for _ in range(2))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty(M, groups, device="cuda") for _ in range(2))
+    dw, db = torch.empty(wide, device="cuda"), torch.empty(wide, device="cuda")
+    bits = lambda t: t.view(torch.int16)
+    B.rwkvq_layer_norm(bits(x), B.F16, M, groups, n, w, b, eps, bits(y), mean, rstd)
+    ws = torch.empty(B.rwkvq_layer_norm_backward_workspace_size(M, groups, n), dtype=torch.uint8, device="cuda")
+    B.rwkvq_layer_norm_backward(bits(dy), bits(x), B.F16, M, groups, n, w, mean, rstd, bits(dx), dw, db, ws)
+    z = x.double().reshape(M, groups, n)
+    m = z.mean(-1, keepdim=True)
+    r = 1.0 / torch.sqrt(((z - m) ** 2).mean(-1, keepdim=True) + eps)
+    xhat = (z - m) * r
+    each = 2 * gamma(n) * (z.abs().amax(-1, keepdim=True) + (z - m).abs().amax(-1, keepdim=True)) * r      # the bar of xhat
+    want = xhat.reshape(M, wide) * w.double() + b.double()
+    bar = (each * w.double().abs().reshape(groups, n)).reshape(M, wide) + 2.0 ** -23 * (want.abs() + b.double().abs())
+    assert bool(((y.double() - want).abs() <= bar + HALF_ULP["f16"] * 1.01 * want.abs() + FLOOR["f16"]).all())
+    d = dy.double()
+    g = (d * w.double()).reshape(M, groups, n)
+    c2 = (g * xhat).mean(-1, keepdim=True)
+    want = (r * (g - g.mean(-1, keepdim=True) - xhat * c2)).reshape(M, wide)
+    big, a2 = xhat.abs() + each, (g.abs() * (xhat.abs() + each)).mean(-1, keepdim=True)
+    bar = r * (4 * gamma(n) * (g.abs() + g.abs().mean(-1, keepdim=True) + big * a2) + each * a2 + big * (g.abs() * each).mean(-1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= bar.reshape(M, wide) + HALF_ULP["f16"] * 1.01 * want.abs() + FLOOR["f16"]).all())
+    flat = xhat.reshape(M, wide)
+    err = (each.expand(M, groups, n).reshape(M, wide) * d.abs()).sum(0) + (M + 32) * 2.0 ** -24 * (d * flat).abs().sum(0) + 2.0 ** -126
+    assert bool(((dw.double() - (d * flat).sum(0)).abs() <= err).all())
+    assert bool(((db.double() - d.sum(0)).abs() <= (M + 32) * 2.0 ** -24 * d.abs().sum(0) + 2.0 ** -126).all())
