@@ -616,14 +616,14 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
 }
 
 // The host struct of the attention calls, checked and translated.
-static int check_heads(const rwkvq_heads* in, HeadsDev* h) {
+static int check_heads(const rwkvq_heads* in, HeadsDev* h, bool grad) {
     if (!in) return RWKVQ_ERR_NULL;
     if (in->n_seqs < 1 || in->n_tokens < 1 || in->n_heads < 1 || in->head_dim < 1) return RWKVQ_ERR_SHAPE;
     if (in->head_dim % 8 != 0 || in->head_dim > 128) return RWKVQ_ERR_UNSUPPORTED;
     if (in->slots && in->n_slots < 1) return RWKVQ_ERR_SHAPE;
     if (!in->offsets && in->n_tokens % in->n_seqs != 0) return RWKVQ_ERR_SHAPE;
     const long long wide = (long long)in->n_heads * in->head_dim;
-    // the work of a call goes out as at most eight workgroups per head and 16 tokens begun
+    // counts of segments and workgroups, two a head at most for every sequence and 128 tokens, are 32-bit numbers
     if (wide > (1 << 24) || (double)in->n_heads * 8.0 * (in->n_tokens / 16.0 + in->n_seqs) > 2147483647.0) return RWKVQ_ERR_SHAPE;
     const int64_t given[4] = {in->r_stride, in->k_stride, in->v_stride, in->out_stride};
     long long stride[4];
@@ -637,12 +637,12 @@ static int check_heads(const rwkvq_heads* in, HeadsDev* h) {
     h->n_seqs = in->n_seqs; h->n_tokens = in->n_tokens; h->H = in->n_heads; h->D = in->head_dim; h->n_slots = in->n_slots;
     h->offsets = in->offsets; h->slots = in->slots;
     h->r_stride = stride[0]; h->k_stride = stride[1]; h->v_stride = stride[2]; h->out_stride = stride[3];
-    return RWKVQ_OK;
+    return attention_fits(*h, grad) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
 }
 
 size_t rwkvq_linear_attention_workspace_size(const rwkvq_heads* heads) {
     HeadsDev h;
-    return check_heads(heads, &h) == RWKVQ_OK ? attention_workspace_bytes(h) : 0;
+    return check_heads(heads, &h, false) == RWKVQ_OK ? attention_workspace_bytes(h) : 0;
 }
 
 int rwkvq_linear_attention(const rwkvq_heads* heads, const void* r, const void* k, const void* v, int x_dtype, const float* w,
@@ -651,7 +651,7 @@ int rwkvq_linear_attention(const rwkvq_heads* heads, const void* r, const void* 
     int st;
     if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK) return st;
     HeadsDev h;
-    if ((st = check_heads(heads, &h)) != RWKVQ_OK) return st;
+    if ((st = check_heads(heads, &h, false)) != RWKVQ_OK) return st;
     if (!workspace && attention_workspace_bytes(h) > 0) return RWKVQ_ERR_NULL;
     if (!aligned16(r) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state) || !aligned16(state_out) ||
         !aligned16(workspace) || !aligned4(w) || !aligned4(u))
@@ -663,7 +663,7 @@ int rwkvq_linear_attention(const rwkvq_heads* heads, const void* r, const void* 
 
 size_t rwkvq_linear_attention_backward_workspace_size(const rwkvq_heads* heads) {
     HeadsDev h;
-    return check_heads(heads, &h) == RWKVQ_OK ? attention_backward_workspace_bytes(h) : 0;
+    return check_heads(heads, &h, true) == RWKVQ_OK ? attention_backward_workspace_bytes(h) : 0;
 }
 
 int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, const void* k, const void* v, const void* dout,
@@ -673,7 +673,7 @@ int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, con
     int st;
     if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK) return st;
     HeadsDev h;
-    if ((st = check_heads(heads, &h)) != RWKVQ_OK) return st;
+    if ((st = check_heads(heads, &h, true)) != RWKVQ_OK) return st;
     if (!aligned16(r) || !aligned16(k) || !aligned16(v) || !aligned16(dout) || !aligned16(state) || !aligned16(dstate) ||
         !aligned16(dr) || !aligned16(dk) || !aligned16(dv) || !aligned16(dstate_in) || !aligned16(workspace) || !aligned4(w) ||
         !aligned4(u) || !aligned4(dw) || !aligned4(du))

@@ -1269,6 +1269,13 @@ static Plan plan_of(const HeadsDev& h, bool grad) {
 }
 static bool single_tokens(const HeadsDev& h) { return !h.offsets && h.n_tokens == h.n_seqs; }
 
+// A launch holds fewer than 2^32 threads along x: 256 for a token's step of a head, 512 or 768 for a segment.
+bool attention_fits(const HeadsDev& h, bool grad) {
+    const Plan p = plan_of(h, grad);
+    const unsigned long long groups = !grad && single_tokens(h) ? (unsigned long long)h.n_seqs * h.H : (unsigned long long)p.slots * h.H * p.blocks;
+    return groups * (!grad ? (single_tokens(h) ? 256 : 512) : h.D > 64 ? 512 : 768) < 1ull << 32;
+}
+
 size_t attention_workspace_bytes(const HeadsDev& h) { return single_tokens(h) ? 0 : plan_of(h, false).part_floats * sizeof(float); }
 size_t attention_backward_workspace_bytes(const HeadsDev& h) {
     const Plan p = plan_of(h, true);

@@ -242,6 +242,7 @@ struct HeadsDev {
     uint16_t *out, *dr, *dk, *dv;
     float *state_out, *dw, *du, *dstate_in, *partial;
 };
+bool attention_fits(const HeadsDev& h, bool grad);      // one launch
 size_t attention_workspace_bytes(const HeadsDev& h);
 hipError_t launch_attention(const HeadsDev& h, int dt, hipStream_t s);
 size_t attention_backward_workspace_bytes(const HeadsDev& h);
