@@ -57,8 +57,11 @@ class TimeMix:
 
     def plan(self, lens: Sequence[int], slots: Optional[Sequence[int]] = None):
         """What calls of one form share: the sequences' lengths, their slots (None: they begin empty and leave no state), and the
-        workspace.  A captured graph replays one plan."""
-        assert sum(lens) <= self.max_tokens and (slots is None or len(set(slots)) == len(lens))
+        workspace.  A captured graph replays one plan.  Each sequence has a slot of the pool to itself."""
+        if min(lens) < 0 or sum(lens) > self.max_tokens:
+            raise ValueError(f"sequences of {list(lens)} tokens in a block for at most {self.max_tokens}")
+        if slots is not None and (len(slots) != len(lens) or len(set(slots)) != len(lens) or not all(0 <= s < self.n_slots for s in slots)):
+            raise ValueError(f"slots {list(slots)} for {len(lens)} sequences in a pool of {self.n_slots}")
         heads = self._heads(lens, slots)
         n = B.rwkvq_linear_attention_workspace_size(heads)
         return lens, slots, heads, torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
