@@ -104,7 +104,7 @@ class TimeMix:
         with torch.cuda.graph(graph):
             out = self.forward(x, plan)
 
-        def replay(keep=(x, plan)):                                  # the graph reads the buffers of both
+        def replay(keep=(self, x, plan)):                            # the graph reads and writes the buffers of all three
             graph.replay()
             return out
 
