@@ -48,6 +48,7 @@ class TimeMix:
         self.mixed, self.proj = rows(4), rows(4)
         self.stats = [torch.empty(max_tokens, n, device=device) for n in (1, 1, self.H, self.H)]
         self.dense: Optional[Dict[str, torch.Tensor]] = None
+        self.holds = None, None                                     # x and plan of the call whose rows the buffers hold
 
     def _heads(self, lens: Sequence[int], slots: Optional[Sequence[int]]) -> B.Heads:
         i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=self.device)
@@ -70,6 +71,7 @@ class TimeMix:
         """x: [tokens][d], the sequences' rows one after the other.  -> [tokens][d], a view that the next call overwrites"""
         lens, slots, heads, workspace = plan
         T, H, dt = sum(lens), self.H, self.dtype
+        self.holds = x, plan
         mean, rstd, head_mean, head_rstd = self.stats
         B.rwkvq_layer_norm(x, dt, T, 1, self.d, *self.ln, self.eps, self.a, mean, rstd)
         first = 0
@@ -105,16 +107,20 @@ class TimeMix:
             out = self.forward(x, plan)
 
         def replay(keep=(self, x, plan)):                            # the graph reads and writes the buffers of all three
+            self.holds = x, plan
             graph.replay()
             return out
 
         return replay
 
     def backward(self, x: torch.Tensor, dout: torch.Tensor, plan) -> Dict[str, torch.Tensor]:
-        """The gradients behind forward(x, plan) with a plan without slots: of x, both norms, w and u.  The products with the
-        transposed matrices are taken on their dense copies, made at the first call."""
+        """The gradients behind forward(x, plan), the last call before this one, with a plan without slots: of x, both norms, w and
+        u.  The products with the transposed matrices are taken on their dense copies, made at the first call."""
         lens, slots, heads, _ = plan
-        assert slots is None
+        if slots is not None:
+            raise ValueError("gradients of sequences that begin with a state of the pool")
+        if self.holds[1] is not plan or self.holds[0].data_ptr() != x.data_ptr():        # x itself or a view of its rows
+            raise ValueError("gradients of a call whose rows the block does not hold any more")
         T, H, D, d, dt = sum(lens), self.H, self.D, self.d, self.dtype
         kind = TYPES[dt]
         if self.dense is None:
