@@ -424,18 +424,18 @@ int rwkvq_linear_dispatch_post(const rwkvq_matrix* mats, const void* const* xs, 
  *   projection; groups = n_heads, n = head_dim is the norm of each head behind the attention.
  *   x, y: [M] rows of groups * n values of x_dtype (fp16, bf16 or binary32), x_stride and y_stride elements
  *   apart (0 = groups * n); weight, bias: DEVICE [groups * n] floats, NULL = 1 and 0; mean, rstd: DEVICE
- *   [M * groups] floats for the backward pass, NULL = not stored.  y may be x.  Binary32 arithmetic, the mean
+ *   [M * groups] floats for the backward pass, NULL = not stored.  y may be x, with its stride.  Binary32 arithmetic, the mean
  *   before the deviations, y rounded once.  eps > 0.
  * rwkvq_layer_norm_backward: the gradients for dy: with xhat = (x - mean) rstd and g = dy (.) weight, per group
  *   dx = rstd (g - mean_n(g) - xhat mean_n(g xhat)),  dweight = sum over rows of dy xhat,  dbias = sum of dy.
- *   mean and rstd as the forward pass stored them.  dx (may be dy) or both of dweight and dbias may be NULL:
+ *   mean and rstd as the forward pass stored them.  dx (may be dy, with its stride) or both of dweight and dbias may be NULL:
  *   not computed.  dweight, dbias: DEVICE [groups * n] floats, overwritten.  workspace: DEVICE,
  *   rwkvq_layer_norm_backward_workspace_size(M, groups, n) bytes, contents irrelevant on entry and undefined on
  *   exit.  Sums in a fixed order: the same bits every time.
  * x, y, dx, dy, workspace 16-byte aligned, floats 4.  Rows whose n and strides are multiples of 16 bytes load and
  *   store 16 bytes at a time.  Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, eps), RWKVQ_ERR_SHAPE (M,
  *   groups or n < 1, groups * n > 2^24, M * groups > 2^31 - 1, a stride below groups * n,
- *   M * stride > 2^40), RWKVQ_ERR_ALIGN, RWKVQ_ERR_DEVICE. */
+ *   M * stride > 2^40, in place with another stride), RWKVQ_ERR_ALIGN, RWKVQ_ERR_DEVICE. */
 int rwkvq_layer_norm(const void* x, int x_dtype, int M, int groups, int n, long long x_stride, const float* weight,
                      const float* bias, double eps, void* y, long long y_stride, float* mean, float* rstd, void* stream);
 size_t rwkvq_layer_norm_backward_workspace_size(int M, int groups, int n);

@@ -583,6 +583,7 @@ int rwkvq_layer_norm(const void* x, int x_dtype, int M, int groups, int n, long 
     long long strides[2] = {x_stride, y_stride};
     const int st = check_norm(x_dtype, M, groups, n, strides, 2);
     if (st != RWKVQ_OK) return st;
+    if (x == y && M > 1 && strides[0] != strides[1]) return RWKVQ_ERR_SHAPE;      // rows would be written before they are read
     if (!((float)eps > 0.0f && eps < 1e30)) return RWKVQ_ERR_UNSUPPORTED;
     if (!aligned16(x) || !aligned16(y) || !aligned4(weight) || !aligned4(bias) || !aligned4(mean) || !aligned4(rstd))
         return RWKVQ_ERR_ALIGN;
@@ -604,6 +605,7 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
     long long strides[3] = {dy_stride, x_stride, dx_stride};
     const int st = check_norm(x_dtype, M, groups, n, strides, 3);
     if (st != RWKVQ_OK) return st;
+    if (dx == dy && M > 1 && strides[0] != strides[2]) return RWKVQ_ERR_SHAPE;
     if (!aligned16(dy) || !aligned16(x) || !aligned16(dx) || !aligned16(workspace) || !aligned4(weight) || !aligned4(mean) ||
         !aligned4(rstd) || !aligned4(dweight) || !aligned4(dbias))
         return RWKVQ_ERR_ALIGN;
