@@ -60,3 +60,13 @@ def test_many_chunks(lens, H, D, dt, w):
     c.check_backward()
     first, again = c.backward(), c.backward()
     assert all(np.array_equal(first[p], again[p]) for p in first)
+
+
+@pytest.mark.parametrize("lens,w", [([10], -2.0), ([40], -2.0), ([3, 40, 0, 7], -1.5), ([64], -1.3), ([66], -1.3), ([64, 1, 65], -1.2)])
+@pytest.mark.parametrize("H,D", [(2, 64), (2, 128)])
+def test_growing_heads_up_to_binary32(lens, w, H, D):
+    """Growth by up to e^86 over a sequence, beyond a chunk of 64 tokens as well."""
+    print(f"attention w={w} lens={lens} D={D}", flush=True)
+    c = Case(lens, H, D, "bf16", seed=24, w=w, scale=2.0 ** -5)
+    c.check_forward()
+    c.check_backward()
