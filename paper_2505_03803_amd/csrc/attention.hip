@@ -752,10 +752,11 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
     const Marks marks(lds + L::marks);
     char* buffer = lds;
     int turn = 0, number = 0;
+    if constexpr (L::passed_too && L::two) publish(N, lds + L::passed);
     auto chunk = [&](auto kind, int nt, int next) {
         constexpr bool tail = decltype(kind)::tail;
         publish(S, buffer + L::state);
-        if constexpr (L::passed_too) publish(N, buffer + L::passed);
+        if constexpr (L::passed_too && !L::two) publish(N, buffer + L::passed);
         rows.store(buffer, marks, turn, number);
         __syncthreads();
         rows.fetch(next);
@@ -763,6 +764,7 @@ __device__ __forceinline__ double carry_state(const HeadsDev& h, const SweepDev&
         if constexpr (L::passed_too) {
             add(N, S, (float)nt);
             scale(N, whole);
+            if (L::two) publish(N, lds + (turn ^ 1) * L::buffer + L::passed);       // nobody reads there since the barrier; beside the products (134 -> 128 us)
         }
         scale(S, whole);
 #pragma unroll
@@ -848,6 +850,13 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                     qr[i] = *(const uint4_t*)(from + 64 * i);
                 }
             }
+        }
+        q_at.pass(nt);
+    };
+    auto fetch_x = [&](int nt) {
+        const int D = per_chunk<L::threads == 768 && !L::swaps>(at.D, nt);
+        if (nt > 0) {
+            const int row = min(a, nt - 1);
             if constexpr (GRAD) {
                 const char* const xf = x_at.at + (nt < kChunk ? row_offset(row, reverse, x_stride, 0) : x_off);
                 if constexpr (passed)
@@ -863,10 +872,11 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 }
             }
         }
-        q_at.pass(nt); x_at.pass(nt);
+        x_at.pass(nt);
     };
     int nt = first_chunk(at.len, reverse);
     fetch(nt);
+    fetch_x(nt);
     const int u0 = U_IN_DOT ? 0 : v0, tid = 64 * wave + at.lane;
     if (tid < DP) *(float*)(lds + L::u + 4 * tid) = u0 + tid < at.D ? h.u[at.head * at.D + u0 + tid] : 0.0f;
 
@@ -913,6 +923,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
             for (int vt = 0; vt < 4; ++vt) xd[vt] = xdr[vt];
         }
         fetch(next);
+        if (GRAD != 1) fetch_x(next);
 
         auto key_frag = [&](int tile, int row, int i) {
             const char* const from = buffer + tile + row * L::key_row + 64 * i;
@@ -949,6 +960,7 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
                 state_dot += (double)sum;
             }
         }
+        if (GRAD == 1) fetch_x(next);             // here, where the registers of x are free again (fp16 187 -> 171 us, 128 channels 199 -> 193)
         if (GRAD && a < nt) dw += state_dot;      // weights of places behind the last token may be infinite
 
         // scores of the wavefront's tokens with those before them
@@ -1172,8 +1184,8 @@ __global__ void __launch_bounds__(512, DP > 64 ? 2 : 4) attend_forward_kernel(He
 
 // Heads of up to 64 channels, backward: twelve wavefronts around one state, of which eight read the tiles.  DK: the sweeps for dv and dk
 // in one (their states are each other's transpose, their scores come from the same two tiles); otherwise the sweep for dr, whose second set of
-// wavefronts has N's shares of dw and those of pairs of one chunk (all shares in one set: dr 133 us instead of 122).  4 sequences of 2048 tokens, 64 heads
-// of 64, bf16: 122 us for dr, 130 for dk and dv (fp16: 180 and 170).
+// wavefronts has N's shares of dw and those of pairs of one chunk (all shares in one set: 154 us instead of 140).  4 sequences of 2048 tokens, 64 heads
+// of 64, bf16: 128 us for dr, 134 for dk and dv (fp16: 171 and 169).
 template <bool BF16, bool DK>
 __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, int cut, int scanned, int* found, char* lds) {
     typedef Lds<64, BF16, 0, true, DK> L;
