@@ -455,7 +455,8 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  *   state: the states in front of the sequences ([n_heads][head_dim][head_dim] floats per slot; NULL: zeros), state_out:
  *   those behind them (may be `state`; NULL: not stored).  slots (DEVICE, n_seqs different entries; NULL: b itself) gives the slot
  *   of each sequence in both; a sequence whose slot is not in 0 .. n_slots - 1 is left out: nothing of it is written.
- *   w: DEVICE [n_heads] (positive forgets), u: DEVICE [n_heads][head_dim].  head_dim: a multiple of 8 up to 128.
+ *   w: DEVICE [n_heads] (positive forgets; a head may grow as far as binary32 holds its weights, exp(-64 w) among them in sequences of 64 tokens
+ *   and more: w > -1.38), u: DEVICE [n_heads][head_dim].  head_dim: a multiple of 8 up to 128.
  *   Products of 16-bit values are exact and every sum is binary32; where a state or a weight that was computed meets the matrix cores it goes in
  *   as a sum of two or three bf16 parts (17 bits for an output, 24 for a state).  The same bits every time.  An
  *   infinity or NaN among r, k, v, dout reaches what its formula makes of it, at times as NaN for an infinity, and no other result.
@@ -463,7 +464,8 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  * rwkvq_linear_attention_backward: the gradients.  dout like out (out_stride); dstate: gradient for the states behind the
  *   sequences (NULL: zeros); dr, dk, dv like r, k, v with their strides; dw [n_heads] and du [n_heads][head_dim] floats,
  *   summed over all sequences and overwritten; dstate_in: gradient for the states in front (NULL: not stored).  state as it
- *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Results may not overlap inputs.
+ *   was in front of the sequences.  slots apply to state, dstate and dstate_in.  Results may not overlap inputs.  dw sums every term with its own lag as its
+ *   weight, in binary64 over tokens, operands held to 24 bits; an infinity or NaN of a head makes its dw NaN, also where its lag is 0.
  * r, k, v, out, dout, dr, dk, dv, states, workspace 16-byte aligned; w, u, dw, du, offsets, slots 4; no call synchronises.
  * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, head_dim), RWKVQ_ERR_SHAPE (a count below 1, n_tokens not a multiple
  *   of n_seqs without offsets, a stride below n_heads * head_dim or above 2^24, more threads than the 2^32 of one launch: 256 for a token and

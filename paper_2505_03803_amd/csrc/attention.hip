@@ -115,10 +115,10 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // the next chunk's operand.  One set of four for both needs more registers than two sets on a unit have (forward, 8192 tokens of 64 heads:
 // 70 us against 61).  Segments of a sequence run side by side; what those in front of one leave in its state is summed up before, by a pass over
 // keys and values alone.
-// What bounds it.  Forward: HBM bandwidth nearly (r, k, v read and out written, 268 MB in 66 us = 4.1 TB/s, behind a pass of 33 us for
-// what segments leave).  Backward: a wavefront's own chain of LDS reads, products and conversions, chunk after chunk (dk and dv: matrix cores
-// busy 22 % of the cycles, LDS 47 %, 0.14 vector instructions a cycle and SIMD; one workgroup of twelve wavefronts a unit, whose registers and LDS leave no
-// room for another).
+// What bounds it.  Forward: HBM bandwidth nearly (r, k, v and parts read and out written, 280 MB by the counters in 66 us = 4.2 TB/s of the 4.88 of a large
+// copy, behind a pass of 33 us for what segments leave), with LDS busy half of the cycles.  Backward: a wavefront's own chain of LDS reads, products and
+// conversions, chunk after chunk (dr; dk and dv: matrix cores busy 20 and 22 % of the cycles, LDS 45 and 46 %, 0.14 vector instructions a cycle and SIMD; one
+// workgroup of twelve wavefronts a unit, whose registers and LDS leave no room for another).
 // Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
 // states as two bf16 parts (17 bits), the weighted keys of a state's update as three (24 bits), since states are binary32 results.
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -1204,7 +1204,7 @@ __device__ __forceinline__ void pair(const HeadsDev& h, const SweepsDev& all, in
 }
 
 // The sweeps of the backward pass need nothing of each other.  KIND 0: dr;
-// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 63 us; two launches 41 + 40).  WHOLE: heads of
+// 1: dk and dv; kEach: all, the longest first (five ragged sequences of 1001 tokens, 16 heads of 128, fp16: 66 us; as two launches 41 + 40).  WHOLE: heads of
 // exactly 128 channels, whose places are all in use, which takes conditions out of a kernel that has too few registers (65 -> 61 us; that of 64 channels
 // gains nothing by it, 138 to 158 us with and without, the forward sweep neither).
 constexpr int kEach = 3;
@@ -1362,7 +1362,7 @@ static hipError_t backward(const HeadsDev& h, hipStream_t s) {
         }
         if (e != hipSuccess) return e;
     } else {
-        // likewise: segments of 128 tokens 63 us instead of 81 (above), of 2048 tokens (4 sequences, 32 heads of 128) 423 instead of 413
+        // likewise: segments of 128 tokens 66 us instead of 81 (above), of 2048 tokens (4 sequences, 32 heads of 128) 423 instead of 413
         if (p.longest <= 256) {
             e = launch_wide<BF16, kEach, WHOLE>(h, all, p, s);
         } else {
