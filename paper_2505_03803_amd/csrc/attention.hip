@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // conversions, chunk after chunk (dr; dk and dv: matrix cores busy 20 and 22 % of the cycles, LDS 45 and 46 %, 0.14 vector instructions a cycle and SIMD; one
 // workgroup of twelve wavefronts a unit, whose registers and LDS leave no room for another).
 // Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
-// states as two bf16 parts (17 bits), the weighted keys of a state's update as three (24 bits), since states are binary32 results.
+// states as two bf16 parts (17 bits: half an ulp of a bf16 or fp16 output is 2^-9 or 2^-12 of it), of which fp16's products of both low parts are left
+// out (2^-18); the weighted keys of a state's update as three (24 bits), since states are binary32 results, and so states behind the gradient of w.
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 constexpr int kChunk = 64;                    // tokens
