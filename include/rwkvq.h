@@ -469,8 +469,8 @@ int rwkvq_layer_norm_backward(const void* dy, long long dy_stride, const void* x
  * r, k, v, out, dout, dr, dk, dv, states, workspace 16-byte aligned; w, u, dw, du, offsets, slots 4; no call synchronises.
  * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, head_dim), RWKVQ_ERR_SHAPE (a count below 1, n_tokens not a multiple
  *   of n_seqs without offsets, a stride below n_heads * head_dim or above 2^24, more threads than the 2^32 of one launch: 256 for a token and
- *   head of a call of single tokens, otherwise 512 (backward 768, 1024 above 64 channels; forward 1024 as well) for a head and segment, of which a call has one for every
- *   sequence and at most one more for every 128 tokens), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8), RWKVQ_ERR_DEVICE. */
+ *   head of a call of single tokens, otherwise 512 (backward 768; above 64 channels 1024 both ways) for a head and segment, of
+ *   which a call has one for every sequence and at most one more for every 128 tokens), RWKVQ_ERR_ALIGN (pointers; strides not a multiple of 8), RWKVQ_ERR_DEVICE. */
 typedef struct rwkvq_heads {
     int32_t n_seqs, n_tokens;
     int32_t n_heads, head_dim;

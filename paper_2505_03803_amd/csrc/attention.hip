@@ -177,7 +177,8 @@ struct Marks {
 
 // LDS of a sweep.  Where it has room for two chunks' tiles and states (`two`), one barrier a chunk is enough: the state behind a chunk is
 // published beside the one that the outputs still read (forward 70 -> 61 us).  Forward sweeps of fp16 heads of up to 64 channels keep one, so that two
-// workgroups fit a unit; dr's of fp16 heads and of heads above 64 channels have room for one beside N.  Rows of 32 or 48 bytes more than the values, for fewer bank conflicts, are no faster (dr 113 and 112 us against 112), and
+// workgroups fit a unit; dr's of fp16 heads and of heads above 64 channels have room for one beside N.
+// Rows of 32 or 48 bytes more than the values, for fewer bank conflicts, are no faster (dr 113 and 112 us against 112), and
 // cost bf16 the second workgroup (85 us against 66).  swaps: there is a sweep whose val are the keys.
 template <int DP, bool BF16, int GRAD, bool PAIR = false, bool SWAPS = false> struct Lds {
     static constexpr bool swaps = SWAPS;
@@ -944,7 +945,8 @@ __device__ __forceinline__ double outputs(const HeadsDev& h, const SweepDev& p, 
 #pragma unroll
                     for (int part = parts - 1; part >= 0; --part) {
                         const char* const from = buffer + state + part * L::part;
-                        const uint4_t st = SWAP ? column_frag<L::key_row>(from, i, vt, n, g) : *(const uint4_t*)(from + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
+                        const uint4_t st = SWAP ? column_frag<L::key_row>(from, i, vt, n, g)
+                                                : *(const uint4_t*)(from + (16 * vt + n) * L::key_row + 2 * (32 * i + 8 * g));
                         o = mfma_bits<true>(st, qh[i], o);
                         if (!BF16 && part < parts - 1) o = mfma_bits<true>(st, ql[i], o);
                     }
