@@ -488,6 +488,92 @@ int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, con
                                     void* dr, void* dk, void* dv, float* dw, float* du, float* dstate_in, void* workspace,
                                     void* stream);
 
+/* ---- what is tuned around frozen matrices: dropout, token embeddings, low-rank adapters -------------
+ *
+ * rwkvq_dropout: y = base + keep (.) x / (1 - p) on M rows of n values (fp16, bf16 or binary32), strides in elements (0 = n); base NULL: 0.
+ *   Which elements stay follows from `seed` (DEVICE, two 64-bit numbers, read when the work runs) and from their place, and is stored nowhere:
+ *   the gradient is the same call on dy.  The generator is Philox 4x32-10 (Salmon, Moraes, Dror, Shaw 2011), key seed[0] (low word first), counter
+ *   (column / 8, row, seed[1] low, seed[1] high); its four words, low half first, are the numbers of the eight columns, and a column is
+ *   dropped where its number is below round(65536 p).  p is taken as that multiple of 2^-16, also in 1 / (1 - p); p in [0, 1].  A dropped element
+ *   is 0 (or base) whatever x was.  Binary32 arithmetic, y rounded once.  y may be x or base, with its stride.
+ *   Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtype, p), RWKVQ_ERR_SHAPE (M or n < 1, n > 2^24, a stride below n, M * stride > 2^40,
+ *   in place with another stride), RWKVQ_ERR_ALIGN (x, base, y 16 bytes, seed 8), RWKVQ_ERR_DEVICE.
+ *
+ * rwkvq_embedding: out[t] = scale * table[tokens[t]], rows of d values, rounded once.  tokens: DEVICE [n_tokens]; one outside 0 .. vocab - 1
+ *   (padding) gives a row of zeros.  table: [vocab][d] of table_dtype, out: rows of out_dtype, out_stride elements apart (0 = d); any of the three types.
+ * rwkvq_embedding_backward: dtable[v] = scale * sum of dout[t] over the t with tokens[t] = v, in the order of t: the same bits every time.
+ *   dtable: DEVICE [vocab][d] floats.  accumulate = 0: overwritten, rows of no token become 0; otherwise the sums are added, and
+ *   rows of no token are not touched.  Rows of dout whose token is padding are not read.  workspace: DEVICE,
+ *   rwkvq_embedding_backward_workspace_size(n_tokens, d) bytes, contents irrelevant on entry and undefined on exit.
+ *   Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, scale not finite), RWKVQ_ERR_SHAPE (n_tokens, vocab or d < 1, d > 2^24, vocab * d > 2^40, a
+ *   stride below d, n_tokens * stride > 2^40; backward: n_tokens > 2^22, more threads than the 2^32 of one launch: two for every
+ *   16 columns of 32 tokens, and four for every row of the table), RWKVQ_ERR_ALIGN (tokens 4 bytes, the others 16), RWKVQ_ERR_DEVICE. */
+int rwkvq_dropout(const void* x, int x_dtype, int M, int n, long long x_stride, const uint64_t* seed, double p, const void* base,
+                  long long base_stride, void* y, long long y_stride, void* stream);
+int rwkvq_embedding(const int32_t* tokens, int n_tokens, const void* table, int table_dtype, int vocab, int d, double scale, void* out,
+                    int out_dtype, long long out_stride, void* stream);
+size_t rwkvq_embedding_backward_workspace_size(int n_tokens, int d);
+int rwkvq_embedding_backward(const int32_t* tokens, int n_tokens, const void* dout, int dout_dtype, long long dout_stride, int vocab, int d,
+                             double scale, float* dtable, int accumulate, void* workspace, void* stream);
+
+/* rwkvq_adapters: low-rank adapters of many requests beside a shared projection.  For matrix i and row t of a sequence with adapter a
+ *     h_t = A_a drop(x_t),      y_t = base_t + s_a B_a h_t,
+ *   base the output of the frozen projection of x (rwkvq_linear_dispatch), NULL: 0.  `rows` (HOST) says which rows belong together: sequence b is rows
+ *   offsets[b] .. offsets[b+1] - 1 of n_tokens (DEVICE, n_seqs + 1 entries, not descending; NULL: n_tokens / n_seqs rows each), of any length, also
+ *   none; its adapter is adapters[b] (DEVICE, NULL: 0), and one outside 0 .. n_adapters - 1 means none: y_t = base_t, h_t = 0.  Rows of no sequence are
+ *   not touched.  scales: s, DEVICE [n_adapters] (NULL: 1).  Offsets are read on the device and limited to 0 .. n_tokens there.
+ *   seed not NULL: drop is rwkvq_dropout of x with p and seed, its call number seed[1] + i for matrix i, its row the row of the call; x is not rounded in
+ *   between.  mats (HOST, read before return): a [n_adapters][rank][K] and b [n_adapters][N][rank] of x_dtype (fp16 or bf16); x: rows of K, base and y:
+ *   rows of N values of y_dtype (fp16, bf16 or binary32), strides in elements (0 = K or N); h: DEVICE [n_tokens][rank] floats for the backward
+ *   pass, NULL: not stored.  y may be base, with its stride.  No other two may overlap; matrices of a call run side by side.
+ *   rank: a multiple of 8 up to 128; K, N: multiples of 8.  Products of 16-bit values are exact and sums binary32; h meets B in 16 bits (bf16) or 22
+ *   (fp16) where y has 16 bits, in 24 or more for binary32 y.  The same bits every time; a row's result does not depend on other sequences.
+ *   An infinity or NaN of a row reaches what its formula makes of it, at times as NaN for an infinity, and no other row.
+ * rwkvq_adapters_backward: the gradients for dy (rows of N values of x_dtype):
+ *     g_t = s_a B_a^T dy_t,  dx_t = base_t + drop(A_a^T g_t),  da_a = sum of g_t drop(x_t)^T,  db_a = sum of s_a dy_t h_t^T,
+ *   base: a gradient of x from elsewhere (the frozen projection), NULL: 0; dx may be base, with its stride; dx NULL: not computed.  base, dx: rows of K values
+ *   of x_dtype.  h as rwkvq_adapters stored it; rows and seed as there.  da, db: DEVICE floats like a and b, overwritten, 0 for adapters of no row.
+ *   g and h enter da and db with 24 bits.  workspace: DEVICE, rwkvq_adapters_backward_workspace_size(..) bytes (of the same rows and
+ *   matrices, whose pointers are not looked at), contents irrelevant on entry and undefined on exit.
+ * a, b, x, base, y, h, dy, dx, da, db, workspace 16-byte aligned; seed 8; offsets, adapters, scales 4; no call synchronises.
+ * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, rank, p outside [0, 1]), RWKVQ_ERR_SHAPE (a count below 1, n_mats > 64, n_tokens not a multiple of n_seqs
+ *   without offsets, K or N above 2^24, a stride below its width or n_tokens * stride > 2^40, x or dy the same as y or dx, in place with another stride, more than
+ *   65535 adapters, more threads than the 2^32 of one launch: 512 for every 16 or 32 rows and every sequence, times matrices), RWKVQ_ERR_ALIGN
+ *   (pointers; K, N or strides not a multiple of 8), RWKVQ_ERR_DEVICE. */
+typedef struct rwkvq_adapter_rows {
+    int32_t n_seqs, n_tokens;
+    int32_t n_adapters, rank;
+    const int32_t* offsets;
+    const int32_t* adapters;
+    const float* scales;
+    const uint64_t* seed;
+    double p;
+} rwkvq_adapter_rows;
+typedef struct rwkvq_adapter {
+    const void *a, *b;
+    const void* x;
+    const void* base;
+    void* y;
+    float* h;
+    int32_t N, K;
+    int64_t x_stride, base_stride, y_stride;
+} rwkvq_adapter;
+typedef struct rwkvq_adapter_grad {
+    const void *a, *b;
+    const void* x;
+    const float* h;
+    const void* dy;
+    const void* base;
+    void* dx;
+    float *da, *db;
+    int32_t N, K;
+    int64_t x_stride, dy_stride, base_stride, dx_stride;
+} rwkvq_adapter_grad;
+int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, int n_mats, int x_dtype, int y_dtype, void* stream);
+size_t rwkvq_adapters_backward_workspace_size(const rwkvq_adapter_rows* rows, const rwkvq_adapter_grad* mats, int n_mats);
+int rwkvq_adapters_backward(const rwkvq_adapter_rows* rows, const rwkvq_adapter_grad* mats, int n_mats, int x_dtype, void* workspace,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

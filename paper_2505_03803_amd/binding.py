@@ -25,7 +25,9 @@ EXPORTS = ["rwkvq_version", "rwkvq_status_string", "rwkvq_sq_prepack", "rwkvq_vq
            "rwkvq_wkv", "rwkvq_relu2", "rwkvq_sigmoid_gate", "rwkvq_linear_dispatch_post", "rwkvq_linear_dispatch_plan", "rwkvq_rkv_wkv", "rwkvq_proxy_static",
            "rwkvq_set_option", "rwkvq_get_option", "rwkvq_proxy_workspace_size", "rwkvq_layer_norm",
            "rwkvq_layer_norm_backward_workspace_size", "rwkvq_layer_norm_backward", "rwkvq_linear_attention_workspace_size",
-           "rwkvq_linear_attention", "rwkvq_linear_attention_backward_workspace_size", "rwkvq_linear_attention_backward"]
+           "rwkvq_linear_attention", "rwkvq_linear_attention_backward_workspace_size", "rwkvq_linear_attention_backward",
+           "rwkvq_dropout", "rwkvq_embedding", "rwkvq_embedding_backward_workspace_size", "rwkvq_embedding_backward", "rwkvq_adapters",
+           "rwkvq_adapters_backward_workspace_size", "rwkvq_adapters_backward"]
 
 
 class rwkvq_mix_input(Structure):
@@ -55,6 +57,22 @@ class rwkvq_heads(Structure):
     _fields_ = [("n_seqs", c_int32), ("n_tokens", c_int32), ("n_heads", c_int32), ("head_dim", c_int32),
                 ("n_slots", c_int32), ("reserved", c_int32), ("offsets", c_void_p), ("slots", c_void_p),
                 ("r_stride", c_int64), ("k_stride", c_int64), ("v_stride", c_int64), ("out_stride", c_int64)]
+
+
+class rwkvq_adapter_rows(Structure):
+    _fields_ = [("n_seqs", c_int32), ("n_tokens", c_int32), ("n_adapters", c_int32), ("rank", c_int32), ("offsets", c_void_p),
+                ("adapters", c_void_p), ("scales", c_void_p), ("seed", c_void_p), ("p", c_double)]
+
+
+class rwkvq_adapter(Structure):
+    _fields_ = [("a", c_void_p), ("b", c_void_p), ("x", c_void_p), ("base", c_void_p), ("y", c_void_p), ("h", c_void_p), ("N", c_int32),
+                ("K", c_int32), ("x_stride", c_int64), ("base_stride", c_int64), ("y_stride", c_int64)]
+
+
+class rwkvq_adapter_grad(Structure):
+    _fields_ = [("a", c_void_p), ("b", c_void_p), ("x", c_void_p), ("h", c_void_p), ("dy", c_void_p), ("base", c_void_p), ("dx", c_void_p),
+                ("da", c_void_p), ("db", c_void_p), ("N", c_int32), ("K", c_int32), ("x_stride", c_int64), ("dy_stride", c_int64),
+                ("base_stride", c_int64), ("dx_stride", c_int64)]
 
 
 class RwkvqError(RuntimeError):
@@ -162,6 +180,22 @@ def lib() -> ctypes.CDLL:
         L.rwkvq_linear_attention_backward_workspace_size.argtypes = [c_void_p]
         L.rwkvq_linear_attention_backward.restype = c_int
         L.rwkvq_linear_attention_backward.argtypes = [c_void_p] * 5 + [c_int] + [c_void_p] * 12
+        L.rwkvq_dropout.restype = c_int
+        L.rwkvq_dropout.argtypes = [c_void_p, c_int, c_int, c_int, c_longlong, c_void_p, c_double, c_void_p, c_longlong, c_void_p, c_longlong,
+                                    c_void_p]
+        L.rwkvq_embedding.restype = c_int
+        L.rwkvq_embedding.argtypes = [c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_double, c_void_p, c_int, c_longlong, c_void_p]
+        L.rwkvq_embedding_backward_workspace_size.restype = c_size_t
+        L.rwkvq_embedding_backward_workspace_size.argtypes = [c_int, c_int]
+        L.rwkvq_embedding_backward.restype = c_int
+        L.rwkvq_embedding_backward.argtypes = [c_void_p, c_int, c_void_p, c_int, c_longlong, c_int, c_int, c_double, c_void_p, c_int, c_void_p,
+                                               c_void_p]
+        L.rwkvq_adapters.restype = c_int
+        L.rwkvq_adapters.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p]
+        L.rwkvq_adapters_backward_workspace_size.restype = c_size_t
+        L.rwkvq_adapters_backward_workspace_size.argtypes = [c_void_p, c_void_p, c_int]
+        L.rwkvq_adapters_backward.restype = c_int
+        L.rwkvq_adapters_backward.argtypes = [c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p]
         _lib = L
     return _lib
 
@@ -640,4 +674,89 @@ def rwkvq_linear_attention_backward(heads: Heads, r, k, v, dout, x_dtype, w, u, 
     st = lib().rwkvq_linear_attention_backward(heads.ref, _ptr(r), _ptr(k), _ptr(v), _ptr(dout), x_dtype, _ptr(w), _ptr(u),
                                                _ptr(state), _ptr(dstate), _ptr(dr), _ptr(dk), _ptr(dv), _ptr(dw), _ptr(du),
                                                _ptr(dstate_in), _ptr(workspace), _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_dropout(x, x_dtype, M, n, seed, p, y, base=None, x_stride=0, base_stride=0, y_stride=0, stream=None, check=True):
+    """seed: two int64 on the GPU, the key and the number of the call."""
+    st = lib().rwkvq_dropout(_ptr(x), x_dtype, M, n, x_stride, _ptr(seed), p, _ptr(base), base_stride, _ptr(y), y_stride, _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_embedding(tokens, n_tokens, table, table_dtype, vocab, d, scale, out, out_dtype, out_stride=0, stream=None, check=True):
+    """tokens: int32 on the GPU."""
+    st = lib().rwkvq_embedding(_ptr(tokens), n_tokens, _ptr(table), table_dtype, vocab, d, scale, _ptr(out), out_dtype, out_stride, _stream(stream))
+    return _check(st) if check else st
+
+
+def rwkvq_embedding_backward_workspace_size(n_tokens: int, d: int) -> int:
+    return int(lib().rwkvq_embedding_backward_workspace_size(n_tokens, d))
+
+
+def rwkvq_embedding_backward(tokens, n_tokens, dout, dout_dtype, vocab, d, scale, dtable, accumulate, workspace, dout_stride=0, stream=None,
+                             check=True):
+    st = lib().rwkvq_embedding_backward(_ptr(tokens), n_tokens, _ptr(dout), dout_dtype, dout_stride, vocab, d, scale, _ptr(dtable),
+                                        int(accumulate), _ptr(workspace), _stream(stream))
+    return _check(st) if check else st
+
+
+class AdapterRows:
+    """The host struct of the adapter calls: which rows are a sequence, its adapter, the adapters' rank and scales, dropout in front of them;
+    reusable across calls.  offsets, adapters: int32, scales: float32, seed: two int64 on the GPU, or None."""
+
+    def __init__(self, n_seqs: int, n_tokens: int, n_adapters: int, rank: int, offsets=None, adapters=None, scales=None, seed=None,
+                 p: float = 0.0):
+        self.desc = rwkvq_adapter_rows(n_seqs, n_tokens, n_adapters, rank, _ptr(offsets), _ptr(adapters), _ptr(scales), _ptr(seed), p)
+        self.ref = ctypes.addressof(self.desc)
+        self.keep = (offsets, adapters, scales, seed)
+
+
+def _each(items, n):
+    return [None] * n if items is None else [items] * n if isinstance(items, int) else items
+
+
+class AdapterTable:
+    """Host array for rwkvq_adapters, from tensors a [adapters][rank][K], b [adapters][N][rank] and the rows of each matrix.  bases, hs: None, or one
+    for each (None among them as well).  Strides in elements, 0 = densely packed: one number for all matrices, or one for each.  Reusable across calls."""
+
+    def __init__(self, as_: Sequence, bs: Sequence, xs: Sequence, ys: Sequence, bases: Optional[Sequence] = None, hs: Optional[Sequence] = None,
+                 x_strides=0, base_strides=0, y_strides=0):
+        self.n = n = len(as_)
+        assert len(bs) == n and len(xs) == n and len(ys) == n
+        self.mats = (rwkvq_adapter * n)(*[
+            rwkvq_adapter(_ptr(a), _ptr(b), _ptr(x), _ptr(base), _ptr(y), _ptr(h), b.shape[1], a.shape[2], *strides)
+            for a, b, x, y, base, h, *strides in zip(as_, bs, xs, ys, _each(bases, n), _each(hs, n), _each(x_strides, n), _each(base_strides, n),
+                                                     _each(y_strides, n))])
+        self.ref = ctypes.addressof(self.mats)
+        self.keep = (as_, bs, xs, ys, bases, hs)
+
+
+def rwkvq_adapters(rows: AdapterRows, table: AdapterTable, x_dtype, y_dtype, stream=None, check=True):
+    st = lib().rwkvq_adapters(rows.ref, table.ref, table.n, x_dtype, y_dtype, _stream(stream))
+    return _check(st) if check else st
+
+
+class AdapterGradTable:
+    """Host array for rwkvq_adapters_backward: as AdapterTable, with h, dy, dx (None: not computed), da and db of each matrix."""
+
+    def __init__(self, as_: Sequence, bs: Sequence, xs: Sequence, hs: Sequence, dys: Sequence, dxs: Optional[Sequence], das: Sequence,
+                 dbs: Sequence, bases: Optional[Sequence] = None, x_strides=0, dy_strides=0, base_strides=0, dx_strides=0):
+        self.n = n = len(as_)
+        assert len(bs) == n and len(xs) == n and len(hs) == n and len(dys) == n and len(das) == n and len(dbs) == n
+        self.mats = (rwkvq_adapter_grad * n)(*[
+            rwkvq_adapter_grad(_ptr(a), _ptr(b), _ptr(x), _ptr(h), _ptr(dy), _ptr(base), _ptr(dx), _ptr(da), _ptr(db), b.shape[1], a.shape[2],
+                               *strides)
+            for a, b, x, h, dy, base, dx, da, db, *strides in zip(as_, bs, xs, hs, dys, _each(bases, n), _each(dxs, n), das, dbs,
+                                                                  _each(x_strides, n), _each(dy_strides, n), _each(base_strides, n),
+                                                                  _each(dx_strides, n))])
+        self.ref = ctypes.addressof(self.mats)
+        self.keep = (as_, bs, xs, hs, dys, dxs, das, dbs, bases)
+
+
+def rwkvq_adapters_backward_workspace_size(rows: AdapterRows, table: AdapterGradTable) -> int:
+    return int(lib().rwkvq_adapters_backward_workspace_size(rows.ref, table.ref, table.n))
+
+
+def rwkvq_adapters_backward(rows: AdapterRows, table: AdapterGradTable, x_dtype, workspace, stream=None, check=True):
+    st = lib().rwkvq_adapters_backward(rows.ref, table.ref, table.n, x_dtype, _ptr(workspace), _stream(stream))
     return _check(st) if check else st

@@ -688,4 +688,168 @@ int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, con
                                                                                                                 : RWKVQ_ERR_DEVICE;
 }
 
+// A stride, 0 becoming the width, or -1 if rows of it are not `width` values apart at least, within 2^40 in all.
+static long long row_stride(long long stride, long long width, long long rows) {
+    if (stride == 0) stride = width;
+    return stride < width || stride > (1ll << 40) / rows ? -1 : stride;
+}
+
+static int check_dropout(const uint64_t* seed, double p, Dropout* drop) {
+    if (!(p >= 0.0 && p <= 1.0)) return RWKVQ_ERR_UNSUPPORTED;
+    if ((uintptr_t)seed & 7u) return RWKVQ_ERR_ALIGN;
+    const uint32_t limit = seed ? (uint32_t)(p * 65536.0 + 0.5) : 0;
+    *drop = Dropout{limit ? seed : nullptr, limit, limit < 65536 ? (float)(65536.0 / (65536.0 - limit)) : 0.0f, 0};
+    return RWKVQ_OK;
+}
+
+int rwkvq_dropout(const void* x, int x_dtype, int M, int n, long long x_stride, const uint64_t* seed, double p, const void* base,
+                  long long base_stride, void* y, long long y_stride, void* stream) {
+    if (!x || !seed || !y) return RWKVQ_ERR_NULL;
+    if (dense_dtype(x_dtype) < 0) return RWKVQ_ERR_UNSUPPORTED;
+    if (M < 1 || n < 1 || n > (1 << 24)) return RWKVQ_ERR_SHAPE;
+    DropoutDev d{};
+    d.x = x; d.base = base; d.y = y; d.M = M; d.n = n;
+    d.x_stride = row_stride(x_stride, n, M); d.base_stride = row_stride(base_stride, n, M); d.y_stride = row_stride(y_stride, n, M);
+    if (d.x_stride < 0 || d.base_stride < 0 || d.y_stride < 0) return RWKVQ_ERR_SHAPE;
+    if (M > 1 && ((x == y && d.x_stride != d.y_stride) || (base == y && d.base_stride != d.y_stride))) return RWKVQ_ERR_SHAPE;
+    const int st = check_dropout(seed, p, &d.drop);
+    if (st != RWKVQ_OK) return st;
+    d.drop.seed = seed;
+    if (!aligned16(x) || !aligned16(base) || !aligned16(y)) return RWKVQ_ERR_ALIGN;
+    return launch_dropout(d, dense_dtype(x_dtype), (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+static int check_embedding(int n_tokens, int vocab, int d, double scale, const int32_t* tokens) {
+    if (!((float)scale - (float)scale == 0.0f)) return RWKVQ_ERR_UNSUPPORTED;
+    if (n_tokens < 1 || vocab < 1 || d < 1 || d > (1 << 24) || (long long)vocab * d > (1ll << 40)) return RWKVQ_ERR_SHAPE;
+    return aligned4(tokens) ? RWKVQ_OK : RWKVQ_ERR_ALIGN;
+}
+
+int rwkvq_embedding(const int32_t* tokens, int n_tokens, const void* table, int table_dtype, int vocab, int d, double scale, void* out,
+                    int out_dtype, long long out_stride, void* stream) {
+    if (!tokens || !table || !out) return RWKVQ_ERR_NULL;
+    if (dense_dtype(table_dtype) < 0 || dense_dtype(out_dtype) < 0) return RWKVQ_ERR_UNSUPPORTED;
+    const int st = check_embedding(n_tokens, vocab, d, scale, tokens);
+    if (st != RWKVQ_OK) return st;
+    EmbeddingDev p{};
+    p.tokens = tokens; p.table = table; p.out = out; p.n_tokens = n_tokens; p.vocab = vocab; p.d = d; p.scale = (float)scale;
+    p.out_stride = row_stride(out_stride, d, n_tokens);
+    if (p.out_stride < 0) return RWKVQ_ERR_SHAPE;
+    if (!aligned16(table) || !aligned16(out)) return RWKVQ_ERR_ALIGN;
+    return launch_embedding(p, dense_dtype(table_dtype), dense_dtype(out_dtype), (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+constexpr int kMaxSorted = 1 << 22;                // tokens of a gradient
+
+size_t rwkvq_embedding_backward_workspace_size(int n_tokens, int d) {
+    return n_tokens < 1 || n_tokens > kMaxSorted || d < 1 || d > (1 << 24) ? 0 : embedding_backward_workspace_bytes(n_tokens, d);
+}
+
+int rwkvq_embedding_backward(const int32_t* tokens, int n_tokens, const void* dout, int dout_dtype, long long dout_stride, int vocab, int d,
+                             double scale, float* dtable, int accumulate, void* workspace, void* stream) {
+    if (!tokens || !dout || !dtable || !workspace) return RWKVQ_ERR_NULL;
+    if (dense_dtype(dout_dtype) < 0) return RWKVQ_ERR_UNSUPPORTED;
+    const int st = check_embedding(n_tokens, vocab, d, scale, tokens);
+    if (st != RWKVQ_OK) return st;
+    EmbeddingDev p{};
+    p.tokens = tokens; p.out = (void*)dout; p.dtable = dtable; p.n_tokens = n_tokens; p.vocab = vocab; p.d = d; p.scale = (float)scale;
+    p.accumulate = accumulate != 0;
+    p.out_stride = row_stride(dout_stride, d, n_tokens);
+    if (p.out_stride < 0 || n_tokens > kMaxSorted || !embedding_backward_fits(n_tokens, vocab, d)) return RWKVQ_ERR_SHAPE;
+    if (!aligned16(dout) || !aligned16(dtable) || !aligned16(workspace)) return RWKVQ_ERR_ALIGN;
+    return launch_embedding_backward(p, dense_dtype(dout_dtype), workspace, (hipStream_t)stream) == hipSuccess ? RWKVQ_OK : RWKVQ_ERR_DEVICE;
+}
+
+constexpr int kMaxAdapterMats = 64;                // of a call: their descriptions are on the stack
+
+// The host structs of the adapter calls, checked and translated.
+static int check_adapter_rows(const rwkvq_adapter_rows* in, AdapterRowsDev* r) {
+    if (!in) return RWKVQ_ERR_NULL;
+    if (in->n_seqs < 1 || in->n_tokens < 1 || in->n_adapters < 1 || in->n_adapters > 65535 || in->rank < 1) return RWKVQ_ERR_SHAPE;
+    if (in->rank % 8 != 0 || in->rank > 128) return RWKVQ_ERR_UNSUPPORTED;
+    if (!in->offsets && in->n_tokens % in->n_seqs != 0) return RWKVQ_ERR_SHAPE;
+    *r = AdapterRowsDev{in->n_seqs, in->n_tokens, in->n_adapters, in->rank, in->offsets, in->adapters, in->scales, {}};
+    const int st = check_dropout(in->seed, in->p, &r->drop);
+    if (st != RWKVQ_OK) return st;
+    return aligned4(in->offsets) && aligned4(in->adapters) && aligned4(in->scales) ? RWKVQ_OK : RWKVQ_ERR_ALIGN;
+}
+static int check_adapter_sizes(const AdapterRowsDev& r, int N, int K) {
+    if (N < 1 || K < 1 || N > (1 << 24) || K > (1 << 24)) return RWKVQ_ERR_SHAPE;
+    if (N % 8 != 0 || K % 8 != 0) return RWKVQ_ERR_ALIGN;
+    return adapters_fit(r, std::max(N, K)) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
+}
+
+int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, int n_mats, int x_dtype, int y_dtype, void* stream) {
+    if (!rows || !mats) return RWKVQ_ERR_NULL;
+    int st;
+    if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK || (st = check_dtype_y(y_dtype)) != RWKVQ_OK) return st;
+    if (n_mats < 1 || n_mats > kMaxAdapterMats) return RWKVQ_ERR_SHAPE;
+    AdapterRowsDev r;
+    if ((st = check_adapter_rows(rows, &r)) != RWKVQ_OK) return st;
+    AdapterMatDev dev[kMaxAdapterMats];
+    for (int i = 0; i < n_mats; ++i) {
+        const rwkvq_adapter& m = mats[i];
+        if (!m.a || !m.b || !m.x || !m.y) return RWKVQ_ERR_NULL;
+        if ((st = check_adapter_sizes(r, m.N, m.K)) != RWKVQ_OK) return st;
+        AdapterMatDev& d = dev[i];
+        d = AdapterMatDev{(const uint16_t*)m.x, (const uint16_t*)m.a, (const uint16_t*)m.b, m.base, m.y, m.h, row_stride(m.x_stride, m.K, r.n_tokens),
+                          row_stride(m.base_stride, m.N, r.n_tokens), row_stride(m.y_stride, m.N, r.n_tokens), m.K, m.N};
+        if (d.x_stride < 0 || d.base_stride < 0 || d.y_stride < 0 || m.x == m.y) return RWKVQ_ERR_SHAPE;
+        if (m.base == m.y && r.n_tokens > 1 && d.base_stride != d.y_stride) return RWKVQ_ERR_SHAPE;
+        if (d.x_stride % 8 != 0 || d.base_stride % 8 != 0 || d.y_stride % 8 != 0) return RWKVQ_ERR_ALIGN;
+        if (!aligned16(m.a) || !aligned16(m.b) || !aligned16(m.x) || !aligned16(m.base) || !aligned16(m.y) || !aligned16(m.h)) return RWKVQ_ERR_ALIGN;
+    }
+    return finish(launch_adapters(r, dev, n_mats, dense_dtype(x_dtype), dense_dtype(y_dtype), (hipStream_t)stream));
+}
+
+// Everything of a backward call but its pointers: the products as rwkvq_adapters' with dy for x, dx for y and the matrices exchanged.
+static int check_adapter_grads(const AdapterRowsDev& r, const rwkvq_adapter_grad* mats, int n_mats, AdapterMatDev* dev, AdapterGradDev* grads) {
+    for (int i = 0; i < n_mats; ++i) {
+        const rwkvq_adapter_grad& m = mats[i];
+        const int st = check_adapter_sizes(r, m.N, m.K);
+        if (st != RWKVQ_OK) return st;
+        AdapterMatDev& d = dev[i];
+        d = AdapterMatDev{(const uint16_t*)m.dy, (const uint16_t*)m.b, (const uint16_t*)m.a, m.base, m.dx, nullptr, row_stride(m.dy_stride, m.N, r.n_tokens),
+                          row_stride(m.base_stride, m.K, r.n_tokens), row_stride(m.dx_stride, m.K, r.n_tokens), m.N, m.K};
+        grads[i] = AdapterGradDev{(const uint16_t*)m.x, m.h, m.da, m.db, row_stride(m.x_stride, m.K, r.n_tokens)};
+        if (d.x_stride < 0 || d.base_stride < 0 || d.y_stride < 0 || grads[i].x_stride < 0) return RWKVQ_ERR_SHAPE;
+        if (d.x_stride % 8 != 0 || d.base_stride % 8 != 0 || d.y_stride % 8 != 0 || grads[i].x_stride % 8 != 0) return RWKVQ_ERR_ALIGN;
+    }
+    return adapters_backward_fit(r, dev, n_mats) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
+}
+
+size_t rwkvq_adapters_backward_workspace_size(const rwkvq_adapter_rows* rows, const rwkvq_adapter_grad* mats, int n_mats) {
+    AdapterRowsDev r;
+    if (!mats || n_mats < 1 || n_mats > kMaxAdapterMats || check_adapter_rows(rows, &r) != RWKVQ_OK) return 0;
+    AdapterMatDev dev[kMaxAdapterMats];
+    AdapterGradDev grads[kMaxAdapterMats];
+    return check_adapter_grads(r, mats, n_mats, dev, grads) == RWKVQ_OK ? adapters_backward_workspace_bytes(r, dev, n_mats) : 0;
+}
+
+int rwkvq_adapters_backward(const rwkvq_adapter_rows* rows, const rwkvq_adapter_grad* mats, int n_mats, int x_dtype, void* workspace,
+                            void* stream) {
+    if (!rows || !mats || !workspace) return RWKVQ_ERR_NULL;
+    int st;
+    if ((st = check_dtype_x(x_dtype)) != RWKVQ_OK) return st;
+    if (n_mats < 1 || n_mats > kMaxAdapterMats) return RWKVQ_ERR_SHAPE;
+    for (int i = 0; i < n_mats; ++i) {
+        const rwkvq_adapter_grad& m = mats[i];
+        if (!m.a || !m.b || !m.x || !m.h || !m.dy || !m.da || !m.db) return RWKVQ_ERR_NULL;
+    }
+    AdapterRowsDev r;
+    if ((st = check_adapter_rows(rows, &r)) != RWKVQ_OK) return st;
+    AdapterMatDev dev[kMaxAdapterMats];
+    AdapterGradDev grads[kMaxAdapterMats];
+    if ((st = check_adapter_grads(r, mats, n_mats, dev, grads)) != RWKVQ_OK) return st;
+    for (int i = 0; i < n_mats; ++i) {
+        const rwkvq_adapter_grad& m = mats[i];
+        if (m.dx && (m.dx == m.dy || m.dx == m.x)) return RWKVQ_ERR_SHAPE;
+        if (m.dx && m.base == m.dx && r.n_tokens > 1 && dev[i].base_stride != dev[i].y_stride) return RWKVQ_ERR_SHAPE;
+        for (const void* p : {m.a, m.b, m.x, (const void*)m.h, m.dy, m.base, (const void*)m.dx, (const void*)m.da, (const void*)m.db})
+            if (!aligned16(p)) return RWKVQ_ERR_ALIGN;
+    }
+    if (!aligned16(workspace)) return RWKVQ_ERR_ALIGN;
+    return finish(launch_adapters_backward(r, dev, grads, n_mats, dense_dtype(x_dtype), workspace, (hipStream_t)stream));
+}
+
 }  // extern "C"

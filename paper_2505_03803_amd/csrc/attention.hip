@@ -6,8 +6,6 @@
 
 namespace rwkvq {
 
-template <bool BF16>
-__device__ __forceinline__ float widen16(uint16_t v) { return BF16 ? bf16_bits_to_f32(v) : f16_bits_to_f32(v); }
 // Rows of sequence b, within 0 .. n_tokens whatever the offsets hold.
 __device__ __forceinline__ void rows_of(const HeadsDev& h, int b, int& t0, int& t1) {
     if (h.offsets) {
@@ -122,7 +120,6 @@ __global__ void __launch_bounds__(256) attend_step_kernel(HeadsDev h) {
 // Precision: 16-bit inputs go in as they are, fp16 ones that meet a computed operand as two bf16 parts (exact); weighted scores and
 // states as two bf16 parts (17 bits: half an ulp of a bf16 or fp16 output is 2^-9 or 2^-12 of it), of which fp16's products of both low parts are left
 // out (2^-18); the weighted keys of a state's update as three (24 bits), since states are binary32 results, and so states behind the gradient of w.
-typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 constexpr int kChunk = 64;                    // tokens
 constexpr int kVals = 64;                     // channels of val of a workgroup
@@ -194,43 +191,6 @@ template <int DP, bool BF16, int GRAD, bool PAIR = false, bool SWAPS = false> st
     static constexpr int marks = sums + (GRAD || PAIR ? 12 * 8 + 4 * 4 * kVals : 0), bytes = marks + Marks::bytes;
     static_assert(bytes <= 160 * 1024, "a unit's LDS");
 };
-
-// Two values as packed bf16 and what is left of them.
-__device__ __forceinline__ uint32_t split2(float& a, float& b) {
-    uint32_t h = Elem<true>::pack(a, b);
-    asm("" : "+v"(h));                            // the compiler would convert a once more for its own half
-    a -= __uint_as_float(h << 16);
-    b -= __uint_as_float(h & 0xFFFF0000u);
-    return h;
-}
-// Four values as two or three bf16 parts, 17 or 24 bits.
-template <int PARTS>
-__device__ __forceinline__ void split4(const float4_t& x, uint2_t (&out)[PARTS]) {
-    float v[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-    for (int i = 0; i < PARTS - 1; ++i) out[i] = uint2_t{split2(v[0], v[1]), split2(v[2], v[3])};
-    out[PARTS - 1] = uint2_t{Elem<true>::pack(v[0], v[1]), Elem<true>::pack(v[2], v[3])};
-}
-// Eight fp16 values as two bf16 parts, exact.
-__device__ __forceinline__ void split_f16(const uint4_t& x, uint4_t& hi, uint4_t& lo) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint2_t p = vq_split(x[i]);
-        hi[i] = p.x; lo[i] = p.y;
-    }
-}
-__device__ __forceinline__ uint2_t lds_transposed(const char* at) {
-    typedef __attribute__((address_space(3))) short4_t* Ptr;
-    return __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)at));
-}
-// The operand whose lane (n, g) holds column 16 c + n of rows 4 g .. + 3 and 16 + 4 g .. + 3 of a tile's rows 32 ks ..: the order of
-// tokens in which scores lie in their registers.
-template <int ROW>
-__device__ __forceinline__ uint4_t column_frag(const char* tile, int ks, int c, int n, int g) {
-    const char* const at = tile + (32 * ks + 4 * g + (n >> 2)) * ROW + 32 * c + 8 * (n & 3);
-    const uint2_t a = lds_transposed(at), b = lds_transposed(at + 16 * ROW);
-    return uint4_t{a.x, a.y, b.x, b.y};
-}
 
 // acc += weight * a state in memory; element (x, vt)[j] is key 16 (KT wave + x) + 4 g + j, val v0 + 16 vt + n.  All loads before the first use.
 template <int KT>

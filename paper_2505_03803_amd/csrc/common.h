@@ -248,6 +248,67 @@ hipError_t launch_attention(const HeadsDev& h, int dt, hipStream_t s);
 size_t attention_backward_workspace_bytes(const HeadsDev& h);
 hipError_t launch_attention_backward(const HeadsDev& h, int dt, hipStream_t s);
 
+// Dropout, embedding and low-rank adapters (dropout.hip, embedding.hip, adapters.hip).
+// Which elements stay: seed[0] is the key, seed[1] + call the number of the call, both on the device; a number of 16 bits below `limit` drops.
+struct Dropout {
+    const uint64_t* seed;                          // NULL: nothing is dropped
+    uint32_t limit;
+    float factor;                                  // 1 / (1 - limit / 65536)
+    uint32_t call;
+};
+struct DropoutDev {
+    const void *x, *base;
+    void* y;
+    long long x_stride, base_stride, y_stride;
+    int M, n;
+    bool whole;                                    // rows begin at multiples of 16 bytes
+    Dropout drop;
+};
+hipError_t launch_dropout(DropoutDev p, int dt, hipStream_t s);
+struct EmbeddingDev {
+    const int32_t* tokens;
+    const void* table;
+    void* out;                                     // backward: their gradient, only read
+    float *dtable, *partial;
+    uint32_t *keys, *tile_keys;
+    int *order, *tile_order;
+    long long out_stride;
+    int n_tokens, vocab, d;
+    float scale;
+    bool accumulate, table_whole, rows_whole;      // whole: rows begin at multiples of 16 bytes
+};
+hipError_t launch_embedding(EmbeddingDev p, int tdt, int odt, hipStream_t s);
+bool embedding_backward_fits(int n_tokens, int vocab, int d);
+size_t embedding_backward_workspace_bytes(int n_tokens, int d);
+hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hipStream_t s);
+struct AdapterRowsDev {
+    int n_seqs, n_tokens, n_adapters, rank;
+    const int32_t *offsets, *adapters;
+    const float* scales;
+    Dropout drop;
+};
+struct AdapterMatDev {                             // y = base + q (p x^T): p [adapters][rank][depth], q [adapters][wide][rank]
+    const uint16_t *x, *p, *q;
+    const void* base;
+    void* y;
+    float* h;
+    long long x_stride, base_stride, y_stride;
+    int depth, wide;
+};
+struct AdapterGradDev {
+    const uint16_t* x;
+    const float* h;
+    float *da, *db;
+    long long x_stride;
+};
+constexpr int kAdapterMats = 8;                    // matrices of a launch
+bool adapters_fit(const AdapterRowsDev& r, int widest);
+hipError_t launch_adapters(const AdapterRowsDev& rows, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s);
+bool adapters_backward_fit(const AdapterRowsDev& r, const AdapterMatDev* mats, int n_mats);
+size_t adapters_backward_workspace_bytes(const AdapterRowsDev& r, const AdapterMatDev* mats, int n_mats);
+hipError_t launch_adapters_backward(const AdapterRowsDev& rows, const AdapterMatDev* mats, const AdapterGradDev* grads, int n_mats, int dt,
+                                    void* workspace, hipStream_t s);
+
 // Lets a kernel take `bytes` of dynamic LDS (beyond 64 KB the runtime wants to be told), once per device; bit d of `raised`,
 // a static of the caller's, says that it was done on device d.
 inline hipError_t raise_lds(const void* kernel, int bytes, std::atomic<unsigned long long>& raised) {
