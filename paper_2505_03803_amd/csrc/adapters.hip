@@ -8,12 +8,14 @@
 
 namespace rwkvq {
 
-struct AdapterCall {
+// Arguments of a launch lie in host memory or behind a cold cache: what a workgroup needs is in four lines of 64 bytes, read together.
+struct alignas(128) AdapterLine { AdapterMatDev m; };
+struct alignas(128) AdapterCall {
     AdapterRowsDev rows;
-    AdapterMatDev mats[kAdapterMats];
-    int y_dt, slice, slices;                       // columns of a workgroup, workgroups of a tile
+    int y_dt, slice;                               // columns of a workgroup
     uint32_t first;                                // number of the first matrix
     bool backward;                                 // x = dy, y = dx, h = g, p = b turned, q = a turned
+    AdapterLine mats[kAdapterMats];
 };
 struct OuterMatDev {
     const uint16_t *x, *dy;
@@ -88,16 +90,6 @@ static long long pieces(const AdapterRowsDev& r, int cut) {
     return (long long)((r.n_tokens / r.n_seqs + cut - 1) / cut) * r.n_seqs;
 }
 
-__device__ __forceinline__ void load8_of(float (&f)[8], const void* p, long long i, int dt) {
-    if (dt == DT_F16) load8<DT_F16>(f, p, i, 8, true);
-    else if (dt == DT_BF16) load8<DT_BF16>(f, p, i, 8, true);
-    else load8<DT_F32>(f, p, i, 8, true);
-}
-__device__ __forceinline__ void store8_of(void* p, long long i, const float (&f)[8], int dt) {
-    if (dt == DT_F16) store8<DT_F16>(p, i, f, 8, true);
-    else if (dt == DT_BF16) store8<DT_BF16>(p, i, f, 8, true);
-    else store8<DT_F32>(p, i, f, 8, true);
-}
 // Eight 16-bit values of which only those with their bit in `keep` stay.
 __device__ __forceinline__ uint4_t kept(uint4_t v, uint32_t keep) {
 #pragma unroll
@@ -108,31 +100,141 @@ __device__ __forceinline__ uint4_t kept(uint4_t v, uint32_t keep) {
     return v;
 }
 
-// Both products of a tile of up to 16 MT rows of one sequence: first h = P x^T (P: rank rows of `depth` values), then y = base + Q h (Q: `wide` rows of
-// rank values).  The eight wavefronts share out the depth of the first, sums meet in LDS, and the columns of the second.  A workgroup takes
+// Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  The
+// workgroup of row b has work if an even sixteen of the rows in front of it have the same adapter, and then takes those of the next sixteen.
+constexpr int kGathered = 2048;                    // rows of such a call at most
+struct Gathered {
+    uint64_t same[kGathered / 64];
+    int rows[16];
+};
+__device__ __forceinline__ int gather_rows(const AdapterRowsDev& r, int b, int id, Gathered& at) {
+    const int lane = threadIdx.x & 63, masks = (r.n_seqs + 63) / 64;
+    for (int i = threadIdx.x >> 6; i < masks; i += blockDim.x >> 6) {
+        const int other = 64 * i + lane;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(other < r.n_seqs && adapter_of(r, min(other, r.n_seqs - 1)) == id);
+        if (lane == 0) at.same[i] = m;
+    }
+    __syncthreads();
+    int before = 0, all = 0, mine = -1;
+    for (int i = 0; i < masks; ++i) {
+        uint64_t m = at.same[i];
+        const int low = b - 64 * i, n = __builtin_popcountll(m), in_front = low >= 64 ? n : low <= 0 ? 0 : __builtin_popcountll(m & ((1ull << low) - 1));
+        before += in_front;
+        // the lane's row is the one with `lane` of the adapter between b and it
+        if (low < 64) {
+            if (low > 0) m &= ~((1ull << low) - 1);
+            const int left = lane - all, here = n - in_front;
+            if (left >= 0 && left < here) {
+                for (int j = 0; j < left; ++j) m &= m - 1;
+                mine = 64 * i + __builtin_ctzll(m);
+            }
+            all += here;
+        }
+    }
+    if (before % 16) return 0;
+    if (threadIdx.x < 16) at.rows[threadIdx.x] = mine;
+    __syncthreads();
+    return min(all, 16);
+}
+
+// Copies of 16 bytes a lane from memory to LDS by the load unit, to `to` + 16 lane.
+__device__ __forceinline__ void copy_to_lds(const void* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+template <int N>
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// A barrier for what went through LDS: copies and loads may stay on their way.
+__device__ __forceinline__ void meet() {
+    wait_lds();
+    RWKVQ_BARRIER();
+}
+// Tiles in LDS have rows of C pieces of 16 bytes; piece c of a row lies at place c ^ swizzle(row), so that the sixteen rows of an operand, whose
+// lanes read the same piece, are in different banks.
+template <int C>
+__device__ __forceinline__ int swizzle(int row) { return (row / (16 / C)) & (C - 1); }
+
+// Both products of a tile of up to 16 MT rows of one adapter: first h = P x^T (P: rank rows of `depth` values), then y = base + Q h (Q: `wide` rows of
+// rank values).  The wavefronts share out the depth of the first, sums meet in LDS, and the columns of the second.  A workgroup takes
 // `slice` columns of y and computes h for itself: where few tiles leave most of the device without work, h is cheaper taken several times than
 // passed on through memory and another launch.
-// h goes into the second product as PARTS parts of 16 bits (two: 16 bits of bf16, 22 of fp16, beside the rounding of a 16-bit y; three for binary32), fp16
+// What bounds it is what goes through a compute unit's cache: sixteen lanes that load 16 bytes of a row each, as the operands want them, get a third of what
+// whole lines give (9.5 against 30 TB/s out of L2).  So tiles of x, P and Q are copied to LDS by whole lines, and y leaves through LDS.
+// h goes into the second product as PARTS parts of 16 bits (two: 16 bits of bf16, 22 of fp16, beside the rounding of a 16-bit y; three for binary32 y), fp16
 // ones under a power of two for each row that brings its largest value to 2^14, so that none is lost below fp16's range.
-template <bool BF16, int RT, int MT, int PARTS>
-__global__ void __launch_bounds__(512) adapter_kernel(AdapterCall p) {
-    constexpr int R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
-    constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;      // bytes of a row of h's parts
-    __shared__ float sums[4][ROWS][PITCH];
-    __shared__ __align__(16) char parts[ROWS * HROW];
-    __shared__ float inverse[ROWS];
-    __shared__ int found;
-    const AdapterRowsDev& r = p.rows;
-    const AdapterMatDev& m = p.mats[blockIdx.y];
+// GATHER: single tokens (gather_rows).  DROP: there is dropout, of x or, backwards, of what is added to y.
+template <int RT, int MT, int PARTS> struct AdapterLds {
+    static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
+    static constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;                      // bytes of a row of h's parts
+    static constexpr int CG = RT <= 4 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
+    static constexpr int D = RT == 1 && MT == 1 ? 2 : 1;                                              // steps of 64 columns on their way
+    static constexpr int step = 128 * (ROWS + R), ring = W * D * step;
+    static constexpr int sums = W / 2 * ROWS * PITCH * 4, out = 16 * YPITCH * 4;                      // out: of a wavefront
+    static constexpr int q = sums > W * out ? sums : W * out, q_tile = CG * R * 2;                    // sums and out share a place
+    static constexpr int parts = q + W * q_tile, inverse = parts + ROWS * HROW, after = inverse + 4 * ROWS;
+    static constexpr int found = ring > after ? ring : after, gathered = found + 16, bytes = gathered + (int)sizeof(Gathered);
+};
+template <bool BF16, int RT, int MT, int PARTS, bool DROP, bool GATHER>
+__global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && PARTS == 3) ? 4 : 2)) adapter_kernel(AdapterCall p) {
+    typedef AdapterLds<RT, MT, PARTS> L;
+    constexpr int W = L::W, R = L::R, ROWS = L::ROWS, D = L::D, CG = L::CG, CT = CG / 16, QS = RT == 1 ? 1 : RT / 2, QC = R / 8;
+    constexpr bool WIDE = PARTS == 3;                                         // y is binary32
+    constexpr int PER = CG / 8, PASS = PER / 4;                               // lanes of a row of y, rounds for sixteen rows
+    extern __shared__ __align__(16) char lds[];
+    const AdapterRowsDev r = p.rows;
+    const AdapterMatDev m = p.mats[blockIdx.z].m;
+    asm volatile("" ::"s"(r.adapters), "s"(m.x), "s"(m.y_stride), "s"(m.wide), "s"(p.slice));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int slot = blockIdx.x / p.slices, part = blockIdx.x % p.slices;
-    const RowSpan s = piece_of(r, ROWS, slot, &found);
-    if (s.t0 >= s.t1) return;
-    const int count = s.t1 - s.t0, id = adapter_of(r, s.b);
+    Gathered& gathered = *(Gathered*)(lds + L::gathered);
+    int count, t0, id;
+    if constexpr (GATHER) {
+        t0 = blockIdx.x;
+        id = adapter_of(r, t0);
+        count = gather_rows(r, t0, id, gathered);
+    } else {
+        const RowSpan s = piece_of(r, ROWS, blockIdx.x, (int*)(lds + L::found));
+        t0 = s.t0; count = s.t1 - s.t0;
+        id = count > 0 ? adapter_of(r, s.b) : -1;
+    }
+    if (count <= 0) return;
+    auto row_at = [&](int i) -> long long { return GATHER ? gathered.rows[min(i, count - 1)] : t0 + min(i, count - 1); };
     const float scale = id >= 0 && r.scales ? r.scales[id] : 1.0f;
     const float before = p.backward ? scale : r.drop.factor, behind = p.backward ? r.drop.factor : scale;
     Dropout drop = r.drop;
-    drop.call += blockIdx.y + p.first;
+    drop.call += blockIdx.z + p.first;
+
+    // y: a wavefront takes CG columns at a time; lane l has 8 of them, PER lanes a row
+    const int from = blockIdx.y * p.slice, to = min(from + p.slice, m.wide), out_col = 8 * (lane % PER), out_at = lane / PER;
+    long long out_row[MT][PASS];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < PASS; ++j) out_row[i][j] = row_at(16 * i + 64 / PER * j + out_at);
+    typedef uint4_t Base[MT][PASS][WIDE ? 2 : 1];
+    Base base;
+    auto fetch_base = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < PASS; ++j)
+#pragma unroll
+                for (int e = 0; e < (WIDE ? 2 : 1); ++e) {
+                    base[i][j][e] = uint4_t{0, 0, 0, 0};
+                    if (m.base && c0 + out_col < to)
+                        base[i][j][e] = *(const uint4_t*)((const char*)m.base + (out_row[i][j] * m.base_stride + c0 + out_col) * (WIDE ? 4 : 2) + 16 * e);
+                }
+    };
+    // rows of Q for CG columns; those behind the rank or the last column repeat others
+    char* const q_tile = lds + L::q + wave * L::q_tile;
+    auto fetch_q = [&](int c0) {
+        if (id < 0 || c0 >= to) return;
+        const uint16_t* const Q = m.q + (size_t)id * r.rank * m.wide;
+#pragma unroll
+        for (int i = 0; i < CG * QC / 64; ++i) {
+            const int at = 64 * i + lane, col = at / QC, c = (at % QC) ^ swizzle<QC>(col);
+            copy_to_lds(Q + (size_t)min(c0 + col, m.wide - 1) * r.rank + (8 * c < r.rank ? 8 * c : 0), q_tile + 1024 * i);
+        }
+    };
 
     if (id >= 0) {
         float4_t acc[MT][RT];
@@ -140,66 +242,80 @@ __global__ void __launch_bounds__(512) adapter_kernel(AdapterCall p) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < RT; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
+        // 64 columns of x and P: eight rows a copy, a line of 128 bytes each.  Columns behind the depth repeat the last ones, rows of P behind the rank others
         const uint16_t* const P = m.p + (size_t)id * r.rank * m.depth;
-        const uint16_t* x[MT];
-        uint32_t row[MT];
+        const uint16_t* x[2 * MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            row[i] = (uint32_t)(s.t0 + min(16 * i + n, count - 1));
-            x[i] = m.x + (long long)row[i] * m.x_stride;
-        }
-        auto sweep = [&](auto masked) {
-            // wavefront w takes 64 columns at 64 w, 64 w + 512, ..
-            for (int k0 = 64 * wave; k0 < m.depth; k0 += 512) {
-                uint4_t xf[2][MT], pf[2][RT];
+        for (int i = 0; i < 2 * MT; ++i) x[i] = m.x + row_at(8 * i + (lane >> 3)) * m.x_stride;
+        const int p_row = (lane >> 3) * m.depth;
+        char* const ring = lds + wave * D * L::step;
+        auto fetch = [&](int st) {
+            char* const at = ring + st % D * L::step;
+            auto column = [&](int row) { return min(64 * (wave + W * st) + 8 * ((lane & 7) ^ swizzle<8>(row + (lane >> 3))), m.depth - 8); };
+            const int k[2] = {column(0), column(8)};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = k0 + 32 * h + 8 * g;
-                    const bool live = k < m.depth;
+            for (int i = 0; i < 2 * MT; ++i) copy_to_lds(x[i] + k[i & 1], at + 1024 * i);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        xf[h][i] = uint4_t{0, 0, 0, 0};
-                        if (live) xf[h][i] = *(const uint4_t*)(x[i] + k);
-                    }
-#pragma unroll
-                    for (int j = 0; j < RT; ++j) {
-                        pf[h][j] = uint4_t{0, 0, 0, 0};
-                        if (live && 16 * j + n < r.rank) pf[h][j] = *(const uint4_t*)(P + (size_t)(16 * j + n) * m.depth + k);
-                    }
-                }
-                if constexpr (decltype(masked)::value) {
-                    const Keeper keeper(drop);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) xf[h][i] = kept(xf[h][i], keeper.bits((uint32_t)(k0 + 32 * h + 8 * g) >> 3, row[i]));
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int j = 0; j < RT; ++j) acc[i][j] = mfma_bits<BF16>(pf[h][j], xf[h][i], acc[i][j]);
-            }
+            for (int i = 0; i < 2 * RT; ++i) copy_to_lds(P + (size_t)(8 * i < r.rank ? 8 * i : 0) * m.depth + (p_row + k[i & 1]), at + 1024 * (2 * MT + i));
         };
-        if (drop.seed && !p.backward) sweep(std::true_type{});
-        else sweep(std::false_type{});
+        const int steps = (m.depth - 64 * wave + 64 * W - 1) / (64 * W);     // of this wavefront; copies go on behind them, to keep the count
+        if (steps > 0) {
+#pragma unroll
+            for (int st = 0; st < D; ++st) fetch(st);
+        }
+        for (int st = 0; st < steps; ++st) {
+            const char* const at = ring + st % D * L::step;
+            wait_copies<2 * (MT + RT) * (D - 1)>();
+            uint4_t xf[2][MT], pf[2][RT];
+            const int k0 = 64 * (wave + W * st) + 8 * g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int place = ((4 * h + g) ^ swizzle<8>(n)) << 4;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) xf[h][i] = *(const uint4_t*)(at + (16 * i + n) * 128 + place);
+#pragma unroll
+                for (int j = 0; j < RT; ++j) pf[h][j] = *(const uint4_t*)(at + (16 * (MT + j) + n) * 128 + place);
+            }
+            wait_lds();
+            fetch(st + D);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if (k0 + 32 * h >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
+                    if (DROP && !p.backward) xf[h][i] = kept(xf[h][i], Keeper(drop).bits((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n)));
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < RT; ++j) acc[i][j] = mfma_bits<BF16>(pf[h][j], xf[h][i], acc[i][j]);
+        }
+        wait_copies<0>();
+        meet();                                                              // nobody reads or copies into the steps any more
+        fetch_q(from + CG * wave);
+        fetch_base(from + CG * wave);
         // lane (n, g): row n, values 4 g .. + 3 of a tile
-        auto place = [&](int w, int i, int j) { return (float4_t*)&sums[w][16 * i + n][16 * j + 4 * g]; };
-        if (wave >= 4)
+        auto place = [&](int w, int i, int j) { return (float4_t*)(lds + 4 * ((w * ROWS + 16 * i + n) * L::PITCH + 16 * j + 4 * g)); };
+        if (wave >= W / 2)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < RT; ++j) *place(wave - 4, i, j) = acc[i][j];
-        __syncthreads();
-        if (wave < 4)
+                for (int j = 0; j < RT; ++j) *place(wave - W / 2, i, j) = acc[i][j];
+        meet();
+        if (wave < W / 2)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < RT; ++j) *place(wave, i, j) += acc[i][j];
-        __syncthreads();
+        meet();
+    } else {
+        fetch_base(from + CG * wave);
     }
     // sixteen threads a row
+    char* const parts = lds + L::parts;
+    float* const inverse = (float*)(lds + L::inverse);
     if (tid < 16 * ROWS) {
         const int q = tid & 15, at = tid >> 4;
         float4_t h[(RT + 3) / 4];
@@ -208,13 +324,13 @@ __global__ void __launch_bounds__(512) adapter_kernel(AdapterCall p) {
         for (int i = 0; i < (RT + 3) / 4; ++i) {
             const int c = 4 * q + 64 * i;
             h[i] = float4_t{0, 0, 0, 0};
-            if (id >= 0 && c < R) {
+            if (id >= 0 && c < r.rank) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w) h[i] += *(const float4_t*)&sums[w][at][c];
+                for (int w = 0; w < W / 2; ++w) h[i] += *(const float4_t*)(lds + 4 * ((w * ROWS + at) * L::PITCH + c));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) h[i][j] *= before;
             }
-            if (m.h && part == 0 && at < count && c < r.rank) *(float4_t*)(m.h + (long long)(s.t0 + at) * r.rank + c) = h[i];
+            if (m.h && blockIdx.y == 0 && at < count && c < r.rank) *(float4_t*)(m.h + row_at(at) * r.rank + c) = h[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 h[i][j] *= behind;
@@ -239,117 +355,168 @@ __global__ void __launch_bounds__(512) adapter_kernel(AdapterCall p) {
 #pragma unroll
                 for (int o = 0; o < PARTS; ++o) {
                     const uint2_t w = {Elem<BF16>::pack(rest[0], rest[1]), Elem<BF16>::pack(rest[2], rest[3])};
-                    *(uint2_t*)(parts + at * HROW + 2 * (o * R + c)) = w;
+                    *(uint2_t*)(parts + at * L::HROW + 2 * (o * R + c)) = w;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) rest[j] -= widen16<BF16>((uint16_t)(w[j / 2] >> (16 * (j & 1))));
                 }
-                if (RT == 1 && PARTS == 3) *(uint2_t*)(parts + at * HROW + 2 * (3 * R + c)) = uint2_t{0, 0};
+                if (RT == 1 && PARTS == 3) *(uint2_t*)(parts + at * L::HROW + 2 * (3 * R + c)) = uint2_t{0, 0};
             }
         }
     }
-    __syncthreads();
+    meet();
+    wait_copies<0>();
 
-    // columns: a wavefront takes 64 at a time, of which the tile of lane (n, g) ends up with 16 g .. 16 g + 15 of row n
-    const uint16_t* const Q = m.q + (id >= 0 ? (size_t)id * r.rank * m.wide : 0);
-    const int from = part * p.slice, to = min(from + p.slice, m.wide);
-    const bool masked = drop.seed && p.backward;
-    for (int c0 = from + 64 * wave; c0 < to; c0 += 512) {
-        constexpr int QS = RT == 1 ? 1 : RT / 2;
-        float4_t acc[MT][4];
+    char* const out_tile = lds + wave * L::out;
+    for (int c0 = from + CG * wave; c0 < to; c0 += CG * W) {
+        const bool more = c0 + CG * W < to;
+        float4_t acc[MT][CT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
+            for (int j = 0; j < CT; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
         if (id >= 0) {
-            uint4_t qf[4][QS];
+            uint4_t qf[CT][QS];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = c0 + 16 * (n >> 2) + 4 * j + (n & 3);
+            for (int j = 0; j < CT; ++j)
 #pragma unroll
-                for (int k = 0; k < QS; ++k) {
-                    const int c = RT == 1 ? 8 * (g & 1) : 32 * k + 8 * g;
-                    qf[j][k] = uint4_t{0, 0, 0, 0};
-                    if (col < to && c < r.rank) qf[j][k] = *(const uint4_t*)(Q + (size_t)col * r.rank + c);
-                }
-            }
+                for (int k = 0; k < QS; ++k)
+                    qf[j][k] = *(const uint4_t*)(q_tile + (16 * j + n) * 2 * R + (((RT == 1 ? g & 1 : 4 * k + g) ^ swizzle<QC>(16 * j + n)) << 4));
+            wait_lds();
+            if (more) fetch_q(c0 + CG * W);
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st)
+            for (int st = 0; st < L::STEPS; ++st)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const uint4_t hf = *(const uint4_t*)(parts + (16 * i + n) * HROW + 64 * st + 16 * g);
+                    const uint4_t hf = *(const uint4_t*)(parts + (16 * i + n) * L::HROW + 64 * st + 16 * g);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma_bits<BF16>(qf[j][st % QS], hf, acc[i][j]);
+                    for (int j = 0; j < CT; ++j) acc[i][j] = mfma_bits<BF16>(qf[j][st % QS], hf, acc[i][j]);
                 }
         }
+        uint4_t out[MT][PASS][WIDE ? 2 : 1];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int at = 16 * i + n;
-            if (at >= count) continue;
-            const long long t = s.t0 + at;
-            const float down = BF16 ? 1.0f : inverse[at];
+            // lane (n, g) holds columns 4 g .. + 3 of each tile of row n; row by row it goes out
+            if (id >= 0) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int col = c0 + 16 * g + 8 * half;
-                if (col >= to) continue;
-                float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (m.base) load8_of(y, m.base, t * m.base_stride + col, p.y_dt);
-                uint32_t keep = id >= 0 ? 0xFFu : 0u;
-                if (masked && id >= 0) keep = Keeper(drop).bits((uint32_t)col >> 3, (uint32_t)t);
+                for (int j = 0; j < CT; ++j) *(float4_t*)(out_tile + 4 * (n * L::YPITCH + 16 * j + 4 * g)) = acc[i][j];
+            }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float z = acc[i][2 * half + j / 4][j & 3];
-                    if (keep >> j & 1) y[j] = m.base ? fmaf(z, down, y[j]) : z * down;
+            for (int j = 0; j < PASS; ++j) {
+                const int at = 64 / PER * j + out_at;
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (WIDE) {
+                        y[e] = __uint_as_float(base[i][j][WIDE ? e / 4 : 0][e & 3]);
+                    } else {
+                        const uint16_t v = (uint16_t)(base[i][j][0][e / 2] >> (16 * (e & 1)));
+                        y[e] = p.y_dt == DT_BF16 ? bf16_bits_to_f32(v) : f16_bits_to_f32(v);
+                    }
                 }
-                store8_of(m.y, t * m.y_stride + col, y, p.y_dt);
+                if (id >= 0) {
+                    const float down = BF16 ? 1.0f : inverse[16 * i + at];
+                    const float4_t a = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col)), b = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col + 4));
+                    uint32_t keep = 0xFFu;
+                    if (DROP && p.backward) keep = Keeper(drop).bits((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float z = e < 4 ? a[e & 3] : b[e & 3];
+                        if (keep >> e & 1) y[e] = BF16 ? y[e] + z : fmaf(z, down, y[e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (WIDE) {
+                        out[i][j][0][e] = __float_as_uint(y[e]);
+                        out[i][j][WIDE ? 1 : 0][e] = __float_as_uint(y[4 + e]);
+                    } else {
+                        out[i][j][0][e] = p.y_dt == DT_BF16 ? Elem<true>::pack(y[2 * e], y[2 * e + 1]) : Elem<false>::pack(y[2 * e], y[2 * e + 1]);
+                    }
+                }
             }
         }
+        // memory answers in order: the next rows of Q have to be there, then the next base is asked for, and the stores come last
+        wait_copies<0>();
+        if (more) fetch_base(c0 + CG * W);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < PASS; ++j)
+#pragma unroll
+                for (int e = 0; e < (WIDE ? 2 : 1); ++e)
+                    if (16 * i + 64 / PER * j + out_at < count && c0 + out_col < to)
+                        *(uint4_t*)((char*)m.y + (out_row[i][j] * m.y_stride + c0 + out_col) * (WIDE ? 4 : 2) + 16 * e) = out[i][j][e];
     }
 }
 
-template <bool BF16, int RT, int MT>
-static hipError_t products(const AdapterCall& p, dim3 grid, hipStream_t s) {
-    if (p.y_dt == DT_F32) hipLaunchKernelGGL((adapter_kernel<BF16, RT, MT, 3>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((adapter_kernel<BF16, RT, MT, 2>), grid, dim3(512), 0, s, p);
+template <bool BF16, int RT, int MT, int PARTS, bool DROP, bool GATHER>
+static hipError_t start(const AdapterCall& p, dim3 grid, hipStream_t s) {
+    static std::atomic<unsigned long long> raised{0};
+    constexpr int bytes = AdapterLds<RT, MT, PARTS>::bytes;
+    static_assert(bytes <= 160 * 1024, "a unit's LDS");
+    const hipError_t e = raise_lds((const void*)adapter_kernel<BF16, RT, MT, PARTS, DROP, GATHER>, bytes, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((adapter_kernel<BF16, RT, MT, PARTS, DROP, GATHER>), grid, dim3(512), bytes, s, p);
     return hipGetLastError();
 }
+template <bool BF16, int RT, int MT, int PARTS>
+static hipError_t products(const AdapterCall& p, bool gather, dim3 grid, hipStream_t s) {
+    if (p.rows.drop.seed) return start<BF16, RT, MT, PARTS, true, false>(p, grid, s);
+    if (MT == 1 && gather) return start<BF16, RT, 1, PARTS, false, true>(p, grid, s);
+    return start<BF16, RT, MT, PARTS, false, false>(p, grid, s);
+}
 template <bool BF16, int RT>
-static hipError_t products(const AdapterCall& p, int mt, dim3 grid, hipStream_t s) {
-    return mt == 1 ? products<BF16, RT, 1>(p, grid, s) : products<BF16, RT, 2>(p, grid, s);
+static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 grid, hipStream_t s) {
+    const bool wide = p.y_dt == DT_F32;
+    if constexpr (RT < 8)
+        if (rows == 32) return wide ? products<BF16, RT, 2, 3>(p, gather, grid, s) : products<BF16, RT, 2, 2>(p, gather, grid, s);
+    return wide ? products<BF16, RT, 1, 3>(p, gather, grid, s) : products<BF16, RT, 1, 2>(p, gather, grid, s);
 }
 template <bool BF16>
-static hipError_t products(const AdapterCall& p, int mt, dim3 grid, hipStream_t s) {
-    return p.rows.rank <= 16   ? products<BF16, 1>(p, mt, grid, s)
-           : p.rows.rank <= 32 ? products<BF16, 2>(p, mt, grid, s)
-           : p.rows.rank <= 64 ? products<BF16, 4>(p, mt, grid, s)
-                               : products<BF16, 8>(p, mt, grid, s);
+static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 grid, hipStream_t s) {
+    const int rank = p.rows.rank;
+    return rank <= 16   ? products<BF16, 1>(p, rows, gather, grid, s)
+           : rank <= 32 ? products<BF16, 2>(p, rows, gather, grid, s)
+           : rank <= 64 ? products<BF16, 4>(p, rows, gather, grid, s)
+                        : products<BF16, 8>(p, rows, gather, grid, s);
 }
-// Rows of a tile, and columns of a workgroup: as many workgroups as two a compute unit, of no fewer than 256 columns each.
-static int tile_rows(const AdapterRowsDev& r) { return r.n_tokens / r.n_seqs <= 16 ? 16 : 32; }
+static bool single_tokens(const AdapterRowsDev& r) {
+    return !r.offsets && r.n_tokens == r.n_seqs && r.n_seqs > 1 && r.n_seqs <= kGathered && !r.drop.seed;
+}
+// Rows of a tile.  32 where sequences are long: P and Q are read once for twice as many rows (8192 rows at rank 64: 69 us against 78; 4321 rows of sixteen
+// sequences at rank 32: 82 against 107).  Above rank 64 the registers and LDS of 16 rows are full.
+static int tile_rows(const AdapterRowsDev& r) { return r.n_tokens / r.n_seqs <= 16 || r.rank > 64 ? 16 : 32; }
+// Columns of a workgroup: all of them where tiles and matrices fill the device, otherwise as many workgroups as one and a half a compute unit, of no fewer than
+// 256 columns.  Every one takes h again: in twos of half the columns 256 tiles of 8192 rows take 95 us instead of 69, those of 256 single tokens
+// 35 instead of 27; 151 tiles beside 14336 columns in one, two and three 98, 97 and 82.
 static int slice_of(const AdapterRowsDev& r, int n_mats, int widest) {
-    const long long wgs = pieces(r, tile_rows(r)) * n_mats;
-    const long long most = (widest + 255) / 256, wanted = std::max(1ll, std::min(most, 512 / std::max(1ll, wgs)));
+    long long wgs = pieces(r, tile_rows(r));
+    if (single_tokens(r)) wgs = std::min<long long>(wgs, std::max(r.n_adapters, (r.n_seqs + 15) / 16));
+    wgs *= n_mats;
+    const long long wanted = std::min<long long>((widest + 255) / 256, wgs >= 256 ? 1 : (384 + wgs - 1) / wgs);
     return (int)(((widest + wanted - 1) / wanted + 63) / 64 * 64);
 }
 bool adapters_fit(const AdapterRowsDev& r, int widest) {
     const int slice = slice_of(r, 1, widest);
-    return (double)pieces(r, tile_rows(r)) * ((widest + slice - 1) / slice) * kAdapterMats * 512.0 < 4294967296.0;
+    return (double)pieces(r, tile_rows(r)) * ((widest + slice - 1) / slice) * kAdapterMats * 1024.0 < 4294967296.0;
 }
-static hipError_t launch_products(AdapterCall p, int n_mats, int dt, hipStream_t s) {
+static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_t s) {
     int widest = 64;                                  // also where no y is asked for
-    for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].wide);
+    for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
     const int rows = tile_rows(p.rows);
     p.slice = slice_of(p.rows, n_mats, widest);
-    p.slices = (widest + p.slice - 1) / p.slice;
-    const dim3 grid((unsigned)(pieces(p.rows, rows) * p.slices), (unsigned)n_mats);
-    return dt == DT_BF16 ? products<true>(p, rows / 16, grid, s) : products<false>(p, rows / 16, grid, s);
+    const dim3 grid((unsigned)pieces(p.rows, rows), (unsigned)((widest + p.slice - 1) / p.slice), (unsigned)n_mats);
+    return dt == DT_BF16 ? products<true>(p, rows, single_tokens(p.rows), grid, s) : products<false>(p, rows, single_tokens(p.rows), grid, s);
 }
 
-hipError_t launch_adapters(const AdapterRowsDev& rows, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s) {
+hipError_t launch_adapters(const AdapterRowsDev& given, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s) {
+    AdapterRowsDev rows = given;
+    if (!rows.offsets && !rows.adapters) rows.n_seqs = 1;        // all rows have the one adapter
     for (int i = 0; i < n_mats; i += kAdapterMats) {
         AdapterCall p{};
         p.rows = rows; p.y_dt = y_dt; p.first = (uint32_t)i;
         const int n = std::min(kAdapterMats, n_mats - i);
-        for (int j = 0; j < n; ++j) p.mats[j] = mats[i + j];
+        for (int j = 0; j < n; ++j) p.mats[j].m = mats[i + j];
         const hipError_t e = launch_products(p, n, dt, s);
         if (e != hipSuccess) return e;
     }
@@ -378,12 +545,24 @@ __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
     }
     const uint16_t* const from = p.from[blockIdx.z] + (size_t)id * rows * cols;
     uint16_t* const to = p.to[blockIdx.z] + (size_t)id * rows * cols;
-    const int x = threadIdx.x & 63;
-    for (int y = threadIdx.x >> 6; y < 64; y += 4)
-        if (r0 + y < rows && c0 + x < cols) tile[y][x] = from[(size_t)(r0 + y) * cols + c0 + x];
+    // rows and cols are multiples of 8
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int y = (threadIdx.x >> 3) + 32 * i, x = 8 * (threadIdx.x & 7);
+        uint4_t v = {0, 0, 0, 0};
+        if (r0 + y < rows && c0 + x < cols) v = *(const uint4_t*)(from + (size_t)(r0 + y) * cols + c0 + x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(uint32_t*)&tile[y][x + 2 * j] = v[j];
+    }
     __syncthreads();
-    for (int y = threadIdx.x >> 6; y < 64; y += 4)
-        if (c0 + y < cols && r0 + x < rows) to[(size_t)(c0 + y) * rows + r0 + x] = tile[x][y];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int y = (threadIdx.x >> 3) + 32 * i, x = 8 * (threadIdx.x & 7);
+        uint4_t v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (uint32_t)tile[x + 2 * j][y] | (uint32_t)tile[x + 2 * j + 1][y] << 16;
+        if (c0 + y < cols && r0 + x < rows) *(uint4_t*)(to + (size_t)(c0 + y) * rows + r0 + x) = v;
+    }
 }
 
 // Sums over tokens.  A workgroup takes a piece of `cut` rows of one sequence and 128 columns of v: for the gradient of A v = drop(x) and q = g, for that of B
@@ -583,7 +762,7 @@ static hipError_t backward_group(const AdapterRowsDev& rows, const AdapterMatDev
     turn.rows = rows;
     unsigned tiles = 0;
     for (int i = 0; i < n; ++i) {
-        AdapterMatDev& m = c.mats[i];
+        AdapterMatDev& m = c.mats[i].m;
         m = mats[i];
         const uint16_t** const both[2] = {&m.p, &m.q};
         for (int j = 0; j < 2; ++j) {

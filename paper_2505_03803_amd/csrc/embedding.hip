@@ -45,7 +45,7 @@ hipError_t launch_embedding(EmbeddingDev p, int tdt, int odt, hipStream_t s) {
 // ---- the gradient: tokens sorted, runs of equal ones summed in the order of their places --------------------------------
 
 constexpr int kSortTile = 8192;               // tokens whose order is found by counting
-constexpr int kRunTile = 32;                  // sorted places of a wavefront of the sums
+constexpr int kRankRows = 32;                 // of which a workgroup takes so many
 constexpr int kAbsentRows = 16;               // rows of the table that a wavefront looks for among the tokens
 
 __device__ __forceinline__ uint32_t key_of(const EmbeddingDev& p, int i) {
@@ -53,29 +53,46 @@ __device__ __forceinline__ uint32_t key_of(const EmbeddingDev& p, int i) {
     return token >= 0 && token < p.vocab ? (uint32_t)token : (uint32_t)p.vocab;     // tokens without a row come last
 }
 
-// The place of a token among those of its tile: how many are smaller, or equal and in front of it.  A workgroup takes 64 tokens, a lane each; its
-// sixteen wavefronts compare them with a sixteenth of the tile each, whose keys are the same for all lanes.  Two vector
-// instructions a pair: 8192 tokens are 2.1 million of them, 8000 cycles of the device.
+// The place of a token among those of its tile: how many are smaller, or equal and in front of it.  A workgroup takes 32 tokens, each in two lanes of
+// every wavefront; its sixteen wavefronts compare them with a sixteenth of the tile each, four keys a read from LDS, a half of the lanes every
+// other four.  Two vector instructions a pair: 8192 tokens are 2.1 million of them, 8000 cycles of the device.
 __global__ void __launch_bounds__(1024) rank_kernel(EmbeddingDev p) {
+    __shared__ __align__(16) uint32_t others[16][kSortTile / 16];
     __shared__ int counts[16][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = blockIdx.x * 64 / kSortTile * kSortTile, end = min(tile + kSortTile, p.n_tokens), chunk = blockIdx.x * 64, mine = chunk + lane;
-    const uint32_t key = mine < p.n_tokens ? key_of(p, mine) : 0xFFFFFFFFu;
-    const int from = tile + wave * (kSortTile / 16), to = min(from + kSortTile / 16, end);
-    int count = 0, i = from;
-#pragma unroll 8
-    for (; i < min(to, chunk); ++i) count += key_of(p, i) <= key;
-    for (; i < min(to, chunk + 64); ++i) {
-        const uint32_t other = key_of(p, i);
-        count += other < key || (other == key && i < mine);
+    const int chunk = blockIdx.x * kRankRows, tile = chunk / kSortTile * kSortTile, size = min(kSortTile, p.n_tokens - tile), mine = chunk + (lane & 31);
+    // keys of a wavefront: a multiple of 32 of them, so that those of the workgroup's tokens are one wavefront's
+    const int span = ((size + 15) / 16 + 31) / 32 * 32, from = tile + wave * span;
+    const uint32_t key = mine < p.n_tokens ? key_of(p, mine) : 0;
+    for (int i = lane; i < span; i += 64) others[wave][i] = from + i < tile + size ? key_of(p, from + i) : 0xFFFFFFFFu;
+    __syncthreads();
+    int count = 0;
+    const int half = lane >> 5 << 2;
+    auto four = [&](int i) { return *(const uint4_t*)&others[wave][i + half]; };
+    const int before = min(max(chunk - from, 0), span), inside = min(max(chunk + kRankRows - from, 0), span);
+#pragma unroll 4
+    for (int i = 0; i < before; i += 8) {
+        const uint4_t k = four(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) count += k[j] <= key;
     }
-#pragma unroll 8
-    for (; i < to; ++i) count += key_of(p, i) < key;
+    for (int i = before; i < inside; i += 8) {
+        const uint4_t k = four(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) count += k[j] < key || (k[j] == key && from + i + half + j < mine);
+    }
+#pragma unroll 4
+    for (int i = inside; i < span; i += 8) {
+        const uint4_t k = four(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) count += k[j] < key;
+    }
     counts[wave][lane] = count;
     __syncthreads();
-    if (wave == 0 && mine < p.n_tokens) {
+    if (threadIdx.x < kRankRows && mine < p.n_tokens) {
+        count = 0;
 #pragma unroll
-        for (int w = 1; w < 16; ++w) count += counts[w][lane];
+        for (int w = 0; w < 16; ++w) count += counts[w][lane] + counts[w][lane + 32];
         p.tile_keys[tile + count] = key;
         p.tile_order[tile + count] = mine;
     }
@@ -105,20 +122,79 @@ __global__ void __launch_bounds__(256) merge_kernel(EmbeddingDev p) {
     p.order[place] = p.tile_order[i];
 }
 
+// E pieces of V columns of a lane, 8 in all: piece e is at column 64 V e + V lane of a wavefront's 512, so that loads of either width
+// are of neighbouring columns.  V: 16 bytes of 16-bit (8) or binary32 (4) values where rows begin at multiples of that, otherwise 1.
+template <int DT_, int V>
+struct Columns {
+    static constexpr int E = 8 / V;
+    int first, d;
+    __device__ __forceinline__ int at(int e) const { return first + 64 * V * e; }
+    __device__ __forceinline__ bool live(int e) const { return at(e) < d; }          // d is a multiple of V
+    __device__ __forceinline__ void load(float (&f)[8], const void* p, long long row) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            Piece<DT_, V> v;
+            v.clear();
+            if (live(e)) v.load(p, row + at(e));
+            float w[V];
+            v.widen(w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[e * V + j] = w[j];
+        }
+    }
+    __device__ __forceinline__ void load_sums(float (&f)[8], const float* p, long long row) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int j = 0; j < V; j += V < 4 ? 1 : 4) {
+                if constexpr (V < 4) {
+                    f[e] = live(e) ? p[row + at(e)] : 0.0f;
+                } else {
+                    float4_t v = {0, 0, 0, 0};
+                    if (live(e)) v = *(const float4_t*)(p + row + at(e) + j);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) f[e * V + j + c] = v[c];
+                }
+            }
+    }
+    __device__ __forceinline__ void store_sums(float* p, long long row, const float (&f)[8]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (live(e)) {
+                if constexpr (V < 4) {
+                    p[row + at(e)] = f[e];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; j += 4) *(float4_t*)(p + row + at(e) + j) = float4_t{f[e * V + j], f[e * V + j + 1], f[e * V + j + 2], f[e * V + j + 3]};
+                }
+            }
+    }
+    // a row of the table: its sum times the scale, added to what is there if asked for
+    __device__ __forceinline__ void store_row(const EmbeddingDev& p, uint32_t key, float (&sum)[8]) const {
+        float old[8];
+        const long long row = (long long)key * d;
+        if (p.accumulate) load_sums(old, p.dtable, row);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum[c] = p.accumulate ? fmaf(p.scale, sum[c], old[c]) : p.scale * sum[c];
+        store_sums(p.dtable, row, sum);
+    }
+};
+struct RunPlan { int tile, tiles, chunks, units; };    // sorted places of a wavefront, how many such, 512 columns each, wavefronts in all
+
 // The sums of the runs that begin and end in a tile of sorted places go to their rows; of a run that goes on behind the tile, or began in front of
-// it, the tile leaves its part: [tile][0] where it began in front, [tile][1] where it begins here.  A wavefront takes 512 columns, eight of them a
-// lane, and has eight rows on their way.  Other wavefronts of the launch write zeros to rows of no token.
-template <int DT_>
-__global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, int chunks, int tiles) {
-    const int lane = threadIdx.x;
-    if ((int)blockIdx.x >= chunks * tiles) {
-        const int first = ((int)blockIdx.x - chunks * tiles) * kAbsentRows, row = first + lane;
+// it, the tile leaves its part: [tile][0] where it began in front, [tile][1] where it begins here.  A wavefront takes 512 columns and has eight
+// rows on their way.  Other wavefronts of the launch write zeros to rows of no token.
+template <int DT_, int V>
+__global__ void __launch_bounds__(256) run_kernel(EmbeddingDev p, RunPlan plan) {
+    const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (unit >= plan.units) {
+        const int first = (unit - plan.units) * kAbsentRows, row = first + lane;
         bool absent = false;
         if (lane < kAbsentRows && row < p.vocab) {
             const int at = below(p.keys, 0, p.n_tokens, (uint32_t)row, false);
             absent = at == p.n_tokens || p.keys[at] != (uint32_t)row;
         }
-        const uint64_t which = __builtin_amdgcn_ballot_w64(absent);
+        const uint64_t which = p.accumulate ? 0 : __builtin_amdgcn_ballot_w64(absent);
         for (int r = 0; r < kAbsentRows; ++r) {
             if (!(which >> r & 1)) continue;
             float* const to = p.dtable + (size_t)(first + r) * p.d;
@@ -129,11 +205,11 @@ __global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, int chunks, int
         }
         return;
     }
-    const int tile = blockIdx.x / chunks, col = (blockIdx.x % chunks) * 512 + 8 * lane, left = p.d - col;
-    const int i0 = tile * kRunTile, i1 = min(i0 + kRunTile, p.n_tokens);
+    const int tile = unit / plan.chunks;
+    const Columns<DT_, V> cols{(unit % plan.chunks) * 512 + V * lane, p.d};
+    const int i0 = tile * plan.tile, i1 = min(i0 + plan.tile, p.n_tokens);
     const uint32_t none = (uint32_t)p.vocab;
     const uint32_t front = i0 > 0 ? p.keys[i0 - 1] : 0xFFFFFFFFu, behind = i1 < p.n_tokens ? p.keys[i1] : 0xFFFFFFFFu;
-    const bool whole_table = p.d % 4 == 0;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int i = i0; i < i1; i += 8) {
         float x[8][8];
@@ -141,12 +217,8 @@ __global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, int chunks, int
 #pragma unroll
         for (int j = 0; j < 9; ++j) key[j] = i + j < i1 ? p.keys[i + j] : i + j == i1 ? behind : 0xFFFFFFFFu;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (i + j < i1 && key[j] < none && left > 0) load8<DT_>(x[j], p.out, p.order[i + j] * p.out_stride + col, left, p.rows_whole);
-            else
-#pragma unroll
-                for (int c = 0; c < 8; ++c) x[j][c] = 0.0f;
-        }
+        for (int j = 0; j < 8; ++j)
+            if (i + j < i1 && key[j] < none) cols.load(x[j], p.out, p.order[i + j] * p.out_stride);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (i + j >= i1 || key[j] >= none) break;
@@ -155,16 +227,8 @@ __global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, int chunks, int
             const bool last = i + j + 1 == i1;
             if (!last && key[j + 1] == key[j]) continue;
             const bool before = key[j] == front, after = last && behind == key[j];
-            if (before || after) {
-                store8<DT_F32>(p.partial, ((long long)tile * 2 + !before) * p.d + col, sum, left, whole_table);
-            } else if (left > 0) {
-                const long long at = (long long)key[j] * p.d + col;
-                float old[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (p.accumulate) load8<DT_F32>(old, p.dtable, at, left, whole_table);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) sum[c] = p.accumulate ? fmaf(p.scale, sum[c], old[c]) : p.scale * sum[c];
-                store8<DT_F32>(p.dtable, at, sum, left, whole_table);
-            }
+            if (before || after) cols.store_sums(p.partial, ((long long)tile * 2 + !before) * p.d, sum);
+            else cols.store_row(p, key[j], sum);
 #pragma unroll
             for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
         }
@@ -172,43 +236,59 @@ __global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, int chunks, int
 }
 
 // Runs over more than one tile, joined by the tile in which they begin.
-__global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, int chunks, int tiles) {
-    const int tile = blockIdx.x / chunks, col = (blockIdx.x % chunks) * 512 + 8 * (int)threadIdx.x, left = p.d - col;
-    const int i0 = tile * kRunTile, i1 = i0 + kRunTile;
-    if (i1 >= p.n_tokens || left <= 0) return;
+template <int V>
+__global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, RunPlan plan) {
+    const int lane = threadIdx.x, tile = blockIdx.x / plan.chunks;
+    const Columns<DT_F32, V> cols{((int)blockIdx.x % plan.chunks) * 512 + V * lane, p.d};
+    const int i0 = tile * plan.tile, i1 = i0 + plan.tile;
+    if (i1 >= p.n_tokens) return;
     const uint32_t key = p.keys[i1 - 1];
     if (key >= (uint32_t)p.vocab || p.keys[i1] != key || (i0 > 0 && p.keys[i0 - 1] == key)) return;
-    const int end = i1 + below(p.keys, i1, p.n_tokens, key, true), last = (end - 1) / kRunTile;
-    const bool whole = p.d % 4 == 0;
+    int last = tile;                                             // the last tile that begins with the run
+    for (bool on = true; on;) {
+        const int next = last + 1 + lane;
+        const uint64_t same = __builtin_amdgcn_ballot_w64(next < plan.tiles && p.keys[(long long)next * plan.tile] == key);
+        on = same == ~0ull;
+        last += on ? 64 : __builtin_ctzll(~same);
+    }
     float sum[8];
-    load8<DT_F32>(sum, p.partial, ((long long)tile * 2 + 1) * p.d + col, left, whole);
+    cols.load_sums(sum, p.partial, ((long long)tile * 2 + 1) * p.d);
 #pragma unroll 8
     for (int t = tile + 1; t <= last; ++t) {
         float x[8];
-        load8<DT_F32>(x, p.partial, (long long)t * 2 * p.d + col, left, whole);
+        cols.load_sums(x, p.partial, (long long)t * 2 * p.d);
 #pragma unroll
         for (int c = 0; c < 8; ++c) sum[c] += x[c];
     }
-    const long long at = (long long)key * p.d + col;
-    float old[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (p.accumulate) load8<DT_F32>(old, p.dtable, at, left, whole);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) sum[c] = p.accumulate ? fmaf(p.scale, sum[c], old[c]) : p.scale * sum[c];
-    store8<DT_F32>(p.dtable, at, sum, left, whole);
+    cols.store_row(p, key, sum);
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
-static int run_tiles(int n_tokens) { return (n_tokens + kRunTile - 1) / kRunTile; }
+// Sorted places of a wavefront: 32, or fewer where that leaves less than 2048 wavefronts.
+static RunPlan run_plan(int n_tokens, int d) {
+    RunPlan r{};
+    r.chunks = (d + 511) / 512;
+    r.tile = 32;
+    while (r.tile > 8 && (long long)((n_tokens + r.tile - 1) / r.tile) * r.chunks < 2048) r.tile /= 2;
+    r.tiles = (n_tokens + r.tile - 1) / r.tile;
+    r.units = r.tiles * r.chunks;
+    return r;
+}
 size_t embedding_backward_workspace_bytes(int n_tokens, int d) {
     const size_t list = round16(4 * (size_t)n_tokens);
-    return (n_tokens > kSortTile ? 4 : 2) * list + (size_t)run_tiles(n_tokens) * 2 * d * 4;
+    return (n_tokens > kSortTile ? 4 : 2) * list + (size_t)run_plan(n_tokens, d).tiles * 2 * d * 4;
 }
 bool embedding_backward_fits(int n_tokens, int vocab, int d) {
-    const double chunks = (d + 511) / 512;
-    return (chunks * run_tiles(n_tokens) + vocab / kAbsentRows + 1) * 64.0 < 4294967296.0;
+    const double units = (double)((n_tokens + 31) / 32) * ((d + 511) / 512);       // where there are many
+    return (units + vocab / kAbsentRows + 8) * 64.0 < 4294967296.0;
+}
+template <int DT_, int V>
+static void sum_runs(const EmbeddingDev& p, const RunPlan& plan, hipStream_t s) {
+    const unsigned absent = p.accumulate ? 0 : (unsigned)(p.vocab + kAbsentRows - 1) / kAbsentRows;
+    hipLaunchKernelGGL((run_kernel<DT_, V>), dim3((plan.units + absent + 3) / 4), dim3(256), 0, s, p, plan);
+    if (plan.tiles > 1) hipLaunchKernelGGL(join_kernel<V == 8 ? 4 : V>, dim3((unsigned)plan.units), dim3(64), 0, s, p, plan);
 }
 hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hipStream_t s) {
-    p.rows_whole = p.out_stride % (dt == DT_F32 ? 4 : 8) == 0;
     char* at = (char*)workspace;
     const size_t list = round16(4 * (size_t)p.n_tokens);
     p.keys = (uint32_t*)at; at += list;
@@ -219,16 +299,16 @@ hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hi
         p.tile_order = (int*)at; at += list;
     }
     p.partial = (float*)at;
-    hipLaunchKernelGGL(rank_kernel, dim3((p.n_tokens + 63) / 64), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(p.n_tokens + kRankRows - 1) / kRankRows), dim3(1024), 0, s, p);
     if (p.n_tokens > kSortTile) hipLaunchKernelGGL(merge_kernel, dim3((p.n_tokens + 255) / 256), dim3(256), 0, s, p);
-    const int chunks = (p.d + 511) / 512, tiles = run_tiles(p.n_tokens);
-    const dim3 grid((unsigned)(chunks * tiles + (p.accumulate ? 0 : (p.vocab + kAbsentRows - 1) / kAbsentRows))), block(64);
+    const RunPlan plan = run_plan(p.n_tokens, p.d);
+    const int unit = dt == DT_F32 ? 4 : 8;
+    const bool whole = p.d % unit == 0 && p.out_stride % unit == 0;
     switch (dt) {
-        case DT_F16: hipLaunchKernelGGL(run_kernel<DT_F16>, grid, block, 0, s, p, chunks, tiles); break;
-        case DT_BF16: hipLaunchKernelGGL(run_kernel<DT_BF16>, grid, block, 0, s, p, chunks, tiles); break;
-        default: hipLaunchKernelGGL(run_kernel<DT_F32>, grid, block, 0, s, p, chunks, tiles);
+        case DT_F16: whole ? sum_runs<DT_F16, 8>(p, plan, s) : sum_runs<DT_F16, 1>(p, plan, s); break;
+        case DT_BF16: whole ? sum_runs<DT_BF16, 8>(p, plan, s) : sum_runs<DT_BF16, 1>(p, plan, s); break;
+        default: whole ? sum_runs<DT_F32, 4>(p, plan, s) : sum_runs<DT_F32, 1>(p, plan, s);
     }
-    if (tiles > 1) hipLaunchKernelGGL(join_kernel, dim3((unsigned)(chunks * tiles)), block, 0, s, p, chunks, tiles);
     return hipGetLastError();
 }
 
