@@ -4,6 +4,7 @@
 #include "matrix_core.h"
 #include "pieces.h"
 
+#include <stdlib.h>
 #include <type_traits>
 
 namespace rwkvq {
@@ -19,7 +20,7 @@ struct alignas(128) AdapterCall {
 };
 struct OuterMatDev {
     const uint16_t *x, *dy;
-    const float *g, *h;
+    const uint16_t *g, *h;                         // in three parts, [token][part][padded rank]
     float *da, *db;
     long long x_stride, dy_stride;
     size_t at;                                     // of its sums among those of a piece
@@ -31,7 +32,7 @@ struct OuterCall {
     int* owner;                                    // adapter of each piece, -1: none
     float* partial;                                // [piece][matrix][rank K | N rank]
     size_t size;                                   // floats of a piece
-    int n_mats, chunks, cut;
+    int n_mats, chunks, cut, slots;
     uint32_t first;
 };
 struct TurnCall {
@@ -39,7 +40,13 @@ struct TurnCall {
     const uint16_t* from[2 * kAdapterMats];
     uint16_t* to[2 * kAdapterMats];
     int height[2 * kAdapterMats], width[2 * kAdapterMats];
+    const float* h[kAdapterMats];
+    uint16_t* h_parts[kAdapterMats];
+    int n_mats;
 };
+
+// The rank as the kernels pad it: 16, 32, 64 or 128.
+__host__ __device__ __forceinline__ int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
 // Rows of sequence b, within 0 .. n_tokens whatever the offsets hold.
 __device__ __forceinline__ void rows_of(const AdapterRowsDev& r, int b, int& t0, int& t1) {
@@ -202,6 +209,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
     const float before = p.backward ? scale : r.drop.factor, behind = p.backward ? r.drop.factor : scale;
     Dropout drop = r.drop;
     drop.call += blockIdx.z + p.first;
+    const Keeper keeper = DROP ? Keeper(drop) : Keeper();
 
     // y: a wavefront takes CG columns at a time; lane l has 8 of them, PER lanes a row
     const int from = blockIdx.y * p.slice, to = min(from + p.slice, m.wide), out_col = 8 * (lane % PER), out_at = lane / PER;
@@ -265,9 +273,15 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
         }
         for (int st = 0; st < steps; ++st) {
             const char* const at = ring + st % D * L::step;
-            wait_copies<2 * (MT + RT) * (D - 1)>();
             uint4_t xf[2][MT], pf[2][RT];
             const int k0 = 64 * (wave + W * st) + 8 * g;
+            uint32_t keep[2][MT];                                            // while the copies are on their way
+            if (DROP && !p.backward)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) keep[h][i] = keeper.bits((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
+            wait_copies<2 * (MT + RT) * (D - 1)>();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int place = ((4 * h + g) ^ swizzle<8>(n)) << 4;
@@ -283,7 +297,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if (k0 + 32 * h >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
-                    if (DROP && !p.backward) xf[h][i] = kept(xf[h][i], Keeper(drop).bits((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n)));
+                    if (DROP && !p.backward) xf[h][i] = kept(xf[h][i], keep[h][i]);
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -330,7 +344,16 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
                 for (int j = 0; j < 4; ++j) h[i][j] *= before;
             }
-            if (m.h && blockIdx.y == 0 && at < count && c < r.rank) *(float4_t*)(m.h + row_at(at) * r.rank + c) = h[i];
+            if (m.h && blockIdx.y == 0 && at < count) {
+                if (!p.backward) {
+                    if (c < r.rank) *(float4_t*)(m.h + row_at(at) * r.rank + c) = h[i];
+                } else if (c < R) {                                          // g, only read by the sums over tokens
+                    uint2_t w[3];
+                    split4<3>(h[i], w);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o) *(uint2_t*)((uint16_t*)m.h + (row_at(at) * 3 + o) * R + c) = w[o];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 h[i][j] *= behind;
@@ -363,6 +386,14 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             }
         }
     }
+    uint32_t keep[MT][PASS];                                                  // of the next columns
+    auto draw = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < PASS; ++j) keep[i][j] = DROP && p.backward ? keeper.bits((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]) : 0xFFu;
+    };
+    draw(from + CG * wave);
     meet();
     wait_copies<0>();
 
@@ -416,12 +447,10 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
                 if (id >= 0) {
                     const float down = BF16 ? 1.0f : inverse[16 * i + at];
                     const float4_t a = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col)), b = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col + 4));
-                    uint32_t keep = 0xFFu;
-                    if (DROP && p.backward) keep = Keeper(drop).bits((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float z = e < 4 ? a[e & 3] : b[e & 3];
-                        if (keep >> e & 1) y[e] = BF16 ? y[e] + z : fmaf(z, down, y[e]);
+                        if (!DROP || keep[i][j] >> e & 1) y[e] = BF16 ? y[e] + z : fmaf(z, down, y[e]);
                     }
                 }
 #pragma unroll
@@ -436,6 +465,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             }
         }
         // memory answers in order: the next rows of Q have to be there, then the next base is asked for, and the stores come last
+        if (more) draw(c0 + CG * W);
         wait_copies<0>();
         if (more) fetch_base(c0 + CG * W);
 #pragma unroll
@@ -530,6 +560,20 @@ __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
     __shared__ uint16_t tile[64][66];
     __shared__ int used;
     const AdapterRowsDev& r = p.rows;
+    if ((int)blockIdx.z >= 2 * p.n_mats) {                                   // h in three parts
+        const int mat = blockIdx.z - 2 * p.n_mats, R = padded_rank(r.rank), step = gridDim.x * gridDim.y * 256;
+        for (long long i = (blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < (long long)r.n_tokens * (R / 4); i += step) {
+            const long long t = i / (R / 4);
+            const int c = 4 * (int)(i % (R / 4));
+            float4_t v = {0, 0, 0, 0};
+            if (c < r.rank) v = *(const float4_t*)(p.h[mat] + t * r.rank + c);
+            uint2_t w[3];
+            split4<3>(v, w);
+#pragma unroll
+            for (int o = 0; o < 3; ++o) *(uint2_t*)(p.h_parts[mat] + (t * 3 + o) * R + c) = w[o];
+        }
+        return;
+    }
     const int rows = p.height[blockIdx.z], cols = p.width[blockIdx.z], id = blockIdx.y, across = (cols + 63) / 64;
     const int r0 = ((int)blockIdx.x / across) * 64, c0 = ((int)blockIdx.x % across) * 64;
     if (r0 >= rows) return;
@@ -565,131 +609,156 @@ __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
     }
 }
 
-// Sums over tokens.  A workgroup takes a piece of `cut` rows of one sequence and 128 columns of v: for the gradient of A v = drop(x) and q = g, for that of B
-// v = dy and q = h; the product of their transposes, 32 tokens at a time, with four wavefronts of 32 columns each.  Tiles of both lie
-// in LDS by token and are read by columns, in the order of tokens that column_frag has, the same for both.
-// q is binary32: three bf16 parts, 24 bits, since the result is a binary32 sum; fp16 values of v as two bf16 parts, exact, of which the products of both
-// lowest parts are left out (2^-24 of the term).
-constexpr int kOuterCols = 128;
+// Sums over tokens.  A workgroup takes a piece of `cut` rows of one sequence and some columns of v: for the gradient of A v = drop(x) and q = g, for that of B
+// v = dy and q = h; the product of their transposes, 32 tokens at a time, with four wavefronts of VC tiles of 16 columns each.  Tiles of both lie in LDS by
+// token and are read by columns, in the order of tokens that column_frag has, the same for both; v is on its way two steps ahead, q one, in registers.
+// q is binary32: three bf16 parts, 24 bits, since the result is a binary32 sum, made once before; fp16 values of v as two bf16 parts, exact, of which the products
+// of both lowest parts are left out (2^-24 of the term).
+// Reads by columns take 32 bytes of eight rows at once: pairs of pieces of a row, C of them, change places with its number.
+template <int C>
+__device__ __forceinline__ int pair_swizzle(int row) { return C >= 8 ? (row & 7) << 1 : (row / (8 / C) & (C - 1)) << 1; }
+constexpr int outer_tiles(int rank) { return rank <= 64 ? 4 : 2; }
+static int outer_cols(int rank) { return 64 * outer_tiles(rank); }
+template <int RT> struct OuterLds {
+    static constexpr int R = 16 * RT, QC = R / 8, VC = outer_tiles(R), COLS = 64 * VC, VROW = 2 * COLS, QROW = 6 * R;
+    static constexpr int v = 32 * VROW, q = 32 * QROW, found = 2 * (v + q), bytes = found + 16;
+};
 template <bool BF16, int RT>
-__global__ void __launch_bounds__(256) outer_kernel(OuterCall p) {
-    constexpr int R = 16 * RT, VROW = 2 * kOuterCols + 16, QROW = 2 * R + 16, PLANES = BF16 ? 1 : 2;
-    __shared__ __align__(16) char vt[PLANES][32 * VROW];
-    __shared__ __align__(16) char qt[3][32 * QROW];
-    __shared__ int found;
-    const AdapterRowsDev& r = p.rows;
-    const int slot = blockIdx.x / p.chunks;
-    int chunk = blockIdx.x % p.chunks, mat = 0;
+__global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
+    typedef OuterLds<RT> L;
+    constexpr int QC = L::QC, VC = L::VC, COLS = L::COLS, VROW = L::VROW, QROW = L::QROW;
+    constexpr int VN = L::v / 4096, QN = (L::q + 4095) / 4096;                // pieces of 16 bytes of a thread and step
+    extern __shared__ __align__(16) char lds[];
+    const AdapterRowsDev r = p.rows;
+    // those of a piece, which read the same q, are `slots` numbers apart: on one die where that is a multiple of eight
+    const int slot = blockIdx.x % p.slots;
+    int chunk = blockIdx.x / p.slots, mat = 0;
     while (chunk >= p.mats[mat].chunks) chunk -= p.mats[mat++].chunks;
-    const OuterMatDev& m = p.mats[mat];
-    const RowSpan s = piece_of(r, p.cut, slot, &found);
+    const OuterMatDev m = p.mats[mat];
+    const RowSpan s = piece_of(r, p.cut, slot, (int*)(lds + L::found));
     const int id = s.t0 < s.t1 ? adapter_of(r, s.b) : -1;
-    if (blockIdx.x % p.chunks == 0 && threadIdx.x == 0) p.owner[slot] = id;
+    if (blockIdx.x < p.slots && threadIdx.x == 0) p.owner[slot] = id;
     if (id < 0) return;
-    const int x_chunks = (m.K + kOuterCols - 1) / kOuterCols;
+    const int x_chunks = (m.K + COLS - 1) / COLS;
     const bool of_a = chunk < x_chunks;
-    const int c0 = (of_a ? chunk : chunk - x_chunks) * kOuterCols, wide = of_a ? m.K : m.N;
+    const int c0 = (of_a ? chunk : chunk - x_chunks) * COLS, wide = of_a ? m.K : m.N;
     const uint16_t* const v = of_a ? m.x : m.dy;
     const long long stride = of_a ? m.x_stride : m.dy_stride;
-    const float* const q = of_a ? m.g : m.h;
+    const uint16_t* const q = of_a ? m.g : m.h;
     Dropout drop = r.drop;
     drop.call += (uint32_t)mat + p.first;
     const bool masked = of_a && drop.seed;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const int steps = (s.t1 - s.t0 + 31) / 32;
 
-    // thread: 16 bytes at column 8 (tid % 16) of tokens tid / 16 and 16 on; and four values of q at a time
-    constexpr int QN = (32 * R / 4 + 255) / 256;
-    uint4_t vn[2];
-    float4_t qn[QN];
-    auto fetch = [&](int t) {
+    // a thread's piece i of a step of v: token PER_V i + .. and eight columns; of q: token, part and eight values.  Places behind the piece and the last column are 0
+    constexpr int PER = COLS / 8, APART = 256 / PER;
+    const int v_row = tid / PER, col = c0 + 8 * (tid % PER);
+    auto fetch_v = [&](uint4_t (&to)[VN], int st) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = t + tid / 16 + 16 * i, col = c0 + 8 * (tid & 15);
-            vn[i] = uint4_t{0, 0, 0, 0};
-            if (at < s.t1 && col < wide) {
-                vn[i] = *(const uint4_t*)(v + (long long)at * stride + col);
-                if (masked) vn[i] = kept(vn[i], Keeper(drop).bits((uint32_t)col >> 3, (uint32_t)at));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < QN; ++i) {
-            const int e = tid + 256 * i, at = t + e / (R / 4), c = 4 * (e % (R / 4));
-            qn[i] = float4_t{0, 0, 0, 0};
-            if (e < 32 * R / 4 && at < s.t1 && c < r.rank) qn[i] = *(const float4_t*)(q + (long long)at * r.rank + c);
+        for (int i = 0; i < VN; ++i) {
+            const int t = s.t0 + 32 * st + v_row + APART * i;
+            to[i] = uint4_t{0, 0, 0, 0};
+            if (t < s.t1 && col < wide) to[i] = *(const uint4_t*)(v + (long long)t * stride + col);
         }
     };
-    float4_t acc[2][RT];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < RT; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
-    fetch(s.t0);
-    for (int t = s.t0; t < s.t1; t += 32) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int to = (tid / 16 + 16 * i) * VROW + 16 * (tid & 15);
-            if constexpr (BF16) {
-                *(uint4_t*)(vt[0] + to) = vn[i];
-            } else {
-                uint4_t hi, lo;
-                split_f16(vn[i], hi, lo);
-                *(uint4_t*)(vt[0] + to) = hi;
-                *(uint4_t*)(vt[PLANES - 1] + to) = lo;
-            }
-        }
+    uint4_t qn[QN];
+    auto fetch_q = [&](int st) {
 #pragma unroll
         for (int i = 0; i < QN; ++i) {
-            const int e = tid + 256 * i, to = (e / (R / 4)) * QROW + 8 * (e % (R / 4));
-            if (e < 32 * R / 4) {
-                uint2_t w[3];
-                split4<3>(qn[i], w);
-#pragma unroll
-                for (int o = 0; o < 3; ++o) *(uint2_t*)(qt[o] + to) = w[o];
-            }
+            const int at = tid + 256 * i, t = s.t0 + 32 * st + at / (3 * QC);
+            qn[i] = uint4_t{0, 0, 0, 0};
+            if (at < 96 * QC && t < s.t1) qn[i] = *(const uint4_t*)(q + ((size_t)t * 3 * QC + at % (3 * QC)) * 8);
         }
-        __syncthreads();
-        if (t + 32 < s.t1) fetch(t + 32);
-        uint4_t vf[PLANES][2];
+    };
+    uint4_t va[VN], vb[VN];
+    fetch_v(va, 0);
+    fetch_q(0);
+    fetch_v(vb, 1);
+    auto sweep = [&](auto first, auto drops) {
+        constexpr bool OF_A = decltype(first)::value, MASKED = decltype(drops)::value;
+        float4_t acc[VC][RT];
 #pragma unroll
-        for (int o = 0; o < PLANES; ++o)
+        for (int i = 0; i < VC; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) vf[o][i] = column_frag<VROW>(vt[o], 0, 2 * wave + i, n, g);
+            for (int j = 0; j < RT; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
+        const Keeper keeper = MASKED ? Keeper(drop) : Keeper();
+        auto step = [&](int st, uint4_t (&vn)[VN]) {
+            char *const vt = lds + (st & 1) * L::v, *const qt = lds + 2 * L::v + (st & 1) * L::q;
 #pragma unroll
-        for (int j = 0; j < RT; ++j)
-#pragma unroll
-            for (int o = 0; o < 3; ++o) {
-                const uint4_t qf = column_frag<QROW>(qt[o], 0, j, n, g);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int u = 0; u < PLANES; ++u)
-                        if (u + o < 3) acc[i][j] = of_a ? mfma_bits<true>(vf[u][i], qf, acc[i][j]) : mfma_bits<true>(qf, vf[u][i], acc[i][j]);
+            for (int i = 0; i < VN; ++i) {
+                const int row = v_row + APART * i;
+                if (MASKED) vn[i] = kept(vn[i], keeper.bits((uint32_t)col >> 3, (uint32_t)(s.t0 + 32 * st + row)));
+                *(uint4_t*)(vt + row * VROW + 16 * ((tid % PER) ^ pair_swizzle<8>(row))) = vn[i];
             }
-        __syncthreads();
-    }
-    // dA: lane (n, g) holds value n of the rank and four columns; dB: column n and four values of the rank
-    float* const out = p.partial + (size_t)slot * p.size + m.at;
-    const float factor = of_a ? r.drop.factor : r.scales ? r.scales[id] : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < QN; ++i) {
+                const int at = tid + 256 * i, row = at / (3 * QC), c = at % (3 * QC);
+                if (at < 96 * QC) *(uint4_t*)(qt + row * QROW + 16 * (c ^ pair_swizzle<RT>(row))) = qn[i];
+            }
+            meet();
+            fetch_q(st + 1);
+            fetch_v(vn, st + 2);
+            // operands by columns: lane (n, g) reads tokens 4 g + n / 4 and 16 on, and ends up with column n of tokens 4 g .. + 3 and 16 + 4 g .. + 3
+            const int row = 4 * g + (n >> 2);
+            auto columns = [&](const char* tile, int pitch, int piece) {
+                const char* const at = tile + row * pitch + 16 * piece + 8 * (n & 1);
+                const uint2_t a = lds_transposed(at), b = lds_transposed(at + 16 * pitch);
+                return uint4_t{a.x, a.y, b.x, b.y};
+            };
+            uint4_t vf[VC], low[BF16 ? 1 : VC];
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-            const int col = c0 + 32 * wave + 16 * i + (of_a ? 4 * g : n), k = 16 * j + (of_a ? n : 4 * g);
-            if (col >= wide || k >= r.rank) continue;
+            for (int i = 0; i < VC; ++i) {
+                vf[i] = columns(vt, VROW, (2 * (VC * wave + i) + (n >> 1 & 1)) ^ pair_swizzle<8>(row));
+                if constexpr (!BF16) {
+                    const uint4_t f = vf[i];
+                    split_f16(f, vf[i], low[i]);
+                }
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] *= factor;
-            *(float4_t*)(out + (of_a ? (size_t)k * m.K + col : (size_t)r.rank * m.K + (size_t)col * r.rank + k)) = acc[i][j];
+            for (int j = 0; j < RT; ++j)
+#pragma unroll
+                for (int o = 0; o < 3; ++o) {
+                    const uint4_t qf = columns(qt, QROW, o * QC + ((2 * j + (n >> 1 & 1)) ^ pair_swizzle<RT>(row)));
+#pragma unroll
+                    for (int i = 0; i < VC; ++i) {
+                        acc[i][j] = OF_A ? mfma_bits<true>(vf[i], qf, acc[i][j]) : mfma_bits<true>(qf, vf[i], acc[i][j]);
+                        if constexpr (!BF16)
+                            if (o < 2) acc[i][j] = OF_A ? mfma_bits<true>(low[i], qf, acc[i][j]) : mfma_bits<true>(qf, low[i], acc[i][j]);
+                    }
+                }
+        };
+        for (int st = 0; st < steps; st += 2) {
+            step(st, va);
+            if (st + 1 < steps) step(st + 1, vb);
         }
+        // dA: lane (n, g) holds value n of the rank and four columns; dB: column n and four values of the rank
+        float* const out = p.partial + (size_t)slot * p.size + m.at;
+        const float factor = OF_A ? r.drop.factor : r.scales ? r.scales[id] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < VC; ++i)
+#pragma unroll
+            for (int j = 0; j < RT; ++j) {
+                const int c = c0 + 16 * (VC * wave + i) + (OF_A ? 4 * g : n), k = 16 * j + (OF_A ? n : 4 * g);
+                if (c >= wide || k >= r.rank) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] *= factor;
+                *(float4_t*)(out + (OF_A ? (size_t)k * m.K + c : (size_t)r.rank * m.K + (size_t)c * r.rank + k)) = acc[i][j];
+            }
+    };
+    if (!of_a) sweep(std::false_type{}, std::false_type{});
+    else if (masked) sweep(std::true_type{}, std::true_type{});
+    else sweep(std::true_type{}, std::false_type{});
 }
 
 // The gradients of an adapter: the sums of its pieces, in their order.
-__global__ void __launch_bounds__(256) gather_kernel(OuterCall p, int slots) {
+__global__ void __launch_bounds__(256) gather_kernel(OuterCall p) {
     const AdapterRowsDev& r = p.rows;
     const int id = blockIdx.y;
     const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
     if (i >= p.size) return;
     float4_t sum = {0, 0, 0, 0};
-    for (int s = 0; s < slots; ++s)
+    for (int s = 0; s < p.slots; ++s)
         if (p.owner[s] == id) sum += *(const float4_t*)(p.partial + (size_t)s * p.size + i);
     int mat = 0;
     while (mat + 1 < p.n_mats && i >= p.mats[mat + 1].at) ++mat;
@@ -702,26 +771,32 @@ __global__ void __launch_bounds__(256) gather_kernel(OuterCall p, int slots) {
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // Rows of a piece: twice as many while a thousand workgroups are left, since every piece leaves sums of rank (K + N) floats.
 static int cut_of(const AdapterRowsDev& r, long long chunks) {
-    int cut = 256;
-    while (cut < 4096 && pieces(r, 2 * cut) * chunks >= 1024) cut *= 2;
+    static int CUT = getenv("CUT") ? atoi(getenv("CUT")) : 256, CW = getenv("CW") ? atoi(getenv("CW")) : 512;
+    int cut = CUT;
+    while (cut < 4096 && pieces(r, 2 * cut) * chunks >= CW) cut *= 2;
     return cut;
 }
-static long long outer_chunks(const AdapterMatDev* mats, int n) {
+static int outer_chunks(const AdapterRowsDev& r, const AdapterMatDev& m) {
+    const int cols = outer_cols(r.rank);
+    return (m.wide + cols - 1) / cols + (m.depth + cols - 1) / cols;
+}
+static long long outer_chunks(const AdapterRowsDev& r, const AdapterMatDev* mats, int n) {
     long long c = 0;
-    for (int i = 0; i < n; ++i) c += (mats[i].wide + kOuterCols - 1) / kOuterCols + (mats[i].depth + kOuterCols - 1) / kOuterCols;
+    for (int i = 0; i < n; ++i) c += outer_chunks(r, mats[i]);
     return c;
 }
-// What a group of matrices needs: turned weights, g, owners of the pieces, their sums.
+static size_t parts_bytes(const AdapterRowsDev& r) { return (size_t)r.n_tokens * 6 * padded_rank(r.rank); }
+// What a group of matrices needs: turned weights, g and h in parts, owners of the pieces, their sums.
 static size_t group_bytes(const AdapterRowsDev& r, const AdapterMatDev* mats, int n, size_t* turned, size_t* owner) {
     size_t weights = 0, sums = 0;
     for (int i = 0; i < n; ++i) {
         weights += (size_t)r.n_adapters * r.rank * ((size_t)mats[i].wide + mats[i].depth) * 2;
         sums += (size_t)r.rank * ((size_t)mats[i].wide + mats[i].depth) * 4;
     }
-    const size_t slots = (size_t)pieces(r, cut_of(r, outer_chunks(mats, n)));
+    const size_t slots = (size_t)pieces(r, cut_of(r, outer_chunks(r, mats, n)));
     *turned = round16(weights);
     *owner = round16(4 * slots);
-    return *turned + (size_t)n * r.n_tokens * r.rank * 4 + *owner + slots * sums;
+    return *turned + 2 * n * parts_bytes(r) + *owner + slots * sums;
 }
 size_t adapters_backward_workspace_bytes(const AdapterRowsDev& r, const AdapterMatDev* mats, int n_mats) {
     size_t most = 0, a, b;
@@ -732,17 +807,32 @@ bool adapters_backward_fit(const AdapterRowsDev& r, const AdapterMatDev* mats, i
     if (r.n_adapters > 65535) return false;
     for (int i = 0; i < n_mats; i += kAdapterMats) {
         const int n = std::min(kAdapterMats, n_mats - i);
-        const long long chunks = outer_chunks(mats + i, n);
+        const long long chunks = outer_chunks(r, mats + i, n);
         if ((double)pieces(r, cut_of(r, chunks)) * chunks * 256.0 >= 4294967296.0) return false;
         double size = 0;
         for (int j = 0; j < n; ++j) {
             size += (double)r.rank * ((double)mats[i + j].wide + mats[i + j].depth);
             const double tiles = ((r.rank + 63) / 64) * (double)((std::max(mats[i + j].wide, mats[i + j].depth) + 63) / 64);
-            if (tiles * r.n_adapters * (2.0 * n) * 256.0 >= 4294967296.0) return false;
+            if (tiles * r.n_adapters * (3.0 * n) * 256.0 >= 4294967296.0) return false;
         }
         if ((size / 4 + 256) * r.n_adapters >= 4294967296.0) return false;
     }
     return true;
+}
+
+template <bool BF16, int RT>
+static hipError_t sum_tokens(const OuterCall& o, dim3 grid, hipStream_t s) {
+    static std::atomic<unsigned long long> raised{0};
+    static_assert(OuterLds<RT>::bytes <= 160 * 1024, "a unit's LDS");
+    const hipError_t e = raise_lds((const void*)outer_kernel<BF16, RT>, OuterLds<RT>::bytes, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((outer_kernel<BF16, RT>), grid, dim3(256), OuterLds<RT>::bytes, s, o);
+    return hipGetLastError();
+}
+template <bool BF16>
+static hipError_t sum_tokens(const OuterCall& o, dim3 grid, hipStream_t s) {
+    const int rank = o.rows.rank;
+    return rank <= 16 ? sum_tokens<BF16, 1>(o, grid, s) : rank <= 32 ? sum_tokens<BF16, 2>(o, grid, s) : rank <= 64 ? sum_tokens<BF16, 4>(o, grid, s) : sum_tokens<BF16, 8>(o, grid, s);
 }
 
 // mats: x = dy, y = dx, h = g (set here), depth = N, wide = K, p = b, q = a; grads: what else a matrix has.
@@ -755,11 +845,11 @@ static hipError_t backward_group(const AdapterRowsDev& rows, const AdapterMatDev
     OuterCall o{};
     o.rows = rows; o.n_mats = n; o.first = (uint32_t)first;
     uint16_t* weights = (uint16_t*)workspace;
-    float* g = (float*)(workspace + turned);
-    o.owner = (int*)((char*)g + (size_t)n * rows.n_tokens * rows.rank * 4);
+    char* parts = workspace + turned;
+    o.owner = (int*)(parts + 2 * n * parts_bytes(rows));
     o.partial = (float*)((char*)o.owner + owner);
     TurnCall turn{};
-    turn.rows = rows;
+    turn.rows = rows; turn.n_mats = n;
     unsigned tiles = 0;
     for (int i = 0; i < n; ++i) {
         AdapterMatDev& m = c.mats[i].m;
@@ -773,31 +863,25 @@ static hipError_t backward_group(const AdapterRowsDev& rows, const AdapterMatDev
             weights += (size_t)rows.n_adapters * rows.rank * length;
             tiles = std::max(tiles, (unsigned)((rows.rank + 63) / 64) * (unsigned)((length + 63) / 64));
         }
-        m.h = g + (size_t)i * rows.n_tokens * rows.rank;
+        m.h = (float*)parts; parts += parts_bytes(rows);
+        turn.h[i] = grads[i].h; turn.h_parts[i] = (uint16_t*)parts; parts += parts_bytes(rows);
         OuterMatDev& d = o.mats[i];
-        d.x = grads[i].x; d.x_stride = grads[i].x_stride; d.dy = m.x; d.dy_stride = m.x_stride; d.g = m.h; d.h = grads[i].h;
+        d.x = grads[i].x; d.x_stride = grads[i].x_stride; d.dy = m.x; d.dy_stride = m.x_stride; d.g = (uint16_t*)m.h; d.h = turn.h_parts[i];
         d.da = grads[i].da; d.db = grads[i].db; d.K = m.wide; d.N = m.depth;
-        d.at = o.size; d.chunks = (d.K + kOuterCols - 1) / kOuterCols + (d.N + kOuterCols - 1) / kOuterCols;
+        d.at = o.size; d.chunks = outer_chunks(rows, m);
         o.size += (size_t)rows.rank * ((size_t)d.K + d.N);
         o.chunks += d.chunks;
         if (!m.y) m.wide = 0;
     }
-    hipLaunchKernelGGL(turn_kernel, dim3(tiles, rows.n_adapters, 2 * n), dim3(256), 0, s, turn);
+    hipLaunchKernelGGL(turn_kernel, dim3(tiles, rows.n_adapters, 3 * n), dim3(256), 0, s, turn);
     const hipError_t e = launch_products(c, n, dt, s);
     if (e != hipSuccess) return e;
     o.cut = cut_of(rows, o.chunks);
-    const long long slots = pieces(rows, o.cut);
-    const dim3 grid((unsigned)(slots * o.chunks));
-    auto outer = [&](auto bf16) {
-        constexpr bool BF16 = decltype(bf16)::value;
-        if (rows.rank <= 16) hipLaunchKernelGGL((outer_kernel<BF16, 1>), grid, dim3(256), 0, s, o);
-        else if (rows.rank <= 32) hipLaunchKernelGGL((outer_kernel<BF16, 2>), grid, dim3(256), 0, s, o);
-        else if (rows.rank <= 64) hipLaunchKernelGGL((outer_kernel<BF16, 4>), grid, dim3(256), 0, s, o);
-        else hipLaunchKernelGGL((outer_kernel<BF16, 8>), grid, dim3(256), 0, s, o);
-    };
-    if (dt == DT_BF16) outer(std::true_type{});
-    else outer(std::false_type{});
-    hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((o.size / 4 + 255) / 256), rows.n_adapters), dim3(256), 0, s, o, (int)slots);
+    o.slots = (int)pieces(rows, o.cut);
+    const dim3 grid((unsigned)o.slots * o.chunks);
+    const hipError_t summed = dt == DT_BF16 ? sum_tokens<true>(o, grid, s) : sum_tokens<false>(o, grid, s);
+    if (summed != hipSuccess) return summed;
+    hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((o.size / 4 + 255) / 256), rows.n_adapters), dim3(256), 0, s, o);
     return hipGetLastError();
 }
 hipError_t launch_adapters_backward(const AdapterRowsDev& rows, const AdapterMatDev* mats, const AdapterGradDev* grads, int n_mats, int dt,

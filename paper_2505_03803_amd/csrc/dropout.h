@@ -22,6 +22,7 @@ __device__ __forceinline__ uint4_t philox(uint4_t c, uint32_t k0, uint32_t k1) {
 // rate of an addition) stays behind what memory takes.
 struct Keeper {
     uint32_t k0, k1, n0, n1, limit;
+    Keeper() = default;
     __device__ __forceinline__ explicit Keeper(const Dropout& d) {
         const uint64_t key = d.seed[0], number = d.seed[1] + d.call;
         k0 = (uint32_t)key; k1 = (uint32_t)(key >> 32);
