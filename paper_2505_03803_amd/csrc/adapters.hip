@@ -4,7 +4,6 @@
 #include "matrix_core.h"
 #include "pieces.h"
 
-#include <stdlib.h>
 #include <type_traits>
 
 namespace rwkvq {
@@ -63,33 +62,39 @@ __device__ __forceinline__ int adapter_of(const AdapterRowsDev& r, int b) {
     const int a = r.adapters ? r.adapters[b] : 0;
     return a >= 0 && a < r.n_adapters ? a : -1;
 }
-// Piece number `slot` of a call: up to `cut` rows of one sequence.  With offsets sequence b has the numbers from offsets[b] / cut + b on, one more than
-// it needs at times: then t0 >= t1.  Every thread of the workgroup calls it.
-struct RowSpan { int b, t0, t1; };
-__device__ __forceinline__ RowSpan piece_of(const AdapterRowsDev& r, int cut, int slot, int* found) {
+// Piece number `slot` of a call: up to `cut` rows of one sequence, its adapter and the adapter's scale.  With offsets sequence b has the numbers from
+// offsets[b] / cut + b on, one more than it needs at times: then t0 >= t1.  Every thread of the workgroup calls it; the one that finds the sequence
+// reads what else there is to know, for all.
+struct RowSpan { int t0, t1, id; float scale; };
+__device__ __forceinline__ RowSpan span_of_sequence(const AdapterRowsDev& r, int cut, int b, int idx, int t0, int t1) {
     RowSpan s;
-    int idx;
-    if (r.offsets) {
-        if (threadIdx.x == 0) *found = -1;
-        __syncthreads();
-        for (int b = threadIdx.x; b < r.n_seqs; b += blockDim.x) {
-            int t0, t1;
-            rows_of(r, b, t0, t1);
-            if (slot >= t0 / cut + b && slot <= t1 / cut + b) *found = b;
-        }
-        __syncthreads();
-        s.b = __builtin_amdgcn_readfirstlane(*found);
-        if (s.b < 0) { s.t0 = s.t1 = 0; return s; }
-        rows_of(r, s.b, s.t0, s.t1);
-        idx = slot - (s.t0 / cut + s.b);
-    } else {
-        const int per = (r.n_tokens / r.n_seqs + cut - 1) / cut;
-        s.b = slot / per;
-        rows_of(r, s.b, s.t0, s.t1);
-        idx = slot - s.b * per;
+    s.t0 = min(t0 + idx * cut, t1);                // idx cut <= n_tokens
+    s.t1 = min(s.t0 + cut, t1);
+    s.id = s.t0 < s.t1 ? adapter_of(r, b) : -1;
+    s.scale = s.id >= 0 && r.scales ? r.scales[s.id] : 1.0f;
+    return s;
+}
+__device__ __forceinline__ RowSpan piece_of(const AdapterRowsDev& r, int cut, int slot, RowSpan* found) {
+    if (!r.offsets) {
+        const int per = (r.n_tokens / r.n_seqs + cut - 1) / cut, b = slot / per;
+        int t0, t1;
+        rows_of(r, b, t0, t1);
+        return span_of_sequence(r, cut, b, slot - b * per, t0, t1);
     }
-    s.t0 = min(s.t0 + idx * cut, s.t1);            // idx cut <= n_tokens
-    s.t1 = min(s.t0 + cut, s.t1);
+    if (threadIdx.x == 0) *found = RowSpan{0, 0, -1, 1.0f};
+    __syncthreads();
+    for (int b = threadIdx.x; b < r.n_seqs; b += blockDim.x) {
+        int t0, t1;
+        rows_of(r, b, t0, t1);
+        const int first = t0 / cut + b;
+        if (slot >= first && slot <= t1 / cut + b) *found = span_of_sequence(r, cut, b, slot - first, t0, t1);
+    }
+    __syncthreads();
+    RowSpan s;
+    s.t0 = __builtin_amdgcn_readfirstlane(found->t0);
+    s.t1 = __builtin_amdgcn_readfirstlane(found->t1);
+    s.id = __builtin_amdgcn_readfirstlane(found->id);
+    s.scale = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(found->scale)));
     return s;
 }
 static long long pieces(const AdapterRowsDev& r, int cut) {
@@ -174,7 +179,7 @@ template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
     static constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;                      // bytes of a row of h's parts
     static constexpr int CG = RT <= 4 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
-    static constexpr int D = RT == 1 && MT == 1 ? 2 : 1;                                              // steps of 64 columns on their way
+    static constexpr int D = RT == 1 && MT == 1 ? 2 : 1;                                            // steps of 64 columns on their way
     static constexpr int step = 128 * (ROWS + R), ring = W * D * step;
     static constexpr int sums = W / 2 * ROWS * PITCH * 4, out = 16 * YPITCH * 4;                      // out: of a wavefront
     static constexpr int q = sums > W * out ? sums : W * out, q_tile = CG * R * 2;                    // sums and out share a place
@@ -194,18 +199,18 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     Gathered& gathered = *(Gathered*)(lds + L::gathered);
     int count, t0, id;
+    float scale = 1.0f;
     if constexpr (GATHER) {
         t0 = blockIdx.x;
         id = adapter_of(r, t0);
         count = gather_rows(r, t0, id, gathered);
+        if (id >= 0 && r.scales) scale = r.scales[id];
     } else {
-        const RowSpan s = piece_of(r, ROWS, blockIdx.x, (int*)(lds + L::found));
-        t0 = s.t0; count = s.t1 - s.t0;
-        id = count > 0 ? adapter_of(r, s.b) : -1;
+        const RowSpan s = piece_of(r, ROWS, blockIdx.x, (RowSpan*)(lds + L::found));
+        t0 = s.t0; count = s.t1 - s.t0; id = s.id; scale = s.scale;
     }
     if (count <= 0) return;
     auto row_at = [&](int i) -> long long { return GATHER ? gathered.rows[min(i, count - 1)] : t0 + min(i, count - 1); };
-    const float scale = id >= 0 && r.scales ? r.scales[id] : 1.0f;
     const float before = p.backward ? scale : r.drop.factor, behind = p.backward ? r.drop.factor : scale;
     Dropout drop = r.drop;
     drop.call += blockIdx.z + p.first;
@@ -266,11 +271,10 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
             for (int i = 0; i < 2 * RT; ++i) copy_to_lds(P + (size_t)(8 * i < r.rank ? 8 * i : 0) * m.depth + (p_row + k[i & 1]), at + 1024 * (2 * MT + i));
         };
-        const int steps = (m.depth - 64 * wave + 64 * W - 1) / (64 * W);     // of this wavefront; copies go on behind them, to keep the count
-        if (steps > 0) {
+        const int steps = (m.depth - 64 * wave + 64 * W - 1) / (64 * W);     // of this wavefront
 #pragma unroll
-            for (int st = 0; st < D; ++st) fetch(st);
-        }
+        for (int st = 0; st < D; ++st)
+            if (st < steps) fetch(st);
         for (int st = 0; st < steps; ++st) {
             const char* const at = ring + st % D * L::step;
             uint4_t xf[2][MT], pf[2][RT];
@@ -281,7 +285,8 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) keep[h][i] = keeper.bits((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
-            wait_copies<2 * (MT + RT) * (D - 1)>();
+            if (st + D <= steps) wait_copies<2 * (MT + RT) * (D - 1)>();     // all but those of the D - 1 steps behind this one
+            else wait_copies<0>();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int place = ((4 * h + g) ^ swizzle<8>(n)) << 4;
@@ -291,7 +296,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
                 for (int j = 0; j < RT; ++j) pf[h][j] = *(const uint4_t*)(at + (16 * (MT + j) + n) * 128 + place);
             }
             wait_lds();
-            fetch(st + D);
+            if (st + D < steps) fetch(st + D);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -635,8 +640,8 @@ __global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
     int chunk = blockIdx.x / p.slots, mat = 0;
     while (chunk >= p.mats[mat].chunks) chunk -= p.mats[mat++].chunks;
     const OuterMatDev m = p.mats[mat];
-    const RowSpan s = piece_of(r, p.cut, slot, (int*)(lds + L::found));
-    const int id = s.t0 < s.t1 ? adapter_of(r, s.b) : -1;
+    const RowSpan s = piece_of(r, p.cut, slot, (RowSpan*)(lds + L::found));
+    const int id = s.id;
     if (blockIdx.x < p.slots && threadIdx.x == 0) p.owner[slot] = id;
     if (id < 0) return;
     const int x_chunks = (m.K + COLS - 1) / COLS;
@@ -734,7 +739,7 @@ __global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
         }
         // dA: lane (n, g) holds value n of the rank and four columns; dB: column n and four values of the rank
         float* const out = p.partial + (size_t)slot * p.size + m.at;
-        const float factor = OF_A ? r.drop.factor : r.scales ? r.scales[id] : 1.0f;
+        const float factor = OF_A ? r.drop.factor : s.scale;
 #pragma unroll
         for (int i = 0; i < VC; ++i)
 #pragma unroll
@@ -769,11 +774,11 @@ __global__ void __launch_bounds__(256) gather_kernel(OuterCall p) {
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
-// Rows of a piece: twice as many while a thousand workgroups are left, since every piece leaves sums of rank (K + N) floats.
+// Rows of a piece: 64, and twice as many while two workgroups a compute unit are left, since every piece leaves sums of rank (K + N) floats (gradients of 8192
+// rows at rank 64: pieces of 256 rows 146 us, of 512 123, of 1024 132).
 static int cut_of(const AdapterRowsDev& r, long long chunks) {
-    static int CUT = getenv("CUT") ? atoi(getenv("CUT")) : 256, CW = getenv("CW") ? atoi(getenv("CW")) : 512;
-    int cut = CUT;
-    while (cut < 4096 && pieces(r, 2 * cut) * chunks >= CW) cut *= 2;
+    int cut = 64;
+    while (cut < 4096 && pieces(r, 2 * cut) * chunks >= 512) cut *= 2;
     return cut;
 }
 static int outer_chunks(const AdapterRowsDev& r, const AdapterMatDev& m) {
@@ -813,7 +818,7 @@ bool adapters_backward_fit(const AdapterRowsDev& r, const AdapterMatDev* mats, i
         for (int j = 0; j < n; ++j) {
             size += (double)r.rank * ((double)mats[i + j].wide + mats[i + j].depth);
             const double tiles = ((r.rank + 63) / 64) * (double)((std::max(mats[i + j].wide, mats[i + j].depth) + 63) / 64);
-            if (tiles * r.n_adapters * (3.0 * n) * 256.0 >= 4294967296.0) return false;
+            if (std::max(tiles, 512.0) * r.n_adapters * (3.0 * n) * 256.0 >= 4294967296.0) return false;
         }
         if ((size / 4 + 256) * r.n_adapters >= 4294967296.0) return false;
     }
@@ -873,6 +878,7 @@ static hipError_t backward_group(const AdapterRowsDev& rows, const AdapterMatDev
         o.chunks += d.chunks;
         if (!m.y) m.wide = 0;
     }
+    tiles = std::max(tiles, (unsigned)std::min<long long>(512, ((long long)rows.n_tokens * (padded_rank(rows.rank) / 4) + 255) / 256));
     hipLaunchKernelGGL(turn_kernel, dim3(tiles, rows.n_adapters, 3 * n), dim3(256), 0, s, turn);
     const hipError_t e = launch_products(c, n, dt, s);
     if (e != hipSuccess) return e;

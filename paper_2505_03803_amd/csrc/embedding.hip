@@ -46,7 +46,6 @@ hipError_t launch_embedding(EmbeddingDev p, int tdt, int odt, hipStream_t s) {
 
 constexpr int kSortTile = 8192;               // tokens whose order is found by counting
 constexpr int kRankRows = 32;                 // of which a workgroup takes so many
-constexpr int kAbsentRows = 16;               // rows of the table that a wavefront looks for among the tokens
 
 __device__ __forceinline__ uint32_t key_of(const EmbeddingDev& p, int i) {
     const int token = p.tokens[i];
@@ -55,7 +54,7 @@ __device__ __forceinline__ uint32_t key_of(const EmbeddingDev& p, int i) {
 
 // The place of a token among those of its tile: how many are smaller, or equal and in front of it.  A workgroup takes 32 tokens, each in two lanes of
 // every wavefront; its sixteen wavefronts compare them with a sixteenth of the tile each, four keys a read from LDS, a half of the lanes every
-// other four.  Two vector instructions a pair: 8192 tokens are 2.1 million of them, 8000 cycles of the device.
+// other four.  Two vector instructions a pair and a read from LDS for every four: 8192 tokens 10.7 us.
 __global__ void __launch_bounds__(1024) rank_kernel(EmbeddingDev p) {
     __shared__ __align__(16) uint32_t others[16][kSortTile / 16];
     __shared__ int counts[16][64];
@@ -169,33 +168,34 @@ struct Columns {
                 }
             }
     }
-    // a row of the table: its sum times the scale, added to what is there if asked for
-    __device__ __forceinline__ void store_row(const EmbeddingDev& p, uint32_t key, float (&sum)[8]) const {
-        float old[8];
+    // a row of the table: its sum times the scale, added to what was there if asked for
+    __device__ __forceinline__ void store_row(const EmbeddingDev& p, uint32_t key, float (&sum)[8], const float (&old)[8]) const {
         const long long row = (long long)key * d;
-        if (p.accumulate) load_sums(old, p.dtable, row);
 #pragma unroll
         for (int c = 0; c < 8; ++c) sum[c] = p.accumulate ? fmaf(p.scale, sum[c], old[c]) : p.scale * sum[c];
         store_sums(p.dtable, row, sum);
     }
 };
-struct RunPlan { int tile, tiles, chunks, units; };    // sorted places of a wavefront, how many such, 512 columns each, wavefronts in all
+// Sorted places of a wavefront, how many such, of how many times 512 columns, in all; rows of the table that a wavefront looks for among the tokens.
+struct RunPlan { int tile, tiles, chunks, units, rows; };
 
 // The sums of the runs that begin and end in a tile of sorted places go to their rows; of a run that goes on behind the tile, or began in front of
 // it, the tile leaves its part: [tile][0] where it began in front, [tile][1] where it begins here.  A wavefront takes 512 columns and has eight
-// rows on their way.  Other wavefronts of the launch write zeros to rows of no token.
+// rows on their way.  Other wavefronts of the launch write zeros to rows of no token.  What bounds it: the table's writing (8192 tokens, 65536 rows of 4096: 1.14 GB
+// in 220 us, 5.2 TB/s).  Clearing the whole table in front, 16 KiB a workgroup, takes 156 us, but leaves its last 256 MB to be written while the sums run: 251 us in all
+// against 244.
 template <int DT_, int V>
-__global__ void __launch_bounds__(256) run_kernel(EmbeddingDev p, RunPlan plan) {
-    const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+__global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, RunPlan plan) {
+    const int lane = threadIdx.x, unit = blockIdx.x;
     if (unit >= plan.units) {
-        const int first = (unit - plan.units) * kAbsentRows, row = first + lane;
+        const int first = (unit - plan.units) * plan.rows, row = first + lane;
         bool absent = false;
-        if (lane < kAbsentRows && row < p.vocab) {
+        if (lane < plan.rows && row < p.vocab) {
             const int at = below(p.keys, 0, p.n_tokens, (uint32_t)row, false);
             absent = at == p.n_tokens || p.keys[at] != (uint32_t)row;
         }
         const uint64_t which = p.accumulate ? 0 : __builtin_amdgcn_ballot_w64(absent);
-        for (int r = 0; r < kAbsentRows; ++r) {
+        for (int r = 0; r < plan.rows; ++r) {
             if (!(which >> r & 1)) continue;
             float* const to = p.dtable + (size_t)(first + r) * p.d;
             if (p.d % 4 == 0)
@@ -212,13 +212,17 @@ __global__ void __launch_bounds__(256) run_kernel(EmbeddingDev p, RunPlan plan) 
     const uint32_t front = i0 > 0 ? p.keys[i0 - 1] : 0xFFFFFFFFu, behind = i1 < p.n_tokens ? p.keys[i1] : 0xFFFFFFFFu;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int i = i0; i < i1; i += 8) {
-        float x[8][8];
+        float x[8][8], old[8][8];
         uint32_t key[9];
 #pragma unroll
         for (int j = 0; j < 9; ++j) key[j] = i + j < i1 ? p.keys[i + j] : i + j == i1 ? behind : 0xFFFFFFFFu;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (i + j < i1 && key[j] < none) cols.load(x[j], p.out, p.order[i + j] * p.out_stride);
+        if (p.accumulate)                                             // rows that end here: asked for before the first is needed
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i + j < i1 && key[j] < none && key[j] != key[j + 1] && key[j] != front) cols.load_sums(old[j], p.dtable, (long long)key[j] * p.d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (i + j >= i1 || key[j] >= none) break;
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(256) run_kernel(EmbeddingDev p, RunPlan plan) 
             if (!last && key[j + 1] == key[j]) continue;
             const bool before = key[j] == front, after = last && behind == key[j];
             if (before || after) cols.store_sums(p.partial, ((long long)tile * 2 + !before) * p.d, sum);
-            else cols.store_row(p, key[j], sum);
+            else cols.store_row(p, key[j], sum, old[j]);
 #pragma unroll
             for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
         }
@@ -244,6 +248,9 @@ __global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, RunPlan plan) 
     if (i1 >= p.n_tokens) return;
     const uint32_t key = p.keys[i1 - 1];
     if (key >= (uint32_t)p.vocab || p.keys[i1] != key || (i0 > 0 && p.keys[i0 - 1] == key)) return;
+    float sum[8], old[8];
+    cols.load_sums(sum, p.partial, ((long long)tile * 2 + 1) * p.d);
+    if (p.accumulate) cols.load_sums(old, p.dtable, (long long)key * p.d);
     int last = tile;                                             // the last tile that begins with the run
     for (bool on = true; on;) {
         const int next = last + 1 + lane;
@@ -251,8 +258,6 @@ __global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, RunPlan plan) 
         on = same == ~0ull;
         last += on ? 64 : __builtin_ctzll(~same);
     }
-    float sum[8];
-    cols.load_sums(sum, p.partial, ((long long)tile * 2 + 1) * p.d);
 #pragma unroll 8
     for (int t = tile + 1; t <= last; ++t) {
         float x[8];
@@ -260,7 +265,7 @@ __global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, RunPlan plan) 
 #pragma unroll
         for (int c = 0; c < 8; ++c) sum[c] += x[c];
     }
-    cols.store_row(p, key, sum);
+    cols.store_row(p, key, sum, old);
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
@@ -278,14 +283,16 @@ size_t embedding_backward_workspace_bytes(int n_tokens, int d) {
     const size_t list = round16(4 * (size_t)n_tokens);
     return (n_tokens > kSortTile ? 4 : 2) * list + (size_t)run_plan(n_tokens, d).tiles * 2 * d * 4;
 }
+// Rows of the table of a wavefront: 64 where that makes a thousand wavefronts (65536 rows of 4096: 244 us, with 16 rows 251), otherwise 16.
+static int absent_rows(int vocab) { return vocab >= 65536 ? 64 : 16; }
 bool embedding_backward_fits(int n_tokens, int vocab, int d) {
     const double units = (double)((n_tokens + 31) / 32) * ((d + 511) / 512);       // where there are many
-    return (units + vocab / kAbsentRows + 8) * 64.0 < 4294967296.0;
+    return (units + vocab / absent_rows(vocab) + 8) * 64.0 < 4294967296.0;
 }
 template <int DT_, int V>
 static void sum_runs(const EmbeddingDev& p, const RunPlan& plan, hipStream_t s) {
-    const unsigned absent = p.accumulate ? 0 : (unsigned)(p.vocab + kAbsentRows - 1) / kAbsentRows;
-    hipLaunchKernelGGL((run_kernel<DT_, V>), dim3((plan.units + absent + 3) / 4), dim3(256), 0, s, p, plan);
+    const unsigned absent = p.accumulate ? 0 : (unsigned)(p.vocab + plan.rows - 1) / plan.rows;
+    hipLaunchKernelGGL((run_kernel<DT_, V>), dim3(plan.units + absent), dim3(64), 0, s, p, plan);
     if (plan.tiles > 1) hipLaunchKernelGGL(join_kernel<V == 8 ? 4 : V>, dim3((unsigned)plan.units), dim3(64), 0, s, p, plan);
 }
 hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hipStream_t s) {
@@ -301,7 +308,8 @@ hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hi
     p.partial = (float*)at;
     hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(p.n_tokens + kRankRows - 1) / kRankRows), dim3(1024), 0, s, p);
     if (p.n_tokens > kSortTile) hipLaunchKernelGGL(merge_kernel, dim3((p.n_tokens + 255) / 256), dim3(256), 0, s, p);
-    const RunPlan plan = run_plan(p.n_tokens, p.d);
+    RunPlan plan = run_plan(p.n_tokens, p.d);
+    plan.rows = absent_rows(p.vocab);
     const int unit = dt == DT_F32 ? 4 : 8;
     const bool whole = p.d % unit == 0 && p.out_stride % unit == 0;
     switch (dt) {

@@ -8,6 +8,10 @@ sequences at once, one token of each (also as a HIP graph), and the gradients of
     z    = norm(o; heads)                                   rwkvq_layer_norm, a group for each head
     out  = Deq(W_o) (sigma(g) z)                            rwkvq_sigmoid_gate, rwkvq_linear_dispatch
 
+Beside the five matrices there may be a pool of low-rank adapters (Adapters), of which a plan gives one to each sequence, or none:
+
+    r, k, v, g += s_a B_ap (A_ap drop(x_p)),  out += s_a B_ao (A_ao drop(sigma(g) z))       rwkvq_adapters
+
 python -m paper_2505_03803_amd.time_mix [--d 4096] [--heads 64] [--tokens 2048] [--steps 64] runs it on synthetic weights."""
 from __future__ import annotations
 
@@ -25,14 +29,34 @@ PROJECTIONS = ("r", "k", "v", "g")
 TYPES = {B.F16: torch.float16, B.BF16: torch.bfloat16}
 
 
+class Adapters:
+    """A pool of n low-rank adapters for each projection of a block of width d: a [n][rank][d] and b [n][d][rank] of the block's type by
+    projection, scales float32 [n].  p: dropout in front of them, in plans that ask for it; `seeds` holds the key and the number of the
+    next call of the first four and of the last one, and advance() moves both on to other masks, also in a captured graph."""
+
+    def __init__(self, d: int, n: int, rank: int, dtype: int = B.F16, p: float = 0.0, seed: int = 0, device: str = "cuda:0"):
+        self.n, self.rank, self.p = n, rank, p
+        gen = torch.Generator().manual_seed(seed)
+        kind = TYPES[dtype]
+        # as adapters begin: A random, B zero, so that a block without training is the block
+        self.a = {q: (torch.randn(n, rank, d, generator=gen) * d ** -0.5).to(kind).to(device) for q in PROJECTIONS + ("o",)}
+        self.b = {q: torch.zeros(n, d, rank, dtype=kind, device=device) for q in PROJECTIONS + ("o",)}
+        self.scales = torch.ones(n, device=device)
+        self.seeds = torch.tensor([[seed, 0], [seed, len(PROJECTIONS)]], dtype=torch.int64, device=device)
+
+    def advance(self) -> None:
+        self.seeds[:, 1] += len(PROJECTIONS) + 1
+
+
 class TimeMix:
     """mats: the quantized matrices r, k, v, g, o (synth.QMatrix, d x d); mus: (indices uint8 [d / 2], codebook uint16 [2^kbits][2])
     of each of r, k, v, g; w: float32 [heads], u: float32 [heads][d / heads]; ln, heads_norm: (weight, bias), float32 [d].
     max_tokens bounds the rows of a call, n_slots is the size of the pool of states."""
+    adapters: Optional[Adapters] = None
 
     def __init__(self, d: int, n_heads: int, mats: Dict[str, synth.QMatrix], mus: Dict[str, Tuple[np.ndarray, np.ndarray]], w, u, ln,
                  heads_norm, n_slots: int, max_tokens: int, kbits: int = 6, dtype: int = B.F16, eps: float = 1e-5,
-                 device: str = "cuda:0"):
+                 device: str = "cuda:0", adapters: Optional[Adapters] = None):
         self.d, self.H, self.D, self.dtype, self.eps, self.kbits = d, n_heads, d // n_heads, dtype, eps, kbits
         self.device, self.n_slots, self.max_tokens = device, n_slots, max_tokens
         self.mats = {p: B.upload(mats[p], device=device) for p in PROJECTIONS + ("o",)}
@@ -47,6 +71,9 @@ class TimeMix:
         self.a, self.o, self.z, self.gated, self.out = rows(5)
         self.mixed, self.proj = rows(4), rows(4)
         self.stats = [torch.empty(max_tokens, n, device=device) for n in (1, 1, self.H, self.H)]
+        if adapters is not None:
+            self.adapters = adapters
+            self.h = {p: torch.empty(max_tokens, adapters.rank, device=device) for p in PROJECTIONS + ("o",)}
         self.dense: Optional[Dict[str, torch.Tensor]] = None
         self.holds = None, None                                     # x and plan of the call whose rows the buffers hold
 
@@ -56,20 +83,47 @@ class TimeMix:
         return B.Heads(len(lens), sum(lens), self.H, self.D, offsets, None if slots is None else i32(list(slots)),
                        0 if slots is None else self.n_slots)
 
-    def plan(self, lens: Sequence[int], slots: Optional[Sequence[int]] = None):
+    def _rows(self, lens: Sequence[int], ids: Sequence[int], drop: bool):
+        """The descriptions of the rows for the adapters of the first four projections and of the last."""
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=self.device)
+        offsets = None if len(set(lens)) == 1 else i32(np.concatenate([[0], np.cumsum(lens)]))
+        pool = self.adapters
+        return [B.AdapterRows(len(lens), sum(lens), pool.n, pool.rank, offsets, i32(list(ids)), pool.scales, seed if drop and pool.p > 0 else None, pool.p)
+                for seed in pool.seeds]
+
+    def plan(self, lens: Sequence[int], slots: Optional[Sequence[int]] = None, adapters: Optional[Sequence[int]] = None, drop: bool = False):
         """What calls of one form share: the sequences' lengths, their slots (None: they begin empty and leave no state), and the
-        workspace.  A captured graph replays one plan.  Each sequence has a slot of the pool to itself."""
+        workspace.  A captured graph replays one plan.  Each sequence has a slot of the pool to itself.  adapters: that of each sequence, -1
+        for none (None: the block without adapters); drop: with dropout in front of them."""
         if min(lens) < 0 or sum(lens) > self.max_tokens:
             raise ValueError(f"sequences of {list(lens)} tokens in a block for at most {self.max_tokens}")
         if slots is not None and (len(slots) != len(lens) or len(set(slots)) != len(lens) or not all(0 <= s < self.n_slots for s in slots)):
             raise ValueError(f"slots {list(slots)} for {len(lens)} sequences in a pool of {self.n_slots}")
+        if adapters is not None and (self.adapters is None or len(adapters) != len(lens) or not all(-1 <= a < self.adapters.n for a in adapters)):
+            raise ValueError(f"adapters {list(adapters)} for {len(lens)} sequences in a block with {self.adapters.n if self.adapters else 0}")
         heads = self._heads(lens, slots)
         n = B.rwkvq_linear_attention_workspace_size(heads)
-        return lens, slots, heads, torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        rows = None if adapters is None else self._rows(lens, adapters, drop)
+        return lens, slots, heads, torch.empty(max(n, 16), dtype=torch.uint8, device=self.device), rows
+
+    def _adapt(self, rows: B.AdapterRows, projections: Sequence[str], xs, ys) -> None:
+        pool = self.adapters
+        table = B.AdapterTable([pool.a[p] for p in projections], [pool.b[p] for p in projections], xs, ys, bases=ys, hs=[self.h[p] for p in projections])
+        B.rwkvq_adapters(rows, table, self.dtype, self.dtype)
+
+    def _adapt_backward(self, rows: B.AdapterRows, projections: Sequence[str], xs, dys, dxs):
+        """Adds the adapters' share to dxs.  -> (da, db) by projection"""
+        pool = self.adapters
+        grads = {p: (torch.empty(pool.a[p].shape, device=self.device), torch.empty(pool.b[p].shape, device=self.device)) for p in projections}
+        table = B.AdapterGradTable([pool.a[p] for p in projections], [pool.b[p] for p in projections], xs, [self.h[p] for p in projections], dys, dxs,
+                                   [grads[p][0] for p in projections], [grads[p][1] for p in projections], bases=dxs)
+        workspace = torch.empty(B.rwkvq_adapters_backward_workspace_size(rows, table), dtype=torch.uint8, device=self.device)
+        B.rwkvq_adapters_backward(rows, table, self.dtype, workspace)
+        return grads
 
     def forward(self, x: torch.Tensor, plan) -> torch.Tensor:
         """x: [tokens][d], the sequences' rows one after the other.  -> [tokens][d], a view that the next call overwrites"""
-        lens, slots, heads, workspace = plan
+        lens, slots, heads, workspace, rows = plan
         T, H, dt = sum(lens), self.H, self.dtype
         self.holds = x, plan
         mean, rstd, head_mean, head_rstd = self.stats
@@ -84,12 +138,16 @@ class TimeMix:
                     last.copy_(self.a[first + n - 1])
             first += n
         B.rwkvq_linear_dispatch(B.DispatchTable([self.mats[p].desc() for p in PROJECTIONS], list(self.mixed), list(self.proj)), T, dt, dt)
+        if rows:
+            self._adapt(rows[0], PROJECTIONS, list(self.mixed), list(self.proj))
         r, k, v, g = self.proj
         state = None if slots is None else self.state
         B.rwkvq_linear_attention(heads, r, k, v, dt, self.w, self.u, state, state, self.o, workspace)
         B.rwkvq_layer_norm(self.o, dt, T, H, self.D, *self.heads_norm, self.eps, self.z, head_mean, head_rstd)
         B.rwkvq_sigmoid_gate(g, self.z, dt, T * self.d, self.gated)
         B.rwkvq_linear_dispatch(B.DispatchTable([self.mats["o"].desc()], [self.gated], [self.out]), T, dt, dt)
+        if rows:
+            self._adapt(rows[1], ("o",), [self.gated], [self.out])
         return self.out[:T]
 
     def capture(self, x: torch.Tensor, plan) -> Callable[[], torch.Tensor]:
@@ -114,9 +172,9 @@ class TimeMix:
         return replay
 
     def backward(self, x: torch.Tensor, dout: torch.Tensor, plan) -> Dict[str, torch.Tensor]:
-        """The gradients behind forward(x, plan), the last call before this one, with a plan without slots: of x, both norms, w and
-        u.  The products with the transposed matrices are taken on their dense copies, made at the first call."""
-        lens, slots, heads, _ = plan
+        """The gradients behind forward(x, plan), the last call before this one, with a plan without slots: of x, both norms, w, u and, where
+        the plan has them, the adapters.  The products with the transposed matrices are taken on their dense copies, made at the first call."""
+        lens, slots, heads, _, rows = plan
         if slots is not None:
             raise ValueError("gradients of sequences that begin with a state of the pool")
         if self.holds[1] is not plan or self.holds[0].data_ptr() != x.data_ptr():        # x itself or a view of its rows
@@ -131,7 +189,9 @@ class TimeMix:
         f32 = lambda *shape: torch.empty(shape, device=self.device)
         scratch = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
 
-        dgated = (dout @ self.dense["o"]).float()
+        dgated = dout @ self.dense["o"]
+        tuned = self._adapt_backward(rows[1], ("o",), [self.gated], [dout.contiguous()], [dgated]) if rows else {}
+        dgated = dgated.float()
         s = torch.sigmoid(g.float())
         dz, dg = (dgated * s).to(kind), (dgated * self.z[:T].float() * s * (1 - s)).to(kind)
         do, dheads_w, dheads_b = like(), f32(d), f32(d)
@@ -144,18 +204,22 @@ class TimeMix:
         starts = np.concatenate([[0], np.cumsum(lens)])
         inner = torch.ones(T, 1, device=self.device)                # 0 at the first token of a sequence: nothing is in front of it
         inner[[int(f) for f, n in zip(starts, lens) if n]] = 0
-        for p, grad, index, book in zip(PROJECTIONS, (dr, dk, dv, dg), self.indices, self.codebooks):
+        through = [grad @ self.dense[p] for p, grad in zip(PROJECTIONS, (dr, dk, dv, dg))]
+        if rows:
+            tuned.update(self._adapt_backward(rows[0], PROJECTIONS, list(self.mixed), [dr, dk, dv, dg], through))
+        for dx, index, book in zip(through, self.indices, self.codebooks):
             mu = book.view(torch.float16).view(-1, 2)[index.long()].reshape(-1).float()
-            dx = (grad @ self.dense[p]).float()
+            dx = dx.float()
             da += mu * dx
             da[:-1] += ((1 - mu) * dx * inner)[1:]
         dx, dln_w, dln_b = like(), f32(d), f32(d)
         B.rwkvq_layer_norm_backward(da.to(kind), x, dt, T, 1, d, self.ln[0], mean, rstd, dx, dln_w, dln_b,
                                     scratch(B.rwkvq_layer_norm_backward_workspace_size(T, 1, d)))
-        return dict(x=dx, ln=(dln_w, dln_b), heads_norm=(dheads_w, dheads_b), w=dw, u=du)
+        return dict(x=dx, ln=(dln_w, dln_b), heads_norm=(dheads_w, dheads_b), w=dw, u=du, adapters=tuned)
 
 
-def synthetic(d: int, n_heads: int, n_slots: int, max_tokens: int, seed: int = 0, dtype: int = B.F16) -> TimeMix:
+def synthetic(d: int, n_heads: int, n_slots: int, max_tokens: int, seed: int = 0, dtype: int = B.F16,
+              adapters: Optional[Adapters] = None) -> TimeMix:
     """A block with random weights of the shapes and spreads of the repository's other synthetic workloads."""
     rng = np.random.default_rng(seed)
     mats = {p: synth.gen_sq(rng, d, d, p) if i % 2 else synth.gen_vq(rng, d, d, 6, p) for i, p in enumerate(PROJECTIONS + ("o",))}
@@ -163,7 +227,18 @@ def synthetic(d: int, n_heads: int, n_slots: int, max_tokens: int, seed: int = 0
     w = np.exp(rng.uniform(-5.0, 1.0, size=n_heads))
     u = 0.5 * rng.standard_normal((n_heads, d // n_heads))
     norms = [(1 + 0.1 * rng.standard_normal(d), 0.1 * rng.standard_normal(d)) for _ in range(2)]
-    return TimeMix(d, n_heads, mats, mus, w, u, norms[0], norms[1], n_slots, max_tokens, dtype=dtype)
+    return TimeMix(d, n_heads, mats, mus, w, u, norms[0], norms[1], n_slots, max_tokens, dtype=dtype, adapters=adapters)
+
+
+def timed(f: Callable[[], object], n: int) -> float:
+    """Seconds of a call, behind one that is not counted."""
+    f()
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    for _ in range(n):
+        f()
+    torch.cuda.synchronize()
+    return (time.perf_counter() - t) / n
 
 
 def main() -> None:
@@ -175,15 +250,6 @@ def main() -> None:
     args = ap.parse_args()
     block = synthetic(args.d, args.heads, 1, args.tokens)
     x = torch.randn(args.tokens, args.d, device="cuda").to(TYPES[block.dtype])
-
-    def timed(f, n):
-        f()
-        torch.cuda.synchronize()
-        t = time.perf_counter()
-        for _ in range(n):
-            f()
-        torch.cuda.synchronize()
-        return (time.perf_counter() - t) / n
 
     prompt = block.plan([args.tokens], [0])
     t = timed(lambda: block.forward(x, prompt), 5)

@@ -1,0 +1,27 @@
+"""CPU-side checks of plans with adapters: those that a block does not have are refused."""
+import types
+
+import pytest
+
+from paper_2505_03803_amd.time_mix import TimeMix
+
+
+def block(n):
+    b = object.__new__(TimeMix)                            # what plan() looks at, without a GPU
+    b.H, b.D, b.max_tokens, b.n_slots, b.device = 2, 64, 40, 5, "cpu"
+    if n:
+        b.adapters = types.SimpleNamespace(n=n, rank=8, p=0.1, scales=None, seeds=[None, None])
+    return b
+
+
+@pytest.mark.parametrize("n,lens,ids", [(0, [3], [0]), (2, [3, 4], [0]), (2, [3, 4], [0, 2]), (2, [3, 4], [-2, 0]), (2, [3], [0, 1]), (2, [3], [2 ** 31])])
+def test_adapters_that_are_refused(n, lens, ids):
+    with pytest.raises(ValueError):
+        block(n).plan(lens, adapters=ids)
+
+
+@pytest.mark.parametrize("lens,ids", [([3, 4], [1, -1]), ([1, 1], [0, 0]), ([40], [1]), ([3, 0, 5], [0, 1, -1])])
+def test_plans(lens, ids):
+    rows = block(2).plan(lens, adapters=ids)[4]
+    assert len(rows) == 2 and all(r.desc.n_adapters == 2 and r.desc.rank == 8 and r.desc.n_tokens == sum(lens) for r in rows)
+    assert block(2).plan(lens)[4] is None
