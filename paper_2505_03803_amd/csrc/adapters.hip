@@ -102,16 +102,6 @@ static long long pieces(const AdapterRowsDev& r, int cut) {
     return (long long)((r.n_tokens / r.n_seqs + cut - 1) / cut) * r.n_seqs;
 }
 
-// Eight 16-bit values of which only those with their bit in `keep` stay.
-__device__ __forceinline__ uint4_t kept(uint4_t v, uint32_t keep) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t k = keep >> (2 * j);
-        v[j] &= ((k & 1) ? 0xFFFFu : 0u) | ((k & 2) ? 0xFFFF0000u : 0u);
-    }
-    return v;
-}
-
 // Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  The
 // workgroup of row b has work if an even sixteen of the rows in front of it have the same adapter, and then takes those of the next sixteen.
 constexpr int kGathered = 2048;                    // rows of such a call at most
@@ -187,7 +177,7 @@ template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int found = ring > after ? ring : after, gathered = found + 16, bytes = gathered + (int)sizeof(Gathered);
 };
 template <bool BF16, int RT, int MT, int PARTS, bool DROP, bool GATHER>
-__global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && PARTS == 3) ? 4 : 2)) adapter_kernel(AdapterCall p) {
+__global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && (PARTS == 3 || DROP)) ? 4 : 2)) adapter_kernel(AdapterCall p) {
     typedef AdapterLds<RT, MT, PARTS> L;
     constexpr int W = L::W, R = L::R, ROWS = L::ROWS, D = L::D, CG = L::CG, CT = CG / 16, QS = RT == 1 ? 1 : RT / 2, QC = R / 8;
     constexpr bool WIDE = PARTS == 3;                                         // y is binary32
@@ -279,12 +269,12 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             const char* const at = ring + st % D * L::step;
             uint4_t xf[2][MT], pf[2][RT];
             const int k0 = 64 * (wave + W * st) + 8 * g;
-            uint32_t keep[2][MT];                                            // while the copies are on their way
+            uint4_t keep[2][MT];                                             // while the copies are on their way
             if (DROP && !p.backward)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) keep[h][i] = keeper.bits((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
+                    for (int i = 0; i < MT; ++i) keep[h][i] = keeper.masks((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
             if (st + D <= steps) wait_copies<2 * (MT + RT) * (D - 1)>();     // all but those of the D - 1 steps behind this one
             else wait_copies<0>();
 #pragma unroll
@@ -302,7 +292,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if (k0 + 32 * h >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
-                    if (DROP && !p.backward) xf[h][i] = kept(xf[h][i], keep[h][i]);
+                    if (DROP && !p.backward) xf[h][i] &= keep[h][i];
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -391,14 +381,14 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             }
         }
     }
-    uint32_t keep[MT][PASS];                                                  // of the next columns
+    uint4_t keep[MT][PASS];                                                   // of the next columns
     auto draw = [&](int c0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < PASS; ++j) keep[i][j] = DROP && p.backward ? keeper.bits((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]) : 0xFFu;
+            for (int j = 0; j < PASS; ++j) keep[i][j] = p.backward ? keeper.masks((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]) : uint4_t{~0u, ~0u, ~0u, ~0u};
     };
-    draw(from + CG * wave);
+    if (DROP) draw(from + CG * wave);
     meet();
     wait_copies<0>();
 
@@ -454,8 +444,9 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
                     const float4_t a = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col)), b = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col + 4));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float z = e < 4 ? a[e & 3] : b[e & 3];
-                        if (!DROP || keep[i][j] >> e & 1) y[e] = BF16 ? y[e] + z : fmaf(z, down, y[e]);
+                        float z = e < 4 ? a[e & 3] : b[e & 3];
+                        if (DROP) z = masked(z, keep[i][j], e);
+                        y[e] = BF16 ? y[e] + z : fmaf(z, down, y[e]);
                     }
                 }
 #pragma unroll
@@ -470,7 +461,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             }
         }
         // memory answers in order: the next rows of Q have to be there, then the next base is asked for, and the stores come last
-        if (more) draw(c0 + CG * W);
+        if (DROP && more) draw(c0 + CG * W);
         wait_copies<0>();
         if (more) fetch_base(c0 + CG * W);
 #pragma unroll
@@ -693,7 +684,7 @@ __global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
 #pragma unroll
             for (int i = 0; i < VN; ++i) {
                 const int row = v_row + APART * i;
-                if (MASKED) vn[i] = kept(vn[i], keeper.bits((uint32_t)col >> 3, (uint32_t)(s.t0 + 32 * st + row)));
+                if (MASKED) vn[i] &= keeper.masks((uint32_t)col >> 3, (uint32_t)(s.t0 + 32 * st + row));
                 *(uint4_t*)(vt + row * VROW + 16 * ((tid % PER) ^ pair_swizzle<8>(row))) = vn[i];
             }
 #pragma unroll
@@ -763,8 +754,16 @@ __global__ void __launch_bounds__(256) gather_kernel(OuterCall p) {
     const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
     if (i >= p.size) return;
     float4_t sum = {0, 0, 0, 0};
-    for (int s = 0; s < p.slots; ++s)
-        if (p.owner[s] == id) sum += *(const float4_t*)(p.partial + (size_t)s * p.size + i);
+    for (int s = 0; s < p.slots; s += 8) {
+        float4_t v[8];                                                       // eight pieces on their way
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = float4_t{0, 0, 0, 0};
+            if (s + j < p.slots && p.owner[s + j] == id) v[j] = *(const float4_t*)(p.partial + (size_t)(s + j) * p.size + i);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += v[j];
+    }
     int mat = 0;
     while (mat + 1 < p.n_mats && i >= p.mats[mat + 1].at) ++mat;
     const OuterMatDev& m = p.mats[mat];

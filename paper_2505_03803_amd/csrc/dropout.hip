@@ -16,12 +16,13 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutDev p) {
         float x[8], y[8];
         load8<DT_>(x, p.x, w.row * p.x_stride + col, left, p.whole);
         if (p.base) load8<DT_>(y, p.base, w.row * p.base_stride + col, left, p.whole);
-        const uint32_t keep = keeper.bits(w.at, w.row);
+        const uint32_t all = ~0u;
+        const uint4_t keep = p.drop.limit ? keeper.masks(w.at, w.row) : uint4_t{all, all, all, all};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool stays = keep >> j & 1;
-            if (p.base) y[j] = stays ? fmaf(x[j], p.drop.factor, y[j]) : y[j];
-            else y[j] = stays ? x[j] * p.drop.factor : 0.0f;
+            const float z = masked(x[j], keep, j);
+            if (p.base) y[j] = masked(1.0f, keep, j) != 0.0f ? fmaf(z, p.drop.factor, y[j]) : y[j];      // -0 stays -0
+            else y[j] = z * p.drop.factor;
         }
         store8<DT_>(p.y, w.row * p.y_stride + col, y, left, p.whole);
     }
