@@ -168,9 +168,9 @@ __device__ __forceinline__ int swizzle(int row) { return (row / (16 / C)) & (C -
 template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
     static constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;                      // bytes of a row of h's parts
-    static constexpr int CG = RT <= 4 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
-    static constexpr int D = RT == 1 && MT == 1 ? 2 : 1;                                            // steps of 64 columns on their way
-    static constexpr int step = 128 * (ROWS + R), ring = W * D * step;
+    static constexpr int CG = RT <= 2 || MT == 2 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
+    static constexpr int CS = RT <= 2 || MT == 2 ? 64 : 32, D = RT == 1 && MT == 1 ? 2 : 1;                      // columns of a step, steps on their way
+    static constexpr int step = 2 * CS * (ROWS + R), ring = W * D * step;
     static constexpr int sums = W / 2 * ROWS * PITCH * 4, out = 16 * YPITCH * 4;                      // out: of a wavefront
     static constexpr int q = sums > W * out ? sums : W * out, q_tile = CG * R * 2;                    // sums and out share a place
     static constexpr int parts = q + W * q_tile, inverse = parts + ROWS * HROW, after = inverse + 4 * ROWS;
@@ -179,7 +179,7 @@ template <int RT, int MT, int PARTS> struct AdapterLds {
 template <bool BF16, int RT, int MT, int PARTS, bool DROP, bool GATHER>
 __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && (PARTS == 3 || DROP)) ? 4 : 2)) adapter_kernel(AdapterCall p) {
     typedef AdapterLds<RT, MT, PARTS> L;
-    constexpr int W = L::W, R = L::R, ROWS = L::ROWS, D = L::D, CG = L::CG, CT = CG / 16, QS = RT == 1 ? 1 : RT / 2, QC = R / 8;
+    constexpr int W = L::W, R = L::R, ROWS = L::ROWS, D = L::D, CS = L::CS, CG = L::CG, CT = CG / 16, QS = RT == 1 ? 1 : RT / 2, QC = R / 8;
     constexpr bool WIDE = PARTS == 3;                                         // y is binary32
     constexpr int PER = CG / 8, PASS = PER / 4;                               // lanes of a row of y, rounds for sixteen rows
     extern __shared__ __align__(16) char lds[];
@@ -245,57 +245,57 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < RT; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
-        // 64 columns of x and P: eight rows a copy, a line of 128 bytes each.  Columns behind the depth repeat the last ones, rows of P behind the rank others
+        // CS columns of x and P, 1 KiB of whole or half lines a copy.  Columns behind the depth repeat the last ones, rows of P behind the rank others
+        constexpr int C = CS / 8, PER_COPY = 64 / C, XC = ROWS / PER_COPY, PC = R / PER_COPY;
         const uint16_t* const P = m.p + (size_t)id * r.rank * m.depth;
-        const uint16_t* x[2 * MT];
+        const uint16_t* x[XC];
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) x[i] = m.x + row_at(8 * i + (lane >> 3)) * m.x_stride;
-        const int p_row = (lane >> 3) * m.depth;
+        for (int i = 0; i < XC; ++i) x[i] = m.x + row_at(PER_COPY * i + lane / C) * m.x_stride;
         char* const ring = lds + wave * D * L::step;
         auto fetch = [&](int st) {
             char* const at = ring + st % D * L::step;
-            auto column = [&](int row) { return min(64 * (wave + W * st) + 8 * ((lane & 7) ^ swizzle<8>(row + (lane >> 3))), m.depth - 8); };
-            const int k[2] = {column(0), column(8)};
+            auto column = [&](int i) { return min(CS * (wave + W * st) + 8 * (lane % C ^ swizzle<C>(PER_COPY * i + lane / C)), m.depth - 8); };
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) copy_to_lds(x[i] + k[i & 1], at + 1024 * i);
+            for (int i = 0; i < XC; ++i) copy_to_lds(x[i] + column(i), at + 1024 * i);
 #pragma unroll
-            for (int i = 0; i < 2 * RT; ++i) copy_to_lds(P + (size_t)(8 * i < r.rank ? 8 * i : 0) * m.depth + (p_row + k[i & 1]), at + 1024 * (2 * MT + i));
+            for (int i = 0; i < PC; ++i)
+                copy_to_lds(P + (size_t)min(PER_COPY * i + lane / C, r.rank - 1) * m.depth + column(i), at + 1024 * (XC + i));
         };
-        const int steps = (m.depth - 64 * wave + 64 * W - 1) / (64 * W);     // of this wavefront
+        const int steps = (m.depth - CS * wave + CS * W - 1) / (CS * W);     // of this wavefront
 #pragma unroll
         for (int st = 0; st < D; ++st)
             if (st < steps) fetch(st);
         for (int st = 0; st < steps; ++st) {
             const char* const at = ring + st % D * L::step;
-            uint4_t xf[2][MT], pf[2][RT];
-            const int k0 = 64 * (wave + W * st) + 8 * g;
-            uint4_t keep[2][MT];                                             // while the copies are on their way
+            uint4_t xf[CS / 32][MT], pf[CS / 32][RT];
+            const int k0 = CS * (wave + W * st) + 8 * g;
+            uint4_t keep[CS / 32][MT];                                       // while the copies are on their way
             if (DROP && !p.backward)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < CS / 32; ++h)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) keep[h][i] = keeper.masks((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
-            if (st + D <= steps) wait_copies<2 * (MT + RT) * (D - 1)>();     // all but those of the D - 1 steps behind this one
+            if (st + D <= steps) wait_copies<(XC + PC) * (D - 1)>();         // all but those of the D - 1 steps behind this one
             else wait_copies<0>();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int place = ((4 * h + g) ^ swizzle<8>(n)) << 4;
+            for (int h = 0; h < CS / 32; ++h) {
+                const int place = ((4 * h + g) ^ swizzle<C>(n)) << 4;
 #pragma unroll
-                for (int i = 0; i < MT; ++i) xf[h][i] = *(const uint4_t*)(at + (16 * i + n) * 128 + place);
+                for (int i = 0; i < MT; ++i) xf[h][i] = *(const uint4_t*)(at + (16 * i + n) * 2 * CS + place);
 #pragma unroll
-                for (int j = 0; j < RT; ++j) pf[h][j] = *(const uint4_t*)(at + (16 * (MT + j) + n) * 128 + place);
+                for (int j = 0; j < RT; ++j) pf[h][j] = *(const uint4_t*)(at + (16 * (MT + j) + n) * 2 * CS + place);
             }
             wait_lds();
             if (st + D < steps) fetch(st + D);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < CS / 32; ++h)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if (k0 + 32 * h >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
                     if (DROP && !p.backward) xf[h][i] &= keep[h][i];
                 }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < CS / 32; ++h)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -494,7 +494,7 @@ static hipError_t products(const AdapterCall& p, bool gather, dim3 grid, hipStre
 template <bool BF16, int RT>
 static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 grid, hipStream_t s) {
     const bool wide = p.y_dt == DT_F32;
-    if constexpr (RT < 8)
+    if constexpr (RT == 2 || RT == 4)
         if (rows == 32) return wide ? products<BF16, RT, 2, 3>(p, gather, grid, s) : products<BF16, RT, 2, 2>(p, gather, grid, s);
     return wide ? products<BF16, RT, 1, 3>(p, gather, grid, s) : products<BF16, RT, 1, 2>(p, gather, grid, s);
 }
@@ -509,28 +509,35 @@ static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 gri
 static bool single_tokens(const AdapterRowsDev& r) {
     return !r.offsets && r.n_tokens == r.n_seqs && r.n_seqs > 1 && r.n_seqs <= kGathered && !r.drop.seed;
 }
-// Rows of a tile.  32 where sequences are long: P and Q are read once for twice as many rows (8192 rows at rank 64: 69 us against 78; 4321 rows of sixteen
-// sequences at rank 32: 82 against 107).  Above rank 64 the registers and LDS of 16 rows are full.
-static int tile_rows(const AdapterRowsDev& r) { return r.n_tokens / r.n_seqs <= 16 || r.rank > 64 ? 16 : 32; }
+// Rows of a tile: 16, of which two workgroups fit a compute unit, one's copies beside the other's products, unless there are enough tiles of 32 as well, or tiles
+// of 16 would take too much of P and Q through the caches.  Measured, 16 against 32 (us): K = N = 4096: 4096 rows at rank 32 30 / 37, 64 40 / 52; 8192 rows at rank
+// 16 45 / 54, 32 49 / 54, 64 76 / 57; 16384 rows at rank 16 82 / 94, 32 92 / 92; K = N = 1024: 16384 rows at rank 32 27 / 24, 64 37 / 31; 4320 rows beside N = 14336:
+// rank 16 79 / 75, 32 107 / 82, 64 130 / 100.  So 32 from 20000 ranks of tiles or 5 2^24 values that tiles of 32 take, never for rank 16.  Above rank 64 the
+// registers of 16 rows are full.
+static int tile_rows(const AdapterCall& p, int n_mats) {
+    const AdapterRowsDev& r = p.rows;
+    if (r.rank <= 16 || r.rank > 64 || r.n_tokens / r.n_seqs <= 16) return 16;
+    double lengths = 0;
+    for (int i = 0; i < n_mats; ++i) lengths += (double)p.mats[i].m.depth + p.mats[i].m.wide;
+    return (double)r.rank * pieces(r, 16) * n_mats > 20000 || r.rank * lengths * pieces(r, 32) > 5 << 24 ? 32 : 16;
+}
 // Columns of a workgroup: all of them where tiles and matrices fill the device, otherwise as many workgroups as one and a half a compute unit, of no fewer than
-// 256 columns.  Every one takes h again: in twos of half the columns 256 tiles of 8192 rows take 95 us instead of 69, those of 256 single tokens
-// 35 instead of 27; 151 tiles beside 14336 columns in one, two and three 98, 97 and 82.
-static int slice_of(const AdapterRowsDev& r, int n_mats, int widest) {
-    long long wgs = pieces(r, tile_rows(r));
+// 256 columns.  Every one takes h again: for 256 single tokens in as many workgroups as two a unit 34 us instead of 26, 4096 rows at rank 64 48 instead of 40;
+// 151 tiles beside 14336 columns in one, two and three 98, 97 and 82.
+static int slice_of(const AdapterRowsDev& r, int rows, int n_mats, int widest) {
+    long long wgs = pieces(r, rows);
     if (single_tokens(r)) wgs = std::min<long long>(wgs, std::max(r.n_adapters, (r.n_seqs + 15) / 16));
     wgs *= n_mats;
     const long long wanted = std::min<long long>((widest + 255) / 256, wgs >= 256 ? 1 : (384 + wgs - 1) / wgs);
     return (int)(((widest + wanted - 1) / wanted + 63) / 64 * 64);
 }
-bool adapters_fit(const AdapterRowsDev& r, int widest) {
-    const int slice = slice_of(r, 1, widest);
-    return (double)pieces(r, tile_rows(r)) * ((widest + slice - 1) / slice) * kAdapterMats * 1024.0 < 4294967296.0;
-}
+// (more than one slice only of fewer than 256 workgroups)
+bool adapters_fit(const AdapterRowsDev& r) { return (double)pieces(r, 16) * 512.0 < 4294967296.0; }
 static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_t s) {
     int widest = 64;                                  // also where no y is asked for
     for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
-    const int rows = tile_rows(p.rows);
-    p.slice = slice_of(p.rows, n_mats, widest);
+    const int rows = tile_rows(p, n_mats);
+    p.slice = slice_of(p.rows, rows, n_mats, widest);
     const dim3 grid((unsigned)pieces(p.rows, rows), (unsigned)((widest + p.slice - 1) / p.slice), (unsigned)n_mats);
     return dt == DT_BF16 ? products<true>(p, rows, single_tokens(p.rows), grid, s) : products<false>(p, rows, single_tokens(p.rows), grid, s);
 }

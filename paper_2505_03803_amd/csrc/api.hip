@@ -776,7 +776,7 @@ static int check_adapter_rows(const rwkvq_adapter_rows* in, AdapterRowsDev* r) {
 static int check_adapter_sizes(const AdapterRowsDev& r, int N, int K) {
     if (N < 1 || K < 1 || N > (1 << 24) || K > (1 << 24)) return RWKVQ_ERR_SHAPE;
     if (N % 8 != 0 || K % 8 != 0) return RWKVQ_ERR_ALIGN;
-    return adapters_fit(r, std::max(N, K)) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
+    return adapters_fit(r) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
 }
 
 int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, int n_mats, int x_dtype, int y_dtype, void* stream) {

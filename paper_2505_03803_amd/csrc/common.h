@@ -302,7 +302,7 @@ struct AdapterGradDev {
     long long x_stride;
 };
 constexpr int kAdapterMats = 8;                    // matrices of a launch
-bool adapters_fit(const AdapterRowsDev& r, int widest);
+bool adapters_fit(const AdapterRowsDev& r);
 hipError_t launch_adapters(const AdapterRowsDev& rows, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s);
 bool adapters_backward_fit(const AdapterRowsDev& r, const AdapterMatDev* mats, int n_mats);
 size_t adapters_backward_workspace_bytes(const AdapterRowsDev& r, const AdapterMatDev* mats, int n_mats);
