@@ -532,7 +532,7 @@ static int slice_of(const AdapterRowsDev& r, int rows, int n_mats, int widest) {
     return (int)(((widest + wanted - 1) / wanted + 63) / 64 * 64);
 }
 // (more than one slice only of fewer than 256 workgroups)
-bool adapters_fit(const AdapterRowsDev& r) { return (double)pieces(r, 16) * 512.0 < 4294967296.0; }
+bool adapters_fit(const AdapterRowsDev& r) { return (double)pieces(r, 16) * kAdapterMats * 512.0 < 4294967296.0; }
 static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_t s) {
     int widest = 64;                                  // also where no y is asked for
     for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
