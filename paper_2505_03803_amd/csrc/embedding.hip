@@ -164,7 +164,10 @@ struct Columns {
                     p[row + at(e)] = f[e];
                 } else {
 #pragma unroll
-                    for (int j = 0; j < V; j += 4) *(float4_t*)(p + row + at(e) + j) = float4_t{f[e * V + j], f[e * V + j + 1], f[e * V + j + 2], f[e * V + j + 3]};
+                    for (int j = 0; j < V; j += 4) {
+                        const float* const v = f + e * V + j;
+                        *(float4_t*)(p + row + at(e) + j) = float4_t{v[0], v[1], v[2], v[3]};
+                    }
                 }
             }
     }
@@ -181,9 +184,9 @@ struct RunPlan { int tile, tiles, chunks, units, rows; };
 
 // The sums of the runs that begin and end in a tile of sorted places go to their rows; of a run that goes on behind the tile, or began in front of
 // it, the tile leaves its part: [tile][0] where it began in front, [tile][1] where it begins here.  A wavefront takes 512 columns and has eight
-// rows on their way.  Other wavefronts of the launch write zeros to rows of no token.  What bounds it: the table's writing (8192 tokens, 65536 rows of 4096: 1.14 GB
-// in 220 us, 5.2 TB/s).  Clearing the whole table in front, 16 KiB a workgroup, takes 156 us, but leaves its last 256 MB to be written while the sums run: 251 us in all
-// against 244.
+// rows on their way.  Other wavefronts of the launch write zeros to rows of no token.  What bounds it: the table's writing (8192 tokens, 65536 rows
+// of 4096: 1.14 GB in 220 us, 5.2 TB/s).  Clearing the whole table in front, 16 KiB a workgroup, takes 156 us, but leaves its last 256 MB to be
+// written while the sums run: 251 us in all against 241.
 template <int DT_, int V>
 __global__ void __launch_bounds__(64) run_kernel(EmbeddingDev p, RunPlan plan) {
     const int lane = threadIdx.x, unit = blockIdx.x;
@@ -268,6 +271,105 @@ __global__ void __launch_bounds__(64) join_kernel(EmbeddingDev p, RunPlan plan) 
     cols.store_row(p, key, sum, old);
 }
 
+// Few tokens, in one launch without sorting: a workgroup takes a token and 512 columns, looks for the token's others, leaves if one is in front of
+// it, and sums the rows of all in the order of their places, shared out to its wavefronts where they are more than 8.  Other workgroups write zeros to
+// rows of no token.  Every workgroup reads all tokens, but nothing waits for a launch in front: 777 tokens of 1023 columns 8.5 us instead of 18.5, 256
+// of 1024 6.6 instead of 15; 1000 of two tokens, the longest runs, 22 instead of 21.  From 2048 workgroups on sorting is faster: 1000 of 4096 columns
+// 20 us instead of 29.
+constexpr int kFewRows = 16, FW = 8;
+template <int DT_, int V>
+__global__ void __launch_bounds__(64 * FW) few_kernel(EmbeddingDev p, RunPlan plan) {
+    __shared__ uint64_t same[64];
+    __shared__ int present[kFewRows];
+    __shared__ float sums[FW - 1][512];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), unit = blockIdx.x;
+    if (unit >= plan.units) {
+        const long long apart = (long long)(gridDim.x - plan.units) * kFewRows;
+        for (long long first = (long long)(unit - plan.units) * kFewRows; first < p.vocab; first += apart) {
+            if (tid < kFewRows) present[tid] = 0;
+            __syncthreads();
+            for (int i = tid; i < p.n_tokens; i += 64 * FW) {
+                const long long at = p.tokens[i] - first;
+                if (at >= 0 && at < kFewRows) present[at] = 1;
+            }
+            __syncthreads();
+            for (int r = 0; r < kFewRows && first + r < p.vocab; ++r) {
+                if (present[r]) continue;
+                float* const to = p.dtable + (size_t)(first + r) * p.d;
+                if (p.d % 4 == 0)
+                    for (int c = 4 * tid; c < p.d; c += 256 * FW) *(float4_t*)(to + c) = float4_t{0, 0, 0, 0};
+                else
+                    for (int c = tid; c < p.d; c += 64 * FW) to[c] = 0.0f;
+            }
+            __syncthreads();
+        }
+        return;
+    }
+    const int i = unit / plan.chunks, words = (p.n_tokens + 63) / 64;
+    const uint32_t key = key_of(p, i);
+    if (key >= (uint32_t)p.vocab) return;
+    for (int w = wave; w < words; w += FW) {
+        const int t = 64 * w + lane;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(t < p.n_tokens && p.tokens[t] == (int)key);
+        if (lane == 0) same[w] = m;
+    }
+    __syncthreads();
+    const uint64_t mine = lane < words ? same[lane] : 0;                        // those of the lane's 64 places
+    const uint64_t earlier = lane < i / 64 ? mine : lane == i / 64 ? mine & ((1ull << (i & 63)) - 1) : 0;
+    if (__builtin_amdgcn_ballot_w64(earlier != 0)) return;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(mine != 0);
+    int count = __popcll(mine);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) count += __shfl_xor(count, o);
+    // the rows of the places in the words of `which`, eight on their way
+    auto run = [&](const Columns<DT_, V>& cols, float (&sum)[8], uint64_t which) {
+        uint64_t m = 0;
+        int w = 0;
+        for (;;) {
+            int at[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!m && which) {
+                    w = __builtin_ctzll(which);
+                    which &= which - 1;
+                    m = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), w) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)mine, w);
+                }
+                at[j] = m ? 64 * w + __builtin_ctzll(m) : -1;
+                m &= m - 1;
+            }
+            if (at[0] < 0) break;
+            float x[8][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at[j] >= 0) cols.load(x[j], p.out, at[j] * p.out_stride);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at[j] >= 0)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) sum[c] += x[j][c];
+        }
+    };
+    const Columns<DT_, V> cols{(unit % plan.chunks) * 512 + V * lane, p.d};
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, old[8];
+    if (p.accumulate && !wave) cols.load_sums(old, p.dtable, (long long)key * p.d);
+    if (count <= 8) {
+        if (wave) return;
+        run(cols, sum, some);
+    } else {
+        const int share = (words + FW - 1) / FW, from = min(share * wave, 63), to = min(share * (wave + 1), 63);
+        run(cols, sum, some & ((1ull << to) - (1ull << from)));
+        if (wave)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sums[wave - 1][64 * c + lane] = sum[c];
+        __syncthreads();
+        if (wave) return;
+        for (int w = 0; w < FW - 1; ++w)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[c] += sums[w][64 * c + lane];
+    }
+    cols.store_row(p, key, sum, old);
+}
+
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // Sorted places of a wavefront: 32, or fewer where that leaves less than 2048 wavefronts.
 static RunPlan run_plan(int n_tokens, int d) {
@@ -279,7 +381,9 @@ static RunPlan run_plan(int n_tokens, int d) {
     r.units = r.tiles * r.chunks;
     return r;
 }
+static bool few(int n_tokens, int d) { return n_tokens <= 1024 && n_tokens * ((d + 511) / 512) <= 2048; }
 size_t embedding_backward_workspace_bytes(int n_tokens, int d) {
+    if (few(n_tokens, d)) return 16;                             // of which nothing is used
     const size_t list = round16(4 * (size_t)n_tokens);
     return (n_tokens > kSortTile ? 4 : 2) * list + (size_t)run_plan(n_tokens, d).tiles * 2 * d * 4;
 }
@@ -291,11 +395,17 @@ bool embedding_backward_fits(int n_tokens, int vocab, int d) {
 }
 template <int DT_, int V>
 static void sum_runs(const EmbeddingDev& p, const RunPlan& plan, hipStream_t s) {
+    if (few(p.n_tokens, p.d)) {
+        const unsigned absent = p.accumulate ? 0 : std::min((p.vocab - 1) / kFewRows + 1, 65536);
+        hipLaunchKernelGGL((few_kernel<DT_, V>), dim3(plan.units + absent), dim3(64 * FW), 0, s, p, plan);
+        return;
+    }
     const unsigned absent = p.accumulate ? 0 : (unsigned)(p.vocab + plan.rows - 1) / plan.rows;
     hipLaunchKernelGGL((run_kernel<DT_, V>), dim3(plan.units + absent), dim3(64), 0, s, p, plan);
     if (plan.tiles > 1) hipLaunchKernelGGL(join_kernel<V == 8 ? 4 : V>, dim3((unsigned)plan.units), dim3(64), 0, s, p, plan);
 }
-hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hipStream_t s) {
+// Keys and places in their order, and where sums of pieces go.
+static void sort_tokens(EmbeddingDev& p, void* workspace, hipStream_t s) {
     char* at = (char*)workspace;
     const size_t list = round16(4 * (size_t)p.n_tokens);
     p.keys = (uint32_t*)at; at += list;
@@ -308,8 +418,16 @@ hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hi
     p.partial = (float*)at;
     hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(p.n_tokens + kRankRows - 1) / kRankRows), dim3(1024), 0, s, p);
     if (p.n_tokens > kSortTile) hipLaunchKernelGGL(merge_kernel, dim3((p.n_tokens + 255) / 256), dim3(256), 0, s, p);
-    RunPlan plan = run_plan(p.n_tokens, p.d);
-    plan.rows = absent_rows(p.vocab);
+}
+hipError_t launch_embedding_backward(EmbeddingDev p, int dt, void* workspace, hipStream_t s) {
+    RunPlan plan{};
+    if (few(p.n_tokens, p.d)) {
+        plan.chunks = (p.d + 511) / 512; plan.units = p.n_tokens * plan.chunks;
+    } else {
+        sort_tokens(p, workspace, s);
+        plan = run_plan(p.n_tokens, p.d);
+        plan.rows = absent_rows(p.vocab);
+    }
     const int unit = dt == DT_F32 ? 4 : 8;
     const bool whole = p.d % unit == 0 && p.out_stride % unit == 0;
     switch (dt) {

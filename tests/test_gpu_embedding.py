@@ -82,6 +82,17 @@ def test_gradient(T, V, d, spread, added):
     check_gradient(SPREADS[spread](rng, T, V), T, V, d, dt, 1.0 if T % 2 else 0.3, added, d + (7 if d % 2 else 8))
 
 
+# at the border between few tokens, taken without sorting, and more: 1024 of them, or 2048 pieces of 512 columns
+@pytest.mark.parametrize("T,V,d", [(1024, 200, 1024), (1024, 90, 1025), (1025, 200, 33), (1025, 64, 512), (700, 50, 1501), (300, 40, 4096), (1024, 3, 3),
+                                   (5, 40000, 72)])
+@pytest.mark.parametrize("spread", ["same", "few", "zipf", "padded"])
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+def test_gradient_of_few_tokens(T, V, d, spread, dt):
+    rng = np.random.default_rng(T + V + d)
+    torch.manual_seed(T + d)
+    check_gradient(SPREADS[spread](rng, T, V), T, V, d, dt, 0.3, dt == "bf16")
+
+
 @pytest.mark.parametrize("T", [8192, 8193, 16384, 20011])
 @pytest.mark.parametrize("spread", ["same", "zipf", "padded", "down"])
 def test_gradient_of_many_tokens(T, spread):
