@@ -169,7 +169,7 @@ template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
     static constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;                      // bytes of a row of h's parts
     static constexpr int CG = RT <= 2 || MT == 2 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
-    static constexpr int CS = RT <= 2 || MT == 2 ? 64 : 32, D = RT == 1 && MT == 1 ? 2 : 1;                      // columns of a step, steps on their way
+    static constexpr int CS = RT <= 2 || MT == 2 ? 64 : 32, D = RT == 1 ? 2 : 1;                      // columns of a step, steps on their way
     static constexpr int step = 2 * CS * (ROWS + R), ring = W * D * step;
     static constexpr int sums = W / 2 * ROWS * PITCH * 4, out = 16 * YPITCH * 4;                      // out: of a wavefront
     static constexpr int q = sums > W * out ? sums : W * out, q_tile = CG * R * 2;                    // sums and out share a place
@@ -252,23 +252,25 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
         for (int i = 0; i < XC; ++i) x[i] = m.x + row_at(PER_COPY * i + lane / C) * m.x_stride;
         char* const ring = lds + wave * D * L::step;
+        // 64 columns for every wavefront, then the next, whatever a step has of them: tiles of either size add in one order
+        auto first = [&](int st) { return CS == 64 ? 64 * (wave + W * st) : 64 * (wave + W * (st >> 1)) + 32 * (st & 1); };
         auto fetch = [&](int st) {
             char* const at = ring + st % D * L::step;
-            auto column = [&](int i) { return min(CS * (wave + W * st) + 8 * (lane % C ^ swizzle<C>(PER_COPY * i + lane / C)), m.depth - 8); };
+            auto column = [&](int i) { return min(first(st) + 8 * (lane % C ^ swizzle<C>(PER_COPY * i + lane / C)), m.depth - 8); };
 #pragma unroll
             for (int i = 0; i < XC; ++i) copy_to_lds(x[i] + column(i), at + 1024 * i);
 #pragma unroll
             for (int i = 0; i < PC; ++i)
                 copy_to_lds(P + (size_t)min(PER_COPY * i + lane / C, r.rank - 1) * m.depth + column(i), at + 1024 * (XC + i));
         };
-        const int steps = (m.depth - CS * wave + CS * W - 1) / (CS * W);     // of this wavefront
+        const int steps = 64 / CS * ((m.depth - 64 * wave + 64 * W - 1) / (64 * W));     // of this wavefront
 #pragma unroll
         for (int st = 0; st < D; ++st)
             if (st < steps) fetch(st);
         for (int st = 0; st < steps; ++st) {
             const char* const at = ring + st % D * L::step;
             uint4_t xf[CS / 32][MT], pf[CS / 32][RT];
-            const int k0 = CS * (wave + W * st) + 8 * g;
+            const int k0 = first(st) + 8 * g;
             uint4_t keep[CS / 32][MT];                                       // while the copies are on their way
             if (DROP && !p.backward)
 #pragma unroll
@@ -542,9 +544,7 @@ static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_
     return dt == DT_BF16 ? products<true>(p, rows, single_tokens(p.rows), grid, s) : products<false>(p, rows, single_tokens(p.rows), grid, s);
 }
 
-hipError_t launch_adapters(const AdapterRowsDev& given, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s) {
-    AdapterRowsDev rows = given;
-    if (!rows.offsets && !rows.adapters) rows.n_seqs = 1;        // all rows have the one adapter
+hipError_t launch_adapters(const AdapterRowsDev& rows, const AdapterMatDev* mats, int n_mats, int dt, int y_dt, hipStream_t s) {
     for (int i = 0; i < n_mats; i += kAdapterMats) {
         AdapterCall p{};
         p.rows = rows; p.y_dt = y_dt; p.first = (uint32_t)i;

@@ -769,6 +769,7 @@ static int check_adapter_rows(const rwkvq_adapter_rows* in, AdapterRowsDev* r) {
     if (in->rank % 8 != 0 || in->rank > 128) return RWKVQ_ERR_UNSUPPORTED;
     if (!in->offsets && in->n_tokens % in->n_seqs != 0) return RWKVQ_ERR_SHAPE;
     *r = AdapterRowsDev{in->n_seqs, in->n_tokens, in->n_adapters, in->rank, in->offsets, in->adapters, in->scales, {}};
+    if (!r->offsets && !r->adapters) r->n_seqs = 1;                                    // all rows have the one adapter
     const int st = check_dropout(in->seed, in->p, &r->drop);
     if (st != RWKVQ_OK) return st;
     return aligned4(in->offsets) && aligned4(in->adapters) && aligned4(in->scales) ? RWKVQ_OK : RWKVQ_ERR_ALIGN;

@@ -4,7 +4,7 @@ Bars.  Matrix cores add 32 products and the running sum, counted as 32 roundings
 the K columns, 64 ceil(K / 512) roundings, then four sums and a factor: gamma(K) = (64 ceil(K / 512) + 8) 2^-23 of sum |A| |x|.  y: h in parts, off by
 2^-16 of itself (bf16) or 2^-22 of the row's largest (fp16), 2^-24 where y is binary32 (2^-23 with the scale's rounding), at most 32 ceil(3 rank / 32) + 4
 further roundings, and half a step of y's type.  Gradients of A and B: a piece of up to 4096 tokens adds at most five products for every 32 tokens, 160
-roundings, and every piece one more; operands of 24 bits, 2^-22 with the products left out."""
+roundings, and every piece, of 64 rows at least, one more; operands of 24 bits, 2^-22 with the products left out."""
 import numpy as np
 import pytest
 
@@ -109,7 +109,8 @@ def check_forward(c, y_dt, ys, hs, bases):
 SHAPES = [
     ([1], [0], 1, 8, 8, 8), ([1], [2], 3, 16, 4096, 1000), ([1] * 20, list(range(5)) * 4, 5, 16, 520, 264), ([16], [0], 1, 16, 512, 64),
     ([17], [0], 1, 24, 72, 136), ([3, 0, 40, 1, 33], [1, 0, 0, -1, 1], 2, 32, 264, 200), ([5, 64, 2], [7, 0, -5], 3, 48, 1000, 328),
-    ([100], [1], 2, 64, 1032, 520), ([31, 32, 33], [0, 0, 1], 2, 128, 584, 72), ([200, 7], [0, 1], 2, 120, 40, 2056), ([0, 0, 9, 0], [0, 1, 1, 0], 2, 8, 4104, 16),
+    ([100], [1], 2, 64, 1032, 520), ([31, 32, 33], [0, 0, 1], 2, 128, 584, 72), ([200, 7], [0, 1], 2, 120, 40, 2056),
+    ([0, 0, 9, 0], [0, 1, 1, 0], 2, 8, 4104, 16),
     ([2, 2, 2, 2], [0, -1, 1, 0], 2, 40, 64, 64),
 ]
 
@@ -166,7 +167,7 @@ def check_backward(c, hs, dxs, das, dbs, bases):
             part = np.abs(g) * 2.0 ** -16 if c.dt == "bf16" else np.abs(g).max(1, keepdims=True) * 2.0 ** -22
             more = (32 * -(-3 * c.r // 32) + 4) * 2.0 ** -23
             ddx[f:e] = (dg + part + more * np.abs(g)) @ np.abs(a[id_])
-            pieces[id_] += (e - f) // 256 + 2
+            pieces[id_] += (e - f) // 64 + 2
             depth = (160 * -(-min(e - f, 4096) // 32)) * 2.0 ** -23 + 2.0 ** -22
             dda[id_] += (dg + depth * np.abs(g)).T @ np.abs(x[f:e])
             ddb[id_] += s[id_] * (np.abs(dy[f:e]).T @ (depth * np.abs(h[f:e])))
@@ -205,6 +206,132 @@ def test_more_than_eight_matrices_backward():
     c = Case([40, 9], [1, 0], 2, 16, 72, 136, "bf16", mats=10, p=0.1)
     hs = forward(c, "bf16")[1]
     check_backward(c, hs, *backward(c, hs))
+
+
+# tiles of 32 rows: eight matrices, whose tiles of 16 together have more than 20000 values of the rank
+MANY = [([300, 0, 340, 33, 31, 200], [0, 1, 1, 0, -1, 1], 2, 64, 136, 72), ([500, 40, 401], [1, -1, 0], 2, 48, 72, 264),
+        ([1000, 40, 700], [1, 5, 0], 2, 24, 72, 200), ([1300], [0], 1, 32, 104, 40)]
+
+
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s[2:])))
+@pytest.mark.parametrize("dt,y_dt,p", [("f16", "f16", 0.0), ("bf16", "bf16", 0.3), ("f16", "f32", 0.3), ("bf16", "f32", 0.0), ("bf16", "f16", 0.0)])
+def test_many_rows(shape, dt, y_dt, p):
+    c = Case(*shape, dt, mats=8, p=p, tail=5)
+    print(shape, dt, y_dt, p, flush=True)
+    check_forward(c, y_dt, *forward(c, y_dt))
+
+
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "x".join(map(str, s[2:])))
+@pytest.mark.parametrize("dt,p", [("f16", 0.0), ("bf16", 0.0), ("bf16", 0.3), ("f16", 0.3)])
+def test_many_rows_backward(shape, dt, p):
+    c = Case(*shape, dt, mats=8, p=p, tail=5)
+    print(shape, dt, p, flush=True)
+    hs = forward(c, dt)[1]
+    check_backward(c, hs, *backward(c, hs))
+
+
+@pytest.mark.parametrize("rank", [8, 24, 32, 40, 64, 120])
+@pytest.mark.parametrize("dt,y_dt", [("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32")])
+def test_a_row_alone(rank, dt, y_dt):
+    """The bits of a row do not depend on the rows beside it: in tiles of 32 and of 16 rows, gathered from single tokens, in slices of the columns, alone."""
+    mats, M, K, N = 8, 2000, 1160, 328
+    big = Case([M], [1], 2, rank, K, N, dt, mats=mats)
+    want, hs, bases = forward(big, y_dt)
+    table = lambda c, rows, ys, at: B.AdapterTable(  # noqa: E731
+        c.a, c.b, [x[at:at + rows] for x in c.x], ys, bases=[b[at:at + rows] for b in bases], x_strides=K + 8, base_strides=N + 8, y_strides=N + 8)
+    ids = lambda n: torch.ones(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    for seqs, rows, at in ((1, 1, 777), (1, 15, 32), (1, 45, 100), (40, 40, 64), (20, 40, 1000), (3, 300, 1700)):
+        ys = [torch.full((rows, N + 8), 9.0, dtype=TYPES[y_dt], device="cuda") for _ in range(mats)]
+        few = B.AdapterRows(seqs, rows, 2, rank, adapters=ids(seqs), scales=big.scales.cuda())
+        B.rwkvq_adapters(few, table(big, rows, ys, at), B.DTYPES[dt], B.DTYPES[y_dt])
+        for y, w in zip(ys, want):
+            assert torch.equal(y[:, :N], w[at:at + rows, :N]), (seqs, rows, at)
+
+
+@pytest.mark.parametrize("n,ids", [(300, lambda i: 0), (2048, lambda i: i * 7 % 5 - 1), (2048, lambda i: 1 if i > 2040 else 0), (2049, lambda i: i % 3),
+                                   (64, lambda i: -1)])
+@pytest.mark.parametrize("rank", [8, 40, 120])
+def test_single_tokens_of_many_users(n, ids, rank):
+    c = Case([1] * n, [ids(i) for i in range(n)], 4, rank, 72, 136, "bf16", ragged=False)
+    check_forward(c, "bf16", *forward(c, "bf16"))
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_one_adapter_for_all(ragged):
+    """No numbers of adapters: all sequences have the first, also where gradients are summed over them."""
+    c = Case([20, 20, 20, 20], [0] * 4, 1, 24, 72, 136, "bf16", mats=2, p=0.2, tail=0)
+    c.rows = B.AdapterRows(4, 80, 1, 24, offsets=c.offsets if ragged else None, scales=c.scales.cuda(), seed=c.rows.keep[3], p=c.p)
+    ys, hs, bases = forward(c, "bf16")
+    check_forward(c, "bf16", ys, hs, bases)
+    check_backward(c, hs, *backward(c, hs))
+
+
+def test_sixty_four_matrices():
+    c = Case([9, 1], [1, 0], 2, 8, 40, 24, "f16", mats=64, p=0.1)
+    ys, hs, bases = forward(c, "f16")
+    check_forward(c, "f16", ys, hs, bases)
+    check_backward(c, hs, *backward(c, hs))
+
+
+def test_offsets_stay_in_bounds():
+    """Offsets that descend or pass the last row are limited to the rows that there are; those in order have their results."""
+    c = Case([20, 30, 10], [0, 1, 0], 2, 16, 72, 40, "bf16", tail=4)
+    good = forward(c, "bf16", base=False)[0][0].clone()
+    for offsets in ([0, 20, 50, 2000], [-5, 20, 10, 64], [2 ** 30] * 4, [-2 ** 31, 20, 2 ** 31 - 1, 0]):
+        c.offsets.copy_(torch.tensor(offsets, dtype=torch.int32))
+        ys, hs, _ = forward(c, "bf16", base=False)
+        if offsets[1] == 20:
+            assert torch.equal(ys[0][:20], good[:20])
+        dxs = backward(c, hs)[0]
+        assert bool((ys[0][:, c.N:] == 9.0).all()) and bool((dxs[0][:, c.K:] == 9.0).all())
+
+
+def test_two_streams():
+    """Calls that run side by side, each with a workspace of its own."""
+    cases = [Case([700, 41], [0, 1], 2, 64, 264, 520, "bf16", mats=2, p=0.1, seed=i) for i in range(2)]
+    want = []
+    for c in cases:
+        hs = forward(c, "bf16", base=False)[1]
+        want.append((hs, backward(c, hs, base=False)[:3]))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for _ in range(3):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                hs = forward(c, "bf16", base=False)[1]
+                got[i] = (hs, backward(c, hs, base=False)[:3])
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for a, b in zip(w[0], g[0]))
+        for a, b in zip(w[1], g[1]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_rows_far_apart():
+    """Places beyond 2^32 elements: rows 2^27 apart."""
+    far, M = 1 << 27, 40
+    c = Case([M - 3, 3], [0, 1], 2, 16, 64, 40, "bf16", pad=8)
+    x, y = (torch.empty(M * far - far + 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rows = lambda t, n: t.as_strided((M, n), (far, 1))  # noqa: E731
+    rows(x, 64).copy_(c.x[0][:, :64])
+    h, plain = torch.empty(M, 16, device="cuda"), torch.empty(M, 40, dtype=torch.bfloat16, device="cuda")
+    B.rwkvq_adapters(c.rows, B.AdapterTable(c.a, c.b, [x], [y], hs=[h], x_strides=far, y_strides=far), B.BF16, B.BF16)
+    B.rwkvq_adapters(c.rows, B.AdapterTable(c.a, c.b, c.x, [plain], x_strides=72), B.BF16, B.BF16)
+    assert torch.equal(rows(y, 40), plain)
+    # gradients: dy in y's place, dx in another
+    dx = torch.empty_like(x)
+    for strided in (True, False):
+        da, db = torch.empty(2, 16, 64, device="cuda"), torch.empty(2, 40, 16, device="cuda")
+        near = torch.empty(M, 64, dtype=torch.bfloat16, device="cuda")
+        if strided:
+            table = B.AdapterGradTable(c.a, c.b, [x], [h], [y], [dx], [da], [db], x_strides=far, dy_strides=far, dx_strides=far)
+        else:
+            table = B.AdapterGradTable(c.a, c.b, c.x, [h], [plain], [near], [da], [db], x_strides=72)
+        ws = torch.empty(B.rwkvq_adapters_backward_workspace_size(c.rows, table), dtype=torch.uint8, device="cuda")
+        B.rwkvq_adapters_backward(c.rows, table, B.BF16, ws)
+        if strided:
+            first = da.clone(), db.clone()
+    assert torch.equal(first[0], da) and torch.equal(first[1], db) and torch.equal(rows(dx, 64), near)
 
 
 def test_gradients_are_differences():

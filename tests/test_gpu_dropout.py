@@ -120,3 +120,13 @@ def test_graph_reads_the_seed_when_it_runs():
         B.rwkvq_dropout(x, B.F32, 40, 72, s, 0.2, want)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and np.array_equal((got != 0).cpu().numpy(), TO.keep((1, number), 0.2, 40, 72)[0])
+
+
+def test_places_beyond_32_bits():
+    far, M, n, p = 1 << 27, 40, 520, 0.3
+    x, y = torch.randn(M, n, device="cuda").half(), torch.empty(M, n, dtype=torch.float16, device="cuda")
+    wide, out = (torch.empty((M - 1) * far + n, dtype=torch.float16, device="cuda") for _ in range(2))
+    wide.as_strided((M, n), (far, 1)).copy_(x)
+    B.rwkvq_dropout(x, B.F16, M, n, seed_of(3, 2 ** 32 - 1), p, y)
+    B.rwkvq_dropout(wide, B.F16, M, n, seed_of(3, 2 ** 32 - 1), p, out, x_stride=far, y_stride=far)
+    assert torch.equal(out.as_strided((M, n), (far, 1)), y)

@@ -139,3 +139,37 @@ def test_captured_and_replayed():
         call(want, other)
         torch.cuda.synchronize()
         assert torch.equal(table, want)
+
+
+def test_places_beyond_32_bits():
+    """A table of 2^32 elements and more, rows of the output 2^27 apart; a gradient of as many."""
+    V, d, T, far = 66000, 65536, 40, 1 << 27
+    rng = np.random.default_rng(1)
+    tokens = rng.integers(0, V, size=T)
+    tokens[:3] = V - 1, 0, V - 1
+    rows = torch.randn(T, d).to(torch.bfloat16).cuda()
+    rows[2] = rows[0]
+    table = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    table[ints(tokens).long()] = rows
+    out = torch.empty((T - 1) * far + d, dtype=torch.bfloat16, device="cuda")
+    B.rwkvq_embedding(ints(tokens), T, table, B.BF16, V, d, 1.0, out, B.BF16, out_stride=far)
+    placed = out.as_strided((T, d), (far, 1))
+    assert torch.equal(placed, table[ints(tokens).long()])
+    del table
+    ws = torch.empty(B.rwkvq_embedding_backward_workspace_size(T, d), dtype=torch.uint8, device="cuda")
+    grad = torch.full((V, d), float("nan"), device="cuda")
+    B.rwkvq_embedding_backward(ints(tokens), T, out, B.BF16, V, d, 1.0, grad, False, ws, dout_stride=far)
+    want = torch.zeros(T, d, dtype=torch.float64)
+    for t in range(T):
+        want[t] = sum(placed[i].double().cpu() for i in range(T) if tokens[i] == tokens[t])
+    got = grad[ints(tokens).long()].cpu().double()
+    assert bool(((got - want).abs() <= T * 2.0 ** -24 * want.abs().max()).all())
+    grad[ints(tokens).long()] = 0.0
+    assert not bool(grad.view(-1)[:1 << 32].any()) and not bool(grad.view(-1)[1 << 32:].any())
+
+
+def test_many_tokens_of_a_training_step():
+    rng = np.random.default_rng(2)
+    torch.manual_seed(3)
+    for dt in ("f16", "bf16"):
+        check_gradient(SPREADS["zipf"](rng, 9000, 900), 9000, 900, 264, dt, 1.0, dt == "f16", 272)
