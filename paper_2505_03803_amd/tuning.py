@@ -31,10 +31,16 @@ class Tuning:
         """Sequences that begin empty, and the adapter of each."""
         return self.block.plan(lens, adapters=adapters, drop=True)
 
+    def _count(self, tokens: torch.Tensor, plan) -> int:
+        T = sum(plan[0])
+        if tokens.dtype != torch.int32 or tokens.shape != (T,) or not tokens.is_contiguous():
+            raise ValueError(f"{tuple(tokens.shape)} tokens of {tokens.dtype} for a plan of {T}, which takes int32 one after the other")
+        return T
+
     def forward(self, tokens: torch.Tensor, plan) -> torch.Tensor:
         """tokens: int32, the sequences' one after the other; one outside the table is padding, a row of zeros.  -> [tokens][d], a view that the next
         call overwrites"""
-        T, dt = sum(plan[0]), self.block.dtype
+        T, dt = self._count(tokens, plan), self.block.dtype
         B.rwkvq_embedding(tokens, T, self.table, dt, self.vocab, self.d, 1.0, self.x, dt)
         y = self.block.forward(self.x[:T], plan)
         B.rwkvq_dropout(y, dt, T, self.d, self.seed, self.p, self.out, base=self.x)
@@ -43,7 +49,12 @@ class Tuning:
     def backward(self, tokens: torch.Tensor, dout: torch.Tensor, plan, dtable: torch.Tensor, accumulate: bool = False) -> Dict[str, object]:
         """The gradients behind forward(tokens, plan), the last call before this one, with the masks that it had: those of the block, and dtable
         (float32 [vocab][d], overwritten or added to)."""
-        T, dt = sum(plan[0]), self.block.dtype
+        T, dt = self._count(tokens, plan), self.block.dtype
+        if dout.shape != (T, self.d) or dout.dtype != self.table.dtype:
+            raise ValueError(f"a gradient {tuple(dout.shape)} of {dout.dtype} for {T} tokens")
+        if dtable.shape != self.table.shape or dtable.dtype != torch.float32 or not dtable.is_contiguous():
+            raise ValueError(f"a table's gradient {tuple(dtable.shape)} of {dtable.dtype}")
+        dout = dout.contiguous()
         B.rwkvq_dropout(dout, dt, T, self.d, self.seed, self.p, self.dy)
         grads = self.block.backward(self.x[:T], self.dy[:T], plan)
         dx = (grads.pop("x").float() + dout.float()).to(self.table.dtype)

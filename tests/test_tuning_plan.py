@@ -2,8 +2,10 @@
 import types
 
 import pytest
+import torch
 
 from paper_2505_03803_amd.time_mix import TimeMix
+from paper_2505_03803_amd.tuning import Tuning
 
 
 def block(n):
@@ -25,3 +27,19 @@ def test_plans(lens, ids):
     rows = block(2).plan(lens, adapters=ids)[4]
     assert len(rows) == 2 and all(r.desc.n_adapters == 2 and r.desc.rank == 8 and r.desc.n_tokens == sum(lens) for r in rows)
     assert block(2).plan(lens)[4] is None
+
+
+def test_what_a_step_refuses():
+    """Tokens of another type or number, gradients of another shape: before anything is launched."""
+    step = object.__new__(Tuning)
+    step.d, step.table, step.block = 16, torch.zeros(9, 16, dtype=torch.float16), types.SimpleNamespace(dtype=0)
+    plan = ([3, 4], None, None, None, None)
+    good, dout, dtable = torch.zeros(7, dtype=torch.int32), torch.zeros(7, 16, dtype=torch.float16), torch.zeros(9, 16)
+    for tokens in (good.long(), good[:6], torch.zeros(14, dtype=torch.int32)[::2], good[None]):
+        with pytest.raises(ValueError):
+            step.forward(tokens, plan)
+        with pytest.raises(ValueError):
+            step.backward(tokens, dout, plan, dtable)
+    for wrong in ((dout[:6], dtable), (dout.float(), dtable), (dout, dtable.double()), (dout, dtable[:8]), (dout, torch.zeros(16, 9).t())):
+        with pytest.raises(ValueError):
+            step.backward(good, wrong[0], plan, wrong[1])
