@@ -12,7 +12,7 @@ namespace rwkvq {
 struct alignas(128) AdapterLine { AdapterMatDev m; };
 struct alignas(128) AdapterCall {
     AdapterRowsDev rows;
-    int y_dt, slice;                               // columns of a workgroup
+    int y_dt, slice, pieces;                       // columns of a workgroup; tiles, of which the grid may have more
     uint32_t first;                                // number of the first matrix
     bool backward;                                 // x = dy, y = dx, h = g, p = b turned, q = a turned
     AdapterLine mats[kAdapterMats];
@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
     const AdapterMatDev m = p.mats[blockIdx.z].m;
     asm volatile("" ::"s"(r.adapters), "s"(m.x), "s"(m.y_stride), "s"(m.wide), "s"(p.slice));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    if ((int)blockIdx.x >= p.pieces) return;
     Gathered& gathered = *(Gathered*)(lds + L::gathered);
     int count, t0, id;
     float scale = 1.0f;
@@ -252,31 +253,38 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
         for (int i = 0; i < XC; ++i) x[i] = m.x + row_at(PER_COPY * i + lane / C) * m.x_stride;
         char* const ring = lds + wave * D * L::step;
-        // 64 columns for every wavefront, then the next, whatever a step has of them: tiles of either size add in one order
-        auto first = [&](int st) { return CS == 64 ? 64 * (wave + W * st) : 64 * (wave + W * (st >> 1)) + 32 * (st & 1); };
+        // 32 columns number h of a step.  Of ranks up to 32 a wavefront has 64 that lie together; above, halves of lines, whose other halves its neighbour reads
+        // at the same time, in one order whatever a step has of them: tiles of either size have the same sums
+        auto first = [&](int st, int h) { return RT <= 2 ? 64 * (wave + W * st) + 32 * h : 32 * (wave + W * (CS / 32 * st + h)); };
         auto fetch = [&](int st) {
             char* const at = ring + st % D * L::step;
-            auto column = [&](int i) { return min(first(st) + 8 * (lane % C ^ swizzle<C>(PER_COPY * i + lane / C)), m.depth - 8); };
+            auto column = [&](int i) {
+                const int c = lane % C ^ swizzle<C>(PER_COPY * i + lane / C);
+                return min(first(st, c >> 2) + 8 * (c & 3), m.depth - 8);
+            };
 #pragma unroll
             for (int i = 0; i < XC; ++i) copy_to_lds(x[i] + column(i), at + 1024 * i);
 #pragma unroll
             for (int i = 0; i < PC; ++i)
                 copy_to_lds(P + (size_t)min(PER_COPY * i + lane / C, r.rank - 1) * m.depth + column(i), at + 1024 * (XC + i));
         };
-        const int steps = 64 / CS * ((m.depth - 64 * wave + 64 * W - 1) / (64 * W));     // of this wavefront
+        constexpr int BLOCK = RT <= 2 ? 64 : 32;
+        const int blocks = (m.depth - BLOCK * wave + BLOCK * W - 1) / (BLOCK * W), steps = (blocks * BLOCK + CS - 1) / CS;     // of this wavefront
 #pragma unroll
         for (int st = 0; st < D; ++st)
             if (st < steps) fetch(st);
         for (int st = 0; st < steps; ++st) {
             const char* const at = ring + st % D * L::step;
             uint4_t xf[CS / 32][MT], pf[CS / 32][RT];
-            const int k0 = first(st) + 8 * g;
+            int k0[CS / 32];
+#pragma unroll
+            for (int h = 0; h < CS / 32; ++h) k0[h] = first(st, h) + 8 * g;
             uint4_t keep[CS / 32][MT];                                       // while the copies are on their way
             if (DROP && !p.backward)
 #pragma unroll
                 for (int h = 0; h < CS / 32; ++h)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) keep[h][i] = keeper.masks((uint32_t)(k0 + 32 * h) >> 3, (uint32_t)row_at(16 * i + n));
+                    for (int i = 0; i < MT; ++i) keep[h][i] = keeper.masks((uint32_t)k0[h] >> 3, (uint32_t)row_at(16 * i + n));
             if (st + D <= steps) wait_copies<(XC + PC) * (D - 1)>();         // all but those of the D - 1 steps behind this one
             else wait_copies<0>();
 #pragma unroll
@@ -293,7 +301,7 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
             for (int h = 0; h < CS / 32; ++h)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    if (k0 + 32 * h >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
+                    if (k0[h] >= m.depth) xf[h][i] = uint4_t{0, 0, 0, 0};
                     if (DROP && !p.backward) xf[h][i] &= keep[h][i];
                 }
 #pragma unroll
@@ -540,7 +548,11 @@ static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_
     for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
     const int rows = tile_rows(p, n_mats);
     p.slice = slice_of(p.rows, rows, n_mats, widest);
-    const dim3 grid((unsigned)pieces(p.rows, rows), (unsigned)((widest + p.slice - 1) / p.slice), (unsigned)n_mats);
+    const unsigned slices = (unsigned)((widest + p.slice - 1) / p.slice);
+    p.pieces = (int)pieces(p.rows, rows);
+    // slices of a tile, which read the same x, are a multiple of eight numbers apart: on one die (4321 rows beside 14336 columns in three 82 -> 80 us, 333
+    // rows of four matrices 17 -> 14); fewer tiles than sixteen, all of whose slices would be on few dies, are not (one token 7 us, on one die 9.5)
+    const dim3 grid((unsigned)(slices > 1 && p.pieces >= 16 ? (p.pieces + 7) / 8 * 8 : p.pieces), slices, (unsigned)n_mats);
     return dt == DT_BF16 ? products<true>(p, rows, single_tokens(p.rows), grid, s) : products<false>(p, rows, single_tokens(p.rows), grid, s);
 }
 
