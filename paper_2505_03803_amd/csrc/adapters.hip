@@ -102,41 +102,89 @@ static long long pieces(const AdapterRowsDev& r, int cut) {
     return (long long)((r.n_tokens / r.n_seqs + cut - 1) / cut) * r.n_seqs;
 }
 
-// Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  The
-// workgroup of row b has work if an even sixteen of the rows in front of it have the same adapter, and then takes those of the next sixteen.
+// Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  With fewer
+// adapters than rows workgroup i takes the i-th sixteen of all adapters', counted in LDS, and the grid is as large as these can be; otherwise, and for up
+// to sixteen rows, that of row b has work if an even sixteen of the rows in front of it have the same adapter.  That costs 1 us less, but workgroups without
+// work come and go, and the others meet on few dies: four matrices at rank 16, 128 rows of 8 adapters 14 us instead of 40, 2048 of 100 87 instead of 164.
 constexpr int kGathered = 2048;                    // rows of such a call at most
 struct Gathered {
     uint64_t same[kGathered / 64];
-    int rows[16];
+    int rows[16], totals[8], id, skip;
 };
-__device__ __forceinline__ int gather_rows(const AdapterRowsDev& r, int b, int id, Gathered& at) {
-    const int lane = threadIdx.x & 63, masks = (r.n_seqs + 63) / 64;
-    for (int i = threadIdx.x >> 6; i < masks; i += blockDim.x >> 6) {
+__host__ __device__ __forceinline__ int groups_of(const AdapterRowsDev& r) {
+    const long long most = (long long)r.n_adapters + 1 + r.n_seqs / 16;
+    return most < r.n_seqs && r.n_seqs > 16 ? (int)most : r.n_seqs;
+}
+constexpr int kGatherScratch = 8 * kGathered + 16;
+__device__ __forceinline__ int gather_rows(const AdapterRowsDev& r, int group, char* scratch, Gathered& at, int& id) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = r.n_seqs, masks = (n + 63) / 64;
+    const bool counted = groups_of(r) < n;
+    int* const ids = (int*)scratch;
+    int* const counts = ids + kGathered;                                      // of none, then of the adapters
+    for (int t = tid; t < n; t += 512) ids[t] = adapter_of(r, t);
+    if (counted)
+        for (int i = tid; i <= r.n_adapters; i += 512) counts[i] = 0;
+    __syncthreads();
+    if (counted) {
+        for (int t = tid; t < n; t += 512) atomicAdd(&counts[ids[t] + 1], 1);
+        __syncthreads();
+        const int per = r.n_adapters / 512 + 1, first = tid * per;
+        int own = 0;
+        for (int i = first; i < min(first + per, r.n_adapters + 1); ++i) own += (counts[i] + 15) / 16;
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 63) at.totals[wave] = sum;
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const int v = at.totals[w];
+            before += w < wave ? v : 0;
+            all += v;
+        }
+        if (group >= all) return 0;
+        int left = group - (before + sum - own);
+        if (left >= 0 && left < own)
+            for (int i = first;; ++i) {
+                const int here = (counts[i] + 15) / 16;
+                if (left < here) {
+                    at.id = i - 1; at.skip = 16 * left;
+                    break;
+                }
+                left -= here;
+            }
+        __syncthreads();
+        id = at.id;
+    } else {
+        id = ids[group];
+    }
+    for (int i = wave; i < masks; i += 8) {
         const int other = 64 * i + lane;
-        const uint64_t m = __builtin_amdgcn_ballot_w64(other < r.n_seqs && adapter_of(r, min(other, r.n_seqs - 1)) == id);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(other < n && ids[min(other, n - 1)] == id);
         if (lane == 0) at.same[i] = m;
     }
     __syncthreads();
-    int before = 0, all = 0, mine = -1;
+    int all = 0, skip = 0;
     for (int i = 0; i < masks; ++i) {
-        uint64_t m = at.same[i];
-        const int low = b - 64 * i, n = __builtin_popcountll(m), in_front = low >= 64 ? n : low <= 0 ? 0 : __builtin_popcountll(m & ((1ull << low) - 1));
-        before += in_front;
-        // the lane's row is the one with `lane` of the adapter between b and it
-        if (low < 64) {
-            if (low > 0) m &= ~((1ull << low) - 1);
-            const int left = lane - all, here = n - in_front;
-            if (left >= 0 && left < here) {
-                for (int j = 0; j < left; ++j) m &= m - 1;
-                mine = 64 * i + __builtin_ctzll(m);
-            }
-            all += here;
-        }
+        const uint64_t m = at.same[i];
+        const int low = group - 64 * i;
+        if (!counted) skip += low >= 64 ? __builtin_popcountll(m) : low <= 0 ? 0 : __builtin_popcountll(m & ((1ull << low) - 1));
+        all += __builtin_popcountll(m);
     }
-    if (before % 16) return 0;
-    if (threadIdx.x < 16) at.rows[threadIdx.x] = mine;
+    if (counted) skip = at.skip;
+    else if (skip % 16) return 0;
+    for (int i = wave; i < masks; i += 8) {
+        const uint64_t m = at.same[i];
+        int rank = __builtin_popcountll(m & ((1ull << lane) - 1)) - skip;
+        for (int j = 0; j < i; ++j) rank += __builtin_popcountll(at.same[j]);
+        if ((m >> lane & 1) && rank >= 0 && rank < 16) at.rows[rank] = 64 * i + lane;
+    }
     __syncthreads();
-    return min(all, 16);
+    return min(all - skip, 16);
 }
 
 // Copies of 16 bytes a lane from memory to LDS by the load unit, to `to` + 16 lane.
@@ -192,9 +240,9 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
     int count, t0, id;
     float scale = 1.0f;
     if constexpr (GATHER) {
-        t0 = blockIdx.x;
-        id = adapter_of(r, t0);
-        count = gather_rows(r, t0, id, gathered);
+        static_assert(L::ring >= kGatherScratch, "the steps' place");
+        t0 = 0;
+        count = gather_rows(r, blockIdx.x, lds, gathered, id);
         if (id >= 0 && r.scales) scale = r.scales[id];
     } else {
         const RowSpan s = piece_of(r, ROWS, blockIdx.x, (RowSpan*)(lds + L::found));
@@ -532,13 +580,15 @@ static int tile_rows(const AdapterCall& p, int n_mats) {
     return (double)r.rank * pieces(r, 16) * n_mats > 20000 || r.rank * lengths * pieces(r, 32) > 5 << 24 ? 32 : 16;
 }
 // Columns of a workgroup: all of them where tiles and matrices fill the device, otherwise as many workgroups as one and a half a compute unit, of no fewer than
-// 256 columns.  Every one takes h again: for 256 single tokens in as many workgroups as two a unit 34 us instead of 26, 4096 rows at rank 64 48 instead of 40;
-// 151 tiles beside 14336 columns in one, two and three 98, 97 and 82.
+// 256 columns.  Every one takes h again: 4096 rows at rank 64 in as many workgroups as two a unit 48 us instead of 40; 151 tiles beside 14336 columns
+// in one, two and three 98, 97 and 82.  Few single tokens, whose weights are read but once: one a unit (four matrices, 16 rows of 16 adapters 9 us
+// instead of 11, 128 of 8 14 instead of 17; 64 rows of 32 at rank 64, in two slices instead of three, 50 instead of 45).
 static int slice_of(const AdapterRowsDev& r, int rows, int n_mats, int widest) {
     long long wgs = pieces(r, rows);
-    if (single_tokens(r)) wgs = std::min<long long>(wgs, std::max(r.n_adapters, (r.n_seqs + 15) / 16));
+    if (single_tokens(r)) wgs = std::min<long long>(groups_of(r), std::max(r.n_adapters, (r.n_seqs + 15) / 16));
     wgs *= n_mats;
-    const long long wanted = std::min<long long>((widest + 255) / 256, wgs >= 256 ? 1 : (384 + wgs - 1) / wgs);
+    const int full = single_tokens(r) && wgs <= 64 ? 256 : 384;
+    const long long wanted = std::min<long long>((widest + 255) / 256, wgs >= 256 ? 1 : (full + wgs - 1) / wgs);
     return (int)(((widest + wanted - 1) / wanted + 63) / 64 * 64);
 }
 // (more than one slice only of fewer than 256 workgroups)
@@ -549,7 +599,7 @@ static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_
     const int rows = tile_rows(p, n_mats);
     p.slice = slice_of(p.rows, rows, n_mats, widest);
     const unsigned slices = (unsigned)((widest + p.slice - 1) / p.slice);
-    p.pieces = (int)pieces(p.rows, rows);
+    p.pieces = single_tokens(p.rows) ? groups_of(p.rows) : (int)pieces(p.rows, rows);
     // slices of a tile, which read the same x, are a multiple of eight numbers apart: on one die (4321 rows beside 14336 columns in three 82 -> 80 us, 333
     // rows of four matrices 17 -> 14); fewer tiles than sixteen, all of whose slices would be on few dies, are not (one token 7 us, on one die 9.5)
     const dim3 grid((unsigned)(slices > 1 && p.pieces >= 16 ? (p.pieces + 7) / 8 * 8 : p.pieces), slices, (unsigned)n_mats);
