@@ -536,10 +536,10 @@ int rwkvq_embedding_backward(const int32_t* tokens, int n_tokens, const void* do
  *   g and h enter da and db with 24 bits.  workspace: DEVICE, rwkvq_adapters_backward_workspace_size(..) bytes (of the same rows and
  *   matrices, whose pointers are not looked at), contents irrelevant on entry and undefined on exit.
  * a, b, x, base, y, h, dy, dx, da, db, workspace 16-byte aligned; seed 8; offsets, adapters, scales 4; no call synchronises.
- * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, rank, p outside [0, 1]), RWKVQ_ERR_SHAPE (a count below 1, n_mats > 64, n_tokens not a multiple of n_seqs
- *   without offsets, K or N above 2^24, a stride below its width or n_tokens * stride > 2^40, x or dy the same as y or dx, in place with another stride, more than
- *   65535 adapters, more threads than the 2^32 of one launch: 512 for every 16 rows and every sequence, times eight), RWKVQ_ERR_ALIGN
- *   (pointers; K, N or strides not a multiple of 8), RWKVQ_ERR_DEVICE. */
+ * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, rank, p outside [0, 1]), RWKVQ_ERR_SHAPE (a count below 1, n_mats > 64, n_tokens not a multiple of
+ *   n_seqs without offsets, K or N above 2^24, a stride below its width or n_tokens * stride > 2^40, x or dy the same as y or dx, in place with another
+ *   stride, more than 65535 adapters, more threads than the 2^32 of one launch: 512 for every 16 rows and every sequence, times eight),
+ *   RWKVQ_ERR_ALIGN (pointers; K, N or strides not a multiple of 8), RWKVQ_ERR_DEVICE. */
 typedef struct rwkvq_adapter_rows {
     int32_t n_seqs, n_tokens;
     int32_t n_adapters, rank;

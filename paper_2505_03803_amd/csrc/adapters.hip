@@ -212,6 +212,8 @@ __device__ __forceinline__ int swizzle(int row) { return (row / (16 / C)) & (C -
 // whole lines give (9.5 against 30 TB/s out of L2).  So tiles of x, P and Q are copied to LDS by whole lines, and y leaves through LDS.
 // h goes into the second product as PARTS parts of 16 bits (two: 16 bits of bf16, 22 of fp16, beside the rounding of a 16-bit y; three for binary32 y), fp16
 // ones under a power of two for each row that brings its largest value to 2^14, so that none is lost below fp16's range.
+// Measured: 8192 rows, K = N = 4096, rank 64 with dropout 58 us (floor 40: 3.5 TB/s of x, base and y, beside 1 MB of P and Q for every 32 rows through a unit's
+// cache), 4321 rows of 4096 beside 14336 columns at rank 32 78 (floor 57), 256 single tokens of 64 adapters, four matrices at rank 16, 25 (floor 18).
 // GATHER: single tokens (gather_rows).  DROP: there is dropout, of x or, backwards, of what is added to y.
 template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
@@ -224,8 +226,11 @@ template <int RT, int MT, int PARTS> struct AdapterLds {
     static constexpr int parts = q + W * q_tile, inverse = parts + ROWS * HROW, after = inverse + 4 * ROWS;
     static constexpr int found = ring > after ? ring : after, gathered = found + 16, bytes = gathered + (int)sizeof(Gathered);
 };
+// Wavefronts a SIMD: those of two workgroups where LDS and, for tiles of 32 rows with binary32 y or masks, registers allow.
+template <int RT, int MT, int PARTS, bool DROP>
+constexpr int waves_of() { return AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && (PARTS == 3 || DROP)) ? 4 : 2; }
 template <bool BF16, int RT, int MT, int PARTS, bool DROP, bool GATHER>
-__global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 * 1024 && !(MT == 2 && (PARTS == 3 || DROP)) ? 4 : 2)) adapter_kernel(AdapterCall p) {
+__global__ void __launch_bounds__(512, (waves_of<RT, MT, PARTS, DROP>())) adapter_kernel(AdapterCall p) {
     typedef AdapterLds<RT, MT, PARTS> L;
     constexpr int W = L::W, R = L::R, ROWS = L::ROWS, D = L::D, CS = L::CS, CG = L::CG, CT = CG / 16, QS = RT == 1 ? 1 : RT / 2, QC = R / 8;
     constexpr bool WIDE = PARTS == 3;                                         // y is binary32
@@ -301,8 +306,8 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
         for (int i = 0; i < XC; ++i) x[i] = m.x + row_at(PER_COPY * i + lane / C) * m.x_stride;
         char* const ring = lds + wave * D * L::step;
-        // 32 columns number h of a step.  Of ranks up to 32 a wavefront has 64 that lie together; above, halves of lines, whose other halves its neighbour reads
-        // at the same time, in one order whatever a step has of them: tiles of either size have the same sums
+        // 32 columns number h of a step.  Of ranks up to 32 a wavefront has 64 that lie together; above, halves of lines, whose other halves its
+        // neighbour reads at the same time, in one order whatever a step has of them: tiles of either size have the same sums
         auto first = [&](int st, int h) { return RT <= 2 ? 64 * (wave + W * st) + 32 * h : 32 * (wave + W * (CS / 32 * st + h)); };
         auto fetch = [&](int st) {
             char* const at = ring + st % D * L::step;
@@ -444,7 +449,10 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < PASS; ++j) keep[i][j] = p.backward ? keeper.masks((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]) : uint4_t{~0u, ~0u, ~0u, ~0u};
+            for (int j = 0; j < PASS; ++j) {
+                keep[i][j] = uint4_t{~0u, ~0u, ~0u, ~0u};
+                if (p.backward) keep[i][j] = keeper.masks((uint32_t)(c0 + out_col) >> 3, (uint32_t)out_row[i][j]);
+            }
     };
     if (DROP) draw(from + CG * wave);
     meet();
@@ -499,7 +507,8 @@ __global__ void __launch_bounds__(512, (AdapterLds<RT, MT, PARTS>::bytes <= 80 *
                 }
                 if (id >= 0) {
                     const float down = BF16 ? 1.0f : inverse[16 * i + at];
-                    const float4_t a = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col)), b = *(const float4_t*)(out_tile + 4 * (at * L::YPITCH + out_col + 4));
+                    const char* const from = out_tile + 4 * (at * L::YPITCH + out_col);
+                    const float4_t a = *(const float4_t*)from, b = *(const float4_t*)(from + 16);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float z = e < 4 ? a[e & 3] : b[e & 3];
@@ -567,11 +576,11 @@ static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 gri
 static bool single_tokens(const AdapterRowsDev& r) {
     return !r.offsets && r.n_tokens == r.n_seqs && r.n_seqs > 1 && r.n_seqs <= kGathered && !r.drop.seed;
 }
-// Rows of a tile: 16, of which two workgroups fit a compute unit, one's copies beside the other's products, unless there are enough tiles of 32 as well, or tiles
-// of 16 would take too much of P and Q through the caches.  Measured, 16 against 32 (us): K = N = 4096: 4096 rows at rank 32 30 / 37, 64 40 / 52; 8192 rows at rank
-// 16 45 / 54, 32 49 / 54, 64 76 / 57; 16384 rows at rank 16 82 / 94, 32 92 / 92; K = N = 1024: 16384 rows at rank 32 27 / 24, 64 37 / 31; 4320 rows beside N = 14336:
-// rank 16 79 / 75, 32 107 / 82, 64 130 / 100.  So 32 from 20000 ranks of tiles or 5 2^24 values that tiles of 32 take, never for rank 16.  Above rank 64 the
-// registers of 16 rows are full.
+// Rows of a tile: 16, of which two workgroups fit a compute unit, one's copies beside the other's products, unless there are enough tiles of 32 as
+// well, or tiles of 16 would take too much of P and Q through the caches.  Measured, 16 against 32 (us): K = N = 4096: 4096 rows at rank 32 30 / 37, 64
+// 40 / 52; 8192 rows at rank 16 45 / 54, 32 49 / 54, 64 76 / 59; 16384 rows at rank 16 82 / 94, 32 92 / 92; K = N = 1024: 16384 rows at rank 32
+// 27 / 24, 64 37 / 31; 4320 rows beside N = 14336: rank 16 79 / 75, 32 107 / 80, 64 130 / 104.  So 32 from 20000 ranks of tiles or 5 2^24 values that
+// tiles of 32 take, never for rank 16.  Above rank 64 the registers of 16 rows are full.
 static int tile_rows(const AdapterCall& p, int n_mats) {
     const AdapterRowsDev& r = p.rows;
     if (r.rank <= 16 || r.rank > 64 || r.n_tokens / r.n_seqs <= 16) return 16;
@@ -620,7 +629,9 @@ hipError_t launch_adapters(const AdapterRowsDev& rows, const AdapterMatDev* mats
 
 // ---- gradients ----------------------------------------------------------------------------------------------------------
 
-// Weights [rows][cols] of each adapter that a sequence has, as [cols][rows]; a workgroup turns 64 x 64 of them.
+// Weights [rows][cols] of each adapter that a sequence has, as [cols][rows], 64 x 64 of them a workgroup through LDS, so that the backward pass is the kernel
+// of the forward one; and h in three bf16 parts, once for all workgroups that read it.  A launch in a chain: 4 us for three adapters of rank 8, 5 for 8192
+// rows at rank 64.
 __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
     __shared__ uint16_t tile[64][66];
     __shared__ int used;
@@ -674,11 +685,12 @@ __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
     }
 }
 
-// Sums over tokens.  A workgroup takes a piece of `cut` rows of one sequence and some columns of v: for the gradient of A v = drop(x) and q = g, for that of B
-// v = dy and q = h; the product of their transposes, 32 tokens at a time, with four wavefronts of VC tiles of 16 columns each.  Tiles of both lie in LDS by
-// token and are read by columns, in the order of tokens that column_frag has, the same for both; v is on its way two steps ahead, q one, in registers.
-// q is binary32: three bf16 parts, 24 bits, since the result is a binary32 sum, made once before; fp16 values of v as two bf16 parts, exact, of which the products
-// of both lowest parts are left out (2^-24 of the term).
+// Sums over tokens.  A workgroup takes a piece of `cut` rows of one sequence and some columns of v: for the gradient of A v = drop(x) and q = g, for
+// that of B v = dy and q = h; the product of their transposes, 32 tokens at a time, with four wavefronts of VC tiles of 16 columns each.  Tiles of both
+// lie in LDS by token and are read by columns, in the order of tokens that column_frag has, the same for both; v is on its way two steps ahead, q one, in
+// registers.  q is binary32: three bf16 parts, 24 bits, since the result is a binary32 sum, made once before; fp16 values of v as two bf16 parts, exact,
+// of which the products of both lowest parts are left out (2^-24 of the term).  What bounds it: v comes once, q for every 256 columns from the caches; 8192
+// tokens of 4096 + 4096 columns at rank 64 41 us, 25.8 GFLOP of parts at 630 TFLOP/s, matrix cores 31 % busy, 141 MB read (3.4 TB/s).
 // Reads by columns take 32 bytes of eight rows at once: pairs of pieces of a row, C of them, change places with its number.
 template <int C>
 __device__ __forceinline__ int pair_swizzle(int row) { return C >= 8 ? (row & 7) << 1 : (row / (8 / C) & (C - 1)) << 1; }
@@ -716,7 +728,8 @@ __global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int steps = (s.t1 - s.t0 + 31) / 32;
 
-    // a thread's piece i of a step of v: token PER_V i + .. and eight columns; of q: token, part and eight values.  Places behind the piece and the last column are 0
+    // a thread's piece i of a step of v: token v_row + APART i and eight columns; of q: token, part and eight values.  Places behind the piece and the
+    // last column are 0
     constexpr int PER = COLS / 8, APART = 256 / PER;
     const int v_row = tid / PER, col = c0 + 8 * (tid % PER);
     auto fetch_v = [&](uint4_t (&to)[VN], int st) {
@@ -816,7 +829,7 @@ __global__ void __launch_bounds__(256, 2) outer_kernel(OuterCall p) {
     else sweep(std::true_type{}, std::false_type{});
 }
 
-// The gradients of an adapter: the sums of its pieces, in their order.
+// The gradients of an adapter: the sums of its pieces, in their order, eight on their way (sixteen of 2 MB 7 us).
 __global__ void __launch_bounds__(256) gather_kernel(OuterCall p) {
     const AdapterRowsDev& r = p.rows;
     const int id = blockIdx.y;
@@ -905,7 +918,10 @@ static hipError_t sum_tokens(const OuterCall& o, dim3 grid, hipStream_t s) {
 template <bool BF16>
 static hipError_t sum_tokens(const OuterCall& o, dim3 grid, hipStream_t s) {
     const int rank = o.rows.rank;
-    return rank <= 16 ? sum_tokens<BF16, 1>(o, grid, s) : rank <= 32 ? sum_tokens<BF16, 2>(o, grid, s) : rank <= 64 ? sum_tokens<BF16, 4>(o, grid, s) : sum_tokens<BF16, 8>(o, grid, s);
+    return rank <= 16   ? sum_tokens<BF16, 1>(o, grid, s)
+           : rank <= 32 ? sum_tokens<BF16, 2>(o, grid, s)
+           : rank <= 64 ? sum_tokens<BF16, 4>(o, grid, s)
+                        : sum_tokens<BF16, 8>(o, grid, s);
 }
 
 // mats: x = dy, y = dx, h = g (set here), depth = N, wide = K, p = b, q = a; grads: what else a matrix has.

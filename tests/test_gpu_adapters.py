@@ -256,6 +256,15 @@ def test_single_tokens_of_many_users(n, ids, rank):
     check_forward(c, "bf16", *forward(c, "bf16"))
 
 
+@pytest.mark.parametrize("n,adapters", [(2, 5), (16, 2), (17, 2), (90, 3), (200, 300)])
+@pytest.mark.parametrize("rank,dt", [(8, "f16"), (40, "bf16"), (128, "bf16")])
+def test_single_tokens_backward(n, adapters, rank, dt):
+    rng = np.random.default_rng(n)
+    c = Case([1] * n, rng.integers(-1, adapters, size=n).tolist(), adapters, rank, 136, 72, dt, mats=2, ragged=False)
+    hs = forward(c, dt)[1]
+    check_backward(c, hs, *backward(c, hs))
+
+
 @pytest.mark.parametrize("ragged", [False, True])
 def test_one_adapter_for_all(ragged):
     """No numbers of adapters: all sequences have the first, also where gradients are summed over them."""
