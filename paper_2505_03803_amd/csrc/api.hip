@@ -769,15 +769,16 @@ static int check_adapter_rows(const rwkvq_adapter_rows* in, AdapterRowsDev* r) {
     if (in->rank % 8 != 0 || in->rank > 128) return RWKVQ_ERR_UNSUPPORTED;
     if (!in->offsets && in->n_tokens % in->n_seqs != 0) return RWKVQ_ERR_SHAPE;
     *r = AdapterRowsDev{in->n_seqs, in->n_tokens, in->n_adapters, in->rank, in->offsets, in->adapters, in->scales, {}};
+    const bool fits = adapters_fit(*r);
     if (!r->offsets && !r->adapters) r->n_seqs = 1;                                    // all rows have the one adapter
     const int st = check_dropout(in->seed, in->p, &r->drop);
     if (st != RWKVQ_OK) return st;
-    return aligned4(in->offsets) && aligned4(in->adapters) && aligned4(in->scales) ? RWKVQ_OK : RWKVQ_ERR_ALIGN;
+    if (!aligned4(in->offsets) || !aligned4(in->adapters) || !aligned4(in->scales)) return RWKVQ_ERR_ALIGN;
+    return fits ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
 }
-static int check_adapter_sizes(const AdapterRowsDev& r, int N, int K) {
+static int check_adapter_sizes(int N, int K) {
     if (N < 1 || K < 1 || N > (1 << 24) || K > (1 << 24)) return RWKVQ_ERR_SHAPE;
-    if (N % 8 != 0 || K % 8 != 0) return RWKVQ_ERR_ALIGN;
-    return adapters_fit(r) ? RWKVQ_OK : RWKVQ_ERR_SHAPE;
+    return N % 8 != 0 || K % 8 != 0 ? RWKVQ_ERR_ALIGN : RWKVQ_OK;
 }
 
 int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, int n_mats, int x_dtype, int y_dtype, void* stream) {
@@ -791,7 +792,7 @@ int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, in
     for (int i = 0; i < n_mats; ++i) {
         const rwkvq_adapter& m = mats[i];
         if (!m.a || !m.b || !m.x || !m.y) return RWKVQ_ERR_NULL;
-        if ((st = check_adapter_sizes(r, m.N, m.K)) != RWKVQ_OK) return st;
+        if ((st = check_adapter_sizes(m.N, m.K)) != RWKVQ_OK) return st;
         AdapterMatDev& d = dev[i];
         d = AdapterMatDev{(const uint16_t*)m.x, (const uint16_t*)m.a, (const uint16_t*)m.b, m.base, m.y, m.h, row_stride(m.x_stride, m.K, r.n_tokens),
                           row_stride(m.base_stride, m.N, r.n_tokens), row_stride(m.y_stride, m.N, r.n_tokens), m.K, m.N};
@@ -807,7 +808,7 @@ int rwkvq_adapters(const rwkvq_adapter_rows* rows, const rwkvq_adapter* mats, in
 static int check_adapter_grads(const AdapterRowsDev& r, const rwkvq_adapter_grad* mats, int n_mats, AdapterMatDev* dev, AdapterGradDev* grads) {
     for (int i = 0; i < n_mats; ++i) {
         const rwkvq_adapter_grad& m = mats[i];
-        const int st = check_adapter_sizes(r, m.N, m.K);
+        const int st = check_adapter_sizes(m.N, m.K);
         if (st != RWKVQ_OK) return st;
         AdapterMatDev& d = dev[i];
         d = AdapterMatDev{(const uint16_t*)m.dy, (const uint16_t*)m.b, (const uint16_t*)m.a, m.base, m.dx, nullptr, row_stride(m.dy_stride, m.N, r.n_tokens),
