@@ -57,6 +57,11 @@ class TimeMix:
     def __init__(self, d: int, n_heads: int, mats: Dict[str, synth.QMatrix], mus: Dict[str, Tuple[np.ndarray, np.ndarray]], w, u, ln,
                  heads_norm, n_slots: int, max_tokens: int, kbits: int = 6, dtype: int = B.F16, eps: float = 1e-5,
                  device: str = "cuda:0", adapters: Optional[Adapters] = None):
+        if adapters is not None:
+            for p in PROJECTIONS + ("o",):
+                a, b = adapters.a[p], adapters.b[p]
+                if a.dtype != TYPES[dtype] or b.dtype != TYPES[dtype] or a.shape != (adapters.n, adapters.rank, d) or b.shape != (adapters.n, d, adapters.rank):
+                    raise ValueError(f"adapters {tuple(a.shape)}, {tuple(b.shape)} of {a.dtype} in a block of width {d} of {TYPES[dtype]}")
         self.d, self.H, self.D, self.dtype, self.eps, self.kbits = d, n_heads, d // n_heads, dtype, eps, kbits
         self.device, self.n_slots, self.max_tokens = device, n_slots, max_tokens
         self.mats = {p: B.upload(mats[p], device=device) for p in PROJECTIONS + ("o",)}

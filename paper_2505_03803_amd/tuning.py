@@ -21,6 +21,8 @@ class Tuning:
     """table: [vocab][d] of the block's type.  p: dropout of the block's output; `seed` holds its key and the number of the next call."""
 
     def __init__(self, block: time_mix.TimeMix, table: torch.Tensor, p: float = 0.0, seed: int = 1):
+        if table.dtype != time_mix.TYPES[block.dtype] or table.dim() != 2 or table.shape[1] != block.d or not table.is_contiguous():
+            raise ValueError(f"a table {tuple(table.shape)} of {table.dtype} for a block of width {block.d} of {time_mix.TYPES[block.dtype]}")
         self.block, self.table, self.p = block, table, p
         self.vocab, self.d = table.shape
         self.seed = torch.tensor([seed, 0], dtype=torch.int64, device=table.device)

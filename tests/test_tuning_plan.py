@@ -4,7 +4,8 @@ import types
 import pytest
 import torch
 
-from paper_2505_03803_amd.time_mix import TimeMix
+from paper_2505_03803_amd import binding as B
+from paper_2505_03803_amd.time_mix import Adapters, TimeMix
 from paper_2505_03803_amd.tuning import Tuning
 
 
@@ -43,3 +44,16 @@ def test_what_a_step_refuses():
     for wrong in ((dout[:6], dtable), (dout.float(), dtable), (dout, dtable.double()), (dout, dtable[:8]), (dout, torch.zeros(16, 9).t())):
         with pytest.raises(ValueError):
             step.backward(good, wrong[0], plan, wrong[1])
+
+
+@pytest.mark.parametrize("d,dtype", [(64, B.BF16), (128, B.F16)])
+def test_adapters_of_another_block(d, dtype):
+    pool = Adapters(d, 2, 8, dtype=dtype, device="cpu")
+    with pytest.raises(ValueError):
+        TimeMix(64, 1, None, None, None, None, None, None, 1, 10, dtype=B.F16, adapters=pool)
+
+
+@pytest.mark.parametrize("table", [torch.zeros(9, 16), torch.zeros(9, 8).half(), torch.zeros(16, 9).half().t(), torch.zeros(16).half()])
+def test_tables_of_another_block(table):
+    with pytest.raises(ValueError):
+        Tuning(types.SimpleNamespace(d=16, dtype=B.F16, max_tokens=4), table)
