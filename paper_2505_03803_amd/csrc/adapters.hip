@@ -588,17 +588,42 @@ static int tile_rows(const AdapterCall& p, int n_mats) {
     for (int i = 0; i < n_mats; ++i) lengths += (double)p.mats[i].m.depth + p.mats[i].m.wide;
     return (double)r.rank * pieces(r, 16) * n_mats > 20000 || r.rank * lengths * pieces(r, 32) > 5 << 24 ? 32 : 16;
 }
-// Columns of a workgroup: all of them where tiles and matrices fill the device, otherwise as many workgroups as one and a half a compute unit, of no fewer than
-// 256 columns.  Every one takes h again: 4096 rows at rank 64 in as many workgroups as two a unit 48 us instead of 40; 151 tiles beside 14336 columns
-// in one, two and three 98, 97 and 82.  Few single tokens, whose weights are read but once: one a unit (four matrices, 16 rows of 16 adapters 9 us
-// instead of 11, 128 of 8 14 instead of 17; 64 rows of 32 at rank 64, in two slices instead of three, 50 instead of 45).
-static int slice_of(const AdapterRowsDev& r, int rows, int n_mats, int widest) {
-    long long wgs = pieces(r, rows);
-    if (single_tokens(r)) wgs = std::min<long long>(groups_of(r), std::max(r.n_adapters, (r.n_seqs + 15) / 16));
-    wgs *= n_mats;
-    const int full = single_tokens(r) && wgs <= 64 ? 256 : 384;
-    const long long wanted = std::min<long long>((widest + 255) / 256, wgs >= 256 ? 1 : (full + wgs - 1) / wgs);
-    return (int)(((widest + wanted - 1) / wanted + 63) / 64 * 64);
+// Slices of a tile, which read the same x, are on one die, a multiple of eight workgroups apart (4321 rows beside 14336 columns in three 82 -> 80 us, 333 rows
+// of four matrices 17 -> 14); those of fewer tiles than sixteen, which would be on few dies, are not (one token 7 us, on one die 9.5).
+static bool spread(long long tiles) { return tiles >= 16; }
+// Columns of a workgroup: all of them from 256 workgroups on; of fewer, as many slices as make the fullest compute unit's time least, by what goes through
+// its cache: every slice takes h again, (rows + rank) values for each of the depth, then rank values of Q, base and y for each of its columns.
+// Workgroups that share a unit take 0.7 of their times together, 0.85 above rank 32; one that fills a unit waits for the one in front.  Measured, 1, 2, 3
+// and 4 slices (us): 3500 rows, K = N = 4096, rank 16 23.3, 21.7, 26.8, 29.3; 2500 rows at rank 64 28.4, 31.2, 32.5, 41.9; 4321 rows beside N = 14336
+// at rank 32 97, 94, 80, 95; 3000 rows with K = 14336 at rank 32 48, 62, 72, 81; 2048 rows at rank 128 in 2 and 3 34 and 53.  Groups of single tokens,
+// whose number the host does not know, as many as one a unit where they are few, otherwise one and a half (four matrices, 16 rows of 16 adapters 9 us,
+// one and a half 11; 128 of 8 14, 17; 64 rows of 32 at rank 64 one and a half 45, one 50).
+static int slice_of(const AdapterCall& p, int rows, int n_mats, int widest) {
+    const AdapterRowsDev& r = p.rows;
+    const int R = padded_rank(r.rank);
+    const int most = (widest + 255) / 256;
+    auto width = [&](long long slices) { return (int)(((widest + slices - 1) / slices + 63) / 64 * 64); };
+    if (single_tokens(r)) {
+        const long long wgs = (long long)n_mats * std::min(groups_of(r), std::max(r.n_adapters, (r.n_seqs + 15) / 16));
+        return width(wgs >= 256 ? 1 : std::min<long long>(most, ((wgs <= 64 ? 256 : 384) + wgs - 1) / wgs));
+    }
+    const long long tiles = pieces(r, rows), wgs = tiles * n_mats;
+    int deepest = 0;
+    for (int i = 0; i < n_mats; ++i) deepest = std::max(deepest, p.mats[i].m.depth);
+    const bool fills = R > 64 || (rows == 32 && (R > 32 || r.drop.seed || p.y_dt == DT_F32));       // a unit (waves_of)
+    const double together = fills ? 1.0 : R > 32 ? 0.85 : 0.7, h = 2.0 * (rows + R) * deepest, column = 2.0 * R + rows * (p.y_dt == DT_F32 ? 8.0 : 4.0);
+    int best = width(1);
+    double least = 0;
+    for (int slices = 1; wgs < 256 && slices <= most && (slices == 1 || slices * wgs <= 768); ++slices) {
+        const int wide = width(slices);
+        const long long die = (tiles + 7) / 8 * slices * n_mats, fullest = slices > 1 && spread(tiles) ? (die + 31) / 32 : (slices * wgs + 255) / 256;
+        const double time = (fullest == 1 ? 1.0 : together * fullest) * (h + column * wide);
+        if (slices == 1 || time < least) {
+            least = time;
+            best = wide;
+        }
+    }
+    return best;
 }
 // (more than one slice only of fewer than 256 workgroups)
 bool adapters_fit(const AdapterRowsDev& r) { return (double)pieces(r, 16) * kAdapterMats * 512.0 < 4294967296.0; }
@@ -606,12 +631,10 @@ static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_
     int widest = 64;                                  // also where no y is asked for
     for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
     const int rows = tile_rows(p, n_mats);
-    p.slice = slice_of(p.rows, rows, n_mats, widest);
+    p.slice = slice_of(p, rows, n_mats, widest);
     const unsigned slices = (unsigned)((widest + p.slice - 1) / p.slice);
     p.pieces = single_tokens(p.rows) ? groups_of(p.rows) : (int)pieces(p.rows, rows);
-    // slices of a tile, which read the same x, are a multiple of eight numbers apart: on one die (4321 rows beside 14336 columns in three 82 -> 80 us, 333
-    // rows of four matrices 17 -> 14); fewer tiles than sixteen, all of whose slices would be on few dies, are not (one token 7 us, on one die 9.5)
-    const dim3 grid((unsigned)(slices > 1 && p.pieces >= 16 ? (p.pieces + 7) / 8 * 8 : p.pieces), slices, (unsigned)n_mats);
+    const dim3 grid((unsigned)(slices > 1 && spread(p.pieces) ? (p.pieces + 7) / 8 * 8 : p.pieces), slices, (unsigned)n_mats);
     return dt == DT_BF16 ? products<true>(p, rows, single_tokens(p.rows), grid, s) : products<false>(p, rows, single_tokens(p.rows), grid, s);
 }
 
