@@ -577,16 +577,16 @@ static bool single_tokens(const AdapterRowsDev& r) {
     return !r.offsets && r.n_tokens == r.n_seqs && r.n_seqs > 1 && r.n_seqs <= kGathered && !r.drop.seed;
 }
 // Rows of a tile: 16, of which two workgroups fit a compute unit, one's copies beside the other's products, unless there are enough tiles of 32 as
-// well, or tiles of 16 would take too much of P and Q through the caches.  Measured, 16 against 32 (us): K = N = 4096: 4096 rows at rank 32 30 / 37, 64
-// 40 / 52; 8192 rows at rank 16 45 / 54, 32 49 / 54, 64 76 / 59; 16384 rows at rank 16 82 / 94, 32 92 / 92; K = N = 1024: 16384 rows at rank 32
-// 27 / 24, 64 37 / 31; 4320 rows beside N = 14336: rank 16 79 / 75, 32 107 / 80, 64 130 / 104.  So 32 from 20000 ranks of tiles or 5 2^24 values that
-// tiles of 32 take, never for rank 16.  Above rank 64 the registers of 16 rows are full.
+// well, or tiles of 16 would take too much of Q through the caches.  Measured, 16 against 32 (us): K = N = 4096, rank 16: 8192 rows 45 / 54; rank 32: 4096
+// rows 30 / 31, 8192 49 / 54, 16384 92 / 95; rank 64: 2048 rows 22 / 25, 3000 30 / 29, 4096 41 / 37, 8192 76 / 59; K = N = 1024, 16384 rows: rank 32
+// 27 / 24, 64 37 / 31; N = 14336: 4320 rows at rank 16 79 / 75, 32 107 / 80, 64 130 / 104, 2000 at rank 64 59 / 48, 1000 28 / 29.  So 32 from 170
+// tiles of 16 above rank 32 and 620 up to it, or 5 2^23 values of Q that tiles of 32 take, never for rank 16.  Above rank 64 the registers of 16 rows are full.
 static int tile_rows(const AdapterCall& p, int n_mats) {
     const AdapterRowsDev& r = p.rows;
     if (r.rank <= 16 || r.rank > 64 || r.n_tokens / r.n_seqs <= 16) return 16;
-    double lengths = 0;
-    for (int i = 0; i < n_mats; ++i) lengths += (double)p.mats[i].m.depth + p.mats[i].m.wide;
-    return (double)r.rank * pieces(r, 16) * n_mats > 20000 || r.rank * lengths * pieces(r, 32) > 5 << 24 ? 32 : 16;
+    double wide = 0;
+    for (int i = 0; i < n_mats; ++i) wide += p.mats[i].m.wide;
+    return pieces(r, 16) * n_mats > (r.rank > 32 ? 170 : 620) || r.rank * wide * pieces(r, 32) > 5 << 23 ? 32 : 16;
 }
 // Slices of a tile, which read the same x, are on one die, a multiple of eight workgroups apart (4321 rows beside 14336 columns in three 82 -> 80 us, 333 rows
 // of four matrices 17 -> 14); those of fewer tiles than sixteen, which would be on few dies, are not (one token 7 us, on one die 9.5).
