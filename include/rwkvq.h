@@ -506,8 +506,8 @@ int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, con
  *   rows of no token are not touched.  Rows of dout whose token is padding are not read.  workspace: DEVICE,
  *   rwkvq_embedding_backward_workspace_size(n_tokens, d) bytes, contents irrelevant on entry and undefined on exit.
  *   Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, scale not finite), RWKVQ_ERR_SHAPE (n_tokens, vocab or d < 1, d > 2^24, vocab * d > 2^40, a
- *   stride below d, n_tokens * stride > 2^40; backward: n_tokens > 2^22, more threads than the 2^32 of one launch: 64 for every
- *   512 columns of 32 tokens, and one to four for every row of the table), RWKVQ_ERR_ALIGN (tokens 4 bytes, the others 16), RWKVQ_ERR_DEVICE. */
+ *   stride below d, n_tokens * stride > 2^40; backward: n_tokens > 2^22, more threads than the 2^32 of one launch: 256 for every
+ *   512 columns of 32 tokens, or 64 for each of these and one to four for every row of the table), RWKVQ_ERR_ALIGN (tokens 4 bytes, the others 16), RWKVQ_ERR_DEVICE. */
 int rwkvq_dropout(const void* x, int x_dtype, int M, int n, long long x_stride, const uint64_t* seed, double p, const void* base,
                   long long base_stride, void* y, long long y_stride, void* stream);
 int rwkvq_embedding(const int32_t* tokens, int n_tokens, const void* table, int table_dtype, int vocab, int d, double scale, void* out,

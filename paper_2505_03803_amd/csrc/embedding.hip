@@ -407,9 +407,11 @@ size_t embedding_backward_workspace_bytes(int n_tokens, int d) {
 }
 // Rows of the table of a wavefront: 64 where that makes a thousand wavefronts (65536 rows of 4096: 244 us, with 16 rows 251), otherwise 16.
 static int absent_rows(int vocab) { return vocab >= 65536 ? 64 : 16; }
+// Both launches over runs, of which the first also clears rows of no token.
 bool embedding_backward_fits(int n_tokens, int vocab, int d) {
     const double units = (double)((n_tokens + 31) / 32) * ((d + 511) / 512);       // where there are many
-    return (units + vocab / absent_rows(vocab) + 8) * 64.0 < 4294967296.0;
+    const double most = std::max((units + vocab / absent_rows(vocab) + 8) * 64.0, units * (64 * JW));
+    return most < 4294967296.0;
 }
 template <int DT_, int V>
 static void sum_runs(const EmbeddingDev& p, const RunPlan& plan, hipStream_t s) {
