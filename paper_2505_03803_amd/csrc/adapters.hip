@@ -99,7 +99,7 @@ __device__ __forceinline__ RowSpan piece_of(const AdapterRowsDev& r, int cut, in
 }
 static long long pieces(const AdapterRowsDev& r, int cut) {
     if (r.offsets) return (long long)r.n_tokens / cut + r.n_seqs;
-    return (long long)((r.n_tokens / r.n_seqs + cut - 1) / cut) * r.n_seqs;
+    return ((long long)(r.n_tokens / r.n_seqs) + cut - 1) / cut * r.n_seqs;
 }
 
 // Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  With fewer
