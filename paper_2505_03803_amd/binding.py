@@ -709,6 +709,12 @@ class AdapterRows:
         self.desc = rwkvq_adapter_rows(n_seqs, n_tokens, n_adapters, rank, _ptr(offsets), _ptr(adapters), _ptr(scales), _ptr(seed), p)
         self.ref = ctypes.addressof(self.desc)
         self.keep = (offsets, adapters, scales, seed)
+        self.seed = seed
+
+    def with_seed(self, seed) -> "AdapterRows":
+        """The same rows with the masks of another seed."""
+        d, (offsets, adapters, scales, _) = self.desc, self.keep
+        return AdapterRows(d.n_seqs, d.n_tokens, d.n_adapters, d.rank, offsets, adapters, scales, seed, d.p)
 
 
 def _each(items, n):

@@ -78,6 +78,7 @@ class TimeMix:
         self.stats = [torch.empty(max_tokens, n, device=device) for n in (1, 1, self.H, self.H)]
         if adapters is not None:
             self.adapters = adapters
+            self.seeds = torch.zeros_like(adapters.seeds)           # those of the masks of the call whose rows the buffers hold
             self.h = {p: torch.empty(max_tokens, adapters.rank, device=device) for p in PROJECTIONS + ("o",)}
         self.dense: Optional[Dict[str, torch.Tensor]] = None
         self.holds = None, None                                     # x and plan of the call whose rows the buffers hold
@@ -131,6 +132,9 @@ class TimeMix:
         lens, slots, heads, workspace, rows = plan
         T, H, dt = sum(lens), self.H, self.dtype
         self.holds = x, plan
+        if rows and rows[0].seed is not None:
+            for kept, r in zip(self.seeds, rows):
+                kept.copy_(r.seed)
         mean, rstd, head_mean, head_rstd = self.stats
         B.rwkvq_layer_norm(x, dt, T, 1, self.d, *self.ln, self.eps, self.a, mean, rstd)
         first = 0
@@ -178,12 +182,15 @@ class TimeMix:
 
     def backward(self, x: torch.Tensor, dout: torch.Tensor, plan) -> Dict[str, torch.Tensor]:
         """The gradients behind forward(x, plan), the last call before this one, with a plan without slots: of x, both norms, w, u and, where
-        the plan has them, the adapters.  The products with the transposed matrices are taken on their dense copies, made at the first call."""
+        the plan has them, the adapters, with the masks that the call had, whatever the pool's seeds are by now.  The products with the
+        transposed matrices are taken on their dense copies, made at the first call."""
         lens, slots, heads, _, rows = plan
         if slots is not None:
             raise ValueError("gradients of sequences that begin with a state of the pool")
         if self.holds[1] is not plan or self.holds[0].data_ptr() != x.data_ptr():        # x itself or a view of its rows
             raise ValueError("gradients of a call whose rows the block does not hold any more")
+        if rows and rows[0].seed is not None:
+            rows = [r.with_seed(kept) for r, kept in zip(rows, self.seeds)]
         T, H, D, d, dt = sum(lens), self.H, self.D, self.d, self.dtype
         kind = TYPES[dt]
         if self.dense is None:

@@ -1,0 +1,78 @@
+"""What a block keeps between a forward call and its gradients: the masks."""
+import pytest
+
+import gpu_util as G
+
+pytestmark = pytest.mark.gpu
+torch = G.torch_()
+D, HEADS = 256, 4
+
+
+def pool_of(seed):
+    from paper_2505_03803_amd import time_mix
+    pool = time_mix.Adapters(D, 2, 8, p=0.4, seed=seed)
+    gen = torch.Generator().manual_seed(seed)
+    for p in pool.b:
+        pool.b[p].copy_((torch.randn(pool.b[p].shape, generator=gen) * 0.1).half())
+    return pool
+
+
+def block_of(pool, seed=0):
+    from paper_2505_03803_amd import time_mix
+    return time_mix.synthetic(D, HEADS, 2, 60, seed=seed, adapters=pool)
+
+
+def flat(grads):
+    """Every tensor of a dictionary of gradients, by name."""
+    out = {}
+    for name, g in grads.items():
+        if isinstance(g, dict):
+            out.update({(name, *((k,) if not isinstance(k, tuple) else k)): v for k, v in flat(g).items()})
+        elif isinstance(g, tuple):
+            out.update({(name, i): v for i, v in enumerate(g)})
+        else:
+            out[name] = g
+    return {k: v.clone() for k, v in out.items()}
+
+
+def same(a, b):
+    assert a.keys() == b.keys()
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+
+
+def test_gradients_of_a_block_have_the_masks_of_their_call():
+    """Also where the numbers of the next call are set in between, by a step or by another block of the pool."""
+    pool = pool_of(3)
+    block, other = block_of(pool), block_of(pool, 1)
+    torch.manual_seed(1)
+    x, dout = torch.randn(30, D, device="cuda").half(), torch.randn(30, D, device="cuda").half()
+    plan, beside = block.plan([20, 10], adapters=[0, 1], drop=True), other.plan([30], adapters=[1], drop=True)
+    first = block.forward(x, plan).clone()
+    want = flat(block.backward(x, dout, plan))
+    pool.advance()
+    same(want, flat(block.backward(x, dout, plan)))
+    out = block.forward(x, plan).clone()
+    assert not torch.equal(out, first)                     # other masks
+    want = flat(block.backward(x, dout, plan))
+    for _ in range(2):
+        other.forward(x, beside)
+        pool.advance()
+    same(want, flat(block.backward(x, dout, plan)))
+
+
+def test_gradients_behind_a_replayed_block_have_its_masks():
+    pool = pool_of(4)
+    block, plain = block_of(pool), block_of(pool)
+    torch.manual_seed(2)
+    x, dout = torch.randn(30, D, device="cuda").half(), torch.randn(30, D, device="cuda").half()
+    plan, eager = block.plan([30], adapters=[1], drop=True), plain.plan([30], adapters=[1], drop=True)
+    replay = block.capture(x, plan)
+    for i in range(3):
+        x.normal_()
+        pool.advance()
+        out = replay()
+        assert torch.equal(out, plain.forward(x, eager))
+        want = flat(plain.backward(x, dout, eager))
+        pool.advance()
+        same(want, flat(block.backward(x, dout, plan)))
