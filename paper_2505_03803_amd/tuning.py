@@ -26,6 +26,7 @@ class Tuning:
         self.block, self.table, self.p = block, table, p
         self.vocab, self.d = table.shape
         self.seed = torch.tensor([seed, 0], dtype=torch.int64, device=table.device)
+        self.drawn, self.drawn_p = torch.zeros_like(self.seed), p           # those of the call before
         rows = lambda: torch.empty(block.max_tokens, self.d, dtype=table.dtype, device=table.device)
         self.x, self.out, self.dy = rows(), rows(), rows()
 
@@ -45,19 +46,21 @@ class Tuning:
         T, dt = self._count(tokens, plan), self.block.dtype
         B.rwkvq_embedding(tokens, T, self.table, dt, self.vocab, self.d, 1.0, self.x, dt)
         y = self.block.forward(self.x[:T], plan)
-        B.rwkvq_dropout(y, dt, T, self.d, self.seed, self.p, self.out, base=self.x)
+        self.drawn_p = self.p
+        self.drawn.copy_(self.seed)
+        B.rwkvq_dropout(y, dt, T, self.d, self.drawn, self.drawn_p, self.out, base=self.x)
         return self.out[:T]
 
     def backward(self, tokens: torch.Tensor, dout: torch.Tensor, plan, dtable: torch.Tensor, accumulate: bool = False) -> Dict[str, object]:
-        """The gradients behind forward(tokens, plan), the last call before this one, with the masks that it had: those of the block, and dtable
-        (float32 [vocab][d], overwritten or added to)."""
+        """The gradients behind forward(tokens, plan), the last call before this one, with the masks that it had, also after advance(): those of the
+        block, and dtable (float32 [vocab][d], overwritten or added to)."""
         T, dt = self._count(tokens, plan), self.block.dtype
         if dout.shape != (T, self.d) or dout.dtype != self.table.dtype:
             raise ValueError(f"a gradient {tuple(dout.shape)} of {dout.dtype} for {T} tokens")
         if dtable.shape != self.table.shape or dtable.dtype != torch.float32 or not dtable.is_contiguous():
             raise ValueError(f"a table's gradient {tuple(dtable.shape)} of {dtable.dtype}")
         dout = dout.contiguous()
-        B.rwkvq_dropout(dout, dt, T, self.d, self.seed, self.p, self.dy)
+        B.rwkvq_dropout(dout, dt, T, self.d, self.drawn, self.drawn_p, self.dy)
         grads = self.block.backward(self.x[:T], self.dy[:T], plan)
         dx = (grads.pop("x").float() + dout.float()).to(self.table.dtype)
         workspace = torch.empty(B.rwkvq_embedding_backward_workspace_size(T, self.d), dtype=torch.uint8, device=self.table.device)

@@ -1,11 +1,12 @@
-"""What a block keeps between a forward call and its gradients: the masks."""
+"""What a block and a tuning step keep between a forward call and its gradients: the masks."""
+import numpy as np
 import pytest
 
 import gpu_util as G
 
 pytestmark = pytest.mark.gpu
 torch = G.torch_()
-D, HEADS = 256, 4
+D, HEADS, VOCAB = 256, 4, 40
 
 
 def pool_of(seed):
@@ -76,3 +77,27 @@ def test_gradients_behind_a_replayed_block_have_its_masks():
         want = flat(plain.backward(x, dout, eager))
         pool.advance()
         same(want, flat(block.backward(x, dout, plan)))
+
+
+@pytest.fixture(scope="module")
+def step():
+    from paper_2505_03803_amd import tuning
+    torch.manual_seed(3)
+    return tuning.Tuning(block_of(pool_of(5)), torch.randn(VOCAB, D).half().cuda(), p=0.3, seed=8)
+
+
+def batch(T, seed):
+    rng = np.random.default_rng(seed)
+    return torch.tensor(rng.integers(-1, VOCAB, size=T), dtype=torch.int32, device="cuda"), torch.from_numpy(rng.standard_normal((T, D))).half().cuda()
+
+
+def test_gradients_of_a_step_have_the_masks_of_their_call(step):
+    tokens, dout = batch(30, 0)
+    plan, dtable = step.plan([11, 19], [1, 0]), torch.empty(VOCAB, D, device="cuda")
+    step.forward(tokens, plan)
+    want = flat(step.backward(tokens, dout, plan, dtable))
+    step.advance()
+    same(want, flat(step.backward(tokens, dout, plan, dtable)))
+    p, step.p = step.p, 0.0
+    same(want, flat(step.backward(tokens, dout, plan, dtable)))
+    step.p = p
