@@ -29,6 +29,7 @@ class Tuning:
         self.drawn, self.drawn_p = torch.zeros_like(self.seed), p           # those of the call before
         rows = lambda: torch.empty(block.max_tokens, self.d, dtype=table.dtype, device=table.device)
         self.x, self.out, self.dy = rows(), rows(), rows()
+        self.holds: Optional[torch.Tensor] = None                           # tokens of the call whose rows x holds
 
     def plan(self, lens: Sequence[int], adapters: Optional[Sequence[int]] = None):
         """Sequences that begin empty, and the adapter of each."""
@@ -44,6 +45,7 @@ class Tuning:
         """tokens: int32, the sequences' one after the other; one outside the table is padding, a row of zeros.  -> [tokens][d], a view that the next
         call overwrites"""
         T, dt = self._count(tokens, plan), self.block.dtype
+        self.holds = tokens
         B.rwkvq_embedding(tokens, T, self.table, dt, self.vocab, self.d, 1.0, self.x, dt)
         y = self.block.forward(self.x[:T], plan)
         self.drawn_p = self.p
@@ -59,6 +61,8 @@ class Tuning:
             raise ValueError(f"a gradient {tuple(dout.shape)} of {dout.dtype} for {T} tokens")
         if dtable.shape != self.table.shape or dtable.dtype != torch.float32 or not dtable.is_contiguous():
             raise ValueError(f"a table's gradient {tuple(dtable.shape)} of {dtable.dtype}")
+        if self.holds is None or self.holds.data_ptr() != tokens.data_ptr():
+            raise ValueError("gradients of tokens whose rows the step does not hold any more")
         dout = dout.contiguous()
         B.rwkvq_dropout(dout, dt, T, self.d, self.drawn, self.drawn_p, self.dy)
         grads = self.block.backward(self.x[:T], self.dy[:T], plan)

@@ -1,4 +1,4 @@
-"""What a block and a tuning step keep between a forward call and its gradients: the masks."""
+"""What a block and a tuning step keep between a forward call and its gradients: masks and tokens."""
 import numpy as np
 import pytest
 
@@ -101,3 +101,14 @@ def test_gradients_of_a_step_have_the_masks_of_their_call(step):
     p, step.p = step.p, 0.0
     same(want, flat(step.backward(tokens, dout, plan, dtable)))
     step.p = p
+
+
+def test_gradients_of_another_batch_are_refused(step):
+    tokens, dout = batch(30, 1)
+    others, _ = batch(30, 2)
+    plan, dtable = step.plan([30], [1]), torch.empty(VOCAB, D, device="cuda")
+    step.forward(tokens, plan)
+    step.forward(others, plan)
+    with pytest.raises(ValueError):
+        step.backward(tokens, dout, plan, dtable)
+    step.backward(others, dout, plan, dtable)
