@@ -55,7 +55,7 @@ class Tuning:
 
     def backward(self, tokens: torch.Tensor, dout: torch.Tensor, plan, dtable: torch.Tensor, accumulate: bool = False) -> Dict[str, object]:
         """The gradients behind forward(tokens, plan), the last call before this one, with the masks that it had, also after advance(): those of the
-        block, and dtable (float32 [vocab][d], overwritten or added to)."""
+        block, and dtable (float32 [vocab][d], overwritten or added to).  tokens: the tensor that this call had."""
         T, dt = self._count(tokens, plan), self.block.dtype
         if dout.shape != (T, self.d) or dout.dtype != self.table.dtype:
             raise ValueError(f"a gradient {tuple(dout.shape)} of {dout.dtype} for {T} tokens")
@@ -66,9 +66,9 @@ class Tuning:
         dout = dout.contiguous()
         B.rwkvq_dropout(dout, dt, T, self.d, self.drawn, self.drawn_p, self.dy)
         grads = self.block.backward(self.x[:T], self.dy[:T], plan)
-        dx = (grads.pop("x").float() + dout.float()).to(self.table.dtype)
+        dx = grads.pop("x").float() + dout                        # binary32: the table's gradient is a sum of these
         workspace = torch.empty(B.rwkvq_embedding_backward_workspace_size(T, self.d), dtype=torch.uint8, device=self.table.device)
-        B.rwkvq_embedding_backward(tokens, T, dx, dt, self.vocab, self.d, 1.0, dtable, accumulate, workspace)
+        B.rwkvq_embedding_backward(tokens, T, dx, B.F32, self.vocab, self.d, 1.0, dtable, accumulate, workspace)
         return dict(grads, table=dtable)
 
     def advance(self) -> None:

@@ -1,6 +1,9 @@
-"""What a block and a tuning step keep between a forward call and its gradients: masks and tokens."""
+"""What a block and a tuning step keep between a forward call and its gradients: masks and tokens; and what
+the table's gradient is summed from."""
 import numpy as np
 import pytest
+
+from oracle import tuning_oracle as TO
 
 import gpu_util as G
 
@@ -112,3 +115,21 @@ def test_gradients_of_another_batch_are_refused(step):
     with pytest.raises(ValueError):
         step.backward(tokens, dout, plan, dtable)
     step.backward(others, dout, plan, dtable)
+
+
+@pytest.mark.parametrize("added", [False, True])
+def test_table_gradients_are_sums_of_binary32(step, added):
+    """dx + dout is binary32, one rounding of 2^-24 in each term: with those of the sum, of the product and of what is added (count + 3) 2^-24."""
+    tokens, dout = batch(50, 4)
+    plan = step.plan([30, 20], [0, 1])
+    step.forward(tokens, plan)
+    before = torch.randn(VOCAB, D, device="cuda") if added else torch.zeros(VOCAB, D, device="cuda")
+    dtable = before.clone()
+    step.backward(tokens, dout, plan, dtable, accumulate=added)
+    dx = step.block.backward(step.x[:50], step.dy[:50], plan)["x"]
+    terms = dx.cpu().double().numpy() + dout.cpu().double().numpy()
+    want, size, count = TO.embedding_backward(tokens.tolist(), terms, VOCAB)
+    old = before.cpu().double().numpy()
+    bar = 2.0 ** -24 * (count[:, None] + 3) * (size + np.abs(old))
+    err = np.abs(dtable.cpu().double().numpy() - want - old)
+    assert (err <= bar).all(), float((err / np.maximum(bar, 1e-300)).max())
