@@ -100,7 +100,8 @@ class TimeMix:
     def plan(self, lens: Sequence[int], slots: Optional[Sequence[int]] = None, adapters: Optional[Sequence[int]] = None, drop: bool = False):
         """What calls of one form share: the sequences' lengths, their slots (None: they begin empty and leave no state), and the
         workspace.  A captured graph replays one plan.  Each sequence has a slot of the pool to itself.  adapters: that of each sequence, -1
-        for none (None: the block without adapters); drop: with dropout in front of them."""
+        for none (None: the block without adapters); drop: with dropout in front of them.  -> lens, slots, heads, workspace, and of a block with
+        adapters their rows, or None"""
         if min(lens) < 0 or sum(lens) > self.max_tokens:
             raise ValueError(f"sequences of {list(lens)} tokens in a block for at most {self.max_tokens}")
         if slots is not None and (len(slots) != len(lens) or len(set(slots)) != len(lens) or not all(0 <= s < self.n_slots for s in slots)):
@@ -109,8 +110,8 @@ class TimeMix:
             raise ValueError(f"adapters {list(adapters)} for {len(lens)} sequences in a block with {self.adapters.n if self.adapters else 0}")
         heads = self._heads(lens, slots)
         n = B.rwkvq_linear_attention_workspace_size(heads)
-        rows = None if adapters is None else self._rows(lens, adapters, drop)
-        return lens, slots, heads, torch.empty(max(n, 16), dtype=torch.uint8, device=self.device), rows
+        plan = lens, slots, heads, torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        return plan if self.adapters is None else (*plan, None if adapters is None else self._rows(lens, adapters, drop))
 
     def _adapt(self, rows: B.AdapterRows, projections: Sequence[str], xs, ys) -> None:
         pool = self.adapters
@@ -129,7 +130,7 @@ class TimeMix:
 
     def forward(self, x: torch.Tensor, plan) -> torch.Tensor:
         """x: [tokens][d], the sequences' rows one after the other.  -> [tokens][d], a view that the next call overwrites"""
-        lens, slots, heads, workspace, rows = plan
+        lens, slots, heads, workspace, rows = plan if len(plan) == 5 else (*plan, None)
         T, H, dt = sum(lens), self.H, self.dtype
         self.holds = x, plan
         if rows and rows[0].seed is not None:
@@ -184,7 +185,7 @@ class TimeMix:
         """The gradients behind forward(x, plan), the last call before this one, with a plan without slots: of x, both norms, w, u and, where
         the plan has them, the adapters, with the masks that the call had, whatever the pool's seeds are by now.  The products with the
         transposed matrices are taken on their dense copies, made at the first call."""
-        lens, slots, heads, _, rows = plan
+        lens, slots, heads, _, rows = plan if len(plan) == 5 else (*plan, None)
         if slots is not None:
             raise ValueError("gradients of sequences that begin with a state of the pool")
         if self.holds[1] is not plan or self.holds[0].data_ptr() != x.data_ptr():        # x itself or a view of its rows
@@ -227,7 +228,8 @@ class TimeMix:
         dx, dln_w, dln_b = like(), f32(d), f32(d)
         B.rwkvq_layer_norm_backward(da.to(kind), x, dt, T, 1, d, self.ln[0], mean, rstd, dx, dln_w, dln_b,
                                     scratch(B.rwkvq_layer_norm_backward_workspace_size(T, 1, d)))
-        return dict(x=dx, ln=(dln_w, dln_b), heads_norm=(dheads_w, dheads_b), w=dw, u=du, adapters=tuned)
+        grads = dict(x=dx, ln=(dln_w, dln_b), heads_norm=(dheads_w, dheads_b), w=dw, u=du)
+        return dict(grads, adapters=tuned) if rows else grads
 
 
 def synthetic(d: int, n_heads: int, n_slots: int, max_tokens: int, seed: int = 0, dtype: int = B.F16,

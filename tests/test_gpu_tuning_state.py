@@ -133,3 +133,12 @@ def test_table_gradients_are_sums_of_binary32(step, added):
     bar = 2.0 ** -24 * (count[:, None] + 3) * (size + np.abs(old))
     err = np.abs(dtable.cpu().double().numpy() - want - old)
     assert (err <= bar).all(), float((err / np.maximum(bar, 1e-300)).max())
+
+
+def test_plans_without_adapters_have_no_gradients_of_them(step):
+    block = step.block
+    x, dout = torch.randn(30, D, device="cuda").half(), torch.randn(30, D, device="cuda").half()
+    for adapters, names in ((None, {"x", "ln", "heads_norm", "w", "u"}), ([1], {"x", "ln", "heads_norm", "w", "u", "adapters"})):
+        plan = block.plan([30], adapters=adapters)
+        block.forward(x, plan)
+        assert set(block.backward(x, dout, plan)) == names
