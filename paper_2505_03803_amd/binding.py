@@ -721,6 +721,19 @@ def _each(items, n):
     return [None] * n if items is None else [items] * n if isinstance(items, int) else items
 
 
+def _pool(as_, bs):
+    """How many adapters matrices a [adapters][rank][K] and b [adapters][N][rank] hold, and their rank."""
+    for a, b in zip(as_, bs):
+        assert a.dim() == 3 and b.dim() == 3 and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2] == as_[0].shape[1]
+    return min((a.shape[0] for a in as_), default=0), as_[0].shape[1] if as_ else 0
+
+
+def _fits(rows, table):
+    """The kernels go by what the rows say of the matrices."""
+    held, rank = table.pool
+    assert table.n == 0 or (rows.desc.n_adapters <= held and rows.desc.rank == rank)
+
+
 class AdapterTable:
     """Host array for rwkvq_adapters, from tensors a [adapters][rank][K], b [adapters][N][rank] and the rows of each matrix.  bases, hs: None, or one
     for each (None among them as well).  Strides in elements, 0 = densely packed: one number for all matrices, or one for each.  Reusable across calls."""
@@ -729,6 +742,7 @@ class AdapterTable:
                  x_strides=0, base_strides=0, y_strides=0):
         self.n = n = len(as_)
         assert len(bs) == n and len(xs) == n and len(ys) == n
+        self.pool = _pool(as_, bs)
         self.mats = (rwkvq_adapter * n)(*[
             rwkvq_adapter(_ptr(a), _ptr(b), _ptr(x), _ptr(base), _ptr(y), _ptr(h), b.shape[1], a.shape[2], *strides)
             for a, b, x, y, base, h, *strides in zip(as_, bs, xs, ys, _each(bases, n), _each(hs, n), _each(x_strides, n), _each(base_strides, n),
@@ -738,6 +752,7 @@ class AdapterTable:
 
 
 def rwkvq_adapters(rows: AdapterRows, table: AdapterTable, x_dtype, y_dtype, stream=None, check=True):
+    _fits(rows, table)
     st = lib().rwkvq_adapters(rows.ref, table.ref, table.n, x_dtype, y_dtype, _stream(stream))
     return _check(st) if check else st
 
@@ -749,6 +764,8 @@ class AdapterGradTable:
                  dbs: Sequence, bases: Optional[Sequence] = None, x_strides=0, dy_strides=0, base_strides=0, dx_strides=0):
         self.n = n = len(as_)
         assert len(bs) == n and len(xs) == n and len(hs) == n and len(dys) == n and len(das) == n and len(dbs) == n
+        self.pool = _pool(as_, bs)
+        assert all(da.numel() == a.numel() and db.numel() == b.numel() for a, b, da, db in zip(as_, bs, das, dbs))
         self.mats = (rwkvq_adapter_grad * n)(*[
             rwkvq_adapter_grad(_ptr(a), _ptr(b), _ptr(x), _ptr(h), _ptr(dy), _ptr(base), _ptr(dx), _ptr(da), _ptr(db), b.shape[1], a.shape[2],
                                *strides)
@@ -760,9 +777,11 @@ class AdapterGradTable:
 
 
 def rwkvq_adapters_backward_workspace_size(rows: AdapterRows, table: AdapterGradTable) -> int:
+    _fits(rows, table)
     return int(lib().rwkvq_adapters_backward_workspace_size(rows.ref, table.ref, table.n))
 
 
 def rwkvq_adapters_backward(rows: AdapterRows, table: AdapterGradTable, x_dtype, workspace, stream=None, check=True):
+    _fits(rows, table)
     st = lib().rwkvq_adapters_backward(rows.ref, table.ref, table.n, x_dtype, _ptr(workspace), _stream(stream))
     return _check(st) if check else st
