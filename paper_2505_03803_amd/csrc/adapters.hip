@@ -1,5 +1,6 @@
 // Low-rank adapters beside frozen matrices (include/rwkvq.h), y_t = base_t + s_a B_a h_t with h_t = A_a drop(x_t), and their gradients:
 //   g_t = s_a B_a^T dy_t,   dx_t = base_t + drop(A_a^T g_t),   dA_a = sum_t g_t drop(x_t)^T,   dB_a = s_a sum_t dy_t h_t^T.
+#include "adapter_plan.h"
 #include "dropout.h"
 #include "matrix_core.h"
 #include "pieces.h"
@@ -43,9 +44,6 @@ struct TurnCall {
     uint16_t* h_parts[kAdapterMats];
     int n_mats;
 };
-
-// The rank as the kernels pad it: 16, 32, 64 or 128.
-__host__ __device__ __forceinline__ int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
 // Rows of sequence b, within 0 .. n_tokens whatever the offsets hold.
 __device__ __forceinline__ void rows_of(const AdapterRowsDev& r, int b, int& t0, int& t1) {
@@ -97,24 +95,14 @@ __device__ __forceinline__ RowSpan piece_of(const AdapterRowsDev& r, int cut, in
     s.scale = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(found->scale)));
     return s;
 }
-static long long pieces(const AdapterRowsDev& r, int cut) {
-    if (r.offsets) return (long long)r.n_tokens / cut + r.n_seqs;
-    return ((long long)(r.n_tokens / r.n_seqs) + cut - 1) / cut * r.n_seqs;
-}
-
 // Single tokens: the rows of a tile are up to sixteen of one adapter, wherever they are, so that its weights are read once for all of them.  With fewer
 // adapters than rows workgroup i takes the i-th sixteen of all adapters', counted in LDS, and the grid is as large as these can be; otherwise, and for up
 // to sixteen rows, that of row b has work if an even sixteen of the rows in front of it have the same adapter.  That costs 1 us less, but workgroups without
 // work come and go, and the others meet on few dies: four matrices at rank 16, 128 rows of 8 adapters 14 us instead of 40, 2048 of 100 87 instead of 164.
-constexpr int kGathered = 2048;                    // rows of such a call at most
 struct Gathered {
     uint64_t same[kGathered / 64];
     int rows[16], totals[8], id, skip;
 };
-__host__ __device__ __forceinline__ int groups_of(const AdapterRowsDev& r) {
-    const long long most = (long long)r.n_adapters + 1 + r.n_seqs / 16;
-    return most < r.n_seqs && r.n_seqs > 16 ? (int)most : r.n_seqs;
-}
 constexpr int kGatherScratch = 8 * kGathered + 16;
 __device__ __forceinline__ int gather_rows(const AdapterRowsDev& r, int group, char* scratch, Gathered& at, int& id) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = r.n_seqs, masks = (n + 63) / 64;
@@ -216,9 +204,9 @@ __device__ __forceinline__ int swizzle(int row) { return (row / (16 / C)) & (C -
 // cache), 4321 rows of 4096 beside 14336 columns at rank 32 78 (floor 57), 256 single tokens of 64 adapters, four matrices at rank 16, 25 (floor 18).
 // GATHER: single tokens (gather_rows).  DROP: there is dropout, of x or, backwards, of what is added to y.
 template <int RT, int MT, int PARTS> struct AdapterLds {
-    static constexpr int W = 8, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
+    static constexpr int W = kAdapterWaves, R = 16 * RT, ROWS = 16 * MT, PITCH = R + 4;
     static constexpr int STEPS = (PARTS * R + 31) / 32, HROW = 64 * STEPS + 16;                      // bytes of a row of h's parts
-    static constexpr int CG = RT <= 2 || MT == 2 ? 64 : 32, YPITCH = CG + 4;                                     // columns of a wavefront at a time
+    static constexpr int CG = wave_cols(RT, MT), YPITCH = CG + 4;                                     // columns of a wavefront at a time
     static constexpr int CS = RT <= 2 || MT == 2 ? 64 : 32, D = RT == 1 ? 2 : 1;                      // columns of a step, steps on their way
     static constexpr int step = 2 * CS * (ROWS + R), ring = W * D * step;
     static constexpr int sums = W / 2 * ROWS * PITCH * 4, out = 16 * YPITCH * 4;                      // out: of a wavefront
@@ -573,65 +561,18 @@ static hipError_t products(const AdapterCall& p, int rows, bool gather, dim3 gri
            : rank <= 64 ? products<BF16, 4>(p, rows, gather, grid, s)
                         : products<BF16, 8>(p, rows, gather, grid, s);
 }
-static bool single_tokens(const AdapterRowsDev& r) {
-    return !r.offsets && r.n_tokens == r.n_seqs && r.n_seqs > 1 && r.n_seqs <= kGathered && !r.drop.seed;
-}
-// Rows of a tile: 16, of which two workgroups fit a compute unit, one's copies beside the other's products, unless there are enough tiles of 32 as
-// well, or tiles of 16 would take too much of Q through the caches.  Measured, 16 against 32 (us): K = N = 4096, rank 16: 8192 rows 45 / 54; rank 32: 4096
-// rows 30 / 31, 8192 49 / 54, 16384 92 / 95; rank 64: 2048 rows 22 / 25, 3000 30 / 29, 4096 41 / 37, 8192 76 / 59; K = N = 1024, 16384 rows: rank 32
-// 27 / 24, 64 37 / 31; N = 14336: 4320 rows at rank 16 79 / 75, 32 107 / 80, 64 130 / 104, 2000 at rank 64 59 / 48, 1000 28 / 29.  So 32 from 170
-// tiles of 16 above rank 32 and 620 up to it, or 5 2^23 values of Q that tiles of 32 take, never for rank 16.  Above rank 64 the registers of 16 rows are full.
-static int tile_rows(const AdapterCall& p, int n_mats) {
-    const AdapterRowsDev& r = p.rows;
-    if (r.rank <= 16 || r.rank > 64 || r.n_tokens / r.n_seqs <= 16) return 16;
-    double wide = 0;
-    for (int i = 0; i < n_mats; ++i) wide += p.mats[i].m.wide;
-    return pieces(r, 16) * n_mats > (r.rank > 32 ? 170 : 620) || r.rank * wide * pieces(r, 32) > 5 << 23 ? 32 : 16;
-}
-// Slices of a tile, which read the same x, are on one die, a multiple of eight workgroups apart (4321 rows beside 14336 columns in three 82 -> 80 us, 333 rows
-// of four matrices 17 -> 14); those of fewer tiles than sixteen, which would be on few dies, are not (one token 7 us, on one die 9.5).
-static bool spread(long long tiles) { return tiles >= 16; }
-// Columns of a workgroup: all of them from 256 workgroups on; of fewer, as many slices as make the fullest compute unit's time least, by what goes through
-// its cache: every slice takes h again, (rows + rank) values for each of the depth, then rank values of Q, base and y for each of its columns.
-// Workgroups that share a unit take 0.7 of their times together, 0.85 above rank 32; one that fills a unit waits for the one in front.  Measured, 1, 2, 3
-// and 4 slices (us): 3500 rows, K = N = 4096, rank 16 23.3, 21.7, 26.8, 29.3; 2500 rows at rank 64 28.4, 31.2, 32.5, 41.9; 4321 rows beside N = 14336
-// at rank 32 97, 94, 80, 95; 3000 rows with K = 14336 at rank 32 48, 62, 72, 81; 2048 rows at rank 128 in 2 and 3 34 and 53.  Groups of single tokens,
-// whose number the host does not know, as many as one a unit where they are few, otherwise one and a half (four matrices, 16 rows of 16 adapters 9 us,
-// one and a half 11; 128 of 8 14, 17; 64 rows of 32 at rank 64 one and a half 45, one 50).
-static int slice_of(const AdapterCall& p, int rows, int n_mats, int widest) {
-    const AdapterRowsDev& r = p.rows;
-    const int R = padded_rank(r.rank);
-    const int most = (widest + 255) / 256;
-    auto width = [&](long long slices) { return (int)(((widest + slices - 1) / slices + 63) / 64 * 64); };
-    if (single_tokens(r)) {
-        const long long wgs = (long long)n_mats * std::min(groups_of(r), std::max(r.n_adapters, (r.n_seqs + 15) / 16));
-        return width(wgs >= 256 ? 1 : std::min<long long>(most, ((wgs <= 64 ? 256 : 384) + wgs - 1) / wgs));
-    }
-    const long long tiles = pieces(r, rows), wgs = tiles * n_mats;
-    int deepest = 0;
-    for (int i = 0; i < n_mats; ++i) deepest = std::max(deepest, p.mats[i].m.depth);
-    const bool fills = R > 64 || (rows == 32 && (R > 32 || r.drop.seed || p.y_dt == DT_F32));       // a unit (waves_of)
-    const double together = fills ? 1.0 : R > 32 ? 0.85 : 0.7, h = 2.0 * (rows + R) * deepest, column = 2.0 * R + rows * (p.y_dt == DT_F32 ? 8.0 : 4.0);
-    int best = width(1);
-    double least = 0;
-    for (int slices = 1; wgs < 256 && slices <= most && (slices == 1 || slices * wgs <= 768); ++slices) {
-        const int wide = width(slices);
-        const long long die = (tiles + 7) / 8 * slices * n_mats, fullest = slices > 1 && spread(tiles) ? (die + 31) / 32 : (slices * wgs + 255) / 256;
-        const double time = (fullest == 1 ? 1.0 : together * fullest) * (h + column * wide);
-        if (slices == 1 || time < least) {
-            least = time;
-            best = wide;
-        }
-    }
-    return best;
-}
 // (more than one slice only of fewer than 256 workgroups)
 bool adapters_fit(const AdapterRowsDev& r) { return (double)pieces(r, 16) * kAdapterMats * 512.0 < 4294967296.0; }
 static hipError_t launch_products(AdapterCall& p, int n_mats, int dt, hipStream_t s) {
-    int widest = 64;                                  // also where no y is asked for
-    for (int i = 0; i < n_mats; ++i) widest = std::max(widest, p.mats[i].m.wide);
-    const int rows = tile_rows(p, n_mats);
-    p.slice = slice_of(p, rows, n_mats, widest);
+    int widest = 64, deepest = 0;                     // also where no y is asked for
+    double wide = 0;
+    for (int i = 0; i < n_mats; ++i) {
+        const AdapterMatDev& m = p.mats[i].m;
+        widest = std::max(widest, m.wide); deepest = std::max(deepest, m.depth);
+        wide += m.wide;
+    }
+    const int rows = tile_rows(p.rows, n_mats, wide);
+    p.slice = slice_of(p.rows, rows, n_mats, widest, deepest, p.y_dt == DT_F32);
     const unsigned slices = (unsigned)((widest + p.slice - 1) / p.slice);
     p.pieces = single_tokens(p.rows) ? groups_of(p.rows) : (int)pieces(p.rows, rows);
     const dim3 grid((unsigned)(slices > 1 && spread(p.pieces) ? (p.pieces + 7) / 8 * 8 : p.pieces), slices, (unsigned)n_mats);
@@ -717,8 +658,6 @@ __global__ void __launch_bounds__(256) turn_kernel(TurnCall p) {
 // Reads by columns take 32 bytes of eight rows at once: pairs of pieces of a row, C of them, change places with its number.
 template <int C>
 __device__ __forceinline__ int pair_swizzle(int row) { return C >= 8 ? (row & 7) << 1 : (row / (8 / C) & (C - 1)) << 1; }
-constexpr int outer_tiles(int rank) { return rank <= 64 ? 4 : 2; }
-static int outer_cols(int rank) { return 64 * outer_tiles(rank); }
 template <int RT> struct OuterLds {
     static constexpr int R = 16 * RT, QC = R / 8, VC = outer_tiles(R), COLS = 64 * VC, VROW = 2 * COLS, QROW = 6 * R;
     static constexpr int v = 32 * VROW, q = 32 * QROW, found = 2 * (v + q), bytes = found + 16;
@@ -878,20 +817,9 @@ __global__ void __launch_bounds__(256) gather_kernel(OuterCall p) {
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
-// Rows of a piece: 64, and twice as many while two workgroups a compute unit are left, since every piece leaves sums of rank (K + N) floats (gradients of 8192
-// rows at rank 64: pieces of 256 rows 146 us, of 512 123, of 1024 132).
-static int cut_of(const AdapterRowsDev& r, long long chunks) {
-    int cut = 64;
-    while (cut < 4096 && pieces(r, 2 * cut) * chunks >= 512) cut *= 2;
-    return cut;
-}
-static int outer_chunks(const AdapterRowsDev& r, const AdapterMatDev& m) {
-    const int cols = outer_cols(r.rank);
-    return (m.wide + cols - 1) / cols + (m.depth + cols - 1) / cols;
-}
 static long long outer_chunks(const AdapterRowsDev& r, const AdapterMatDev* mats, int n) {
     long long c = 0;
-    for (int i = 0; i < n; ++i) c += outer_chunks(r, mats[i]);
+    for (int i = 0; i < n; ++i) c += outer_chunks(r.rank, mats[i].depth, mats[i].wide);
     return c;
 }
 static size_t parts_bytes(const AdapterRowsDev& r) { return (size_t)r.n_tokens * 6 * padded_rank(r.rank); }
@@ -980,7 +908,7 @@ static hipError_t backward_group(const AdapterRowsDev& rows, const AdapterMatDev
         OuterMatDev& d = o.mats[i];
         d.x = grads[i].x; d.x_stride = grads[i].x_stride; d.dy = m.x; d.dy_stride = m.x_stride; d.g = (uint16_t*)m.h; d.h = turn.h_parts[i];
         d.da = grads[i].da; d.db = grads[i].db; d.K = m.wide; d.N = m.depth;
-        d.at = o.size; d.chunks = outer_chunks(rows, m);
+        d.at = o.size; d.chunks = outer_chunks(rows.rank, d.N, d.K);
         o.size += (size_t)rows.rank * ((size_t)d.K + d.N);
         o.chunks += d.chunks;
         if (!m.y) m.wide = 0;
