@@ -507,7 +507,8 @@ int rwkvq_linear_attention_backward(const rwkvq_heads* heads, const void* r, con
  *   rwkvq_embedding_backward_workspace_size(n_tokens, d) bytes, contents irrelevant on entry and undefined on exit.
  *   Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, scale not finite), RWKVQ_ERR_SHAPE (n_tokens, vocab or d < 1, d > 2^24, vocab * d > 2^40, a
  *   stride below d, n_tokens * stride > 2^40; backward: n_tokens > 2^22, more threads than the 2^32 of one launch: 256 for every
- *   512 columns of 32 tokens, or 64 for each of these and one to four for every row of the table), RWKVQ_ERR_ALIGN (tokens 4 bytes, the others 16), RWKVQ_ERR_DEVICE. */
+ *   512 columns of 32 tokens, or 64 for each of these and one to four for every row of the table), RWKVQ_ERR_ALIGN (tokens 4 bytes, the others 16),
+ *   RWKVQ_ERR_DEVICE. */
 int rwkvq_dropout(const void* x, int x_dtype, int M, int n, long long x_stride, const uint64_t* seed, double p, const void* base,
                   long long base_stride, void* y, long long y_stride, void* stream);
 int rwkvq_embedding(const int32_t* tokens, int n_tokens, const void* table, int table_dtype, int vocab, int d, double scale, void* out,
@@ -534,7 +535,10 @@ int rwkvq_embedding_backward(const int32_t* tokens, int n_tokens, const void* do
  *   base: a gradient of x from elsewhere (the frozen projection), NULL: 0; dx may be base, with its stride; dx NULL: not computed.  base, dx: rows of K values
  *   of x_dtype.  h as rwkvq_adapters stored it; rows and seed as there.  da, db: DEVICE floats like a and b, overwritten, 0 for adapters of no row.
  *   g and h enter da and db with 24 bits.  workspace: DEVICE, rwkvq_adapters_backward_workspace_size(..) bytes (of the same rows and
- *   matrices, whose pointers are not looked at), contents irrelevant on entry and undefined on exit.
+ *   matrices, whose pointers are not looked at), contents irrelevant on entry and undefined on exit.  It holds rank (K + N) floats of each of up to eight
+ *   matrices for every piece of rows; a piece is 64 to 4096 rows of one sequence, or all of them where it has fewer, so that its size grows with the sequences.
+ * Rows of different sequences share a tile, and what is read of A and B for it, in calls of one token a sequence: without offsets, with up to
+ *   2048 sequences and no dropout.  In other calls every sequence has tiles of its own, of 16 or 32 rows.
  * a, b, x, base, y, h, dy, dx, da, db, workspace 16-byte aligned; seed 8; offsets, adapters, scales 4; no call synchronises.
  * Errors: RWKVQ_ERR_NULL, RWKVQ_ERR_UNSUPPORTED (dtypes, rank, p outside [0, 1]), RWKVQ_ERR_SHAPE (a count below 1, n_mats > 64, n_tokens not a multiple of
  *   n_seqs without offsets, K or N above 2^24, a stride below its width or n_tokens * stride > 2^40, x or dy the same as y or dx, in place with another

@@ -18,7 +18,8 @@ from . import time_mix
 
 
 class Tuning:
-    """table: [vocab][d] of the block's type.  p: dropout of the block's output; `seed` holds its key and the number of the next call."""
+    """table: [vocab][d] of the block's type.  p: dropout of the block's output; `seed` holds its key and the number of the next call; a key
+    other than the adapters', whose numbers begin at 0 as well."""
 
     def __init__(self, block: time_mix.TimeMix, table: torch.Tensor, p: float = 0.0, seed: int = 1):
         if table.dtype != time_mix.TYPES[block.dtype] or table.dim() != 2 or table.shape[1] != block.d or not table.is_contiguous():
